@@ -12,7 +12,9 @@
  * them, the content-aware keyframe selection of Sec. 3.1 (frame similarity and
  * Alg. 1's scan), the per-layer rolling cache of App. B.2, whose projected
  * hidden states are the skipped frames' keys and values, and the progressive
- * asynchronous schedule (Eq. 2, Alg. 2) that says which step is which. Three
+ * asynchronous schedule (Eq. 2, Alg. 2) that says which step is which, and the
+ * operators of a block around the attention (rotary positions, attention to the
+ * prompt, matrix products with their epilogue) on the same frames' rows. Three
  * device probes, measurement support outside the method, report the rates the
  * matrix cores, LDS and HBM sustain on this device.
  *
@@ -22,9 +24,9 @@
  *    failure on the calling thread.
  *  - Every argument is validated before any HIP call, so a rejected call has
  *    no effect on the device. The one HIP call that may come first is a query
- *    of the current device's compute-unit and XCD counts (bf16 attention and
- *    the plan queries with compute_units = 0), made once per device; a failed
- *    query returns RF_ERR_HIP.
+ *    of the current device's compute-unit and XCD counts (bf16 attention, the
+ *    block operators and the plan queries with compute_units = 0), made once
+ *    per device; a failed query returns RF_ERR_HIP.
  *  - Device buffers are owned by the caller, must stay alive until the stream
  *    has passed the launched work, and are never retained by the library.
  *    Host arrays are read during the call only; the caller may free them when
@@ -567,6 +569,177 @@ typedef struct rf_step_plan {
  */
 int rf_async_schedule(int32_t T, int32_t T_w, int32_t T_mid, int32_t n_small, int32_t n_large,
                       rf_step_plan *plan_out, int32_t *n_rhythmic_out, int32_t *n_skipped_out);
+
+/* ---- A block's operators around the attention ----
+ * What a DiT block does with the rows of the listed frames directly before and
+ * after keyframe-query attention: rotary positions of queries and keys,
+ * attention to an encoder's states (the prompt), and the matrix products with
+ * their bias, activation, gate and residual.
+ *
+ * Rows of frames come and go in one of two layouts, per call and side:
+ *   compact: M*N rows, row m*N + n is row n of the m-th listed frame (what a
+ *            skipped step computes, rf_keyframe_attention's output);
+ *   full:    T*N rows at their frames' positions (the layout of q, k and v of
+ *            the attention calls); rows of frames that are not listed are
+ *            neither read nor written.
+ * So a gather or a scatter of frames needs no pass of its own.
+ */
+#define RF_ROWS_IN_FULL 1u      /* input rows are read at full positions (default: compact) */
+#define RF_ROWS_OUT_FULL 2u     /* output rows (and the residual's) are at full positions (default: compact) */
+#define RF_GATE_PER_FRAME 4u    /* rf_frame_linear: gate is [T][out_features], frames have their own */
+#define RF_ROTARY_HALVES 16u    /* rf_rotary: pair p is dimensions p and p + R/2 (default: 2p and 2p + 1) */
+#define RF_ROTARY_INVERSE 32u   /* rf_rotary: rotate by the negative angles */
+
+/*
+ * The axes of rotary positions: time (frame index), height (row) and width
+ * (column). Axis a turns dims[a] of a head's dimensions; the R = sum of dims
+ * leading dimensions of a head turn, the others pass unchanged. The R/2 pairs
+ * are numbered axis by axis; the j-th pair of axis a turns by
+ *   phi = (origin[a] + step[a] * index) * theta[a]^(-2 j / dims[a]).
+ * dims: even, >= 0, 2 <= R <= head_dim. theta: >= 1. origin, step: finite, every
+ * |origin[a]| + |step[a]| * 2^16 at most 2^31 (a fractional step stretches positions).
+ */
+typedef struct rf_rotary_axes {
+    int32_t dims[3];
+    double theta[3];
+    double origin[3];
+    double step[3];
+} rf_rotary_axes;
+
+/*
+ * Rotary positions of queries and keys. For every row of the listed frames and
+ * every head, each pair (a, b) becomes (a cos phi - b sin phi, a sin phi +
+ * b cos phi). Frame f's index is f itself, also for compact rows. Angles are
+ * formed in double, reduced to one turn there, their sine and cosine and the
+ * products in fp32; bf16 results are rounded once, to nearest even.
+ * RF_ROTARY_INVERSE undoes a rotation (up to rounding); being its transpose it
+ * also takes a gradient of the rotated rows to one of the rows before.
+ *
+ * q, q_out: device, rows of q_heads*head_dim contiguous elements, q_stride and
+ *   q_out_stride elements from row to row (0: rows are contiguous; a view of a
+ *   fused projection has a longer stride). k, k_out: the same with k_heads;
+ *   k == NULL rotates q only (k_out, k_heads and the strides are then ignored).
+ * Rows and strides are multiples of 16 bytes. q_out may be exactly q, and k_out
+ *   exactly k, with the same stride and layout (with M == T both layouts are
+ *   one); otherwise no output row may overlap another row of the call. Rows of
+ *   one stride may interleave (q and k as views of one buffer).
+ * head_dim: a multiple of 8 up to 256; with RF_ROTARY_HALVES R is a multiple of 16.
+ * frame_ids, M, T: as rf_keyframe_attention. H, W: token grid, up to 65536 each.
+ * flags: RF_ROWS_IN_FULL, RF_ROWS_OUT_FULL, RF_ROTARY_HALVES, RF_ROTARY_INVERSE.
+ * Errors: RF_ERR_INVALID_ARG (NULL, sizes <= 0, ids, unknown flags, axes, a
+ *   stride below the row, overlap), RF_ERR_RANGE (ids, T, H, W, positions, sizes
+ *   whose byte counts would pass 4e18), RF_ERR_UNSUPPORTED (head_dim, R, dtype,
+ *   alignment), RF_ERR_HIP.
+ */
+int rf_rotary(const void *q, void *q_out, const void *k, void *k_out, const int32_t *frame_ids, int32_t M,
+              int32_t T, int32_t H, int32_t W, int32_t q_heads, int32_t k_heads, int32_t head_dim,
+              const rf_rotary_axes *axes, int64_t q_stride, int64_t q_out_stride, int64_t k_stride,
+              int64_t k_out_stride, uint32_t flags, int32_t dtype, void *stream);
+
+/* Element strides of a cross attention's tensors: {batch, token, head}; the
+   head_dim elements of a head are contiguous. */
+typedef struct rf_cross_layout {
+    int64_t q[3];
+    int64_t k[3];
+    int64_t v[3];
+    int64_t out[3];
+} rf_cross_layout;
+
+/*
+ * Attention to an encoder's states of another length: for every sequence b,
+ * head h and query i,
+ *   out = softmax over the valid keys of (q k^T / sqrt(head_dim)) v,
+ * with h reading the keys and values of head h / (heads / kv_heads). Key j of
+ * sequence b is valid where j < kv_lengths[b] and key_mask[b][j] != 0. A query
+ * without any valid key gives a row of zeros. Keys and values that are not valid
+ * have no effect, whatever they hold (infinities and NaN among it).
+ *
+ * q, out: device [B][Lq][heads][head_dim]; k, v: device [B][Lk][kv_heads][head_dim],
+ *   contiguous in this order (layout == NULL) or of layout's strides: multiples of
+ *   16 bytes, not negative; an input's stride may be 0 (one prompt for a whole
+ *   batch), out's elements must be distinct. out must not overlap the memory
+ *   between the first and last element of q, k or v.
+ * kv_lengths: device int32 [B], or NULL (Lk for all); read by the kernel, values
+ *   outside [0, Lk] count as the nearer end. key_mask: device bytes [B][Lk], or NULL.
+ * B, Lq, Lk, heads: >= 1; heads a multiple of kv_heads. head_dim: 64 or 128.
+ * dtype: RF_BF16 (products on the bf16 matrix cores, probabilities rounded to
+ *   bf16 for the second one, fp32 softmax and sums, one rounding of the output) or
+ *   RF_F32 (fp32 throughout).
+ * workspace: NULL, or device scratch, 16-byte aligned, of at least
+ *   rf_cross_attention_workspace bytes, overlapping no tensor of the call: launches
+ *   with few query rows then split the key axis over workgroups, whose parts a
+ *   second kernel joins in a fixed order. Its contents mean nothing afterwards; two
+ *   calls, or two captured graphs, that may run at the same time need one each.
+ *   Results of a split differ from those without in fp32 summation order and in
+ *   the references that probabilities are rounded to bf16 against.
+ * Errors: RF_ERR_INVALID_ARG (NULL, sizes <= 0, heads % kv_heads, strides, overlap,
+ *   workspace too small), RF_ERR_RANGE (sizes whose byte counts or strides would
+ *   pass 4e18, more than 2^31 - 1 query tiles), RF_ERR_UNSUPPORTED (head_dim, dtype,
+ *   alignment, a token stride of 16 MB and more in k or v), RF_ERR_HIP.
+ */
+int rf_cross_attention(const void *q, const void *k, const void *v, void *out, const int32_t *kv_lengths,
+                       const uint8_t *key_mask, int32_t B, int32_t Lq, int32_t Lk, int32_t heads,
+                       int32_t kv_heads, int32_t head_dim, const rf_cross_layout *layout, int32_t dtype,
+                       void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace rf_cross_attention uses for these sizes (0: the key axis is
+   not split) on a device of compute_units compute units, or 0 for the current
+   device's count (queried once per device).
+   Errors: RF_ERR_INVALID_ARG (NULL, sizes <= 0, heads % kv_heads), RF_ERR_RANGE
+   (sizes, compute_units), RF_ERR_UNSUPPORTED (head_dim, dtype), RF_ERR_HIP. */
+int rf_cross_attention_workspace(int32_t B, int32_t Lq, int32_t Lk, int32_t heads, int32_t kv_heads,
+                                 int32_t head_dim, int32_t dtype, int32_t compute_units, int64_t *bytes_out);
+
+/* Activations of rf_frame_linear. */
+#define RF_ACT_NONE 0
+#define RF_ACT_GELU 1        /* x/2 (1 + erf(x / sqrt 2)) */
+#define RF_ACT_GELU_TANH 2   /* x/2 (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))) */
+#define RF_ACT_SILU 3        /* x / (1 + exp(-x)) */
+
+/*
+ * Matrix product with bias, activation, gate and residual in its epilogue, on
+ * the rows of the listed frames:
+ *   y[r] = residual[r] + gate * act(x[r] weight^T + bias).
+ * Plain rows of any kind (a prompt's tokens, timestep embeddings) are one frame
+ * of that many rows: M = T = 1 with id 0.
+ *
+ * x: device rows of in_features elements, contiguous; weight: device
+ *   [out_features][in_features]; y, residual: device rows of out_features
+ *   elements, contiguous. x is compact, or full with RF_ROWS_IN_FULL; y and
+ *   residual are compact, or full with RF_ROWS_OUT_FULL.
+ * bias: device [out_features], or NULL (none). gate: device [out_features], with
+ *   RF_GATE_PER_FRAME [T][out_features] (frames denoised at times of their own have
+ *   modulations of their own), or NULL (1). residual: or NULL (0). y may be exactly
+ *   residual (the residual is updated in place); it overlaps nothing else.
+ * All tensors have one dtype: RF_BF16 (products on the bf16 matrix cores, sums, bias,
+ *   activation, gate and residual in fp32, one rounding at the end) or RF_F32
+ *   (fp32 throughout).
+ * in_features, out_features: rows of a multiple of 16 bytes. rows_per_frame >= 1,
+ *   M * rows_per_frame < 2^31.
+ * workspace: NULL, or device scratch, 16-byte aligned, of at least
+ *   rf_frame_linear_workspace bytes, overlapping no tensor of the call: products
+ *   of few output tiles then split in_features over workgroups, whose parts a second
+ *   kernel adds in a fixed order. Its contents mean nothing afterwards; two calls, or
+ *   two captured graphs, that may run at the same time need one each.
+ * frame_ids, M, T: as rf_keyframe_attention.
+ * flags: RF_ROWS_IN_FULL, RF_ROWS_OUT_FULL, RF_GATE_PER_FRAME (which needs a gate).
+ * Errors: RF_ERR_INVALID_ARG (NULL x, weight, y; sizes <= 0, ids, unknown flags or
+ *   activation, overlap, workspace too small), RF_ERR_RANGE (ids, T, rows, sizes
+ *   whose byte counts would pass 4e18), RF_ERR_UNSUPPORTED (dtype, alignment, row
+ *   sizes, in_features of 8 MB and more), RF_ERR_HIP.
+ */
+int rf_frame_linear(const void *x, const void *weight, const void *bias, const void *gate, const void *residual,
+                    void *y, const int32_t *frame_ids, int32_t M, int32_t T, int64_t rows_per_frame,
+                    int32_t in_features, int32_t out_features, int32_t activation, uint32_t flags, int32_t dtype,
+                    void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace rf_frame_linear uses for M frames of rows_per_frame rows (0:
+   in_features are not split) on a device of compute_units compute units, or 0 for the
+   current device's count (queried once per device).
+   Errors: RF_ERR_INVALID_ARG (NULL, sizes <= 0), RF_ERR_RANGE (rows, sizes,
+   compute_units), RF_ERR_UNSUPPORTED (dtype, row sizes), RF_ERR_HIP. */
+int rf_frame_linear_workspace(int32_t M, int64_t rows_per_frame, int32_t in_features, int32_t out_features,
+                              int32_t dtype, int32_t compute_units, int64_t *bytes_out);
 
 /* ---- Device probes (measurement support, not part of the method) ----
  * Sustained whole-chip rates of this device under a pure load of one kind, to

@@ -26,6 +26,12 @@ RF_F32 = 1
 RF_SEL_NO_FORCE_FIRST = 1
 RF_SEL_INTENT_SIGN = 1
 RF_MAX_FRAMES = 256
+RF_ROWS_IN_FULL = 1
+RF_ROWS_OUT_FULL = 2
+RF_GATE_PER_FRAME = 4
+RF_ROTARY_HALVES = 16
+RF_ROTARY_INVERSE = 32
+ACTIVATIONS = {"none": 0, "gelu": 1, "gelu_tanh": 2, "silu": 3}
 
 EXPORTED = [
     "rf_status_string", "rf_last_error", "rf_abi_version",
@@ -37,6 +43,8 @@ EXPORTED = [
     "rf_frame_similarity", "rf_frame_similarity_workspace", "rf_select_keyframes_adaptive",
     "rf_cache_store_bytes", "rf_cache_init", "rf_cache_shift_store", "rf_cache_alpha",
     "rf_cache_project_kv", "rf_keyframe_attention_cached", "rf_async_schedule",
+    "rf_rotary", "rf_cross_attention", "rf_cross_attention_workspace",
+    "rf_frame_linear", "rf_frame_linear_workspace",
     "rf_probe_mfma_bf16", "rf_probe_hbm_read", "rf_probe_lds_read",
 ]
 
@@ -89,6 +97,21 @@ class rf_attention_split(ctypes.Structure):
         ("compute_units", ctypes.c_int32),
         ("shared_keys", ctypes.c_int32),
     ]
+
+
+class rf_rotary_axes(ctypes.Structure):
+    """The C struct rf_rotary_axes (the axes of rotary positions: time, height, width)."""
+    _fields_ = [
+        ("dims", ctypes.c_int32 * 3),
+        ("theta", ctypes.c_double * 3),
+        ("origin", ctypes.c_double * 3),
+        ("step", ctypes.c_double * 3),
+    ]
+
+
+class rf_cross_layout(ctypes.Structure):
+    """The C struct rf_cross_layout (batch, token and head strides in elements)."""
+    _fields_ = [(name, ctypes.c_int64 * 3) for name in ("q", "k", "v", "out")]
 
 
 class RhymeFlowError(RuntimeError):
@@ -175,6 +198,19 @@ lib.rf_keyframe_attention_cached.argtypes = [_vp, _vp, _vp, _vp, _vp, _i32, _i32
 lib.rf_keyframe_attention_cached.restype = ctypes.c_int
 lib.rf_async_schedule.argtypes = [_i32, _i32, _i32, _i32, _i32, ctypes.POINTER(rf_step_plan), _i32p, _i32p]
 lib.rf_async_schedule.restype = ctypes.c_int
+lib.rf_rotary.argtypes = [_vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _i32,
+                          ctypes.POINTER(rf_rotary_axes), _i64, _i64, _i64, _i64, ctypes.c_uint32, _i32, _vp]
+lib.rf_rotary.restype = ctypes.c_int
+lib.rf_cross_attention.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32,
+                                   ctypes.POINTER(rf_cross_layout), _i32, _vp, _i64, _vp]
+lib.rf_cross_attention.restype = ctypes.c_int
+lib.rf_cross_attention_workspace.argtypes = [_i32, _i32, _i32, _i32, _i32, _i32, _i32, _i32, ctypes.POINTER(_i64)]
+lib.rf_cross_attention_workspace.restype = ctypes.c_int
+lib.rf_frame_linear.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i64, _i32, _i32, _i32,
+                                ctypes.c_uint32, _i32, _vp, _i64, _vp]
+lib.rf_frame_linear.restype = ctypes.c_int
+lib.rf_frame_linear_workspace.argtypes = [_i32, _i64, _i32, _i32, _i32, _i32, ctypes.POINTER(_i64)]
+lib.rf_frame_linear_workspace.restype = ctypes.c_int
 lib.rf_probe_mfma_bf16.argtypes = [_vp, _i32, _i32, _vp, _vp]
 lib.rf_probe_mfma_bf16.restype = ctypes.c_int
 lib.rf_probe_hbm_read.argtypes = [_vp, _i64, _i32, _vp, _vp]
@@ -686,6 +722,226 @@ def rf_async_schedule(T: int, T_w: int, T_mid: int, n_small: int, n_large: int):
                         t_start=p.t_start if skip else None, t_end=p.t_end if skip else None,
                         alpha=p.alpha if skip else None))
     return out
+
+
+# --- a block's operators around the attention -------------------------------------
+
+def _on_device(tensors):
+    """The addresses of device tensors (a dict by name; None stays None) of any
+    strides, all on torch's current device: the device the stream and the launch
+    belong to."""
+    index, out = None, []
+    for name, t in tensors.items():
+        if t is None:
+            out.append(None)
+            continue
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name} must be a torch.Tensor")
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a device tensor")
+        if index is None:
+            index = torch.cuda.current_device()
+        if t.device.index != index:
+            raise ValueError(f"{name} is on {t.device}, the current device is cuda:{index}")
+        out.append(t.data_ptr())
+    return out
+
+
+def _same_dtype(tensors):
+    dt = next(iter(tensors.values())).dtype
+    for name, t in tensors.items():
+        if t is not None and t.dtype != dt:
+            raise TypeError(f"{name} has dtype {t.dtype}, the call's is {dt}")
+    return _dtype_code(dt)
+
+
+def _head_rows(t, name, heads, d):
+    """Row stride in elements of a [rows][heads][head_dim] tensor whose rows are contiguous."""
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d:
+        raise ValueError(f"{name} must be [rows][{heads}][{d}]")
+    if (d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d):
+        raise ValueError(f"{name}: the elements of a row must be contiguous")
+    if t.shape[0] > 1 and t.stride(0) < heads * d:
+        raise ValueError(f"{name}: rows overlap")
+    return t.stride(0) if t.shape[0] > 1 else heads * d
+
+
+def rf_rotary(q, frame_ids, T: int, H: int, W: int, dims, k=None, out=None, k_out=None, theta=10000.0,
+              origin=(0.0, 0.0, 0.0), step=(1.0, 1.0, 1.0), in_full: bool = False, out_full: bool = False,
+              halves: bool = False, inverse: bool = False, stream=None):
+    """Rotary positions over (frame, row, column) of q, and of k if given: rows of
+    the listed frames, [M*H*W][heads][head_dim] or, with in_full, [T*H*W][...];
+    a view with a longer row stride is taken as it is. dims, theta (one or three),
+    origin and step as rf_rotary_axes. out / k_out: rows at compact or, with
+    out_full, full positions (required then unless M = T, as rows of other frames
+    are left as they are); q / k themselves rotate in place. Returns out, or
+    (out, k_out) if k is given."""
+    ids, ids_p = _ids(frame_ids)
+    M = ids.size
+    if q.dim() != 3:
+        raise ValueError("q must be [rows][heads][head_dim]")
+    d = q.shape[2]
+    rows_in, rows_out = H * W * (T if in_full else M), H * W * (T if out_full else M)
+
+    def output(y, x, name):
+        if y is not None:
+            return y
+        if out_full and M != T:
+            raise ValueError(f"{name} must be given with out_full: rows of other frames are left as they are")
+        return _empty((rows_out, x.shape[1], d), x.dtype, x.device, stream)
+    pairs = [("q", q, "out", output(out, q, "out"))]
+    if k is not None:
+        if k.dim() != 3:
+            raise ValueError("k must be [rows][heads][head_dim]")
+        pairs.append(("k", k, "k_out", output(k_out, k, "k_out")))
+    strides, heads = [], []
+    for xn, x, yn, y in pairs:
+        for t, name, rows in ((x, xn, rows_in), (y, yn, rows_out)):
+            strides.append(_head_rows(t, name, x.shape[1], d))
+            if t.shape[0] != rows:
+                raise ValueError(f"{name} has {t.shape[0]} rows, the layout asks for {rows}")
+        heads.append(x.shape[1])
+    code = _same_dtype({n: t for xn, x, yn, y in pairs for n, t in ((xn, x), (yn, y))})
+    ptrs = _on_device({n: t for xn, x, yn, y in pairs for n, t in ((xn, x), (yn, y))})
+    if k is None:
+        strides += [0, 0]
+        heads.append(0)
+        ptrs += [None, None]
+    axes = rf_rotary_axes()
+    axes.dims[:] = [int(n) for n in dims]
+    axes.theta[:] = [float(theta)] * 3 if np.isscalar(theta) else [float(x) for x in theta]
+    axes.origin[:] = [float(x) for x in origin]
+    axes.step[:] = [float(x) for x in step]
+    flags = ((RF_ROWS_IN_FULL if in_full else 0) | (RF_ROWS_OUT_FULL if out_full else 0) |
+             (RF_ROTARY_HALVES if halves else 0) | (RF_ROTARY_INVERSE if inverse else 0))
+    _check(lib.rf_rotary(*ptrs, ids_p, M, T, H, W, heads[0], heads[1], d, ctypes.byref(axes), *strides, flags, code,
+                         _stream(stream)))
+    return pairs[0][3] if k is None else (pairs[0][3], pairs[1][3])
+
+
+def rf_cross_attention_workspace(B: int, Lq: int, Lk: int, heads: int, kv_heads: int, head_dim: int, dtype,
+                                 compute_units: int = 0) -> int:
+    """Bytes of workspace rf_cross_attention uses (0: the key axis is not split)
+    on a device of compute_units compute units (0: the current device)."""
+    n = _i64(0)
+    code = dtype if isinstance(dtype, int) else _dtype_code(dtype)
+    _check(lib.rf_cross_attention_workspace(B, Lq, Lk, heads, kv_heads, head_dim, code, compute_units,
+                                            ctypes.byref(n)))
+    return int(n.value)
+
+
+def rf_cross_attention(q, k, v, kv_lengths=None, key_mask=None, out=None, workspace=None, stream=None):
+    """q [B][Lq][heads][head_dim] attends to k, v [B][Lk][kv_heads][head_dim], of
+    any strides whose head_dim elements are contiguous, -> out as q. kv_lengths:
+    int32 [B], key_mask: bool or uint8 [B][Lk] (nonzero: valid), both on the
+    device. A query without a valid key gives zeros. The workspace (a device
+    tensor) is allocated here if not given."""
+    if q.dim() != 4 or k.dim() != 4 or v.shape != k.shape or k.shape[0] != q.shape[0] or k.shape[3] != q.shape[3]:
+        raise ValueError("q must be [B][Lq][heads][head_dim], k and v [B][Lk][kv_heads][head_dim]")
+    B, Lq, heads, d = q.shape
+    Lk, kvh = k.shape[1], k.shape[2]
+    if out is None:
+        out = _empty((B, Lq, heads, d), q.dtype, q.device, stream)
+    if out.shape != q.shape:
+        raise ValueError("out must have q's shape")
+    code = _same_dtype({"q": q, "k": k, "v": v, "out": out})
+    layout = rf_cross_layout()
+    for name, t in (("q", q), ("k", k), ("v", v), ("out", out)):
+        if d > 1 and t.stride(3) != 1:
+            raise ValueError(f"{name}: the elements of a head must be contiguous")
+        # (the stride of an axis of one element is never taken)
+        getattr(layout, name)[:] = [t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)]
+    if kv_lengths is not None:
+        if kv_lengths.dtype != torch.int32 or kv_lengths.shape != (B,) or not kv_lengths.is_contiguous():
+            raise ValueError("kv_lengths must be contiguous int32 [B]")
+    if key_mask is not None:
+        if key_mask.dtype not in (torch.uint8, torch.bool) or key_mask.shape != (B, Lk) or not key_mask.is_contiguous():
+            raise ValueError("key_mask must be contiguous bool or uint8 [B][Lk]")
+    ptrs = _on_device({"q": q, "k": k, "v": v, "out": out, "kv_lengths": kv_lengths, "key_mask": key_mask})
+    if workspace is None and q.numel() > 0 and k.numel() > 0:
+        need = rf_cross_attention_workspace(B, Lq, Lk, heads, kvh, d, code)
+        workspace = _empty(need, torch.uint8, q.device, stream) if need > 0 else None
+    ws_p, wbytes = _workspace_arg(workspace)
+    _check(lib.rf_cross_attention(*ptrs, B, Lq, Lk, heads, kvh, d, ctypes.byref(layout), code, ws_p, wbytes,
+                                  _stream(stream)))
+    return out
+
+
+def _workspace_arg(workspace):
+    if workspace is None:
+        return None, 0
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return _on_device({"workspace": workspace})[0], workspace.numel() * workspace.element_size()
+
+
+def rf_frame_linear_workspace(M: int, rows_per_frame: int, in_features: int, out_features: int, dtype,
+                              compute_units: int = 0) -> int:
+    """Bytes of workspace rf_frame_linear uses for M frames (0: in_features are
+    not split) on a device of compute_units compute units (0: the current device)."""
+    n = _i64(0)
+    code = dtype if isinstance(dtype, int) else _dtype_code(dtype)
+    _check(lib.rf_frame_linear_workspace(M, rows_per_frame, in_features, out_features, code, compute_units,
+                                         ctypes.byref(n)))
+    return int(n.value)
+
+
+def rf_frame_linear(x, weight, bias=None, activation: str = "none", gate=None, residual=None, frame_ids=None,
+                    T=None, rows_per_frame=None, in_full: bool = False, out_full: bool = False, out=None,
+                    workspace=None, stream=None):
+    """residual + gate * act(x weight^T + bias) on the rows of the listed frames;
+    without frame_ids on all of x's rows. x [rows][in], weight [out][in], bias
+    [out], gate [out] or [T][out] (each frame its own), residual and out
+    [rows][out]; x is compact or, with in_full, full; residual and out compact or,
+    with out_full, full (out is required then unless M = T, as rows of other frames
+    are left as they are). out may be residual itself. activation: "none", "gelu",
+    "gelu_tanh" or "silu". The workspace is allocated here if not given."""
+    if x.dim() != 2 or weight.dim() != 2 or weight.shape[1] != x.shape[1]:
+        raise ValueError("x must be [rows][in_features], weight [out_features][in_features]")
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"unknown activation {activation!r}: one of {sorted(ACTIVATIONS)}")
+    n_out, K = weight.shape
+    if frame_ids is None:
+        if T is not None or rows_per_frame is not None or in_full or out_full:
+            raise ValueError("T, rows_per_frame, in_full and out_full go with frame_ids")
+        frame_ids, T, rows_per_frame = _FRAME0, 1, x.shape[0]
+    elif T is None or rows_per_frame is None:
+        raise ValueError("frame_ids needs T and rows_per_frame")
+    ids, ids_p = _ids(frame_ids)
+    M = ids.size
+    rows_in, rows_out = rows_per_frame * (T if in_full else M), rows_per_frame * (T if out_full else M)
+    if x.shape[0] != rows_in:
+        raise ValueError(f"x has {x.shape[0]} rows, the layout asks for {rows_in}")
+    if out is None:
+        if out_full and M != T:
+            raise ValueError("out must be given with out_full: rows of other frames are left as they are")
+        out = _empty((rows_out, n_out), x.dtype, x.device, stream)
+    for t, name in ((out, "out"), (residual, "residual")):
+        if t is not None and t.shape != (rows_out, n_out):
+            raise ValueError(f"{name} must be [{rows_out}][{n_out}]")
+    if bias is not None and bias.shape != (n_out,):
+        raise ValueError(f"bias must be [{n_out}]")
+    flags = (RF_ROWS_IN_FULL if in_full else 0) | (RF_ROWS_OUT_FULL if out_full else 0)
+    if gate is not None and gate.shape != (n_out,):
+        if gate.shape != (T, n_out):
+            raise ValueError(f"gate must be [{n_out}] or [{T}][{n_out}]")
+        flags |= RF_GATE_PER_FRAME
+    tensors = {"x": x, "weight": weight, "bias": bias, "gate": gate, "residual": residual, "out": out}
+    code = _same_dtype(tensors)
+    for name, t in tensors.items():
+        if t is not None and not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+    ptrs = _on_device(tensors)
+    if workspace is None and M > 0 and rows_per_frame > 0 and weight.numel() > 0:
+        need = rf_frame_linear_workspace(M, rows_per_frame, K, n_out, code)
+        workspace = _empty(need, torch.uint8, x.device, stream) if need > 0 else None
+    ws_p, wbytes = _workspace_arg(workspace)
+    _check(lib.rf_frame_linear(*ptrs, ids_p, M, T, rows_per_frame, K, n_out, ACTIVATIONS[activation], flags, code,
+                               ws_p, wbytes, _stream(stream)))
+    return out
+
+
+_FRAME0 = np.zeros(1, dtype=np.int32)
 
 
 # --- device probes (measurement support) ------------------------------------------

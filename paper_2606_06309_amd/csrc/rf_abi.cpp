@@ -860,6 +860,390 @@ int rf_async_schedule(int32_t T, int32_t T_w, int32_t T_mid, int32_t n_small, in
     return ok();
 }
 
+// --- a block's operators around the attention ---
+
+// Where the rows of the M listed frames are: compact (frame m) or full (frame ids[m]).
+static void row_frames(const int32_t *ids, int32_t M, bool full, int16_t *dst) {
+    for (int32_t m = 0; m < M; ++m) dst[m] = static_cast<int16_t>(full ? ids[m] : m);
+}
+
+static int64_t abs_diff(uintptr_t a, uintptr_t b) { return static_cast<int64_t>(a > b ? a - b : b - a); }
+
+// Two sets of rows of a_row and b_row bytes, `stride` bytes apart each, share memory.
+// With one stride for both, rows may interleave (views of one buffer).
+static bool rows_overlap(const void *a, int64_t a_rows, int64_t a_stride, int64_t a_row, const void *b,
+                         int64_t b_rows, int64_t b_stride, int64_t b_row) {
+    if (!overlaps(a, (a_rows - 1) * a_stride + a_row, b, (b_rows - 1) * b_stride + b_row)) return false;
+    if (a_stride != b_stride) return true;
+    const uintptr_t pa = reinterpret_cast<uintptr_t>(a), pb = reinterpret_cast<uintptr_t>(b);
+    const int64_t off = abs_diff(pa, pb) % a_stride;   // of the later set's rows after the earlier one's
+    const int64_t first = pa <= pb ? a_row : b_row, second = pa <= pb ? b_row : a_row;
+    return off < first || off + second > a_stride;
+}
+
+static int rotary_call(const void *q, void *q_out, const void *k, void *k_out, const int32_t *frame_ids, int32_t M,
+                       int32_t T, int32_t H, int32_t W, int32_t q_heads, int32_t k_heads, int32_t head_dim,
+                       const rf_rotary_axes *axes, const int64_t (&strides)[4], uint32_t flags, int32_t dtype,
+                       void *stream, const char *fn) {
+    if (!q || !q_out || !axes || (k && !k_out)) return fail(RF_ERR_INVALID_ARG, "%s: NULL argument", fn);
+    const uint32_t known = RF_ROWS_IN_FULL | RF_ROWS_OUT_FULL | RF_ROTARY_HALVES | RF_ROTARY_INVERSE;
+    if (flags & ~known) return fail(RF_ERR_INVALID_ARG, "%s: unknown flags 0x%x", fn, flags);
+    if (H <= 0 || W <= 0 || q_heads <= 0 || (k && k_heads <= 0) || head_dim <= 0)
+        return fail(RF_ERR_INVALID_ARG, "%s: sizes must be positive (H=%d W=%d q_heads=%d k_heads=%d head_dim=%d)", fn,
+                    H, W, q_heads, k_heads, head_dim);
+    if (H > 65536 || W > 65536) return fail(RF_ERR_RANGE, "%s: H = %d or W = %d exceeds 65536", fn, H, W);
+    int32_t ids[RF_MAX_FRAMES];
+    const int rc = check_id_list(frame_ids, M, T, ids, fn);
+    if (rc != RF_OK) return rc;
+    int64_t R = 0;
+    for (int a = 0; a < 3; ++a) {
+        if (axes->dims[a] < 0 || (axes->dims[a] & 1))
+            return fail(RF_ERR_INVALID_ARG, "%s: axis %d turns %d dimensions (even, not negative)", fn, a, axes->dims[a]);
+        if (!(axes->theta[a] >= 1.0) || !isfinite(axes->theta[a]))
+            return fail(RF_ERR_INVALID_ARG, "%s: axis %d: theta must be finite and at least 1", fn, a);
+        if (!isfinite(axes->origin[a]) || !isfinite(axes->step[a]))
+            return fail(RF_ERR_INVALID_ARG, "%s: axis %d: origin and step must be finite", fn, a);
+        if (fabs(axes->origin[a]) + 65536.0 * fabs(axes->step[a]) > 2147483648.0)
+            return fail(RF_ERR_RANGE, "%s: axis %d: positions pass 2^31", fn, a);
+        R += axes->dims[a];
+    }
+    if (R < 2 || R > head_dim)
+        return fail(RF_ERR_INVALID_ARG, "%s: the axes turn %lld dimensions, a head has %d", fn,
+                    static_cast<long long>(R), head_dim);
+    if (head_dim % 8 != 0 || head_dim > 2 * rf::kMaxRotaryPairs)
+        return fail(RF_ERR_UNSUPPORTED, "%s: head_dim %d is no multiple of 8 up to %d", fn, head_dim,
+                    2 * rf::kMaxRotaryPairs);
+    if ((flags & RF_ROTARY_HALVES) && R % 16 != 0)
+        return fail(RF_ERR_UNSUPPORTED, "%s: halves of %lld dimensions (a multiple of 16)", fn,
+                    static_cast<long long>(R));
+    if (dtype != RF_BF16 && dtype != RF_F32) return fail(RF_ERR_UNSUPPORTED, "%s: unknown dtype %d", fn, dtype);
+    const int64_t esize = dtype == RF_F32 ? 4 : 2;
+    const int64_t N = static_cast<int64_t>(H) * W;
+    const bool in_full = (flags & RF_ROWS_IN_FULL) != 0 || M == T, out_full = (flags & RF_ROWS_OUT_FULL) != 0 || M == T;
+    const int64_t in_rows = N * (in_full ? T : M), out_rows = N * (out_full ? T : M);
+    const int64_t heads[2] = {q_heads, k ? k_heads : 0};
+    const void *in[2] = {q, k};
+    void *out[2] = {q_out, k_out};
+    rf::RotaryParams p{};
+    int64_t row[2], is[2], os[2];
+    for (int t = 0; t < (k ? 2 : 1); ++t) {
+        const int64_t width = heads[t] * head_dim;
+        is[t] = strides[2 * t] == 0 ? width : strides[2 * t];
+        os[t] = strides[2 * t + 1] == 0 ? width : strides[2 * t + 1];
+        if (is[t] < width || os[t] < width)
+            return fail(RF_ERR_INVALID_ARG, "%s: a row stride is below the row's %lld elements", fn,
+                        static_cast<long long>(width));
+        if (static_cast<double>(N) * T * static_cast<double>(is[t]) * 4.0 > kMaxBytes ||
+            static_cast<double>(N) * T * static_cast<double>(os[t]) * 4.0 > kMaxBytes)
+            return fail(RF_ERR_RANGE, "%s: sizes overflow 64-bit byte counts", fn);
+        if (!aligned16(in[t]) || !aligned16(out[t]) || (is[t] * esize) % 16 != 0 || (os[t] * esize) % 16 != 0)
+            return fail(RF_ERR_UNSUPPORTED, "%s: pointers and row strides must be multiples of 16 bytes", fn);
+        row[t] = width * esize;
+        is[t] *= esize;
+        os[t] *= esize;
+        p.x[t] = in[t];
+        p.y[t] = out[t];
+        p.x_stride[t] = is[t] / esize;
+        p.y_stride[t] = os[t] / esize;
+        p.heads[t] = static_cast<int32_t>(heads[t]);
+    }
+    for (int t = 0; t < (k ? 2 : 1); ++t)
+        for (int u = 0; u < (k ? 2 : 1); ++u) {
+            const bool in_place = t == u && in[u] == out[t] && is[u] == os[t] && in_full == out_full;
+            if (!in_place && rows_overlap(out[t], out_rows, os[t], row[t], in[u], in_rows, is[u], row[u]))
+                return fail(RF_ERR_INVALID_ARG, "%s: an output overlaps an input", fn);
+        }
+    if (k && rows_overlap(q_out, out_rows, os[0], row[0], k_out, out_rows, os[1], row[1]))
+        return fail(RF_ERR_INVALID_ARG, "%s: q_out overlaps k_out", fn);
+    p.head_dim = head_dim;
+    p.dtype = dtype;
+    p.M = M;
+    p.H = H;
+    p.W = W;
+    p.halves = (flags & RF_ROTARY_HALVES) != 0;
+    p.pairs = static_cast<int32_t>(R / 2);
+    p.pair_end[0] = axes->dims[0] / 2;
+    p.pair_end[1] = (axes->dims[0] + axes->dims[1]) / 2;
+    int32_t pair = 0;
+    for (int a = 0; a < 3; ++a) {
+        p.origin[a] = axes->origin[a];
+        p.step[a] = axes->step[a];
+        for (int32_t j = 0; j < axes->dims[a] / 2; ++j) {
+            const double turns = pow(axes->theta[a], -2.0 * j / axes->dims[a]) / 6.283185307179586476925;
+            p.turns[pair++] = (flags & RF_ROTARY_INVERSE) ? -turns : turns;
+        }
+    }
+    for (int32_t m = 0; m < M; ++m) p.frame[m] = static_cast<int16_t>(ids[m]);
+    row_frames(ids, M, in_full, p.src_frame);
+    row_frames(ids, M, out_full, p.dst_frame);
+    return launched(rf::launch_rotary(p, static_cast<hipStream_t>(stream)), fn);
+}
+
+int rf_rotary(const void *q, void *q_out, const void *k, void *k_out, const int32_t *frame_ids, int32_t M,
+              int32_t T, int32_t H, int32_t W, int32_t q_heads, int32_t k_heads, int32_t head_dim,
+              const rf_rotary_axes *axes, int64_t q_stride, int64_t q_out_stride, int64_t k_stride,
+              int64_t k_out_stride, uint32_t flags, int32_t dtype, void *stream) {
+    const int64_t strides[4] = {q_stride, q_out_stride, k_stride, k_out_stride};
+    return rotary_call(q, q_out, k, k_out, frame_ids, M, T, H, W, q_heads, k_heads, head_dim, axes, strides, flags,
+                       dtype, stream, "rf_rotary");
+}
+
+// Sizes common to a cross attention and its workspace query.
+static int cross_sizes(int32_t B, int32_t Lq, int32_t Lk, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                       int32_t dtype, const char *fn) {
+    if (B <= 0 || Lq <= 0 || Lk <= 0 || heads <= 0 || kv_heads <= 0)
+        return fail(RF_ERR_INVALID_ARG, "%s: sizes must be positive (B=%d Lq=%d Lk=%d heads=%d kv_heads=%d)", fn, B,
+                    Lq, Lk, heads, kv_heads);
+    if (heads % kv_heads != 0)
+        return fail(RF_ERR_INVALID_ARG, "%s: %d heads are no multiple of %d key heads", fn, heads, kv_heads);
+    if (head_dim != 64 && head_dim != 128)
+        return fail(RF_ERR_UNSUPPORTED, "%s: head_dim %d not in {64, 128}", fn, head_dim);
+    if (dtype != RF_BF16 && dtype != RF_F32) return fail(RF_ERR_UNSUPPORTED, "%s: unknown dtype %d", fn, dtype);
+    if (static_cast<double>(B) * Lq * heads * head_dim * 4.0 > kMaxBytes ||
+        static_cast<double>(B) * Lk * kv_heads * head_dim * 4.0 > kMaxBytes)
+        return fail(RF_ERR_RANGE, "%s: sizes overflow 64-bit byte counts", fn);
+    if ((static_cast<double>(Lq) / 32 + 1) * B * heads > 2147483647.0)
+        return fail(RF_ERR_RANGE, "%s: more than 2^31 - 1 query tiles", fn);
+    return RF_OK;
+}
+
+// The compute units an operator's workspace is planned for (0: the current device's).
+static int plan_units(int32_t compute_units, int32_t *cus, const char *fn) {
+    if (compute_units < 0 || compute_units > RF_MAX_COMPUTE_UNITS)
+        return fail(RF_ERR_RANGE, "%s: compute_units = %d outside 0..%d", fn, compute_units, RF_MAX_COMPUTE_UNITS);
+    *cus = compute_units;
+    if (compute_units > 0) return RF_OK;
+    rf::DeviceGeometry geo;
+    const int rc = query_geometry(&geo, fn);
+    if (rc == RF_OK) *cus = geo.cus;
+    return rc;
+}
+
+int rf_cross_attention_workspace(int32_t B, int32_t Lq, int32_t Lk, int32_t heads, int32_t kv_heads,
+                                 int32_t head_dim, int32_t dtype, int32_t compute_units, int64_t *bytes_out) {
+    const char *fn = "rf_cross_attention_workspace";
+    if (!bytes_out) return fail(RF_ERR_INVALID_ARG, "%s: NULL output", fn);
+    int rc = cross_sizes(B, Lq, Lk, heads, kv_heads, head_dim, dtype, fn);
+    if (rc != RF_OK) return rc;
+    int32_t cus = 0;
+    rc = plan_units(compute_units, &cus, fn);
+    if (rc != RF_OK) return rc;
+    *bytes_out = rf::cross_workspace(B, Lq, Lk, heads, kv_heads, head_dim, dtype, cus);
+    return ok();
+}
+
+// Bytes from the first to behind the last element of a [B][L][heads][head_dim]
+// tensor of these strides (elements), or -1 where that passes kMaxBytes.
+static int64_t strided_bytes(const int64_t (&st)[3], int64_t B, int64_t L, int64_t heads, int64_t d, int64_t esize) {
+    const double top = (static_cast<double>(B - 1) * st[0] + static_cast<double>(L - 1) * st[1] +
+                        static_cast<double>(heads - 1) * st[2] + d) * esize;
+    if (top > kMaxBytes) return -1;
+    return ((B - 1) * st[0] + (L - 1) * st[1] + (heads - 1) * st[2] + d) * esize;
+}
+
+// No element of a tensor of these strides lies in another's place: taken from the
+// shortest stride up, each passes everything that the ones before span.
+static bool distinct(const int64_t (&st)[3], int64_t B, int64_t L, int64_t heads, int64_t d) {
+    const int64_t n[3] = {B, L, heads};
+    bool used[3] = {n[0] == 1, n[1] == 1, n[2] == 1};
+    double span = static_cast<double>(d);
+    for (int i = 0; i < 3; ++i) {
+        int at = -1;
+        for (int j = 0; j < 3; ++j)
+            if (!used[j] && (at < 0 || st[j] < st[at])) at = j;
+        if (at < 0) break;
+        if (static_cast<double>(st[at]) < span) return false;
+        span += static_cast<double>(st[at]) * static_cast<double>(n[at] - 1);
+        used[at] = true;
+    }
+    return true;
+}
+
+int rf_cross_attention(const void *q, const void *k, const void *v, void *out, const int32_t *kv_lengths,
+                       const uint8_t *key_mask, int32_t B, int32_t Lq, int32_t Lk, int32_t heads,
+                       int32_t kv_heads, int32_t head_dim, const rf_cross_layout *layout, int32_t dtype,
+                       void *workspace, int64_t workspace_bytes, void *stream) {
+    const char *fn = "rf_cross_attention";
+    if (!q || !k || !v || !out) return fail(RF_ERR_INVALID_ARG, "%s: NULL tensor", fn);
+    int rc = cross_sizes(B, Lq, Lk, heads, kv_heads, head_dim, dtype, fn);
+    if (rc != RF_OK) return rc;
+    rf::CrossParams p{};
+    const int64_t esize = dtype == RF_F32 ? 4 : 2;
+    const int64_t qrow = static_cast<int64_t>(heads) * head_dim, krow = static_cast<int64_t>(kv_heads) * head_dim;
+    const rf_cross_layout plain = {{Lq * qrow, qrow, head_dim}, {Lk * krow, krow, head_dim},
+                                   {Lk * krow, krow, head_dim}, {Lq * qrow, qrow, head_dim}};
+    const rf_cross_layout &l = layout ? *layout : plain;
+    const int64_t *const sets[4] = {l.q, l.k, l.v, l.out};
+    int64_t *const dst[4] = {p.qs, p.ks, p.vs, p.os};
+    for (int i = 0; i < 4; ++i)
+        for (int j = 0; j < 3; ++j) {
+            if (sets[i][j] < 0) return fail(RF_ERR_INVALID_ARG, "%s: negative stride", fn);
+            if (static_cast<double>(sets[i][j]) * 4.0 > kMaxBytes) return fail(RF_ERR_RANGE, "%s: a stride overflows", fn);
+            if (sets[i][j] * esize % 16 != 0)
+                return fail(RF_ERR_UNSUPPORTED, "%s: strides must be multiples of 16 bytes", fn);
+            dst[i][j] = sets[i][j];
+        }
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out))
+        return fail(RF_ERR_UNSUPPORTED, "%s: pointers must be 16-byte aligned", fn);
+    if (reinterpret_cast<uintptr_t>(kv_lengths) & 3u)
+        return fail(RF_ERR_UNSUPPORTED, "%s: kv_lengths must be 4-byte aligned", fn);
+    // (byte offsets inside a tile of keys are 32-bit)
+    if (p.ks[1] * esize >= (1 << 24) || p.vs[1] * esize >= (1 << 24))
+        return fail(RF_ERR_UNSUPPORTED, "%s: a token stride of k or v reaches 16 MB", fn);
+    if (!distinct(p.os, B, Lq, heads, head_dim))
+        return fail(RF_ERR_INVALID_ARG, "%s: out's strides put elements into one place", fn);
+    const int64_t qb = strided_bytes(p.qs, B, Lq, heads, head_dim, esize);
+    const int64_t kb = strided_bytes(p.ks, B, Lk, kv_heads, head_dim, esize);
+    const int64_t vb = strided_bytes(p.vs, B, Lk, kv_heads, head_dim, esize);
+    const int64_t ob = strided_bytes(p.os, B, Lq, heads, head_dim, esize);
+    if (qb < 0 || kb < 0 || vb < 0 || ob < 0) return fail(RF_ERR_RANGE, "%s: strides overflow 64-bit byte counts", fn);
+    const int64_t mask_bytes = static_cast<int64_t>(B) * Lk;
+    if (overlaps(out, ob, q, qb) || overlaps(out, ob, k, kb) || overlaps(out, ob, v, vb) ||
+        (kv_lengths && overlaps(out, ob, kv_lengths, 4 * static_cast<int64_t>(B))) ||
+        (key_mask && overlaps(out, ob, key_mask, mask_bytes)))
+        return fail(RF_ERR_INVALID_ARG, "%s: out overlaps an input", fn);
+    if (workspace) {
+        if (workspace_bytes < 0) return fail(RF_ERR_INVALID_ARG, "%s: workspace_bytes < 0", fn);
+        if (!aligned16(workspace)) return fail(RF_ERR_UNSUPPORTED, "%s: workspace must be 16-byte aligned", fn);
+        const int64_t wb = workspace_bytes;
+        if (wb > 0 && (overlaps(workspace, wb, q, qb) || overlaps(workspace, wb, k, kb) ||
+                       overlaps(workspace, wb, v, vb) || overlaps(workspace, wb, out, ob) ||
+                       (kv_lengths && overlaps(workspace, wb, kv_lengths, 4 * static_cast<int64_t>(B))) ||
+                       (key_mask && overlaps(workspace, wb, key_mask, mask_bytes))))
+            return fail(RF_ERR_INVALID_ARG, "%s: workspace overlaps a tensor", fn);
+    }
+    rc = query_geometry(&p.geo, fn);
+    if (rc != RF_OK) return rc;
+    if (workspace) {
+        const int64_t need = rf::cross_workspace(B, Lq, Lk, heads, kv_heads, head_dim, dtype, p.geo.cus);
+        if (workspace_bytes < need)
+            return fail(RF_ERR_INVALID_ARG, "%s: workspace of %lld bytes, %lld needed on %d compute units", fn,
+                        static_cast<long long>(workspace_bytes), static_cast<long long>(need), p.geo.cus);
+        p.ws = need > 0 ? workspace : nullptr;
+    }
+    p.q = q;
+    p.k = k;
+    p.v = v;
+    p.out = out;
+    p.kv_lengths = kv_lengths;
+    p.key_mask = key_mask;
+    p.B = B;
+    p.Lq = Lq;
+    p.Lk = Lk;
+    p.heads = heads;
+    p.kv_heads = kv_heads;
+    p.head_dim = head_dim;
+    p.dtype = dtype;
+    return launched(rf::launch_cross(p, static_cast<hipStream_t>(stream)), fn);
+}
+
+// Sizes common to a matrix product and its workspace query.
+static int linear_sizes(int32_t M, int64_t N, int32_t K, int32_t n_out, int32_t dtype, const char *fn) {
+    if (M <= 0 || N <= 0 || K <= 0 || n_out <= 0)
+        return fail(RF_ERR_INVALID_ARG, "%s: sizes must be positive (M=%d rows_per_frame=%lld in=%d out=%d)", fn, M,
+                    static_cast<long long>(N), K, n_out);
+    if (static_cast<double>(M) * static_cast<double>(N) > 2147483647.0)
+        return fail(RF_ERR_RANGE, "%s: %d frames of %lld rows exceed 2^31 - 1 rows", fn, M, static_cast<long long>(N));
+    if (dtype != RF_BF16 && dtype != RF_F32) return fail(RF_ERR_UNSUPPORTED, "%s: unknown dtype %d", fn, dtype);
+    const int32_t vec = dtype == RF_F32 ? 4 : 8;
+    if (K % vec != 0 || n_out % vec != 0)
+        return fail(RF_ERR_UNSUPPORTED, "%s: %d in_features or %d out_features make no rows of 16-byte multiples", fn,
+                    K, n_out);
+    // (byte offsets inside a tile of 256 rows are 32-bit)
+    if (K >= (1 << 23) / (dtype == RF_F32 ? 4 : 2))
+        return fail(RF_ERR_UNSUPPORTED, "%s: rows of in_features = %d reach 8 MB", fn, K);
+    return RF_OK;
+}
+
+int rf_frame_linear_workspace(int32_t M, int64_t rows_per_frame, int32_t in_features, int32_t out_features,
+                              int32_t dtype, int32_t compute_units, int64_t *bytes_out) {
+    const char *fn = "rf_frame_linear_workspace";
+    if (!bytes_out) return fail(RF_ERR_INVALID_ARG, "%s: NULL output", fn);
+    int rc = linear_sizes(M, rows_per_frame, in_features, out_features, dtype, fn);
+    if (rc != RF_OK) return rc;
+    int32_t cus = 0;
+    rc = plan_units(compute_units, &cus, fn);
+    if (rc != RF_OK) return rc;
+    *bytes_out = rf::linear_workspace(M * rows_per_frame, in_features, out_features, dtype, cus);
+    return ok();
+}
+
+int rf_frame_linear(const void *x, const void *weight, const void *bias, const void *gate, const void *residual,
+                    void *y, const int32_t *frame_ids, int32_t M, int32_t T, int64_t rows_per_frame,
+                    int32_t in_features, int32_t out_features, int32_t activation, uint32_t flags, int32_t dtype,
+                    void *workspace, int64_t workspace_bytes, void *stream) {
+    const char *fn = "rf_frame_linear";
+    if (!x || !weight || !y) return fail(RF_ERR_INVALID_ARG, "%s: NULL tensor", fn);
+    if (flags & ~(RF_ROWS_IN_FULL | RF_ROWS_OUT_FULL | RF_GATE_PER_FRAME))
+        return fail(RF_ERR_INVALID_ARG, "%s: unknown flags 0x%x", fn, flags);
+    if ((flags & RF_GATE_PER_FRAME) && !gate) return fail(RF_ERR_INVALID_ARG, "%s: a gate per frame needs a gate", fn);
+    if (activation < RF_ACT_NONE || activation > RF_ACT_SILU)
+        return fail(RF_ERR_INVALID_ARG, "%s: unknown activation %d", fn, activation);
+    int32_t ids[RF_MAX_FRAMES];
+    int rc = check_id_list(frame_ids, M, T, ids, fn);
+    if (rc != RF_OK) return rc;
+    rc = linear_sizes(M, rows_per_frame, in_features, out_features, dtype, fn);
+    if (rc != RF_OK) return rc;
+    if (static_cast<double>(T) * static_cast<double>(rows_per_frame) * (in_features > out_features ? in_features : out_features) * 4.0 >
+        kMaxBytes)
+        return fail(RF_ERR_RANGE, "%s: sizes overflow 64-bit byte counts", fn);
+    if (!aligned16(x) || !aligned16(weight) || !aligned16(y) || !aligned16(bias) || !aligned16(gate) ||
+        !aligned16(residual))
+        return fail(RF_ERR_UNSUPPORTED, "%s: pointers must be 16-byte aligned", fn);
+    const int64_t esize = dtype == RF_F32 ? 4 : 2;
+    const int64_t in_rows = rows_per_frame * ((flags & RF_ROWS_IN_FULL) ? T : M);
+    const int64_t out_rows = rows_per_frame * ((flags & RF_ROWS_OUT_FULL) ? T : M);
+    const int64_t out_row = out_features * esize;
+    struct Range {
+        const void *p;
+        int64_t n;
+    };
+    const Range ins[5] = {{x, in_rows * in_features * esize},
+                          {weight, static_cast<int64_t>(out_features) * in_features * esize},
+                          {bias, out_row},
+                          {gate, out_row * ((flags & RF_GATE_PER_FRAME) ? T : 1)},
+                          {residual == y ? nullptr : residual, out_rows * out_row}};
+    for (const Range &r : ins)
+        if (r.p && overlaps(y, out_rows * out_row, r.p, r.n))
+            return fail(RF_ERR_INVALID_ARG, "%s: y overlaps an input", fn);
+    if (workspace) {
+        if (workspace_bytes < 0) return fail(RF_ERR_INVALID_ARG, "%s: workspace_bytes < 0", fn);
+        if (!aligned16(workspace)) return fail(RF_ERR_UNSUPPORTED, "%s: workspace must be 16-byte aligned", fn);
+        if (workspace_bytes > 0) {
+            bool hit = overlaps(workspace, workspace_bytes, y, out_rows * out_row);
+            for (const Range &r : ins) hit = hit || (r.p && overlaps(workspace, workspace_bytes, r.p, r.n));
+            if (hit) return fail(RF_ERR_INVALID_ARG, "%s: workspace overlaps a tensor", fn);
+        }
+    }
+    rf::LinearParams p{};
+    rc = query_geometry(&p.geo, fn);
+    if (rc != RF_OK) return rc;
+    if (workspace) {
+        const int64_t need = rf::linear_workspace(M * rows_per_frame, in_features, out_features, dtype, p.geo.cus);
+        if (workspace_bytes < need)
+            return fail(RF_ERR_INVALID_ARG, "%s: workspace of %lld bytes, %lld needed on %d compute units", fn,
+                        static_cast<long long>(workspace_bytes), static_cast<long long>(need), p.geo.cus);
+        p.ws = need > 0 ? workspace : nullptr;
+    }
+    p.x = x;
+    p.weight = weight;
+    p.bias = bias;
+    p.gate = gate;
+    p.residual = residual;
+    p.y = y;
+    p.N = rows_per_frame;
+    p.M = M;
+    p.K = in_features;
+    p.n_out = out_features;
+    p.activation = activation;
+    p.dtype = dtype;
+    p.gate_rows = (flags & RF_GATE_PER_FRAME) != 0;
+    for (int32_t m = 0; m < M; ++m) p.frame[m] = static_cast<int16_t>(ids[m]);
+    row_frames(ids, M, (flags & RF_ROWS_IN_FULL) != 0, p.src_frame);
+    row_frames(ids, M, (flags & RF_ROWS_OUT_FULL) != 0, p.dst_frame);
+    return launched(rf::launch_linear(p, static_cast<hipStream_t>(stream)), fn);
+}
+
 int rf_probe_mfma_bf16(const void *operands, int32_t workgroups, int32_t rounds, float *sink, void *stream) {
     const char *fn = "rf_probe_mfma_bf16";
     if (!operands || !sink) return fail(RF_ERR_INVALID_ARG, "%s: NULL argument", fn);

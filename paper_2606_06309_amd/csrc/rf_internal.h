@@ -159,6 +159,70 @@ struct SimParams {
 
 hipError_t launch_similarity(const SimParams &p, hipStream_t stream);
 
+// Rotary positions: tensor 0 is q, tensor 1 is k (heads[1] = 0: none). Strides
+// in elements; row r of the call is row src_frame[m] * N + n of x and
+// dst_frame[m] * N + n of y (m = r / N).
+constexpr int kMaxRotaryPairs = 128;
+struct RotaryParams {
+    const void *x[2];
+    void *y[2];
+    int64_t x_stride[2];
+    int64_t y_stride[2];
+    int32_t heads[2];
+    int32_t head_dim;
+    int32_t dtype;
+    int32_t M, H, W;
+    int32_t halves;
+    int32_t pairs;                       // R / 2
+    int32_t pair_end[2];                 // pairs of axis 0, and of axes 0 and 1
+    double origin[3], step[3];
+    double turns[kMaxRotaryPairs];       // each pair's turns per unit of position, negative for the inverse
+    int16_t frame[kMaxFrames];           // frame index, the position on the time axis
+    int16_t src_frame[kMaxFrames];
+    int16_t dst_frame[kMaxFrames];
+};
+
+hipError_t launch_rotary(const RotaryParams &p, hipStream_t stream);
+
+// Cross attention; strides {batch, token, head} in elements.
+struct CrossParams {
+    const void *q, *k, *v;
+    void *out;
+    const int32_t *kv_lengths;   // device [B] or NULL
+    const uint8_t *key_mask;     // device [B][Lk] or NULL
+    int32_t B, Lq, Lk, heads, kv_heads, head_dim;
+    int32_t dtype;
+    int64_t qs[3], ks[3], vs[3], os[3];
+    void *ws;                    // NULL: no split
+    DeviceGeometry geo;
+};
+
+// Bytes of workspace the launch's split of the key axis takes (0: none).
+int64_t cross_workspace(int32_t B, int32_t Lq, int32_t Lk, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                        int32_t dtype, int32_t cus);
+hipError_t launch_cross(const CrossParams &p, hipStream_t stream);
+
+// Matrix product with epilogue: y = residual + gate * act(x weight^T + bias).
+// Row r of the product is row src_frame[m] * N + n of x and dst_frame[m] * N + n of
+// y and residual (m = r / N); gate row frame[m] with gate_rows, else row 0.
+struct LinearParams {
+    const void *x, *weight, *bias, *gate, *residual;
+    void *y;
+    int64_t N;                   // rows per frame
+    int32_t M, K, n_out;
+    int32_t activation;
+    int32_t dtype;
+    int32_t gate_rows;
+    int16_t frame[kMaxFrames];
+    int16_t src_frame[kMaxFrames];
+    int16_t dst_frame[kMaxFrames];
+    void *ws;                    // NULL: no split
+    DeviceGeometry geo;
+};
+
+int64_t linear_workspace(int64_t rows, int32_t K, int32_t n_out, int32_t dtype, int32_t cus);
+hipError_t launch_linear(const LinearParams &p, hipStream_t stream);
+
 // Device probes (measurement support): threads per workgroup of the matrix and
 // LDS probes, and of the HBM read probe.
 constexpr int kProbeThreads = 256;

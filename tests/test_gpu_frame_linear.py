@@ -1,0 +1,173 @@
+"""Matrix product with bias, activation, gate and residual against its definition in 64 bits."""
+import pytest
+import torch
+
+import block_reference as ref
+
+rf = pytest.importorskip("paper_2606_06309_amd.binding")
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def draw(shape, dtype, seed, scale=1.0):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return (torch.randn(shape, generator=g, device="cuda", dtype=F32) * scale).to(dtype)
+
+
+# rows, in_features, out_features: one row and many, edges of every tile, odd numbers of 8 features
+SIZES = [(1, 8, 8), (1, 1536, 1536), (2, 24, 40), (6, 1536, 9216), (15, 40, 264), (16, 256, 128), (17, 264, 136),
+         (33, 64, 1000), (63, 72, 64), (64, 128, 128), (65, 520, 72), (100, 5120, 96), (128, 64, 256), (129, 192, 248),
+         (255, 320, 264), (256, 256, 256), (257, 1000, 520), (500, 4096, 320), (700, 136, 1544), (1581, 320, 960),
+         (300, 9000, 256), (2100, 64, 2056)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("size", SIZES)
+def test_sizes(size, dtype):
+    rows, K, n = size
+    x, w = draw((rows, K), dtype, 1), draw((n, K), dtype, 2, K ** -0.5)
+    ref.assert_within(rf.rf_frame_linear(x, w), *ref.linear(x, w), f"{size}")
+    b, g, r = draw((n,), dtype, 3), draw((n,), dtype, 4), draw((rows, n), dtype, 5)
+    y = rf.rf_frame_linear(x, w, b, "gelu_tanh", g, r)
+    ref.assert_within(y, *ref.linear(x, w, b, "gelu_tanh", g, r), f"{size}")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("act", ["none", "gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("rows", [3, 200, 1100])
+def test_epilogue(rows, act, dtype):
+    """Every part of the epilogue alone and with the others; large arguments of the activations among them."""
+    K, n = 96, 328
+    x, w = draw((rows, K), dtype, 6), draw((n, K), dtype, 7, 0.6)
+    b, g, r = draw((n,), dtype, 8), draw((n,), dtype, 9), draw((rows, n), dtype, 10)
+    w[:8] *= 40
+    for bias in (None, b):
+        for gate in (None, g):
+            for res in (None, r):
+                ref.assert_within(rf.rf_frame_linear(x, w, bias, act, gate, res), *ref.linear(x, w, bias, act, gate, res),
+                                  f"{act} {bias is None} {gate is None} {res is None}")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N", [1, 5, 63, 130, 700])
+@pytest.mark.parametrize("in_full,out_full", [(False, False), (False, True), (True, False), (True, True)])
+def test_frames(N, in_full, out_full, dtype):
+    T, ids, K, n = 7, [1, 2, 6], 72, 264
+    x, w = draw((T * N, K), dtype, 11), draw((n, K), dtype, 12, K ** -0.5)
+    b, gate = draw((n,), dtype, 13), draw((T, n), dtype, 14)
+    full = draw((T * N, n), dtype, 15)
+    pos = ref.positions(ids, N, "cuda")
+    want, bound = ref.linear(x[pos], w, b, "silu", gate[torch.tensor(ids, device="cuda")].repeat_interleave(N, 0), full[pos])
+    xs = x if in_full else x[pos]
+    res = full if out_full else full[pos]
+    kw = dict(frame_ids=ids, T=T, rows_per_frame=N, in_full=in_full, out_full=out_full)
+    out = draw(res.shape, dtype, 16)
+    old = out.clone()
+    rf.rf_frame_linear(xs, w, b, "silu", gate, res, out=out, **kw)
+    ref.assert_within(out[pos] if out_full else out, want, bound)
+    if out_full:
+        other = torch.ones(T * N, dtype=torch.bool, device="cuda")
+        other[pos] = False
+        assert torch.equal(out[other], old[other])
+    # in place on the residual: the same, and rows of other frames keep the residual
+    y = res.clone()
+    assert rf.rf_frame_linear(xs, w, b, "silu", gate, y, out=y, **kw) is y
+    assert torch.equal(y[pos] if out_full else y, out[pos] if out_full else out)
+    if out_full:
+        assert torch.equal(y[other], full[other])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_unlisted_rows_are_not_read(dtype):
+    """Rows of other frames, and the gates of other frames, hold NaN."""
+    T, ids, N, K, n = 4, [0, 3], 37, 128, 136
+    x, w, gate = draw((T * N, K), dtype, 17), draw((n, K), dtype, 18, K ** -0.5), draw((T, n), dtype, 19)
+    x[N:3 * N] = float("nan")
+    gate[1:3] = float("nan")
+    pos = ref.positions(ids, N, "cuda")
+    y = rf.rf_frame_linear(x, w, gate=gate, frame_ids=ids, T=T, rows_per_frame=N, in_full=True)
+    g = gate[torch.tensor(ids, device="cuda")].repeat_interleave(N, 0)
+    ref.assert_within(y, *ref.linear(x[pos], w, gate=g))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows", [4, 90, 600])
+def test_not_a_number_spoils_only_its_row_and_column(rows, dtype):
+    K, n = 264, 272
+    x, w = draw((rows, K), dtype, 20), draw((n, K), dtype, 21, K ** -0.5)
+    want, bound = ref.linear(x, w)
+    x[2, 7], w[5, K - 1] = float("nan"), float("inf")
+    y = rf.rf_frame_linear(x, w)
+    assert bool(torch.isnan(y[2]).all())
+    ok = torch.ones((rows, n), dtype=torch.bool, device="cuda")
+    ok[2], ok[:, 5] = False, False
+    assert not bool(torch.isfinite(y[:, 5]).any())
+    ref.assert_within(torch.where(ok, y.double(), 0), torch.where(ok, want, 0), torch.where(ok, bound, 0))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_activations_of_large_arguments(dtype):
+    """x = +-1, w = +-1 sums: arguments from -30000 to 30000, where the exponentials leave the range."""
+    K = 64
+    x = torch.ones((8, K), dtype=dtype, device="cuda")
+    w = torch.zeros((72, K), dtype=dtype, device="cuda")
+    for i in range(72):
+        w[i, 0] = (-1) ** i * 2.0 ** (i / 4.0 - 3)
+    for act in ("gelu", "gelu_tanh", "silu"):
+        ref.assert_within(rf.rf_frame_linear(x, w, activation=act), *ref.linear(x, w, act=act), act)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,K,n", [(1, 8192, 64), (70, 8192, 256), (200, 20000, 128)])
+def test_workspace_or_none(rows, K, n, dtype):
+    x, w, r = draw((rows, K), dtype, 22), draw((n, K), dtype, 23, K ** -0.5), draw((rows, n), dtype, 24)
+    want, bound = ref.linear(x, w, residual=r)
+    need = rf.rf_frame_linear_workspace(1, rows, K, n, dtype)
+    a = rf.rf_frame_linear(x, w, residual=r)
+    ref.assert_within(a, want, bound)
+    ws = torch.full((need + 4096,), 99, dtype=torch.uint8, device="cuda")
+    b = rf.rf_frame_linear(x, w, residual=r, workspace=ws[:max(need, 16)])
+    assert torch.equal(a, b) and bool((ws[max(need, 16):] == 99).all())
+    out = torch.empty_like(a)
+    ids = rf._FRAME0
+    rf._check(rf.lib.rf_frame_linear(x.data_ptr(), w.data_ptr(), None, None, r.data_ptr(), out.data_ptr(),
+                                     rf._addr(ids), 1, 1, rows, K, n, 0, 0, rf._dtype_code(dtype), None, 0,
+                                     rf._stream(None)))
+    ref.assert_within(out, want, bound)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,K,n", [(2, 2048, 256), (300, 4096, 256), (900, 128, 640)])
+def test_stream_and_graph(rows, K, n, dtype):
+    x, w, r = draw((rows, K), dtype, 25), draw((n, K), dtype, 26, K ** -0.5), draw((rows, n), dtype, 27)
+    eager = rf.rf_frame_linear(x, w, residual=r)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    y = rf.rf_frame_linear(x, w, residual=r, stream=s)
+    s.synchronize()
+    assert torch.equal(y, eager)
+    out = torch.empty_like(eager)
+    ws = torch.empty(max(16, rf.rf_frame_linear_workspace(1, rows, K, n, dtype)), dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        rf.rf_frame_linear(x, w, residual=r, out=out, workspace=ws)
+    for i in range(4):
+        x.copy_(draw(x.shape, dtype, 40 + i))
+        out.fill_(5.0)
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, rf.rf_frame_linear(x, w, residual=r))
+
+
+def test_offsets_past_32_bits():
+    """x and y of more than 4 GB; the first and last rows are checked."""
+    rows, K, n = 1_100_000, 2048, 2048
+    x = torch.zeros((rows, K), dtype=BF16, device="cuda")
+    w = draw((n, K), BF16, 28, K ** -0.5)
+    at = torch.tensor([0, 1, rows // 2, rows - 257, rows - 2, rows - 1], device="cuda")
+    x[at] = draw((6, K), BF16, 29)
+    y = rf.rf_frame_linear(x, w)
+    ref.assert_within(y[at], *ref.linear(x[at], w))
+    assert not bool(y[2:1000].any())
