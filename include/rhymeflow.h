@@ -651,17 +651,19 @@ typedef struct rf_cross_layout {
  *   out = softmax over the valid keys of (q k^T / sqrt(head_dim)) v,
  * with h reading the keys and values of head h / (heads / kv_heads). Key j of
  * sequence b is valid where j < kv_lengths[b] and key_mask[b][j] != 0. A query
- * without any valid key gives a row of zeros. Keys and values that are not valid
+ * without any valid key, or whose valid scores are all -infinity, gives zeros. Keys and values that are not valid
  * have no effect, whatever they hold (infinities and NaN among it).
  *
  * q, out: device [B][Lq][heads][head_dim]; k, v: device [B][Lk][kv_heads][head_dim],
  *   contiguous in this order (layout == NULL) or of layout's strides: multiples of
  *   16 bytes, not negative; an input's stride may be 0 (one prompt for a whole
- *   batch), out's elements must be distinct. out must not overlap the memory
+ *   batch) but for the token strides of k and v, which are head_dim or more with
+ *   Lk > 1; out's elements must be distinct. out must not overlap the memory
  *   between the first and last element of q, k or v.
  * kv_lengths: device int32 [B], or NULL (Lk for all); read by the kernel, values
  *   outside [0, Lk] count as the nearer end. key_mask: device bytes [B][Lk], or NULL.
- * B, Lq, Lk, heads: >= 1; heads a multiple of kv_heads. head_dim: 64 or 128.
+ * B, Lq, Lk, heads: >= 1, Lk <= 2^30, ceil(Lq / 32) * B * heads up to about 2^24;
+ *   heads a multiple of kv_heads. head_dim: 64 or 128.
  * dtype: RF_BF16 (products on the bf16 matrix cores, probabilities rounded to
  *   bf16 for the second one, fp32 softmax and sums, one rounding of the output) or
  *   RF_F32 (fp32 throughout).
@@ -673,8 +675,8 @@ typedef struct rf_cross_layout {
  *   Results of a split differ from those without in fp32 summation order and in
  *   the references that probabilities are rounded to bf16 against.
  * Errors: RF_ERR_INVALID_ARG (NULL, sizes <= 0, heads % kv_heads, strides, overlap,
- *   workspace too small), RF_ERR_RANGE (sizes whose byte counts or strides would
- *   pass 4e18, more than 2^31 - 1 query tiles), RF_ERR_UNSUPPORTED (head_dim, dtype,
+ *   workspace too small), RF_ERR_RANGE (sizes above these, byte counts or strides
+ *   that would pass 4e18), RF_ERR_UNSUPPORTED (head_dim, dtype,
  *   alignment, a token stride of 16 MB and more in k or v), RF_ERR_HIP.
  */
 int rf_cross_attention(const void *q, const void *k, const void *v, void *out, const int32_t *kv_lengths,

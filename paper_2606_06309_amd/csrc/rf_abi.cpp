@@ -1002,8 +1002,9 @@ static int cross_sizes(int32_t B, int32_t Lq, int32_t Lk, int32_t heads, int32_t
     if (static_cast<double>(B) * Lq * heads * head_dim * 4.0 > kMaxBytes ||
         static_cast<double>(B) * Lk * kv_heads * head_dim * 4.0 > kMaxBytes)
         return fail(RF_ERR_RANGE, "%s: sizes overflow 64-bit byte counts", fn);
-    if ((static_cast<double>(Lq) / 32 + 1) * B * heads > 2147483647.0)
-        return fail(RF_ERR_RANGE, "%s: more than 2^31 - 1 query tiles", fn);
+    if (Lk > (1 << 30)) return fail(RF_ERR_RANGE, "%s: Lk = %d exceeds 2^30", fn, Lk);
+    if ((static_cast<double>(Lq) / 32 + 1) * B * heads > 16777216.0)
+        return fail(RF_ERR_RANGE, "%s: more than 2^24 tiles of 32 queries", fn);
     return RF_OK;
 }
 
@@ -1087,6 +1088,10 @@ int rf_cross_attention(const void *q, const void *k, const void *v, void *out, c
         return fail(RF_ERR_UNSUPPORTED, "%s: pointers must be 16-byte aligned", fn);
     if (reinterpret_cast<uintptr_t>(kv_lengths) & 3u)
         return fail(RF_ERR_UNSUPPORTED, "%s: kv_lengths must be 4-byte aligned", fn);
+    // (keys past a tile's last valid one lie past its memory: tokens do not overlap)
+    if (Lk == 1) p.ks[1] = p.vs[1] = head_dim;
+    if (p.ks[1] < head_dim || p.vs[1] < head_dim)
+        return fail(RF_ERR_INVALID_ARG, "%s: a token stride of k or v is below head_dim", fn);
     // (byte offsets inside a tile of keys are 32-bit)
     if (p.ks[1] * esize >= (1 << 24) || p.vs[1] * esize >= (1 << 24))
         return fail(RF_ERR_UNSUPPORTED, "%s: a token stride of k or v reaches 16 MB", fn);

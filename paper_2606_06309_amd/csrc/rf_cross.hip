@@ -1,90 +1,628 @@
-// Attention to an encoder's states of another length for gfx950.
+// Attention to an encoder's states of another length for gfx950, bf16 (the fp32
+// kernels are in rf_cross_f32.hip).
 //
-// One wave per (sequence, head, query): lane l scores keys l, l + 64, ..., the
-// running maximum and sum of the softmax are the wave's, and lane l owns every
-// 64th dimension of the output.
-#include "rf_internal.h"
+// The method is that of keyframe-query attention, one pass over the keys with
+// a running softmax; what differs is that keys are few (a prompt) and rows many,
+// or rows few (a caption's next word) and keys many, that a sequence has a length
+// and a mask of its own, and that tensors come with strides.
+//
+//  * Scores are computed transposed, S^T = K Q^T (v_mfma_f32_32x32x16_bf16): K
+//    rows from LDS are the A operand, a wave's 32 query rows, in registers, the B
+//    operand. A lane then holds 16 of 32 scores of ONE row (lane l and l ^ 32
+//    share row l % 32), and those, rounded to bf16, are the B operand of
+//    O^T = V^T P^T as they stand. V^T operands are transposing LDS reads of the
+//    natural [key][dim] tile.
+//  * K and V tiles go from memory straight into LDS. The buffer resource of a tile
+//    ends at its last key within the sequence's length; a masked key's lanes load
+//    from past the resource. Either way the row reads as zero, so what the memory
+//    holds there (NaN, infinities) has no effect, and its score becomes -inf.
+//  * Softmax in the log2 domain against a reference that is a past row maximum,
+//    replaced when a row's probabilities of a tile sum to more than 256 (the sum
+//    bounds each of them). A walk's first tile takes its own maximum.
+#include "rf_cross.h"
 
 namespace rf {
 namespace {
 
-template <typename E>
-__device__ __forceinline__ float widen(E x);
-template <>
-__device__ __forceinline__ float widen<float>(float x) { return x; }
-template <>
-__device__ __forceinline__ float widen<uint16_t>(uint16_t x) { return __uint_as_float(static_cast<uint32_t>(x) << 16); }
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef short i16x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) i16x4_t lds_i16x4_t;
 
-__device__ __forceinline__ void put(float *p, float x) { *p = x; }
-__device__ __forceinline__ void put(uint16_t *p, float x) {
-    *p = __builtin_bit_cast(uint16_t, static_cast<__bf16>(x));
+constexpr float kInf = __builtin_huge_valf();
+constexpr float kRebaseBound = 256.0f;
+
+__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
+    const bf16x2_t v = {static_cast<__bf16>(lo), static_cast<__bf16>(hi)};
+    return __builtin_bit_cast(uint32_t, v);
+}
+__device__ __forceinline__ bf16x8_t as_bf16x8(u32x4_t w) { return __builtin_bit_cast(bf16x8_t, w); }
+__device__ __forceinline__ float add_bf16x2(uint32_t word, float acc) {
+    const bf16x2_t one = {static_cast<__bf16>(1.0f), static_cast<__bf16>(1.0f)};
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, word), one, acc, false);
 }
 
-template <typename E, int D>
-__global__ __launch_bounds__(256) void cross_kernel(const CrossParams p) {
-    __shared__ float qs[4][D];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * 4 + wave;
-    const int b = blockIdx.z, h = blockIdx.y, hk = h / (p.heads / p.kv_heads);
-    const bool live = i < p.Lq;
-    const E *q = static_cast<const E *>(p.q) + b * p.qs[0] + i * p.qs[1] + h * p.qs[2];
-    if (live)
-        for (int d = lane; d < D; d += 64) qs[wave][d] = widen(q[d]);
-    __syncthreads();
-    if (!live) return;
-    const E *k = static_cast<const E *>(p.k) + b * p.ks[0] + hk * p.ks[2];
-    const E *v = static_cast<const E *>(p.v) + b * p.vs[0] + hk * p.vs[2];
-    int n = p.Lk;
-    if (p.kv_lengths) n = p.kv_lengths[b] < 0 ? 0 : p.kv_lengths[b] < p.Lk ? p.kv_lengths[b] : p.Lk;
-    const uint8_t *mask = p.key_mask ? p.key_mask + static_cast<int64_t>(b) * p.Lk : nullptr;
-    const float scale = static_cast<float>(1.0 / sqrt(static_cast<double>(D)));
-    float m = -__builtin_huge_valf(), l = 0.0f, o[D / 64] = {};
-    bool any = false;
-    for (int j0 = 0; j0 < n; j0 += 64) {
-        const int j = j0 + lane;
-        const bool ok = j < n && (!mask || mask[j]);
-        const uint64_t valid = __ballot(ok);
-        if (valid == 0) continue;
-        any = true;
-        float s = -__builtin_huge_valf();
-        if (ok) {
-            s = 0.0f;
-            for (int d = 0; d < D; ++d) s = fmaf(qs[wave][d], widen(k[j * p.ks[1] + d]), s);
-            s *= scale;
-        }
-        float mx = s;
-        for (int x = 32; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor(mx, x));
-        mx = fmaxf(m, mx);
-        const float ref = mx == -__builtin_huge_valf() ? 0.0f : mx;
-        const float corr = m == -__builtin_huge_valf() ? 0.0f : expf(m - ref);
-        const float e = ok ? expf(s - ref) : 0.0f;
-        float sum = e;
-        for (int x = 32; x > 0; x >>= 1) sum += __shfl_xor(sum, x);
-        l = l * corr + sum;
-        for (int c = 0; c < D / 64; ++c) o[c] *= corr;
-        for (int t = 0; t < 64; ++t) {
-            if (!((valid >> t) & 1)) continue;
-            const float pt = __shfl(e, t);
-            for (int c = 0; c < D / 64; ++c) o[c] = fmaf(pt, widen(v[(j0 + t) * p.vs[1] + lane + 64 * c]), o[c]);
-        }
-        m = mx;
+// An LDS tile's rows are 2 D bytes without padding (a wave's load fills 1 KB of
+// them in order). The 16-byte slots of a row are permuted by the key so that the
+// 16 lanes of a K read, and the 32 of a transposing V read, meet different banks.
+template <int D>
+struct Tile {
+    static constexpr int kRow = 2 * D;
+    static constexpr int kSlots = kRow / 16;
+    static constexpr int kRowsPerWin = 256 / kRow;
+    static constexpr int kRowsPerLoad = 1024 / kRow;
+    __host__ __device__ static constexpr int kswz(int key) { return (key / kRowsPerWin) % kSlots; }
+    __host__ __device__ static constexpr int vswz(int key) { return 4 * ((key / kRowsPerWin) % (kSlots / 4)); }
+};
+
+// One wave's 32 query rows, their running softmax and O^T.
+template <int D>
+struct Wave {
+    u32x4_t qf[D / 16];
+    f32x16_t o[D / 32];
+    float m;      // reference: a past maximum of the raw scores, -inf before the first
+    float mref;   // m in the log2 domain, rounded; what probabilities are taken against
+    float l;      // this lane's part of the row sum
+};
+
+template <int D>
+__device__ __forceinline__ void start(const CrossKArgs &a, const CrossTile &t, int64_t row, int grp, Wave<D> &w) {
+    const uint16_t *q = static_cast<const uint16_t *>(a.q);
+    if (row < a.rows) {
+        const uint16_t *qp = q + row_offset(a, a.qs, t, row) + grp * 8;
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) w.qf[kk] = *reinterpret_cast<const u32x4_t *>(qp + kk * 16);
+    } else {
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) w.qf[kk] = u32x4_t{0u, 0u, 0u, 0u};
     }
-    E *out = static_cast<E *>(p.out) + b * p.os[0] + i * p.os[1] + h * p.os[2];
-    for (int c = 0; c < D / 64; ++c) put(out + lane + 64 * c, any ? o[c] / l : 0.0f);
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) w.o[db][r] = 0.0f;
+    w.m = w.mref = -kInf;
+    w.l = 0.0f;
+}
+
+// LDS offsets of a lane's K fragments (block 0) and of its V^T operand halves.
+template <int D>
+struct Fragments {
+    int k[D / 16], v[D / 32];
+    __device__ __forceinline__ explicit Fragments(int lane) {
+        using L = Tile<D>;
+        const int col = lane & 31, grp = lane >> 5;
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) k[kk] = col * L::kRow + (((2 * kk) ^ grp ^ L::kswz(col)) * 16);
+        const int g16 = (lane >> 4) & 1, j = lane & 15;
+        const int rr = grp * 4 + j / 4;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) v[db] = rr * L::kRow + (((2 * db + g16) ^ (L::vswz(rr) / 2)) * 32) + 8 * (j % 4);
+    }
+};
+
+// S^T of kNB blocks of 32 keys; fragments are read four ahead of the matrix core.
+template <int D, int kNB>
+__device__ __forceinline__ void scores(const uint8_t *kb, const Fragments<D> &f, const u32x4_t (&qf)[D / 16],
+                                       f32x16_t (&s)[kNB]) {
+    constexpr int kSteps = D / 16, kNF = kNB * kSteps, kLead = 4;
+    u32x4_t ring[kLead];
+    auto rd = [&](int i) {
+        return *reinterpret_cast<const u32x4_t *>(kb + f.k[i % kSteps] + (i / kSteps) * 32 * Tile<D>::kRow);
+    };
+#pragma unroll
+    for (int i = 0; i < kLead; ++i) ring[i] = rd(i);
+#pragma unroll
+    for (int i = 0; i < kNF; ++i) {
+        const int b = i / kSteps, kk = i % kSteps;
+        const f32x16_t c = kk == 0 ? f32x16_t{} : s[b];
+        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(ring[i % kLead]), as_bf16x8(qf[kk]), c, 0, 0, 0);
+        if (i + kLead < kNF) ring[i % kLead] = rd(i + kLead);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x100, kLead, 0);
+#pragma unroll
+    for (int i = 0; i < kNF - kLead; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, kLead, 0);
+}
+
+// O^T += V^T P^T of kNB blocks; operands are read three ahead.
+template <int D, int kNB>
+__device__ __forceinline__ void values(const uint8_t *vb, const Fragments<D> &f, const u32x4_t (&pw)[2 * kNB],
+                                       f32x16_t (&o)[D / 32]) {
+    constexpr int kNF = 2 * kNB * (D / 32), kLead = 3, kRow = Tile<D>::kRow;
+    u32x4_t ring[kLead];
+    auto rd = [&](int i) {
+        const uint8_t *p = vb + f.v[i % (D / 32)] + (i / (D / 32)) * 16 * kRow;
+        const i16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)p);
+        const i16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)(p + 8 * kRow));
+        return __builtin_shufflevector(__builtin_bit_cast(u32x2_t, lo), __builtin_bit_cast(u32x2_t, hi), 0, 1, 2, 3);
+    };
+#pragma unroll
+    for (int i = 0; i < kLead; ++i) ring[i] = rd(i);
+#pragma unroll
+    for (int i = 0; i < kNF; ++i) {
+        const int c = i / (D / 32), db = i % (D / 32);
+        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(ring[i % kLead]), as_bf16x8(pw[c]), o[db], 0, 0, 0);
+        if (i + kLead < kNF) ring[i % kLead] = rd(i + kLead);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x100, 2 * kLead, 0);
+#pragma unroll
+    for (int i = 0; i < kNF - kLead; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, kLead, 0);
+}
+
+// A reference so large that the rounding of its log2 form (2^-24 of it) would
+// show in a probability: then (s - m) * scale is formed instead.
+constexpr float kFarReference = 4096.0f;
+
+// Probabilities of kNB blocks of 32 keys, packed as the B operand of the second
+// product, and the running softmax. `bits`: the tile's valid keys.
+template <int D, int kNB>
+__device__ __forceinline__ void softmax(Wave<D> &w, f32x16_t (&s)[kNB], const uint64_t (&bits)[(kNB + 1) / 2], int grp,
+                                        float sl2, bool first, u32x4_t (&pw)[2 * kNB]) {
+#pragma unroll
+    for (int b = 0; b < kNB; ++b) {
+        const uint32_t word = static_cast<uint32_t>(bits[b / 2] >> (32 * (b % 2)));
+        if (word == 0xffffffffu) continue;
+        const uint32_t mine = word >> (4 * grp);   // accumulator r holds key (r/4)*8 + grp*4 + r%4
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            if (!((mine >> ((r / 4) * 8 + r % 4)) & 1u)) s[b][r] = -kInf;
+    }
+    auto probs = [&](float m, float mref) {
+        // four partial sums, of the rounded values that the matrix cores take
+        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        const bool far = __builtin_amdgcn_ballot_w64(fabsf(mref) > kFarReference && fabsf(mref) < kInf) != 0;
+        auto body = [&](auto arg) {
+#pragma unroll
+            for (int b = 0; b < kNB; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; r += 2) {
+                    const uint32_t word = pack_bf16x2(fast_exp2(arg(s[b][r])), fast_exp2(arg(s[b][r + 1])));
+                    sum[(r / 2) % 4] = add_bf16x2(word, sum[(r / 2) % 4]);
+                    pw[b * 2 + r / 8][(r % 8) / 2] = word;
+                }
+        };
+        if (far) {
+            const bool mine = fabsf(mref) > kFarReference;
+            body([&](float x) { return mine ? (x - m) * sl2 : fmaf(x, sl2, -mref); });
+        } else {
+            body([&](float x) { return fmaf(x, sl2, -mref); });
+        }
+        return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    };
+    float ls = 0.0f;
+    bool need = first;
+    if (!first) {
+        // (before any score is met mref is -inf: the sum is then inf or NaN)
+        ls = probs(w.m, w.mref);
+        need = !(halves_sum(ls) <= kRebaseBound);
+    }
+    if (need) {   // both lanes of a row take it
+        float mx = -kInf;
+#pragma unroll
+        for (int b = 0; b < kNB; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[b][r]);
+        const float m = fmaxf(w.m, halves_max(mx)), mref = m * sl2;
+        const bool far = fabsf(w.mref) > kFarReference || fabsf(mref) > kFarReference;
+        const float corr = w.m == -kInf ? 0.0f : fast_exp2(far ? (w.m - m) * sl2 : w.mref - mref);
+        w.m = m;
+        w.mref = mref;
+        w.l *= corr;
+        if (!first) {
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) w.o[db][r] *= corr;
+        }
+        // rows without any score above -inf so far: against 0 every probability is 0
+        ls = probs(m == -kInf ? 0.0f : m, m == -kInf ? 0.0f : mref);
+    }
+    w.l += ls;
+}
+
+// This wave's global->LDS loads i0 .. i0 + kN - 1 of a tile (each fills 1 KB).
+// bits: the valid keys, taken for masked launches only.
+template <int D, bool kMask, int kN>
+__device__ __forceinline__ void issue(const uint16_t *head, int64_t stride, int32_t key0, int32_t left,
+                                      const uint64_t (&bits)[2], uint8_t *dst, int i0, const int (&go)[kN], int lane) {
+    // the resource starts at the tile's first key and ends at the length's last one
+    const int64_t span = ((static_cast<int64_t>(left) - 1) * stride + D) * 2;
+    const int32_t rec = __builtin_amdgcn_readfirstlane(static_cast<int32_t>(
+        left <= 0 ? 0 : span < kNowhere ? span : kNowhere));
+    const __amdgpu_buffer_rsrc_t r =
+        __builtin_amdgcn_make_buffer_rsrc(uniform_ptr(head + key0 * stride), 0, rec, kBufferWord3);
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+        int at = go[i];
+        if constexpr (kMask) {
+            const int key = (i0 + i) * Tile<D>::kRowsPerLoad + lane / Tile<D>::kSlots;
+            const uint64_t word = key < 64 ? bits[0] : bits[1];
+            if (!((word >> (key & 63)) & 1)) at = kNowhere;
+        }
+        load_lds16(r, (lds_void_t *)(dst + (i0 + i) * 1024), at);
+    }
+}
+
+template <int D, bool kKey, int kN>
+__device__ __forceinline__ void load_offsets(int64_t stride, int i0, int lane, int (&go)[kN]) {
+    using L = Tile<D>;
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+        const int key = (i0 + i) * L::kRowsPerLoad + lane / L::kSlots, slot = lane % L::kSlots;
+        go[i] = static_cast<int>(key * stride * 2) + (slot ^ (kKey ? L::kswz(key) : L::vswz(key))) * 16;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Many rows: a workgroup of 4 waves owns 128 rows of one key head; its waves
+// share double-buffered tiles (64 KB of LDS), one barrier a tile.
+// ---------------------------------------------------------------------------
+
+constexpr int kTileWaves = 4;
+constexpr int kTileRows = 32 * kTileWaves;
+__host__ __device__ constexpr int tile_keys(int head_dim) { return head_dim == 64 ? 128 : 64; }
+
+template <int D, bool kMask>
+__global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu(2)))
+void cross_tile_kernel(const CrossKArgs a) {
+    constexpr int kBc = tile_keys(D), kNB = kBc / 32, kTileBytes = kBc * Tile<D>::kRow;
+    constexpr int kN = kTileBytes / 1024 / kTileWaves;
+    __shared__ __attribute__((aligned(1024))) uint8_t k0[kTileBytes];
+    __shared__ __attribute__((aligned(1024))) uint8_t k1[kTileBytes];
+    __shared__ __attribute__((aligned(1024))) uint8_t v0[kTileBytes];
+    __shared__ __attribute__((aligned(1024))) uint8_t v1[kTileBytes];
+    CrossTile t;
+    if (!cross_tile<kTileRows>(a, blockIdx.x, t)) return;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 31, grp = lane >> 5;
+    const int64_t row = t.row0 + wave * 32 + col;
+    const int32_t n = key_count(a, t.b);
+    const uint16_t *kh = static_cast<const uint16_t *>(a.k) + t.b * a.ks[0] + t.hk * a.ks[2];
+    const uint16_t *vh = static_cast<const uint16_t *>(a.v) + t.b * a.vs[0] + t.hk * a.vs[2];
+    int kgo[kN], vgo[kN];
+    load_offsets<D, true, kN>(a.ks[1], wave * kN, lane, kgo);
+    load_offsets<D, false, kN>(a.vs[1], wave * kN, lane, vgo);
+    auto tile_bits = [&](int32_t i, uint64_t (&bits)[2]) {
+        bits[0] = key_bits<kMask>(a, t.b, i * kBc, n, lane);
+        bits[1] = kBc == 128 ? key_bits<kMask>(a, t.b, i * kBc + 64, n, lane) : 0;
+    };
+    auto load = [&](int32_t i, const uint64_t (&bits)[2], uint8_t *kd, uint8_t *vd) {
+        issue<D, kMask, kN>(kh, a.ks[1], i * kBc, n - i * kBc, bits, kd, wave * kN, kgo, lane);
+        issue<D, kMask, kN>(vh, a.vs[1], i * kBc, n - i * kBc, bits, vd, wave * kN, vgo, lane);
+    };
+    const Fragments<D> f(lane);
+    Wave<D> w;
+    const int32_t tiles = static_cast<int32_t>((static_cast<int64_t>(n) + kBc - 1) / kBc);
+    uint64_t cur[2], nxt[2];
+    if (tiles > 0) {
+        tile_bits(0, cur);
+        load(0, cur, k0, v0);
+        tile_bits(1, nxt);
+    }
+    start<D>(a, t, row, grp, w);
+    auto compute = [&](int32_t i, const uint64_t (&bits)[2], const uint8_t *kb, const uint8_t *vb) {
+        if (kMask && bits[0] == 0 && bits[1] == 0 && i > 0) return;
+        f32x16_t s[kNB];
+        scores<D, kNB>(kb, f, w.qf, s);
+        u32x4_t pw[2 * kNB];
+        uint64_t word[(kNB + 1) / 2];
+#pragma unroll
+        for (int x = 0; x < (kNB + 1) / 2; ++x) word[x] = bits[x];
+        softmax<D, kNB>(w, s, word, grp, a.scale_log2, i == 0, pw);
+        values<D, kNB>(vb, f, pw, w.o);
+    };
+    auto tile_done = [&]() {
+        wait_loads<0>();   // this wave's loads have reached LDS
+        __syncthreads();
+    };
+    if (tiles > 0) tile_done();
+    for (int32_t i = 0; i < tiles; i += 2) {
+        uint64_t next[2];
+        if (i + 1 < tiles) {
+            load(i + 1, nxt, k1, v1);
+            tile_bits(i + 2, next);
+        }
+        compute(i, cur, k0, v0);
+        tile_done();
+        if (i + 1 >= tiles) break;
+        if (i + 2 < tiles) {
+            cur[0] = next[0];
+            cur[1] = next[1];
+            load(i + 2, cur, k0, v0);
+            tile_bits(i + 3, next);
+        }
+        compute(i + 1, nxt, k1, v1);
+        nxt[0] = next[0];
+        nxt[1] = next[1];
+        tile_done();
+    }
+    if (row >= a.rows) return;
+    const float l = halves_sum(w.l), inv = l == 0.0f ? 0.0f : 1.0f / l;
+    uint16_t *op = static_cast<uint16_t *>(a.out) + row_offset(a, a.os, t, row);
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int g4 = 0; g4 < 4; ++g4) {
+            const int r = g4 * 4;   // accumulator r holds dimension db*32 + (r/4)*8 + grp*4 + r%4
+            const u32x2_t x = {pack_bf16x2(w.o[db][r] * inv, w.o[db][r + 1] * inv),
+                               pack_bf16x2(w.o[db][r + 2] * inv, w.o[db][r + 3] * inv)};
+            *reinterpret_cast<u32x2_t *>(op + db * 32 + g4 * 8 + grp * 4) = x;
+        }
+}
+
+// ---------------------------------------------------------------------------
+// Few rows: a workgroup owns 32 rows and a part of the key axis, which its 8
+// waves share out (wave w of part p takes tiles 8 p + w, 8 p + w + 8 parts, ...),
+// each streaming tiles into LDS of its own, without barriers; the waves' results
+// are merged through LDS, the parts' by the join kernel.
+// ---------------------------------------------------------------------------
+
+constexpr int kFewWaves = 8;
+constexpr int kFewRows = 32;
+__host__ __device__ constexpr int few_keys(int head_dim) { return head_dim == 64 ? 64 : 32; }
+
+template <int D, bool kMask>
+__global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(2)))
+void cross_few_kernel(const CrossKArgs a) {
+    constexpr int kBc = few_keys(D), kNB = kBc / 32, kTileBytes = kBc * Tile<D>::kRow, kN = kTileBytes / 1024;
+    __shared__ __attribute__((aligned(1024))) uint8_t ks[kFewWaves * kTileBytes];
+    __shared__ __attribute__((aligned(1024))) uint8_t vs[kFewWaves * kTileBytes];
+    __shared__ float ml[kFewWaves][kFewRows][2];
+    const int part = blockIdx.x % a.parts;
+    CrossTile t;
+    if (!cross_tile<kFewRows>(a, blockIdx.x / a.parts, t)) return;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, grp = lane >> 5;
+    const int32_t n = key_count(a, t.b);
+    const uint16_t *kh = static_cast<const uint16_t *>(a.k) + t.b * a.ks[0] + t.hk * a.ks[2];
+    const uint16_t *vh = static_cast<const uint16_t *>(a.v) + t.b * a.vs[0] + t.hk * a.vs[2];
+    uint8_t *kb = ks + wave * kTileBytes, *vb = vs + wave * kTileBytes;
+    int kgo[kN], vgo[kN];
+    load_offsets<D, true, kN>(a.ks[1], 0, lane, kgo);
+    load_offsets<D, false, kN>(a.vs[1], 0, lane, vgo);
+    const Fragments<D> f(lane);
+    const int64_t tiles = (static_cast<int64_t>(n) + kBc - 1) / kBc;
+    const int64_t first = part * kFewWaves + wave, step = static_cast<int64_t>(a.parts) * kFewWaves;
+    auto tile_bits = [&](int64_t i, uint64_t (&bits)[2]) {
+        uint64_t x = key_bits<kMask>(a, t.b, static_cast<int32_t>(i) * kBc, n, lane);
+        if (kBc == 32) x &= 0xffffffffull;
+        bits[0] = x;
+        bits[1] = 0;
+    };
+    Wave<D> w;
+    uint64_t cur[2], nxt[2];
+    if (first < tiles) {
+        const int32_t key0 = static_cast<int32_t>(first) * kBc;
+        tile_bits(first, cur);
+        issue<D, kMask, kN>(kh, a.ks[1], key0, n - key0, cur, kb, 0, kgo, lane);
+        issue<D, kMask, kN>(vh, a.vs[1], key0, n - key0, cur, vb, 0, vgo, lane);
+    }
+    start<D>(a, t, t.row0 + col, grp, w);
+    if (first < tiles) {
+        asm volatile("" ::: "memory");
+        wait_loads<0>();
+        for (int64_t i = first; i < tiles; i += step) {
+            // (past the last tile it is fetched again and not used: with the loads on every
+            // path the waits below can be counted)
+            const int64_t next = i + step < tiles ? i + step : i;
+            const int32_t key0 = static_cast<int32_t>(next) * kBc;
+            tile_bits(next, nxt);
+            wait_loads<kN>();       // K is there; V may still be in flight
+            f32x16_t s[kNB];
+            scores<D, kNB>(kb, f, w.qf, s);
+            wait_lds_reads();       // K is read: its buffer is free
+            issue<D, kMask, kN>(kh, a.ks[1], key0, n - key0, nxt, kb, 0, kgo, lane);
+            u32x4_t pw[2 * kNB];
+            const uint64_t word[1] = {cur[0]};
+            softmax<D, kNB>(w, s, word, grp, a.scale_log2, i == first, pw);
+            wait_loads<kN>();       // V is there; the next K may still be in flight
+            values<D, kNB>(vb, f, pw, w.o);
+            wait_lds_reads();
+            issue<D, kMask, kN>(vh, a.vs[1], key0, n - key0, nxt, vb, 0, vgo, lane);
+            cur[0] = nxt[0];
+        }
+        wait_loads<0>();   // nothing lands in the buffers any more
+    }
+
+    // ---- merge: dimensions 0..63 of a wave's O rows go into its own K buffer, 64..127
+    // into its V buffer, 256 bytes a row, their 16-byte units permuted by row % 16 ----
+    const float l = halves_sum(w.l);
+    if (grp == 0) {
+        ml[wave][col][0] = w.m;
+        ml[wave][col][1] = l;
+    }
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int g4 = 0; g4 < 4; ++g4) {
+            const int unit = ((db % 2) * 8 + g4 * 2 + grp) ^ (col & 15);
+            *reinterpret_cast<f32x4_t *>((db < 2 ? kb : vb) + col * 256 + unit * 16) =
+                f32x4_t{w.o[db][g4 * 4], w.o[db][g4 * 4 + 1], w.o[db][g4 * 4 + 2], w.o[db][g4 * 4 + 3]};
+        }
+    __syncthreads();
+    const int r = tid / 16, unit = tid % 16;   // 512 threads: 32 rows x 16 units
+    const int64_t row = t.row0 + r;
+    if (row >= a.rows) return;
+    float m = ml[0][r][0];
+#pragma unroll
+    for (int p = 1; p < kFewWaves; ++p) m = fmaxf(m, ml[p][r][0]);
+    const float ref = m == -kInf ? 0.0f : m;
+    float wgt[kFewWaves], lsum = 0.0f;
+#pragma unroll
+    for (int p = 0; p < kFewWaves; ++p) {
+        wgt[p] = fast_exp2((ml[p][r][0] - ref) * a.scale_log2);
+        lsum = fmaf(wgt[p], ml[p][r][1], lsum);
+    }
+    const int64_t slot = (static_cast<int64_t>(t.tile) * a.parts + part) * kFewRows + r;
+    const float inv = a.parts > 1 ? 1.0f : lsum == 0.0f ? 0.0f : 1.0f / lsum;
+    if (a.parts > 1 && unit == 0) *reinterpret_cast<f32x2_t *>(a.ws_ml + slot * 2) = f32x2_t{m, lsum};
+    uint16_t *op = static_cast<uint16_t *>(a.out) + row_offset(a, a.os, t, row) + unit * 4;
+#pragma unroll
+    for (int half = 0; half < D / 64; ++half) {
+        f32x4_t x = {};
+#pragma unroll
+        for (int p = 0; p < kFewWaves; ++p) {
+            const f32x4_t y = *reinterpret_cast<const f32x4_t *>((half == 0 ? ks : vs) + p * kTileBytes + r * 256 +
+                                                                 (unit ^ (r & 15)) * 16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = fmaf(wgt[p], y[e], x[e]);
+        }
+        if (a.parts > 1) {
+            *reinterpret_cast<f32x4_t *>(a.ws_o + slot * D + half * 64 + unit * 4) = x;
+        } else {
+            const u32x2_t y = {pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv)};
+            *reinterpret_cast<u32x2_t *>(op + half * 64) = y;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Join of a split key axis: for each row the parts' references m_p (raw scores),
+// sums l_p and unnormalised outputs O_p give, with w_p = 2^((m_p - max m) scale),
+// sum w_p O_p / sum w_p l_p. A wave owns a row; parts are added in their order.
+// ---------------------------------------------------------------------------
+
+template <int D, typename E>
+__global__ __launch_bounds__(256) void cross_join_kernel(const CrossKArgs a) {
+    const int64_t id = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    CrossTile t;
+    t.tile = static_cast<int32_t>(id / kFewRows);
+    if (t.tile >= a.tiles) return;
+    const int r = static_cast<int>(id % kFewRows), head = t.tile / a.q_tiles;
+    t.row0 = static_cast<int64_t>(t.tile - head * a.q_tiles) * kFewRows;
+    t.b = head / a.kv_heads;
+    t.hk = head - t.b * a.kv_heads;
+    if (t.row0 + r >= a.rows) return;
+    const int64_t slot0 = static_cast<int64_t>(t.tile) * a.parts * kFewRows + r;
+    float m = -kInf;
+    for (int p = lane; p < a.parts; p += 64) m = fmaxf(m, a.ws_ml[(slot0 + static_cast<int64_t>(p) * kFewRows) * 2]);
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
+    const float ref = m == -kInf ? 0.0f : m;
+    constexpr int kE = D / 64;
+    float l = 0.0f, o[kE] = {};
+#pragma unroll 4
+    for (int p = 0; p < a.parts; ++p) {
+        const int64_t slot = slot0 + static_cast<int64_t>(p) * kFewRows;
+        const f32x2_t ml = *reinterpret_cast<const f32x2_t *>(a.ws_ml + slot * 2);
+        const float wgt = fast_exp2((ml[0] - ref) * a.scale_log2);
+        l = fmaf(wgt, ml[1], l);
+#pragma unroll
+        for (int e = 0; e < kE; ++e) o[e] = fmaf(wgt, a.ws_o[slot * D + lane * kE + e], o[e]);
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    E *op = static_cast<E *>(a.out) + row_offset(a, a.os, t, t.row0 + r) + lane * kE;
+#pragma unroll
+    for (int e = 0; e < kE; ++e) {
+        if constexpr (sizeof(E) == 4) op[e] = o[e] * inv;
+        else op[e] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(o[e] * inv));
+    }
+}
+
+// How a launch is cut: tiles of 128 rows, or of 32 with the keys shared out and
+// `parts` workgroups to a tile.
+struct CrossPlan {
+    bool few;
+    int32_t parts;
+    int64_t tiles;
+};
+
+CrossPlan cross_plan(int32_t B, int64_t rows, int32_t kv_heads, int32_t Lk, int32_t head_dim, int32_t cus) {
+    CrossPlan c{};
+    const int64_t heads = static_cast<int64_t>(B) * kv_heads;
+    const int64_t whole = (rows + kTileRows - 1) / kTileRows * heads, few = (rows + kFewRows - 1) / kFewRows * heads;
+    c.few = whole < 2 * cus;
+    c.tiles = c.few ? few : whole;
+    c.parts = 1;
+    if (c.few) {
+        const int64_t key_tiles = (static_cast<int64_t>(Lk) + few_keys(head_dim) - 1) / few_keys(head_dim);
+        const int64_t most = (key_tiles + 2 * kFewWaves - 1) / (2 * kFewWaves);   // two tiles a wave
+        const int64_t want = cus / few;
+        c.parts = static_cast<int32_t>(want < 1 ? 1 : want < most ? want : most);
+    }
+    return c;
 }
 
 }  // namespace
 
-int64_t cross_workspace(int32_t, int32_t, int32_t, int32_t, int32_t, int32_t, int32_t, int32_t) { return 0; }
+int64_t cross_workspace(int32_t B, int32_t Lq, int32_t Lk, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                        int32_t dtype, int32_t cus) {
+    if (dtype == RF_F32) return 0;
+    const CrossPlan c = cross_plan(B, static_cast<int64_t>(heads / kv_heads) * Lq, kv_heads, Lk, head_dim, cus);
+    return c.parts > 1 ? c.tiles * c.parts * kFewRows * (static_cast<int64_t>(head_dim) * 4 + 8) : 0;
+}
 
 hipError_t launch_cross(const CrossParams &p, hipStream_t stream) {
-    const int64_t blocks = (static_cast<int64_t>(p.Lq) + 3) / 4;
-    if (blocks > 0x7fffffffLL || p.heads > 65535 || p.B > 65535) return hipErrorInvalidConfiguration;
-    const dim3 grid(static_cast<uint32_t>(blocks), p.heads, p.B);
-    if (p.dtype == RF_F32 && p.head_dim == 128) hipLaunchKernelGGL((cross_kernel<float, 128>), grid, dim3(256), 0, stream, p);
-    else if (p.dtype == RF_F32) hipLaunchKernelGGL((cross_kernel<float, 64>), grid, dim3(256), 0, stream, p);
-    else if (p.head_dim == 128) hipLaunchKernelGGL((cross_kernel<uint16_t, 128>), grid, dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL((cross_kernel<uint16_t, 64>), grid, dim3(256), 0, stream, p);
+    const int32_t xcds = p.geo.xcds;
+    if (p.geo.cus < 1 || xcds < 1 || xcds > 64) return hipErrorInvalidValue;
+    CrossKArgs a{};
+    a.q = p.q;
+    a.k = p.k;
+    a.v = p.v;
+    a.out = p.out;
+    a.kv_lengths = p.kv_lengths;
+    a.key_mask = p.key_mask;
+    for (int i = 0; i < 3; ++i) {
+        a.qs[i] = p.qs[i];
+        a.ks[i] = p.ks[i];
+        a.vs[i] = p.vs[i];
+        a.os[i] = p.os[i];
+    }
+    a.Lq = p.Lq;
+    a.Lk = p.Lk;
+    a.kv_heads = p.kv_heads;
+    a.group = p.heads / p.kv_heads;
+    a.rows = static_cast<int64_t>(a.group) * p.Lq;
+    a.scale_log2 = static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(p.head_dim)));
+    a.xcds = xcds;
+    if (p.dtype == RF_F32) return launch_cross_f32(p, a, stream);
+    CrossPlan c = cross_plan(p.B, a.rows, p.kv_heads, p.Lk, p.head_dim, p.geo.cus);
+    if (!p.ws) c.parts = 1;
+    a.parts = c.parts;
+    const int64_t rows = c.few ? kFewRows : kTileRows;
+    if (c.tiles > 0x7fffffffLL / 64) return hipErrorInvalidConfiguration;
+    a.q_tiles = static_cast<int32_t>((a.rows + rows - 1) / rows);
+    a.tiles = static_cast<int32_t>(c.tiles);
+    a.per_xcd = (a.tiles + xcds - 1) / xcds;
+    const int64_t grid = static_cast<int64_t>(a.per_xcd) * xcds * c.parts;
+    if (grid > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    if (c.parts > 1) {
+        a.ws_o = static_cast<float *>(p.ws);
+        a.ws_ml = a.ws_o + c.tiles * c.parts * kFewRows * p.head_dim;
+    }
+    const dim3 g(static_cast<uint32_t>(grid)), block(64 * (c.few ? kFewWaves : kTileWaves));
+    const bool mask = p.key_mask != nullptr;
+    if (p.head_dim == 128) {
+        if (c.few && mask) hipLaunchKernelGGL((cross_few_kernel<128, true>), g, block, 0, stream, a);
+        else if (c.few) hipLaunchKernelGGL((cross_few_kernel<128, false>), g, block, 0, stream, a);
+        else if (mask) hipLaunchKernelGGL((cross_tile_kernel<128, true>), g, block, 0, stream, a);
+        else hipLaunchKernelGGL((cross_tile_kernel<128, false>), g, block, 0, stream, a);
+    } else {
+        if (c.few && mask) hipLaunchKernelGGL((cross_few_kernel<64, true>), g, block, 0, stream, a);
+        else if (c.few) hipLaunchKernelGGL((cross_few_kernel<64, false>), g, block, 0, stream, a);
+        else if (mask) hipLaunchKernelGGL((cross_tile_kernel<64, true>), g, block, 0, stream, a);
+        else hipLaunchKernelGGL((cross_tile_kernel<64, false>), g, block, 0, stream, a);
+    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || c.parts == 1) return e;
+    const dim3 jg(static_cast<uint32_t>(c.tiles * kFewRows / 4));
+    if (p.head_dim == 128) hipLaunchKernelGGL((cross_join_kernel<128, uint16_t>), jg, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((cross_join_kernel<64, uint16_t>), jg, dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 

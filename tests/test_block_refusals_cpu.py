@@ -77,7 +77,8 @@ def cross(q=dev(0), k=dev(1), v=dev(2), out=dev(3), lens=None, mask=None, B=2, L
     (dict(kvh=0), INVALID), (dict(kvh=3), INVALID), (dict(heads=2, kvh=4), INVALID), (dict(d=32), UNSUPPORTED),
     (dict(d=96), UNSUPPORTED), (dict(dtype=2), UNSUPPORTED), (dict(q=dev(0) + 2), UNSUPPORTED),
     (dict(out=dev(3) + 8), UNSUPPORTED), (dict(lens=dev(4) + 2), UNSUPPORTED),
-    (dict(B=2 ** 30, Lq=2 ** 30, heads=64, kvh=64), RANGE), (dict(B=2 ** 20, Lq=2 ** 18, heads=8, kvh=8), RANGE),
+    (dict(B=2 ** 30, Lq=2 ** 30, heads=64, kvh=64), RANGE), (dict(B=2 ** 16, Lq=2 ** 14, heads=8, kvh=8), RANGE),
+    (dict(Lk=2 ** 30 + 1), RANGE), (dict(layout=dict(k=(0, 56, 64))), INVALID), (dict(layout=dict(v=(0, 0, 64))), INVALID),
     (dict(out=dev(0)), INVALID), (dict(out=dev(1) + 64), INVALID), (dict(out=dev(2) - 256), INVALID),
     (dict(out=dev(3), lens=dev(3) + 16), INVALID), (dict(out=dev(3), mask=dev(3) + 5), INVALID),
     (dict(layout=dict(q=(-64, 256, 64))), INVALID), (dict(layout=dict(k=(0, 132, 64))), UNSUPPORTED),
