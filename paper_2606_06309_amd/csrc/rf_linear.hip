@@ -1,91 +1,539 @@
 // Matrix product with bias, activation, gate and residual in its epilogue for
 // gfx950: y = residual + gate * act(x W^T + bias), on the rows of listed frames.
 //
-// A workgroup of 256 threads owns 64 x 64 outputs; 16 reduction steps at a
-// time go through LDS, a thread owns 4 x 4 outputs.
-#include "rf_internal.h"
+// x and W both hold their reduction index contiguously, so a 16-byte piece of a
+// row of either is a lane's operand of a matrix instruction as it stands. Both
+// types work in the same bytes: a step is 128 bytes of every row, 64 bf16 or 32
+// fp32, and a pair of 16-byte pieces feeds one 32x32x16 bf16 instruction or four
+// 32x32x2 fp32 ones (whose two half-waves then hold reduction indices that are four
+// apart; both operands agree on it, and a sum's order is free).
+//
+// W's rows are the A operand, x's rows the B operand: a lane then holds one row
+// of y and runs of four features.
+//
+//  * linear_tile_kernel: a workgroup owns kBM rows x kBN features, 8 or 4 waves of
+//    32 kRB x 64. Steps go from memory straight into LDS, double-buffered, one
+//    barrier a step. Rows of 128 bytes are stored without padding, their eight
+//    16-byte slots permuted by (row / 2) % 8, so the 16 lanes of a read pass meet 16
+//    different slots of the 256-byte bank window.
+//  * linear_few_kernel: up to 64 rows, where reading W is all that costs: a workgroup
+//    owns 16 features, its 8 waves share out the reduction index, operands go
+//    straight to registers, and the waves' sums meet in LDS.
+//  * A reduction index may also be split over workgroups, whose fp32 parts go to the
+//    workspace; linear_join_kernel adds them in order and runs the epilogue.
+#include "rf_device.h"
 
 namespace rf {
 namespace {
 
-template <typename E>
-__device__ __forceinline__ float widen(E x);
-template <>
-__device__ __forceinline__ float widen<float>(float x) { return x; }
-template <>
-__device__ __forceinline__ float widen<uint16_t>(uint16_t x) { return __uint_as_float(static_cast<uint32_t>(x) << 16); }
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
-__device__ __forceinline__ void put(float *p, float x) { *p = x; }
-__device__ __forceinline__ void put(uint16_t *p, float x) {
-    *p = __builtin_bit_cast(uint16_t, static_cast<__bf16>(x));
+constexpr int kStep = 128;   // bytes of a row that a step takes
+
+struct LinearKArgs {
+    const uint8_t *x, *w;
+    const void *bias, *gate, *residual;
+    void *y;
+    float *ws;                 // parts > 1: [part][rows][n_out]
+    int64_t row_bytes;         // of x and W
+    uint32_t rows, N;          // N: rows per frame
+    int32_t n_out;
+    int32_t steps;             // of the whole reduction
+    int32_t steps_per_part, parts;
+    int32_t row_tiles, col_tiles, tiles, per_xcd, xcds;
+    int32_t activation, gate_rows;
+    int16_t frame[kMaxFrames], src_frame[kMaxFrames], dst_frame[kMaxFrames];
+};
+
+// What lanes past the end of a row load.
+__device__ const u32x4_t kZeros = {0u, 0u, 0u, 0u};
+
+// 16 bytes per lane from memory straight into LDS: lane l's bytes land at dst + 16 l.
+// (Kept out of the kernel templates: the host pass drops the launch stub of a
+// template that names this builtin.)
+__device__ __forceinline__ void global_lds16(const uint8_t *p, uint8_t *dst) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)p, (lds_void_t *)dst, 16, 0, 0);
 }
 
+template <typename E>
+__device__ __forceinline__ f32x16_t mma32(u32x4_t a, u32x4_t b, f32x16_t c) {
+    if constexpr (sizeof(E) == 2) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b),
+                                                       c, 0, 0, 0);
+    } else {
+        const f32x4_t fa = __builtin_bit_cast(f32x4_t, a), fb = __builtin_bit_cast(f32x4_t, b);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(fa[e], fb[e], c, 0, 0, 0);
+        return c;
+    }
+}
+template <typename E>
+__device__ __forceinline__ f32x4_t mma16(u32x4_t a, u32x4_t b, f32x4_t c) {
+    if constexpr (sizeof(E) == 2) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b),
+                                                       c, 0, 0, 0);
+    } else {
+        const f32x4_t fa = __builtin_bit_cast(f32x4_t, a), fb = __builtin_bit_cast(f32x4_t, b);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[e], fb[e], c, 0, 0, 0);
+        return c;
+    }
+}
+
+// kN (4 or 8) consecutive elements, widened / rounded once to nearest even.
+template <typename E, int kN>
+__device__ __forceinline__ void load_n(const void *p, int64_t at, float (&v)[kN]) {
+    if constexpr (sizeof(E) == 4) {
+#pragma unroll
+        for (int i = 0; i < kN; i += 4) {
+            const f32x4_t x = *reinterpret_cast<const f32x4_t *>(static_cast<const float *>(p) + at + i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[i + e] = x[e];
+        }
+    } else {
+        typedef uint32_t raw_t __attribute__((ext_vector_type(kN / 2)));
+        const raw_t x = *reinterpret_cast<const raw_t *>(static_cast<const uint16_t *>(p) + at);
+#pragma unroll
+        for (int e = 0; e < kN / 2; ++e) {
+            v[2 * e] = __uint_as_float(x[e] << 16);
+            v[2 * e + 1] = __uint_as_float(x[e] & 0xffff0000u);
+        }
+    }
+}
+template <typename E, int kN>
+__device__ __forceinline__ void store_n(void *p, int64_t at, const float (&v)[kN]) {
+    if constexpr (sizeof(E) == 4) {
+#pragma unroll
+        for (int i = 0; i < kN; i += 4)
+            *reinterpret_cast<f32x4_t *>(static_cast<float *>(p) + at + i) = f32x4_t{v[i], v[i + 1], v[i + 2], v[i + 3]};
+    } else {
+        typedef uint32_t raw_t __attribute__((ext_vector_type(kN / 2)));
+        raw_t x;
+#pragma unroll
+        for (int e = 0; e < kN / 2; ++e) {
+            const bf16x2_t b = {static_cast<__bf16>(v[2 * e]), static_cast<__bf16>(v[2 * e + 1])};
+            x[e] = __builtin_bit_cast(uint32_t, b);
+        }
+        *reinterpret_cast<raw_t *>(static_cast<uint16_t *>(p) + at) = x;
+    }
+}
+
+// x / (1 + 2^t): both sigmoid forms. 2^t = inf gives 0.
+__device__ __forceinline__ float gated(float x, float t) {
+    return x * __builtin_amdgcn_rcpf(1.0f + fast_exp2(t));
+}
 __device__ __forceinline__ float activate(int kind, float x) {
+    constexpr float kLog2e = 1.4426950408889634f;
     switch (kind) {
-        case RF_ACT_GELU: return 0.5f * x * (1.0f + erff(x * 0.70710678f));
-        case RF_ACT_GELU_TANH: return 0.5f * x * (1.0f + tanhf(0.79788456f * (x + 0.044715f * x * x * x)));
-        case RF_ACT_SILU: return x / (1.0f + expf(-x));
+        case RF_ACT_GELU: return 0.5f * x * (1.0f + erff(x * 0.70710678118654752f));
+        // x/2 (1 + tanh u) = x / (1 + e^(-2u))
+        case RF_ACT_GELU_TANH:
+            return gated(x, (-2.0f * 0.79788456080286536f * kLog2e) * (x + 0.044715f * (x * x * x)));
+        case RF_ACT_SILU: return gated(x, -kLog2e * x);
         default: return x;
     }
 }
 
-template <typename E>
-__global__ __launch_bounds__(256) void linear_kernel(const LinearParams p) {
-    __shared__ float xs[16][65], ws[16][65];
-    const int64_t rows = p.M * p.N;
-    const int64_t r0 = static_cast<int64_t>(blockIdx.y) * 64;
-    const int c0 = blockIdx.x * 64;
-    const int tid = threadIdx.x, tr = tid / 16, tc = tid % 16;
-    float acc[4][4] = {};
-    for (int k0 = 0; k0 < p.K; k0 += 16) {
-        for (int i = tid; i < 64 * 16; i += 256) {
-            const int kk = i % 16, rr = i / 16;
-            const int64_t r = r0 + rr;
-            float x = 0.0f, w = 0.0f;
-            if (r < rows && k0 + kk < p.K) {
-                const int64_t m = r / p.N;
-                x = widen(static_cast<const E *>(p.x)[(p.src_frame[m] * p.N + (r - m * p.N)) * p.K + k0 + kk]);
-            }
-            if (c0 + rr < p.n_out && k0 + kk < p.K)
-                w = widen(static_cast<const E *>(p.weight)[static_cast<int64_t>(c0 + rr) * p.K + k0 + kk]);
-            xs[kk][rr] = x;
-            ws[kk][rr] = w;
-        }
-        __syncthreads();
-        for (int kk = 0; kk < 16; ++kk)
-            for (int i = 0; i < 4; ++i)
-                for (int j = 0; j < 4; ++j)
-                    acc[i][j] = fmaf(xs[kk][tr + 16 * i], ws[kk][tc + 16 * j], acc[i][j]);
-        __syncthreads();
+// The epilogue of kN neighbouring features c.. of product row r.
+template <typename E, int kN>
+__device__ __forceinline__ void finish(const LinearKArgs &a, uint32_t r, int c, float (&v)[kN]) {
+    const uint32_t m = r / a.N;
+    const int64_t dst = static_cast<int64_t>(a.dst_frame[m]) * a.N + (r - m * a.N);
+    float t[kN];
+    if (a.bias) {
+        load_n<E, kN>(a.bias, c, t);
+#pragma unroll
+        for (int e = 0; e < kN; ++e) v[e] += t[e];
     }
-    for (int i = 0; i < 4; ++i) {
-        const int64_t r = r0 + tr + 16 * i;
-        if (r >= rows) continue;
-        const int64_t m = r / p.N, dst = p.dst_frame[m] * p.N + (r - m * p.N);
-        for (int j = 0; j < 4; ++j) {
-            const int c = c0 + tc + 16 * j;
-            if (c >= p.n_out) continue;
-            float x = acc[i][j];
-            if (p.bias) x += widen(static_cast<const E *>(p.bias)[c]);
-            x = activate(p.activation, x);
-            if (p.gate)
-                x *= widen(static_cast<const E *>(p.gate)[static_cast<int64_t>(p.gate_rows ? p.frame[m] : 0) * p.n_out + c]);
-            if (p.residual) x += widen(static_cast<const E *>(p.residual)[dst * p.n_out + c]);
-            put(static_cast<E *>(p.y) + dst * p.n_out + c, x);
+    if (a.activation != RF_ACT_NONE) {
+#pragma unroll
+        for (int e = 0; e < kN; ++e) v[e] = activate(a.activation, v[e]);
+    }
+    if (a.gate) {
+        load_n<E, kN>(a.gate, a.gate_rows ? static_cast<int64_t>(a.frame[m]) * a.n_out + c : c, t);
+#pragma unroll
+        for (int e = 0; e < kN; ++e) v[e] *= t[e];
+    }
+    if (a.residual) {
+        load_n<E, kN>(a.residual, dst * a.n_out + c, t);
+#pragma unroll
+        for (int e = 0; e < kN; ++e) v[e] += t[e];
+    }
+    store_n<E, kN>(a.y, dst * a.n_out + c, v);
+}
+
+// Product row r's (clamped to the last one) first byte in x.
+__device__ __forceinline__ const uint8_t *x_row(const LinearKArgs &a, uint32_t r) {
+    if (r >= a.rows) r = a.rows - 1;
+    const uint32_t m = r / a.N;
+    return a.x + (static_cast<int64_t>(a.src_frame[m]) * a.N + (r - m * a.N)) * a.row_bytes;
+}
+__device__ __forceinline__ const uint8_t *w_row(const LinearKArgs &a, int c) {
+    return a.w + static_cast<int64_t>(c < a.n_out ? c : a.n_out - 1) * a.row_bytes;
+}
+
+// Workgroup id -> tile. Ids go round-robin to the XCDs: each takes a contiguous
+// range of tiles, walked in bands of eight row tiles, so the workgroups that share
+// an L2 at a time form a block of both operands.
+constexpr int kBand = 8;
+__device__ __forceinline__ bool tile_of(const LinearKArgs &a, int bid, int &rt, int &ct) {
+    const int tile = (bid % a.xcds) * a.per_xcd + bid / a.xcds;
+    if (tile >= a.tiles) return false;
+    const int band = tile / (kBand * a.col_tiles), first = band * kBand;
+    const int height = a.row_tiles - first < kBand ? a.row_tiles - first : kBand;
+    const int in = tile - band * kBand * a.col_tiles;
+    ct = in / height;
+    rt = first + in - ct * height;
+    return true;
+}
+
+// kRB blocks of 32 rows to a wave, kWR x kWC waves of (32 kRB rows x 64 features).
+template <typename E, int kRB, int kWR, int kWC>
+__global__ __launch_bounds__(64 * kWR * kWC) __attribute__((amdgpu_waves_per_eu(2)))
+void linear_tile_kernel(const LinearKArgs a) {
+    constexpr int kWaves = kWR * kWC, kBM = 32 * kRB * kWR, kBN = 64 * kWC;
+    constexpr int kXLoads = kBM / 8 / kWaves, kWLoads = kBN / 8 / kWaves;   // 8 rows each
+    constexpr int kBuf = (kBM + kBN) * kStep;
+    static_assert(kWaves * 8192 <= 2 * kBuf, "the epilogue's rows fit the buffers");
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kBuf];
+    int rt, ct;
+    const int part = blockIdx.x % a.parts;
+    if (!tile_of(a, blockIdx.x / a.parts, rt, ct)) return;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 31, grp = lane >> 5;
+    const int wr = wave / kWC, wc = wave % kWC;
+
+    // this lane's 16 bytes of each load: row lane / 8 of eight, the piece whose slot is lane % 8
+    const uint8_t *xp[kXLoads], *wp[kWLoads];
+    int piece;
+    {
+        const int sub = lane / 8;
+        piece = (lane % 8) ^ ((sub / 2) % 8);   // (row / 2) % 8 of row 8 i + sub: 4 (i % 2) more
+#pragma unroll
+        for (int i = 0; i < kXLoads; ++i) {
+            const int row = (wave * kXLoads + i) * 8 + sub;
+            xp[i] = x_row(a, static_cast<uint32_t>(rt) * kBM + row);
         }
+#pragma unroll
+        for (int i = 0; i < kWLoads; ++i) {
+            const int row = (wave * kWLoads + i) * 8 + sub;
+            wp[i] = w_row(a, ct * kBN + row);
+        }
+    }
+    auto issue = [&](int step, uint8_t *buf) {
+        const int64_t at0 = static_cast<int64_t>(step) * kStep;
+        // the last step may be short: pieces past the row's end come from zeros
+        const bool cut = at0 + kStep > a.row_bytes;
+#pragma unroll
+        for (int i = 0; i < kXLoads; ++i) {
+            const int64_t at = at0 + 16 * (piece ^ (((wave * kXLoads + i) % 2) * 4));
+            const uint8_t *p = cut && at >= a.row_bytes ? reinterpret_cast<const uint8_t *>(&kZeros) : xp[i] + at;
+            global_lds16(p, buf + (wave * kXLoads + i) * 1024);
+        }
+#pragma unroll
+        for (int i = 0; i < kWLoads; ++i) {
+            const int64_t at = at0 + 16 * (piece ^ (((wave * kWLoads + i) % 2) * 4));
+            const uint8_t *p = cut && at >= a.row_bytes ? reinterpret_cast<const uint8_t *>(&kZeros) : wp[i] + at;
+            global_lds16(p, buf + kBM * kStep + (wave * kWLoads + i) * 1024);
+        }
+    };
+
+    f32x16_t acc[2][kRB];
+#pragma unroll
+    for (int f = 0; f < 2; ++f)
+#pragma unroll
+        for (int b = 0; b < kRB; ++b) acc[f][b] = f32x16_t{};
+    // a lane's pieces 2 kk + grp of its row in each block
+    const int xbase = (wr * kRB * 32 + col) * kStep, wbase = (kBM + wc * 64 + col) * kStep;
+    const int swz = (col / 2) % 8;
+    // four pairs of pieces to a step; the next pair's operands are read while this one's multiply
+    auto compute = [&](const uint8_t *buf) {
+        u32x4_t wf[2][2], xf[2][kRB];
+        auto read = [&](int kk) {
+            const int at = ((2 * kk + grp) ^ swz) * 16;
+#pragma unroll
+            for (int f = 0; f < 2; ++f)
+                wf[kk % 2][f] = *reinterpret_cast<const u32x4_t *>(buf + wbase + f * 32 * kStep + at);
+#pragma unroll
+            for (int b = 0; b < kRB; ++b)
+                xf[kk % 2][b] = *reinterpret_cast<const u32x4_t *>(buf + xbase + b * 32 * kStep + at);
+        };
+        read(0);
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+            if (kk + 1 < 4) read(kk + 1);
+#pragma unroll
+            for (int b = 0; b < kRB; ++b)
+#pragma unroll
+                for (int f = 0; f < 2; ++f) acc[f][b] = mma32<E>(wf[kk % 2][f], xf[kk % 2][b], acc[f][b]);
+        }
+        constexpr int kReads = 2 + kRB, kMma = 2 * kRB * (sizeof(E) == 2 ? 1 : 4);
+        __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
+#pragma unroll
+        for (int kk = 0; kk < 3; ++kk) {
+#pragma unroll
+            for (int i = 0; i < kReads; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, kMma / kReads, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, kMma - kMma / kReads * kReads, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, kMma, 0);
+    };
+    const int s0 = part * a.steps_per_part;
+    const int s1 = s0 + a.steps_per_part < a.steps ? s0 + a.steps_per_part : a.steps;
+    auto step_done = [&]() {
+        wait_loads<0>();   // this wave's loads have reached LDS
+        __syncthreads();
+    };
+    issue(s0, lds);
+    step_done();
+    for (int s = s0; s < s1; s += 2) {
+        if (s + 1 < s1) issue(s + 1, lds + kBuf);
+        compute(lds);
+        step_done();
+        if (s + 1 >= s1) break;
+        if (s + 2 < s1) issue(s + 2, lds);
+        compute(lds + kBuf);
+        step_done();
+    }
+
+    // ---- epilogue: 32 rows x 64 features at a time through 8 KB of the wave's own, 256
+    // bytes a row, 16-byte units permuted by row % 16; a lane then has 8 neighbouring
+    // features of a row, and eight lanes whole lines of y ----
+    uint8_t *mine = lds + wave * 8192;
+    const int c = ct * kBN + wc * 64 + (lane % 8) * 8;
+#pragma unroll
+    for (int b = 0; b < kRB; ++b) {
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+            for (int g4 = 0; g4 < 4; ++g4) {
+                const int unit = (f * 8 + g4 * 2 + grp) ^ (col & 15);
+                *reinterpret_cast<f32x4_t *>(mine + col * 256 + unit * 16) =
+                    f32x4_t{acc[f][b][g4 * 4], acc[f][b][g4 * 4 + 1], acc[f][b][g4 * 4 + 2], acc[f][b][g4 * 4 + 3]};
+            }
+        wait_lds_reads();   // (a wave's LDS accesses run in order; this orders the compiler's)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int lr = i * 8 + lane / 8;
+            const uint32_t r = static_cast<uint32_t>(rt) * kBM + (wr * kRB + b) * 32 + lr;
+            float v[8];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const f32x4_t x =
+                    *reinterpret_cast<const f32x4_t *>(mine + lr * 256 + ((((lane % 8) * 2 + h) ^ (lr & 15)) * 16));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[h * 4 + e] = x[e];
+            }
+            if (r >= a.rows || c >= a.n_out) continue;
+            // (fp32 may end in the middle of eight features)
+            if (sizeof(E) == 4 && c + 8 > a.n_out) {
+                float lo[4] = {v[0], v[1], v[2], v[3]};
+                if (a.parts > 1) store_n<float, 4>(a.ws, (static_cast<int64_t>(part) * a.rows + r) * a.n_out + c, lo);
+                else finish<E, 4>(a, r, c, lo);
+                continue;
+            }
+            if (a.parts > 1) store_n<float, 8>(a.ws, (static_cast<int64_t>(part) * a.rows + r) * a.n_out + c, v);
+            else finish<E, 8>(a, r, c, v);
+        }
+        wait_lds_reads();
+    }
+}
+
+constexpr int kFewWaves = 8;
+
+// kR blocks of 16 rows. The reduction goes in pieces of 64 bytes (16 bytes a lane, four
+// lanes to a row); wave w of part p owns a run of them.
+template <typename E, int kR>
+__global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(const LinearKArgs a) {
+    __shared__ __attribute__((aligned(16))) float sums[kFewWaves][16 * kR][16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int part = blockIdx.x % a.parts, tile = blockIdx.x / a.parts;
+    const int rt = tile / a.col_tiles, c0 = (tile - rt * a.col_tiles) * 16;
+    const uint32_t r0 = static_cast<uint32_t>(rt) * (16 * kR);
+    const int l16 = lane & 15, grp = lane >> 4;
+    const uint8_t *wp = w_row(a, c0 + l16) + grp * 16;
+    const uint8_t *xp[kR];
+#pragma unroll
+    for (int b = 0; b < kR; ++b) xp[b] = x_row(a, r0 + b * 16 + l16) + grp * 16;
+    f32x4_t acc[kR];
+#pragma unroll
+    for (int b = 0; b < kR; ++b) acc[b] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    constexpr int kAhead = 4;
+    // (steps here are pieces of 64 bytes; steps_per_part a wave's share of them)
+    const int s0 = (part * kFewWaves + wave) * a.steps_per_part;
+    const int s1 = s0 + a.steps_per_part < a.steps ? s0 + a.steps_per_part : a.steps;
+    const int64_t end = a.row_bytes - grp * 16;
+    for (int s = s0; s < s1; s += kAhead) {
+        u32x4_t wf[kAhead], xf[kAhead][kR];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int64_t at = static_cast<int64_t>(s + i) * 64;
+            const bool in = s + i < s1 && at < end;
+            wf[i] = in ? *reinterpret_cast<const u32x4_t *>(wp + at) : u32x4_t{0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int b = 0; b < kR; ++b)
+                xf[i][b] = in ? *reinterpret_cast<const u32x4_t *>(xp[b] + at) : u32x4_t{0u, 0u, 0u, 0u};
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+            for (int b = 0; b < kR; ++b) acc[b] = mma16<E>(wf[i], xf[i][b], acc[b]);
+    }
+    // lane: row l16 of a block, features 4 grp .. 4 grp + 3
+#pragma unroll
+    for (int b = 0; b < kR; ++b) *reinterpret_cast<f32x4_t *>(&sums[wave][b * 16 + l16][grp * 4]) = acc[b];
+    __syncthreads();
+    for (int i = tid; i < 16 * kR * 4; i += 64 * kFewWaves) {
+        const int lr = i / 4, q = i % 4;
+        const uint32_t r = r0 + lr;
+        const int c = c0 + q * 4;
+        if (r >= a.rows || c >= a.n_out) continue;
+        f32x4_t x = *reinterpret_cast<const f32x4_t *>(&sums[0][lr][q * 4]);
+#pragma unroll
+        for (int w = 1; w < kFewWaves; ++w) {
+            const f32x4_t y = *reinterpret_cast<const f32x4_t *>(&sums[w][lr][q * 4]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] += y[e];
+        }
+        float v[4] = {x[0], x[1], x[2], x[3]};
+        if (a.parts > 1) store_n<float, 4>(a.ws, (static_cast<int64_t>(part) * a.rows + r) * a.n_out + c, v);
+        else finish<E, 4>(a, r, c, v);
+    }
+}
+
+template <typename E>
+__global__ __launch_bounds__(256) void linear_join_kernel(const LinearKArgs a) {
+    const int64_t per_row = a.n_out / 4, id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    if (id >= per_row * a.rows) return;
+    const uint32_t r = static_cast<uint32_t>(id / per_row);
+    const int c = static_cast<int>(id - r * per_row) * 4;
+    f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f};
+    const float *p = a.ws + static_cast<int64_t>(r) * a.n_out + c;
+    const int64_t step = static_cast<int64_t>(a.rows) * a.n_out;
+#pragma unroll 8
+    for (int i = 0; i < a.parts; ++i) {
+        const f32x4_t y = *reinterpret_cast<const f32x4_t *>(p + i * step);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] += y[e];
+    }
+    float v[4] = {x[0], x[1], x[2], x[3]};
+    finish<E, 4>(a, r, c, v);
+}
+
+enum LinearForm { kFew16, kFew32, kFew64, kTile128, kTile256 };
+struct LinearPlan {
+    LinearForm form;
+    int64_t row_tiles, col_tiles;
+    int32_t steps, per_part, parts;
+};
+
+LinearPlan linear_plan(int64_t rows, int32_t K, int32_t n_out, int32_t dtype, int32_t cus, bool may_split) {
+    LinearPlan p{};
+    const int64_t bytes = static_cast<int64_t>(K) * (dtype == RF_F32 ? 4 : 2);
+    auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
+    if (rows <= 64) {
+        p.form = rows <= 16 ? kFew16 : rows <= 32 ? kFew32 : kFew64;
+        p.row_tiles = 1;
+        p.col_tiles = up(n_out, 16);
+        p.steps = static_cast<int32_t>(up(bytes, 64));
+        // a wave takes at least four pieces; two workgroups to a compute unit
+        const int64_t want = up(2 * cus, p.col_tiles), most = up(p.steps, 4 * kFewWaves);
+        p.parts = static_cast<int32_t>(!may_split || p.col_tiles >= cus ? 1 : want < most ? want : most);
+        p.per_part = static_cast<int32_t>(up(p.steps, static_cast<int64_t>(p.parts) * kFewWaves));
+        p.parts = static_cast<int32_t>(up(p.steps, static_cast<int64_t>(p.per_part) * kFewWaves));
+        return p;
+    }
+    const int64_t big = up(rows, 256) * up(n_out, 256), small = up(rows, 128) * up(n_out, 128);
+    p.form = big * 8 >= cus * 6 ? kTile256 : kTile128;
+    const int64_t t = p.form == kTile256 ? 256 : 128, tiles = p.form == kTile256 ? big : small;
+    p.row_tiles = up(rows, t);
+    p.col_tiles = up(n_out, t);
+    p.steps = static_cast<int32_t>(up(bytes, kStep));
+    p.parts = 1;
+    if (may_split && p.form == kTile128 && tiles < cus) {
+        const int64_t want = 2 * cus / tiles, most = p.steps / 8;
+        p.parts = static_cast<int32_t>(want < most ? want : most);
+        if (p.parts < 1) p.parts = 1;
+        if (p.parts > 16) p.parts = 16;
+    }
+    p.per_part = static_cast<int32_t>(up(p.steps, p.parts));
+    p.parts = static_cast<int32_t>(up(p.steps, p.per_part));
+    return p;
+}
+
+template <typename E>
+void run(const LinearPlan &p, const LinearKArgs &a, dim3 grid, hipStream_t stream) {
+    switch (p.form) {
+        case kFew16: hipLaunchKernelGGL((linear_few_kernel<E, 1>), grid, dim3(512), 0, stream, a); break;
+        case kFew32: hipLaunchKernelGGL((linear_few_kernel<E, 2>), grid, dim3(512), 0, stream, a); break;
+        case kFew64: hipLaunchKernelGGL((linear_few_kernel<E, 4>), grid, dim3(512), 0, stream, a); break;
+        case kTile128: hipLaunchKernelGGL((linear_tile_kernel<E, 2, 2, 2>), grid, dim3(256), 0, stream, a); break;
+        case kTile256: hipLaunchKernelGGL((linear_tile_kernel<E, 4, 2, 4>), grid, dim3(512), 0, stream, a); break;
     }
 }
 
 }  // namespace
 
-int64_t linear_workspace(int64_t, int32_t, int32_t, int32_t, int32_t) { return 0; }
+int64_t linear_workspace(int64_t rows, int32_t K, int32_t n_out, int32_t dtype, int32_t cus) {
+    const LinearPlan p = linear_plan(rows, K, n_out, dtype, cus, true);
+    return p.parts > 1 ? p.parts * rows * n_out * 4 : 0;
+}
 
 hipError_t launch_linear(const LinearParams &p, hipStream_t stream) {
-    const int64_t by = (p.M * p.N + 63) / 64;
-    if (by > 65535) return hipErrorInvalidConfiguration;
-    const dim3 grid(static_cast<uint32_t>((p.n_out + 63) / 64), static_cast<uint32_t>(by));
-    if (p.dtype == RF_F32) hipLaunchKernelGGL(linear_kernel<float>, grid, dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL(linear_kernel<uint16_t>, grid, dim3(256), 0, stream, p);
+    const int32_t xcds = p.geo.xcds;
+    if (p.geo.cus < 1 || xcds < 1 || xcds > 64) return hipErrorInvalidValue;
+    const int64_t rows = p.M * p.N;
+    const LinearPlan plan = linear_plan(rows, p.K, p.n_out, p.dtype, p.geo.cus, p.ws != nullptr);
+    LinearKArgs a{};
+    a.x = static_cast<const uint8_t *>(p.x);
+    a.w = static_cast<const uint8_t *>(p.weight);
+    a.bias = p.bias;
+    a.gate = p.gate;
+    a.residual = p.residual;
+    a.y = p.y;
+    a.ws = static_cast<float *>(p.ws);
+    a.row_bytes = static_cast<int64_t>(p.K) * (p.dtype == RF_F32 ? 4 : 2);
+    a.rows = static_cast<uint32_t>(rows);
+    a.N = static_cast<uint32_t>(p.N);
+    a.n_out = p.n_out;
+    a.steps = plan.steps;
+    a.steps_per_part = plan.per_part;
+    a.parts = plan.parts;
+    a.activation = p.activation;
+    a.gate_rows = p.gate_rows;
+    for (int i = 0; i < p.M; ++i) {
+        a.frame[i] = p.frame[i];
+        a.src_frame[i] = p.src_frame[i];
+        a.dst_frame[i] = p.dst_frame[i];
+    }
+    const int64_t tiles = plan.row_tiles * plan.col_tiles;
+    if (tiles > 0x7fffffffLL / 64) return hipErrorInvalidConfiguration;
+    a.row_tiles = static_cast<int32_t>(plan.row_tiles);
+    a.col_tiles = static_cast<int32_t>(plan.col_tiles);
+    a.tiles = static_cast<int32_t>(tiles);
+    a.xcds = xcds;
+    a.per_xcd = (a.tiles + xcds - 1) / xcds;
+    const bool few = plan.form <= kFew64;
+    const int64_t grid = (few ? tiles : static_cast<int64_t>(a.per_xcd) * xcds) * plan.parts;
+    if (grid > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    const dim3 g(static_cast<uint32_t>(grid));
+    if (p.dtype == RF_F32) run<float>(plan, a, g, stream);
+    else run<uint16_t>(plan, a, g, stream);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || plan.parts == 1) return e;
+    const int64_t blocks = (rows * (p.n_out / 4) + 255) / 256;
+    if (blocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    const dim3 jg(static_cast<uint32_t>(blocks));
+    if (p.dtype == RF_F32) hipLaunchKernelGGL(linear_join_kernel<float>, jg, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL(linear_join_kernel<uint16_t>, jg, dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 
