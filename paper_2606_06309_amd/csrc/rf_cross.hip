@@ -270,8 +270,7 @@ __device__ __forceinline__ void load_offsets(int64_t stride, int i0, int lane, i
 // share double-buffered tiles (64 KB of LDS), one barrier a tile.
 // ---------------------------------------------------------------------------
 
-constexpr int kTileWaves = 4;
-constexpr int kTileRows = 32 * kTileWaves;
+constexpr int kTileWaves = kCrossTileRows / 32;
 __host__ __device__ constexpr int tile_keys(int head_dim) { return head_dim == 64 ? 128 : 64; }
 
 template <int D, bool kMask>
@@ -284,7 +283,7 @@ void cross_tile_kernel(const CrossKArgs a) {
     __shared__ __attribute__((aligned(1024))) uint8_t v0[kTileBytes];
     __shared__ __attribute__((aligned(1024))) uint8_t v1[kTileBytes];
     CrossTile t;
-    if (!cross_tile<kTileRows>(a, blockIdx.x, t)) return;
+    if (!cross_tile<kCrossTileRows>(a, blockIdx.x, t)) return;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, grp = lane >> 5;
@@ -371,7 +370,6 @@ void cross_tile_kernel(const CrossKArgs a) {
 // ---------------------------------------------------------------------------
 
 constexpr int kFewWaves = 8;
-constexpr int kFewRows = 32;
 __host__ __device__ constexpr int few_keys(int head_dim) { return head_dim == 64 ? 64 : 32; }
 
 template <int D, bool kMask>
@@ -380,10 +378,10 @@ void cross_few_kernel(const CrossKArgs a) {
     constexpr int kBc = few_keys(D), kNB = kBc / 32, kTileBytes = kBc * Tile<D>::kRow, kN = kTileBytes / 1024;
     __shared__ __attribute__((aligned(1024))) uint8_t ks[kFewWaves * kTileBytes];
     __shared__ __attribute__((aligned(1024))) uint8_t vs[kFewWaves * kTileBytes];
-    __shared__ float ml[kFewWaves][kFewRows][2];
+    __shared__ float ml[kFewWaves][kCrossFewRows][2];
     const int part = blockIdx.x % a.parts;
     CrossTile t;
-    if (!cross_tile<kFewRows>(a, blockIdx.x / a.parts, t)) return;
+    if (!cross_tile<kCrossFewRows>(a, blockIdx.x / a.parts, t)) return;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, grp = lane >> 5;
@@ -467,7 +465,7 @@ void cross_few_kernel(const CrossKArgs a) {
         wgt[p] = fast_exp2((ml[p][r][0] - ref) * a.scale_log2);
         lsum = fmaf(wgt[p], ml[p][r][1], lsum);
     }
-    const int64_t slot = (static_cast<int64_t>(t.tile) * a.parts + part) * kFewRows + r;
+    const int64_t slot = (static_cast<int64_t>(t.tile) * a.parts + part) * kCrossFewRows + r;
     const float inv = a.parts > 1 ? 1.0f : lsum == 0.0f ? 0.0f : 1.0f / lsum;
     if (a.parts > 1 && unit == 0) *reinterpret_cast<f32x2_t *>(a.ws_ml + slot * 2) = f32x2_t{m, lsum};
     uint16_t *op = static_cast<uint16_t *>(a.out) + row_offset(a, a.os, t, row) + unit * 4;
@@ -501,16 +499,16 @@ __global__ __launch_bounds__(256) void cross_join_kernel(const CrossKArgs a) {
     const int64_t id = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
     CrossTile t;
-    t.tile = static_cast<int32_t>(id / kFewRows);
+    t.tile = static_cast<int32_t>(id / kCrossFewRows);
     if (t.tile >= a.tiles) return;
-    const int r = static_cast<int>(id % kFewRows), head = t.tile / a.q_tiles;
-    t.row0 = static_cast<int64_t>(t.tile - head * a.q_tiles) * kFewRows;
+    const int r = static_cast<int>(id % kCrossFewRows), head = t.tile / a.q_tiles;
+    t.row0 = static_cast<int64_t>(t.tile - head * a.q_tiles) * kCrossFewRows;
     t.b = head / a.kv_heads;
     t.hk = head - t.b * a.kv_heads;
     if (t.row0 + r >= a.rows) return;
-    const int64_t slot0 = static_cast<int64_t>(t.tile) * a.parts * kFewRows + r;
+    const int64_t slot0 = static_cast<int64_t>(t.tile) * a.parts * kCrossFewRows + r;
     float m = -kInf;
-    for (int p = lane; p < a.parts; p += 64) m = fmaxf(m, a.ws_ml[(slot0 + static_cast<int64_t>(p) * kFewRows) * 2]);
+    for (int p = lane; p < a.parts; p += 64) m = fmaxf(m, a.ws_ml[(slot0 + static_cast<int64_t>(p) * kCrossFewRows) * 2]);
 #pragma unroll
     for (int x = 32; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
     const float ref = m == -kInf ? 0.0f : m;
@@ -518,7 +516,7 @@ __global__ __launch_bounds__(256) void cross_join_kernel(const CrossKArgs a) {
     float l = 0.0f, o[kE] = {};
 #pragma unroll 4
     for (int p = 0; p < a.parts; ++p) {
-        const int64_t slot = slot0 + static_cast<int64_t>(p) * kFewRows;
+        const int64_t slot = slot0 + static_cast<int64_t>(p) * kCrossFewRows;
         const f32x2_t ml = *reinterpret_cast<const f32x2_t *>(a.ws_ml + slot * 2);
         const float wgt = fast_exp2((ml[0] - ref) * a.scale_log2);
         l = fmaf(wgt, ml[1], l);
@@ -542,16 +540,19 @@ struct CrossPlan {
     int64_t tiles;
 };
 
-CrossPlan cross_plan(int32_t B, int64_t rows, int32_t kv_heads, int32_t Lk, int32_t head_dim, int32_t cus) {
+CrossPlan cross_plan(int32_t B, int64_t rows, int32_t kv_heads, int32_t Lk, int32_t head_dim, int32_t dtype,
+                     int32_t cus) {
     CrossPlan c{};
     const int64_t heads = static_cast<int64_t>(B) * kv_heads;
-    const int64_t whole = (rows + kTileRows - 1) / kTileRows * heads, few = (rows + kFewRows - 1) / kFewRows * heads;
+    const int64_t whole = (rows + kCrossTileRows - 1) / kCrossTileRows * heads, few = (rows + kCrossFewRows - 1) / kCrossFewRows * heads;
     c.few = whole < 2 * cus;
     c.tiles = c.few ? few : whole;
     c.parts = 1;
     if (c.few) {
-        const int64_t key_tiles = (static_cast<int64_t>(Lk) + few_keys(head_dim) - 1) / few_keys(head_dim);
-        const int64_t most = (key_tiles + 2 * kFewWaves - 1) / (2 * kFewWaves);   // two tiles a wave
+        const int64_t keys = dtype == RF_F32 ? 32 : few_keys(head_dim);
+        const int64_t waves = dtype == RF_F32 && head_dim == 128 ? 4 : kFewWaves;
+        const int64_t key_tiles = (static_cast<int64_t>(Lk) + keys - 1) / keys;
+        const int64_t most = (key_tiles + 2 * waves - 1) / (2 * waves);   // two tiles a wave
         const int64_t want = cus / few;
         c.parts = static_cast<int32_t>(want < 1 ? 1 : want < most ? want : most);
     }
@@ -562,9 +563,8 @@ CrossPlan cross_plan(int32_t B, int64_t rows, int32_t kv_heads, int32_t Lk, int3
 
 int64_t cross_workspace(int32_t B, int32_t Lq, int32_t Lk, int32_t heads, int32_t kv_heads, int32_t head_dim,
                         int32_t dtype, int32_t cus) {
-    if (dtype == RF_F32) return 0;
-    const CrossPlan c = cross_plan(B, static_cast<int64_t>(heads / kv_heads) * Lq, kv_heads, Lk, head_dim, cus);
-    return c.parts > 1 ? c.tiles * c.parts * kFewRows * (static_cast<int64_t>(head_dim) * 4 + 8) : 0;
+    const CrossPlan c = cross_plan(B, static_cast<int64_t>(heads / kv_heads) * Lq, kv_heads, Lk, head_dim, dtype, cus);
+    return c.parts > 1 ? c.tiles * c.parts * kCrossFewRows * (static_cast<int64_t>(head_dim) * 4 + 8) : 0;
 }
 
 hipError_t launch_cross(const CrossParams &p, hipStream_t stream) {
@@ -590,11 +590,10 @@ hipError_t launch_cross(const CrossParams &p, hipStream_t stream) {
     a.rows = static_cast<int64_t>(a.group) * p.Lq;
     a.scale_log2 = static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(p.head_dim)));
     a.xcds = xcds;
-    if (p.dtype == RF_F32) return launch_cross_f32(p, a, stream);
-    CrossPlan c = cross_plan(p.B, a.rows, p.kv_heads, p.Lk, p.head_dim, p.geo.cus);
+    CrossPlan c = cross_plan(p.B, a.rows, p.kv_heads, p.Lk, p.head_dim, p.dtype, p.geo.cus);
     if (!p.ws) c.parts = 1;
     a.parts = c.parts;
-    const int64_t rows = c.few ? kFewRows : kTileRows;
+    const int64_t rows = c.few ? kCrossFewRows : kCrossTileRows;
     if (c.tiles > 0x7fffffffLL / 64) return hipErrorInvalidConfiguration;
     a.q_tiles = static_cast<int32_t>((a.rows + rows - 1) / rows);
     a.tiles = static_cast<int32_t>(c.tiles);
@@ -603,11 +602,14 @@ hipError_t launch_cross(const CrossParams &p, hipStream_t stream) {
     if (grid > 0x7fffffffLL) return hipErrorInvalidConfiguration;
     if (c.parts > 1) {
         a.ws_o = static_cast<float *>(p.ws);
-        a.ws_ml = a.ws_o + c.tiles * c.parts * kFewRows * p.head_dim;
+        a.ws_ml = a.ws_o + c.tiles * c.parts * kCrossFewRows * p.head_dim;
     }
     const dim3 g(static_cast<uint32_t>(grid)), block(64 * (c.few ? kFewWaves : kTileWaves));
     const bool mask = p.key_mask != nullptr;
-    if (p.head_dim == 128) {
+    if (p.dtype == RF_F32) {
+        const hipError_t e = launch_cross_f32(a, p.head_dim, c.few, static_cast<uint32_t>(grid), stream);
+        if (e != hipSuccess) return e;
+    } else if (p.head_dim == 128) {
         if (c.few && mask) hipLaunchKernelGGL((cross_few_kernel<128, true>), g, block, 0, stream, a);
         else if (c.few) hipLaunchKernelGGL((cross_few_kernel<128, false>), g, block, 0, stream, a);
         else if (mask) hipLaunchKernelGGL((cross_tile_kernel<128, true>), g, block, 0, stream, a);
@@ -620,8 +622,11 @@ hipError_t launch_cross(const CrossParams &p, hipStream_t stream) {
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || c.parts == 1) return e;
-    const dim3 jg(static_cast<uint32_t>(c.tiles * kFewRows / 4));
-    if (p.head_dim == 128) hipLaunchKernelGGL((cross_join_kernel<128, uint16_t>), jg, dim3(256), 0, stream, a);
+    const dim3 jg(static_cast<uint32_t>(c.tiles * kCrossFewRows / 4));
+    if (p.dtype == RF_F32 && p.head_dim == 128)
+        hipLaunchKernelGGL((cross_join_kernel<128, float>), jg, dim3(256), 0, stream, a);
+    else if (p.dtype == RF_F32) hipLaunchKernelGGL((cross_join_kernel<64, float>), jg, dim3(256), 0, stream, a);
+    else if (p.head_dim == 128) hipLaunchKernelGGL((cross_join_kernel<128, uint16_t>), jg, dim3(256), 0, stream, a);
     else hipLaunchKernelGGL((cross_join_kernel<64, uint16_t>), jg, dim3(256), 0, stream, a);
     return hipGetLastError();
 }

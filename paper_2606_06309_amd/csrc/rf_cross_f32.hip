@@ -1,86 +1,328 @@
-// Attention to an encoder's states of another length for gfx950.
+// Attention to an encoder's states of another length for gfx950, fp32 throughout
+// on the fp32 matrix instructions; the method and the layouts are those of the
+// bf16 kernels in rf_cross.hip, with these differences:
 //
-// One wave per (sequence, head, query): lane l scores keys l, l + 64, ..., the
-// running maximum and sum of the softmax are the wave's, and lane l owns every
-// 64th dimension of the output.
+//  * v_mfma_f32_32x32x2_f32 takes one fp32 per lane of either operand, so a
+//    16-byte LDS read of a K row feeds four of them; the accumulators of
+//    S^T = K Q^T are, step by step, the B operand of O^T = V^T P^T, whose row i
+//    may stand for any dimension: lane i takes dimensions i D/32 .. + D/32 - 1, one
+//    wide LDS read of a V row.
+//  * The reference is the exact running maximum, subtracted before the scale, so the
+//    largest score gives exactly 1 however large it is.
+//  * A tile is 32 keys, 16 KB (head dimension 128) or 8 KB (64) of K and of V.
+//
+// What bounds it: the fp32 matrix instructions (64 cycles each); one 16-byte LDS
+// read feeds four, and the other pipes are far from their limits.
 #include "rf_cross.h"
 
 namespace rf {
 namespace {
 
-template <typename E>
-__device__ __forceinline__ float widen(E x);
-template <>
-__device__ __forceinline__ float widen<float>(float x) { return x; }
-template <>
-__device__ __forceinline__ float widen<uint16_t>(uint16_t x) { return __uint_as_float(static_cast<uint32_t>(x) << 16); }
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
 
-__device__ __forceinline__ void put(float *p, float x) { *p = x; }
-__device__ __forceinline__ void put(uint16_t *p, float x) {
-    *p = __builtin_bit_cast(uint16_t, static_cast<__bf16>(x));
+constexpr float kInf = __builtin_huge_valf();
+constexpr int kKeys = 32;   // of a tile
+
+template <int D>
+struct Tile {
+    static constexpr int kRow = 4 * D;
+    static constexpr int kSlots = kRow / 16;
+    static constexpr int kBytes = kKeys * kRow;
+    static constexpr int kRowsPerLoad = 1024 / kRow;
+    static constexpr int kLoads = kBytes / 1024;
+};
+
+template <int D>
+struct Wave {
+    static constexpr int kDb = D / 32;
+    f32x4_t qf[D / 8];
+    f32x16_t o[kDb];
+    float m, l;   // running maximum of the raw scores; this lane's part of the row sum
+};
+
+template <int D>
+__device__ __forceinline__ void start(const CrossKArgs &a, const CrossTile &t, int64_t row, int grp, Wave<D> &w) {
+    if (row < a.rows) {
+        const float *qp = static_cast<const float *>(a.q) + row_offset(a, a.qs, t, row) + grp * 4;
+#pragma unroll
+        for (int c = 0; c < D / 8; ++c) w.qf[c] = *reinterpret_cast<const f32x4_t *>(qp + c * 8);
+    } else {
+#pragma unroll
+        for (int c = 0; c < D / 8; ++c) w.qf[c] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+#pragma unroll
+    for (int db = 0; db < Wave<D>::kDb; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) w.o[db][r] = 0.0f;
+    w.m = -kInf;
+    w.l = 0.0f;
 }
 
-template <typename E, int D>
-__global__ __launch_bounds__(256) void cross_kernel(const CrossParams p) {
-    __shared__ float qs[4][D];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * 4 + wave;
-    const int b = blockIdx.z, h = blockIdx.y, hk = h / (p.heads / p.kv_heads);
-    const bool live = i < p.Lq;
-    const E *q = static_cast<const E *>(p.q) + b * p.qs[0] + i * p.qs[1] + h * p.qs[2];
-    if (live)
-        for (int d = lane; d < D; d += 64) qs[wave][d] = widen(q[d]);
-    __syncthreads();
-    if (!live) return;
-    const E *k = static_cast<const E *>(p.k) + b * p.ks[0] + hk * p.ks[2];
-    const E *v = static_cast<const E *>(p.v) + b * p.vs[0] + hk * p.vs[2];
-    int n = p.Lk;
-    if (p.kv_lengths) n = p.kv_lengths[b] < 0 ? 0 : p.kv_lengths[b] < p.Lk ? p.kv_lengths[b] : p.Lk;
-    const uint8_t *mask = p.key_mask ? p.key_mask + static_cast<int64_t>(b) * p.Lk : nullptr;
-    const float scale = static_cast<float>(1.0 / sqrt(static_cast<double>(D)));
-    float m = -__builtin_huge_valf(), l = 0.0f, o[D / 64] = {};
-    bool any = false;
-    for (int j0 = 0; j0 < n; j0 += 64) {
-        const int j = j0 + lane;
-        const bool ok = j < n && (!mask || mask[j]);
-        const uint64_t valid = __ballot(ok);
-        if (valid == 0) continue;
-        any = true;
-        float s = -__builtin_huge_valf();
-        if (ok) {
-            s = 0.0f;
-            for (int d = 0; d < D; ++d) s = fmaf(qs[wave][d], widen(k[j * p.ks[1] + d]), s);
-            s *= scale;
+// Loads i0 .. i0 + kN - 1 of a tile into LDS (1 KB each); K's 16-byte slots permuted by key % 16.
+template <int D, bool kMask, bool kKey, int kN>
+__device__ __forceinline__ void issue(const float *head, int64_t stride, int32_t key0, int32_t left, uint64_t bits,
+                                      uint8_t *dst, int i0, int lane) {
+    using L = Tile<D>;
+    const int64_t span = ((static_cast<int64_t>(left) - 1) * stride + D) * 4;
+    const int32_t rec = __builtin_amdgcn_readfirstlane(static_cast<int32_t>(span < kNowhere ? span : kNowhere));
+    const __amdgpu_buffer_rsrc_t r =
+        __builtin_amdgcn_make_buffer_rsrc(uniform_ptr(head + key0 * stride), 0, rec, kBufferWord3);
+    const int sub = lane / L::kSlots, slot = lane % L::kSlots;
+    const int step = static_cast<int>(L::kRowsPerLoad * stride * 4), at0 = static_cast<int>(sub * stride * 4);
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+        const int key = (i0 + i) * L::kRowsPerLoad + sub;
+        int at = at0 + (i0 + i) * step + (kKey ? slot ^ (key & 15) : slot) * 16;
+        if constexpr (kMask) {
+            if (!((bits >> key) & 1)) at = kNowhere;
         }
-        float mx = s;
-        for (int x = 32; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor(mx, x));
-        mx = fmaxf(m, mx);
-        const float ref = mx == -__builtin_huge_valf() ? 0.0f : mx;
-        const float corr = m == -__builtin_huge_valf() ? 0.0f : expf(m - ref);
-        const float e = ok ? expf(s - ref) : 0.0f;
-        float sum = e;
-        for (int x = 32; x > 0; x >>= 1) sum += __shfl_xor(sum, x);
-        l = l * corr + sum;
-        for (int c = 0; c < D / 64; ++c) o[c] *= corr;
-        for (int t = 0; t < 64; ++t) {
-            if (!((valid >> t) & 1)) continue;
-            const float pt = __shfl(e, t);
-            for (int c = 0; c < D / 64; ++c) o[c] = fmaf(pt, widen(v[(j0 + t) * p.vs[1] + lane + 64 * c]), o[c]);
-        }
-        m = mx;
+        load_lds16(r, (lds_void_t *)(dst + (i0 + i) * 1024), at);
     }
-    E *out = static_cast<E *>(p.out) + b * p.os[0] + i * p.os[1] + h * p.os[2];
-    for (int c = 0; c < D / 64; ++c) put(out + lane + 64 * c, any ? o[c] / l : 0.0f);
+}
+
+template <int D>
+__device__ __forceinline__ f32x16_t scores(const uint8_t *kb, int col, int grp, const f32x4_t (&qf)[D / 8]) {
+    const uint8_t *row = kb + col * (4 * D);
+    const int base = (grp ^ (col & 15)) * 16;
+    f32x16_t s = {};
+#pragma unroll
+    for (int c = 0; c < D / 8; ++c) {
+        const f32x4_t kf = *reinterpret_cast<const f32x4_t *>(row + (base ^ (c * 32)));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], qf[c][e], s, 0, 0, 0);
+    }
+    return s;
+}
+
+template <int D>
+__device__ __forceinline__ void softmax(Wave<D> &w, f32x16_t &s, uint32_t word, int grp, float sl2) {
+    if (word != 0xffffffffu) {
+        const uint32_t mine = word >> (4 * grp);
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            if (!((mine >> ((r / 4) * 8 + r % 4)) & 1u)) s[r] = -kInf;
+    }
+    float mx = s[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+    mx = fmaxf(w.m, halves_max(mx));
+    // rows whose maximum stays keep O and l as they are (their factor is exactly 1)
+    if (__builtin_amdgcn_ballot_w64(mx > w.m) != 0) {
+        const float corr = mx > w.m ? fast_exp2((w.m - mx) * sl2) : 1.0f;   // 0 from -inf on
+        w.l *= corr;
+#pragma unroll
+        for (int db = 0; db < Wave<D>::kDb; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) w.o[db][r] *= corr;
+        w.m = mx;
+    }
+    const float ref = mx == -kInf ? 0.0f : mx;   // no score above -inf so far: every probability is 0
+    float sum[4];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        s[r] = fast_exp2((s[r] - ref) * sl2);
+        sum[r / 4] = r % 4 == 0 ? s[r] : sum[r / 4] + s[r];
+    }
+    w.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+}
+
+template <int D>
+__device__ __forceinline__ void values(Wave<D> &w, const uint8_t *vb, const f32x16_t &p, int col, int grp) {
+    constexpr int kDb = D / 32;
+    typedef float vread_t __attribute__((ext_vector_type(kDb)));
+    const uint8_t *lane0 = vb + grp * 4 * (4 * D) + col * (4 * kDb);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const vread_t v = *reinterpret_cast<const vread_t *>(lane0 + ((r / 4) * 8 + r % 4) * (4 * D));
+#pragma unroll
+        for (int db = 0; db < kDb; ++db) w.o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[db], p[r], w.o[db], 0, 0, 0);
+    }
+}
+
+// Many rows: 4 waves, 128 rows, shared double-buffered tiles.
+constexpr int kTileWaves = kCrossTileRows / 32;
+
+template <int D, bool kMask>
+__global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu(2)))
+void cross_f32_tile_kernel(const CrossKArgs a) {
+    using L = Tile<D>;
+    constexpr int kN = L::kLoads / kTileWaves;
+    __shared__ __attribute__((aligned(1024))) uint8_t kb[2][L::kBytes];
+    __shared__ __attribute__((aligned(1024))) uint8_t vb[2][L::kBytes];
+    CrossTile t;
+    if (!cross_tile<kCrossTileRows>(a, blockIdx.x, t)) return;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 31, grp = lane >> 5;
+    const int64_t row = t.row0 + wave * 32 + col;
+    const int32_t n = key_count(a, t.b);
+    const float *kh = static_cast<const float *>(a.k) + t.b * a.ks[0] + t.hk * a.ks[2];
+    const float *vh = static_cast<const float *>(a.v) + t.b * a.vs[0] + t.hk * a.vs[2];
+    auto load = [&](int32_t i, uint64_t bits, int buf) {
+        issue<D, kMask, true, kN>(kh, a.ks[1], i * kKeys, n - i * kKeys, bits, kb[buf], wave * kN, lane);
+        issue<D, kMask, false, kN>(vh, a.vs[1], i * kKeys, n - i * kKeys, bits, vb[buf], wave * kN, lane);
+    };
+    Wave<D> w;
+    const int32_t tiles = static_cast<int32_t>((static_cast<int64_t>(n) + kKeys - 1) / kKeys);
+    // the bits of 64 keys, of which a tile takes its 32
+    auto tile_bits = [&](int32_t i) { return key_bits<kMask>(a, t.b, i * kKeys, n, lane) & 0xffffffffull; };
+    uint64_t cur = 0, nxt = 0;
+    if (tiles > 0) {
+        cur = tile_bits(0);
+        load(0, cur, 0);
+        nxt = tile_bits(1);
+    }
+    start<D>(a, t, row, grp, w);
+    for (int32_t i = 0; i < tiles; ++i) {
+        wait_loads<0>();   // this wave's loads have reached LDS
+        __syncthreads();   // and everybody's; the other buffer is read
+        uint64_t next = 0;
+        if (i + 1 < tiles) {
+            load(i + 1, nxt, (i + 1) & 1);
+            next = tile_bits(i + 2);
+        }
+        if (!kMask || cur != 0) {
+            f32x16_t s = scores<D>(kb[i & 1], col, grp, w.qf);
+            softmax<D>(w, s, static_cast<uint32_t>(cur), grp, a.scale_log2);
+            values<D>(w, vb[i & 1], s, col, grp);
+        }
+        cur = nxt;
+        nxt = next;
+    }
+    if (row >= a.rows) return;
+    const float l = halves_sum(w.l), inv = l == 0.0f ? 0.0f : 1.0f / l;
+    constexpr int kDb = D / 32;
+    typedef float vread_t __attribute__((ext_vector_type(kDb)));
+    float *op = static_cast<float *>(a.out) + row_offset(a, a.os, t, row);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        vread_t x;
+#pragma unroll
+        for (int db = 0; db < kDb; ++db) x[db] = w.o[db][r] * inv;
+        *reinterpret_cast<vread_t *>(op + ((r / 4) * 8 + grp * 4 + r % 4) * kDb) = x;
+    }
+}
+
+// Few rows: 32 rows, the keys of a part shared out among the waves, merged through LDS.
+template <int D> constexpr int kWaves = D == 128 ? 4 : 8;
+
+template <int D, bool kMask>
+__global__ __launch_bounds__(64 * kWaves<D>) __attribute__((amdgpu_waves_per_eu(kWaves<D> / 4)))
+void cross_f32_few_kernel(const CrossKArgs a) {
+    using L = Tile<D>;
+    constexpr int kW = kWaves<D>, kDb = D / 32, kN = L::kLoads;
+    typedef float vread_t __attribute__((ext_vector_type(kDb)));
+    __shared__ __attribute__((aligned(1024))) uint8_t ks[kW * L::kBytes];
+    __shared__ __attribute__((aligned(1024))) uint8_t vs[kW * L::kBytes];
+    __shared__ float ml[kW][kCrossFewRows][2];
+    const int part = blockIdx.x % a.parts;
+    CrossTile t;
+    if (!cross_tile<kCrossFewRows>(a, blockIdx.x / a.parts, t)) return;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, grp = lane >> 5;
+    const int32_t n = key_count(a, t.b);
+    const float *kh = static_cast<const float *>(a.k) + t.b * a.ks[0] + t.hk * a.ks[2];
+    const float *vh = static_cast<const float *>(a.v) + t.b * a.vs[0] + t.hk * a.vs[2];
+    uint8_t *kb = ks + wave * L::kBytes, *vb = vs + wave * L::kBytes;
+    const int64_t tiles = (static_cast<int64_t>(n) + kKeys - 1) / kKeys;
+    const int64_t first = part * kW + wave, step = static_cast<int64_t>(a.parts) * kW;
+    auto tile_bits = [&](int64_t i) {
+        return key_bits<kMask>(a, t.b, static_cast<int32_t>(i) * kKeys, n, lane) & 0xffffffffull;
+    };
+    Wave<D> w;
+    uint64_t cur = 0;
+    if (first < tiles) {
+        const int32_t key0 = static_cast<int32_t>(first) * kKeys;
+        cur = tile_bits(first);
+        issue<D, kMask, true, kN>(kh, a.ks[1], key0, n - key0, cur, kb, 0, lane);
+        issue<D, kMask, false, kN>(vh, a.vs[1], key0, n - key0, cur, vb, 0, lane);
+    }
+    start<D>(a, t, t.row0 + col, grp, w);
+    if (first < tiles) {
+        wait_loads<0>();
+        for (int64_t i = first; i < tiles; i += step) {
+            // (past the last tile it is fetched again and not used: with the loads on every
+            // path the waits below can be counted)
+            const int64_t next = i + step < tiles ? i + step : i;
+            const int32_t key0 = static_cast<int32_t>(next) * kKeys;
+            const uint64_t nxt = tile_bits(next);
+            wait_loads<kN>();       // K is there; V may still be in flight
+            f32x16_t s = scores<D>(kb, col, grp, w.qf);
+            wait_lds_reads();       // K is read: its buffer is free
+            issue<D, kMask, true, kN>(kh, a.ks[1], key0, n - key0, nxt, kb, 0, lane);
+            softmax<D>(w, s, static_cast<uint32_t>(cur), grp, a.scale_log2);
+            wait_loads<kN>();       // V is there; the next K may still be in flight
+            values<D>(w, vb, s, col, grp);
+            wait_lds_reads();
+            issue<D, kMask, false, kN>(vh, a.vs[1], key0, n - key0, nxt, vb, 0, lane);
+            cur = nxt;
+        }
+        wait_loads<0>();   // nothing lands in the buffers any more
+    }
+
+    // ---- merge: every wave's O rows into its own K buffer, units permuted by row % 16 ----
+    const float l = halves_sum(w.l);
+    if (grp == 0) {
+        ml[wave][col][0] = w.m;
+        ml[wave][col][1] = l;
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        vread_t x;
+#pragma unroll
+        for (int db = 0; db < kDb; ++db) x[db] = w.o[db][r];
+        const int unit = ((r / 4) * 8 + grp * 4 + r % 4) ^ (col & 15);
+        *reinterpret_cast<vread_t *>(kb + col * L::kRow + unit * (4 * kDb)) = x;
+    }
+    __syncthreads();
+    for (int u = tid; u < kCrossFewRows * 32; u += 64 * kW) {
+        const int r = u / 32, unit = u % 32;
+        const int64_t row = t.row0 + r;
+        if (row >= a.rows) break;
+        float m = ml[0][r][0];
+#pragma unroll
+        for (int p = 1; p < kW; ++p) m = fmaxf(m, ml[p][r][0]);
+        const float ref = m == -kInf ? 0.0f : m;
+        float lsum = 0.0f;
+        vread_t x = {};
+#pragma unroll
+        for (int p = 0; p < kW; ++p) {
+            const float wgt = fast_exp2((ml[p][r][0] - ref) * a.scale_log2);
+            lsum = fmaf(wgt, ml[p][r][1], lsum);
+            const vread_t y =
+                *reinterpret_cast<const vread_t *>(ks + p * L::kBytes + r * L::kRow + (unit ^ (r & 15)) * (4 * kDb));
+#pragma unroll
+            for (int db = 0; db < kDb; ++db) x[db] = fmaf(wgt, y[db], x[db]);
+        }
+        if (a.parts > 1) {
+            const int64_t slot = (static_cast<int64_t>(t.tile) * a.parts + part) * kCrossFewRows + r;
+            if (unit == 0) *reinterpret_cast<f32x2_t *>(a.ws_ml + slot * 2) = f32x2_t{m, lsum};
+            *reinterpret_cast<vread_t *>(a.ws_o + slot * D + unit * kDb) = x;
+            continue;
+        }
+        const float inv = lsum == 0.0f ? 0.0f : 1.0f / lsum;
+#pragma unroll
+        for (int db = 0; db < kDb; ++db) x[db] *= inv;
+        *reinterpret_cast<vread_t *>(static_cast<float *>(a.out) + row_offset(a, a.os, t, row) + unit * kDb) = x;
+    }
+}
+
+template <int D>
+void run(const CrossKArgs &a, bool few, bool mask, dim3 grid, hipStream_t stream) {
+    if (few && mask) hipLaunchKernelGGL((cross_f32_few_kernel<D, true>), grid, dim3(64 * kWaves<D>), 0, stream, a);
+    else if (few) hipLaunchKernelGGL((cross_f32_few_kernel<D, false>), grid, dim3(64 * kWaves<D>), 0, stream, a);
+    else if (mask) hipLaunchKernelGGL((cross_f32_tile_kernel<D, true>), grid, dim3(64 * kTileWaves), 0, stream, a);
+    else hipLaunchKernelGGL((cross_f32_tile_kernel<D, false>), grid, dim3(64 * kTileWaves), 0, stream, a);
 }
 
 }  // namespace
 
-hipError_t launch_cross_f32(const CrossParams &p, const CrossKArgs &, hipStream_t stream) {
-    const int64_t blocks = (static_cast<int64_t>(p.Lq) + 3) / 4;
-    if (blocks > 0x7fffffffLL || p.heads > 65535 || p.B > 65535) return hipErrorInvalidConfiguration;
-    const dim3 grid(static_cast<uint32_t>(blocks), p.heads, p.B);
-    if (p.head_dim == 128) hipLaunchKernelGGL((cross_kernel<float, 128>), grid, dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL((cross_kernel<float, 64>), grid, dim3(256), 0, stream, p);
+hipError_t launch_cross_f32(const CrossKArgs &a, int32_t head_dim, bool few, uint32_t grid, hipStream_t stream) {
+    if (head_dim == 128) run<128>(a, few, a.key_mask != nullptr, dim3(grid), stream);
+    else run<64>(a, few, a.key_mask != nullptr, dim3(grid), stream);
     return hipGetLastError();
 }
 
