@@ -60,6 +60,11 @@ __device__ __forceinline__ void global_lds16(const uint8_t *p, uint8_t *dst) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)p, (lds_void_t *)dst, 16, 0, 0);
 }
 
+// The same from a buffer resource; an offset of -1 reads as zero.
+__device__ __forceinline__ void buffer_lds16(__amdgpu_buffer_rsrc_t r, uint8_t *dst, int voffset, int soffset) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t *)dst, 16, voffset, soffset, 0, 0);
+}
+
 template <typename E>
 __device__ __forceinline__ f32x16_t mma32(u32x4_t a, u32x4_t b, f32x16_t c) {
     if constexpr (sizeof(E) == 2) {
@@ -127,15 +132,20 @@ __device__ __forceinline__ void store_n(void *p, int64_t at, const float (&v)[kN
 __device__ __forceinline__ float gated(float x, float t) {
     return x * __builtin_amdgcn_rcpf(1.0f + fast_exp2(t));
 }
-__device__ __forceinline__ float activate(int kind, float x) {
+template <int kN>
+__device__ __forceinline__ void activate(int kind, float (&v)[kN]) {
     constexpr float kLog2e = 1.4426950408889634f;
-    switch (kind) {
-        case RF_ACT_GELU: return 0.5f * x * (1.0f + erff(x * 0.70710678118654752f));
+    if (kind == RF_ACT_GELU) {
+#pragma unroll
+        for (int e = 0; e < kN; ++e) v[e] = 0.5f * v[e] * (1.0f + erff(v[e] * 0.70710678118654752f));
+    } else if (kind == RF_ACT_GELU_TANH) {
         // x/2 (1 + tanh u) = x / (1 + e^(-2u))
-        case RF_ACT_GELU_TANH:
-            return gated(x, (-2.0f * 0.79788456080286536f * kLog2e) * (x + 0.044715f * (x * x * x)));
-        case RF_ACT_SILU: return gated(x, -kLog2e * x);
-        default: return x;
+#pragma unroll
+        for (int e = 0; e < kN; ++e)
+            v[e] = gated(v[e], (-2.0f * 0.79788456080286536f * kLog2e) * (v[e] + 0.044715f * (v[e] * v[e] * v[e])));
+    } else {
+#pragma unroll
+        for (int e = 0; e < kN; ++e) v[e] = gated(v[e], -kLog2e * v[e]);
     }
 }
 
@@ -150,10 +160,7 @@ __device__ __forceinline__ void finish(const LinearKArgs &a, uint32_t r, int c, 
 #pragma unroll
         for (int e = 0; e < kN; ++e) v[e] += t[e];
     }
-    if (a.activation != RF_ACT_NONE) {
-#pragma unroll
-        for (int e = 0; e < kN; ++e) v[e] = activate(a.activation, v[e]);
-    }
+    if (a.activation != RF_ACT_NONE) activate(a.activation, v);
     if (a.gate) {
         load_n<E, kN>(a.gate, a.gate_rows ? static_cast<int64_t>(a.frame[m]) * a.n_out + c : c, t);
 #pragma unroll
@@ -193,14 +200,17 @@ __device__ __forceinline__ bool tile_of(const LinearKArgs &a, int bid, int &rt, 
 }
 
 // kRB blocks of 32 rows to a wave, kWR x kWC waves of (32 kRB rows x 64 features).
-template <typename E, int kRB, int kWR, int kWC>
+// kFar: rows of x may lie further than 2 GB from the tile's first (64-bit addresses).
+template <typename E, int kRB, int kWR, int kWC, bool kFar>
 __global__ __launch_bounds__(64 * kWR * kWC) __attribute__((amdgpu_waves_per_eu(2)))
 void linear_tile_kernel(const LinearKArgs a) {
     constexpr int kWaves = kWR * kWC, kBM = 32 * kRB * kWR, kBN = 64 * kWC;
     constexpr int kXLoads = kBM / 8 / kWaves, kWLoads = kBN / 8 / kWaves;   // 8 rows each
-    constexpr int kBuf = (kBM + kBN) * kStep;
-    static_assert(kWaves * 8192 <= 2 * kBuf, "the epilogue's rows fit the buffers");
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kBuf];
+    constexpr int kXBuf = kBM * kStep, kWBuf = kBN * kStep;
+    // [x, even step][x, odd][W, even][W, odd]
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * (kXBuf + kWBuf)];
+    static_assert(kWaves * 8192 <= 2 * (kXBuf + kWBuf), "the epilogue's rows fit the buffers");
+    static_assert(kXBuf == kWBuf && (kXBuf & (kXBuf - 1)) == 0, "a step's parity is one bit of an LDS offset");
     int rt, ct;
     const int part = blockIdx.x % a.parts;
     if (!tile_of(a, blockIdx.x / a.parts, rt, ct)) return;
@@ -209,39 +219,55 @@ void linear_tile_kernel(const LinearKArgs a) {
     const int col = lane & 31, grp = lane >> 5;
     const int wr = wave / kWC, wc = wave % kWC;
 
-    // this lane's 16 bytes of each load: row lane / 8 of eight, the piece whose slot is lane % 8
-    const uint8_t *xp[kXLoads], *wp[kWLoads];
-    int piece;
-    {
-        const int sub = lane / 8;
-        piece = (lane % 8) ^ ((sub / 2) % 8);   // (row / 2) % 8 of row 8 i + sub: 4 (i % 2) more
+    // A load fills 8 rows: this lane's are row lane / 8 and the piece whose slot is lane % 8;
+    // (row / 2) % 8 of row 8 i + sub is sub / 2, and 4 more where i is odd.
+    const int sub = lane / 8, piece = (lane % 8) ^ (sub / 2);
+    const uint32_t row0 = static_cast<uint32_t>(rt) * kBM;
+    const int32_t rb = static_cast<int32_t>(a.row_bytes);
+    const uint8_t *const x0 = static_cast<const uint8_t *>(uniform_ptr(x_row(a, row0)));
+    const __amdgpu_buffer_rsrc_t wres = __builtin_amdgcn_make_buffer_rsrc(
+        uniform_ptr(w_row(a, ct * kBN)), 0, 0x7fffffff, kBufferWord3);
+    const __amdgpu_buffer_rsrc_t xres =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(x0), 0, 0x7fffffff, kBufferWord3);
+    [[maybe_unused]] const uint8_t *xp[kXLoads];
+    [[maybe_unused]] int32_t xo[kXLoads], wo[kWLoads];
 #pragma unroll
-        for (int i = 0; i < kXLoads; ++i) {
-            const int row = (wave * kXLoads + i) * 8 + sub;
-            xp[i] = x_row(a, static_cast<uint32_t>(rt) * kBM + row);
-        }
-#pragma unroll
-        for (int i = 0; i < kWLoads; ++i) {
-            const int row = (wave * kWLoads + i) * 8 + sub;
-            wp[i] = w_row(a, ct * kBN + row);
-        }
+    for (int i = 0; i < kXLoads; ++i) {
+        const int at = wave * kXLoads + i;
+        const uint8_t *p = x_row(a, row0 + at * 8 + sub) + 16 * (piece ^ ((at % 2) * 4));
+        if constexpr (kFar) xp[i] = p;
+        else xo[i] = static_cast<int32_t>(p - x0);
     }
-    auto issue = [&](int step, uint8_t *buf) {
-        const int64_t at0 = static_cast<int64_t>(step) * kStep;
-        // the last step may be short: pieces past the row's end come from zeros
-        const bool cut = at0 + kStep > a.row_bytes;
+#pragma unroll
+    for (int i = 0; i < kWLoads; ++i) {
+        const int at = wave * kWLoads + i, c = at * 8 + sub, most = a.n_out - 1 - ct * kBN;
+        wo[i] = (c < most ? c : most) * rb + 16 * (piece ^ ((at % 2) * 4));
+    }
+    // Loads of a step, x's and W's, into the buffers of its parity. The reduction's last
+    // step may be short: from then on lanes past the row's end load zeros.
+    const int32_t tail = rb % kStep;
+    auto issue = [&](int step, int odd) {
+        const int32_t at0 = step * kStep;
+        if (tail != 0 && at0 + kStep > rb) {
+#pragma unroll
+            for (int i = 0; i < kXLoads; ++i)
+                if (16 * (piece ^ (((wave * kXLoads + i) % 2) * 4)) >= tail) {
+                    if constexpr (kFar) xp[i] = reinterpret_cast<const uint8_t *>(&kZeros) - at0;
+                    else xo[i] = -1;
+                }
+#pragma unroll
+            for (int i = 0; i < kWLoads; ++i)
+                if (16 * (piece ^ (((wave * kWLoads + i) % 2) * 4)) >= tail) wo[i] = -1;
+        }
+        uint8_t *xd = lds + odd * kXBuf + wave * kXLoads * 1024;
+        uint8_t *wd = lds + 2 * kXBuf + odd * kWBuf + wave * kWLoads * 1024;
 #pragma unroll
         for (int i = 0; i < kXLoads; ++i) {
-            const int64_t at = at0 + 16 * (piece ^ (((wave * kXLoads + i) % 2) * 4));
-            const uint8_t *p = cut && at >= a.row_bytes ? reinterpret_cast<const uint8_t *>(&kZeros) : xp[i] + at;
-            global_lds16(p, buf + (wave * kXLoads + i) * 1024);
+            if constexpr (kFar) global_lds16(xp[i] + at0, xd + i * 1024);
+            else buffer_lds16(xres, xd + i * 1024, xo[i], at0);
         }
 #pragma unroll
-        for (int i = 0; i < kWLoads; ++i) {
-            const int64_t at = at0 + 16 * (piece ^ (((wave * kWLoads + i) % 2) * 4));
-            const uint8_t *p = cut && at >= a.row_bytes ? reinterpret_cast<const uint8_t *>(&kZeros) : wp[i] + at;
-            global_lds16(p, buf + kBM * kStep + (wave * kWLoads + i) * 1024);
-        }
+        for (int i = 0; i < kWLoads; ++i) buffer_lds16(wres, wd + i * 1024, wo[i], at0);
     };
 
     f32x16_t acc[2][kRB];
@@ -249,60 +275,68 @@ void linear_tile_kernel(const LinearKArgs a) {
     for (int f = 0; f < 2; ++f)
 #pragma unroll
         for (int b = 0; b < kRB; ++b) acc[f][b] = f32x16_t{};
-    // a lane's pieces 2 kk + grp of its row in each block
-    const int xbase = (wr * kRB * 32 + col) * kStep, wbase = (kBM + wc * 64 + col) * kStep;
-    const int swz = (col / 2) % 8;
-    // four pairs of pieces to a step; the next pair's operands are read while this one's multiply
-    auto compute = [&](const uint8_t *buf) {
-        u32x4_t wf[2][2], xf[2][kRB];
-        auto read = [&](int kk) {
-            const int at = ((2 * kk + grp) ^ swz) * 16;
+    // this lane's pieces 2 kk + grp of its row in each block
+    int xat[4], wat[4];
 #pragma unroll
-            for (int f = 0; f < 2; ++f)
-                wf[kk % 2][f] = *reinterpret_cast<const u32x4_t *>(buf + wbase + f * 32 * kStep + at);
+    for (int kk = 0; kk < 4; ++kk) {
+        const int at = ((2 * kk + grp) ^ ((col / 2) % 8)) * 16;
+        xat[kk] = (wr * kRB * 32 + col) * kStep + at;
+        wat[kk] = 2 * kXBuf + (wc * 64 + col) * kStep + at;
+    }
+    // Four pairs of pieces to a step; the next pair's operands are read while this one's
+    // multiply, across the steps' border too: at the last pair a wave waits for its loads
+    // of the next step and its reads of this one, meets the others (so the next step is
+    // whole and this one's buffer free), sends for the step after the next and reads on.
+    u32x4_t wf[2][2], xf[2][kRB];
+    auto read = [&](int kk) {
 #pragma unroll
-            for (int b = 0; b < kRB; ++b)
-                xf[kk % 2][b] = *reinterpret_cast<const u32x4_t *>(buf + xbase + b * 32 * kStep + at);
-        };
-        read(0);
+        for (int f = 0; f < 2; ++f) wf[kk % 2][f] = *reinterpret_cast<const u32x4_t *>(lds + wat[kk] + f * 32 * kStep);
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-            if (kk + 1 < 4) read(kk + 1);
+        for (int b = 0; b < kRB; ++b) xf[kk % 2][b] = *reinterpret_cast<const u32x4_t *>(lds + xat[kk] + b * 32 * kStep);
+    };
+    constexpr int kReads = 2 + kRB, kMma = 2 * kRB * (sizeof(E) == 2 ? 1 : 4);
+    auto multiply = [&](int kk) {
 #pragma unroll
-            for (int b = 0; b < kRB; ++b)
+        for (int b = 0; b < kRB; ++b)
 #pragma unroll
-                for (int f = 0; f < 2; ++f) acc[f][b] = mma32<E>(wf[kk % 2][f], xf[kk % 2][b], acc[f][b]);
+            for (int f = 0; f < 2; ++f) acc[f][b] = mma32<E>(wf[kk % 2][f], xf[kk % 2][b], acc[f][b]);
+    };
+    auto interleaved = [&]() {   // one read after every kMma / kReads matrix instructions
+#pragma unroll
+        for (int i = 0; i < kReads; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, kMma / kReads, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
-        constexpr int kReads = 2 + kRB, kMma = 2 * kRB * (sizeof(E) == 2 ? 1 : 4);
-        __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
-#pragma unroll
-        for (int kk = 0; kk < 3; ++kk) {
-#pragma unroll
-            for (int i = 0; i < kReads; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x008, kMma / kReads, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            }
-            __builtin_amdgcn_sched_group_barrier(0x008, kMma - kMma / kReads * kReads, 0);
-        }
-        __builtin_amdgcn_sched_group_barrier(0x008, kMma, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, kMma - kMma / kReads * kReads, 0);
     };
     const int s0 = part * a.steps_per_part;
     const int s1 = s0 + a.steps_per_part < a.steps ? s0 + a.steps_per_part : a.steps;
-    auto step_done = [&]() {
-        wait_loads<0>();   // this wave's loads have reached LDS
+    issue(s0, 0);
+    wait_loads<0>();
+    __syncthreads();
+    if (s0 + 1 < s1) issue(s0 + 1, 1);
+    read(0);
+    for (int s = s0; s < s1; ++s) {
+#pragma unroll
+        for (int kk = 0; kk < 3; ++kk) {
+            read(kk + 1);
+            multiply(kk);
+            interleaved();
+        }
+        wait_loads<0>();
+        wait_lds_reads();
         __syncthreads();
-    };
-    issue(s0, lds);
-    step_done();
-    for (int s = s0; s < s1; s += 2) {
-        if (s + 1 < s1) issue(s + 1, lds + kBuf);
-        compute(lds);
-        step_done();
-        if (s + 1 >= s1) break;
-        if (s + 2 < s1) issue(s + 2, lds);
-        compute(lds + kBuf);
-        step_done();
+        if (s + 2 < s1) issue(s + 2, (s - s0) & 1);
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+            xat[kk] ^= kXBuf;
+            wat[kk] ^= kWBuf;
+        }
+        read(0);   // (after the last step: what is there, and not used)
+        multiply(3);
     }
+    wait_lds_reads();
+    __syncthreads();
 
     // ---- epilogue: 32 rows x 64 features at a time through 8 KB of the wave's own, 256
     // bytes a row, 16-byte units permuted by row % 16; a lane then has 8 neighbouring
@@ -320,10 +354,10 @@ void linear_tile_kernel(const LinearKArgs a) {
                     f32x4_t{acc[f][b][g4 * 4], acc[f][b][g4 * 4 + 1], acc[f][b][g4 * 4 + 2], acc[f][b][g4 * 4 + 3]};
             }
         wait_lds_reads();   // (a wave's LDS accesses run in order; this orders the compiler's)
-#pragma unroll
+#pragma unroll 1
         for (int i = 0; i < 4; ++i) {
-            const int lr = i * 8 + lane / 8;
-            const uint32_t r = static_cast<uint32_t>(rt) * kBM + (wr * kRB + b) * 32 + lr;
+            const int lr = i * 8 + sub;
+            const uint32_t r = row0 + (wr * kRB + b) * 32 + lr;
             float v[8];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -435,7 +469,8 @@ struct LinearPlan {
     int32_t steps, per_part, parts;
 };
 
-LinearPlan linear_plan(int64_t rows, int32_t K, int32_t n_out, int32_t dtype, int32_t cus, bool may_split) {
+// far: rows of a tile may lie 2 GB apart (only the smaller tile's kernel takes them).
+LinearPlan linear_plan(int64_t rows, int32_t K, int32_t n_out, int32_t dtype, int32_t cus, bool far, bool may_split) {
     LinearPlan p{};
     const int64_t bytes = static_cast<int64_t>(K) * (dtype == RF_F32 ? 4 : 2);
     auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
@@ -452,7 +487,7 @@ LinearPlan linear_plan(int64_t rows, int32_t K, int32_t n_out, int32_t dtype, in
         return p;
     }
     const int64_t big = up(rows, 256) * up(n_out, 256), small = up(rows, 128) * up(n_out, 128);
-    p.form = big * 8 >= cus * 6 ? kTile256 : kTile128;
+    p.form = big * 8 >= cus * 6 && !far ? kTile256 : kTile128;
     const int64_t t = p.form == kTile256 ? 256 : 128, tiles = p.form == kTile256 ? big : small;
     p.row_tiles = up(rows, t);
     p.col_tiles = up(n_out, t);
@@ -470,28 +505,46 @@ LinearPlan linear_plan(int64_t rows, int32_t K, int32_t n_out, int32_t dtype, in
 }
 
 template <typename E>
-void run(const LinearPlan &p, const LinearKArgs &a, dim3 grid, hipStream_t stream) {
+void run(const LinearPlan &p, const LinearKArgs &a, bool far, dim3 grid, hipStream_t stream) {
     switch (p.form) {
         case kFew16: hipLaunchKernelGGL((linear_few_kernel<E, 1>), grid, dim3(512), 0, stream, a); break;
         case kFew32: hipLaunchKernelGGL((linear_few_kernel<E, 2>), grid, dim3(512), 0, stream, a); break;
         case kFew64: hipLaunchKernelGGL((linear_few_kernel<E, 4>), grid, dim3(512), 0, stream, a); break;
-        case kTile128: hipLaunchKernelGGL((linear_tile_kernel<E, 2, 2, 2>), grid, dim3(256), 0, stream, a); break;
-        case kTile256: hipLaunchKernelGGL((linear_tile_kernel<E, 4, 2, 4>), grid, dim3(512), 0, stream, a); break;
+        case kTile128:
+            if (far) hipLaunchKernelGGL((linear_tile_kernel<E, 2, 2, 2, true>), grid, dim3(256), 0, stream, a);
+            else hipLaunchKernelGGL((linear_tile_kernel<E, 2, 2, 2, false>), grid, dim3(256), 0, stream, a);
+            break;
+        case kTile256: hipLaunchKernelGGL((linear_tile_kernel<E, 4, 2, 4, false>), grid, dim3(512), 0, stream, a); break;
     }
 }
 
 }  // namespace
 
 int64_t linear_workspace(int64_t rows, int32_t K, int32_t n_out, int32_t dtype, int32_t cus) {
-    const LinearPlan p = linear_plan(rows, K, n_out, dtype, cus, true);
-    return p.parts > 1 ? p.parts * rows * n_out * 4 : 0;
+    // (far or not is the frame list's: room for either)
+    int64_t bytes = 0;
+    for (const bool far : {false, true}) {
+        const LinearPlan p = linear_plan(rows, K, n_out, dtype, cus, far, true);
+        const int64_t need = p.parts > 1 ? p.parts * rows * n_out * 4 : 0;
+        bytes = need > bytes ? need : bytes;
+    }
+    return bytes;
 }
 
 hipError_t launch_linear(const LinearParams &p, hipStream_t stream) {
     const int32_t xcds = p.geo.xcds;
     if (p.geo.cus < 1 || xcds < 1 || xcds > 64) return hipErrorInvalidValue;
     const int64_t rows = p.M * p.N;
-    const LinearPlan plan = linear_plan(rows, p.K, p.n_out, p.dtype, p.geo.cus, p.ws != nullptr);
+    const int64_t row_bytes = static_cast<int64_t>(p.K) * (p.dtype == RF_F32 ? 4 : 2);
+    // a tile's rows span 256 rows and what lies between the frames that it meets
+    int64_t gaps = 0;
+    for (int i = 0, j = 0; i < p.M; ++i) {
+        while ((i - j) * p.N > 256) ++j;   // frames j..i may meet in one tile
+        const int64_t gap = (p.src_frame[i] - p.src_frame[j] - (i - j)) * p.N;
+        gaps = gap > gaps ? gap : gaps;
+    }
+    const bool far = static_cast<double>(gaps + 257) * static_cast<double>(row_bytes) >= 2147483647.0;
+    const LinearPlan plan = linear_plan(rows, p.K, p.n_out, p.dtype, p.geo.cus, far, p.ws != nullptr);
     LinearKArgs a{};
     a.x = static_cast<const uint8_t *>(p.x);
     a.w = static_cast<const uint8_t *>(p.weight);
@@ -500,7 +553,7 @@ hipError_t launch_linear(const LinearParams &p, hipStream_t stream) {
     a.residual = p.residual;
     a.y = p.y;
     a.ws = static_cast<float *>(p.ws);
-    a.row_bytes = static_cast<int64_t>(p.K) * (p.dtype == RF_F32 ? 4 : 2);
+    a.row_bytes = row_bytes;
     a.rows = static_cast<uint32_t>(rows);
     a.N = static_cast<uint32_t>(p.N);
     a.n_out = p.n_out;
@@ -525,8 +578,8 @@ hipError_t launch_linear(const LinearParams &p, hipStream_t stream) {
     const int64_t grid = (few ? tiles : static_cast<int64_t>(a.per_xcd) * xcds) * plan.parts;
     if (grid > 0x7fffffffLL) return hipErrorInvalidConfiguration;
     const dim3 g(static_cast<uint32_t>(grid));
-    if (p.dtype == RF_F32) run<float>(plan, a, g, stream);
-    else run<uint16_t>(plan, a, g, stream);
+    if (p.dtype == RF_F32) run<float>(plan, a, far, g, stream);
+    else run<uint16_t>(plan, a, far, g, stream);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || plan.parts == 1) return e;
     const int64_t blocks = (rows * (p.n_out / 4) + 255) / 256;
