@@ -301,13 +301,16 @@ void linear_tile_kernel(const LinearKArgs a) {
 #pragma unroll
             for (int f = 0; f < 2; ++f) acc[f][b] = mma32<E>(wf[kk % 2][f], xf[kk % 2][b], acc[f][b]);
     };
-    auto interleaved = [&]() {   // one read after every kMma / kReads matrix instructions
+    // The order that the compiler keeps: one read after every kMma / kReads matrix
+    // instructions (left alone it reads a pair's operands right before they multiply).
+    auto interleaved = [&]() {
 #pragma unroll
         for (int i = 0; i < kReads; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, kMma / kReads, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
         __builtin_amdgcn_sched_group_barrier(0x008, kMma - kMma / kReads * kReads, 0);
+        __builtin_amdgcn_sched_barrier(0);
     };
     const int s0 = part * a.steps_per_part;
     const int s1 = s0 + a.steps_per_part < a.steps ? s0 + a.steps_per_part : a.steps;
@@ -317,6 +320,7 @@ void linear_tile_kernel(const LinearKArgs a) {
     if (s0 + 1 < s1) issue(s0 + 1, 1);
     read(0);
     for (int s = s0; s < s1; ++s) {
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int kk = 0; kk < 3; ++kk) {
             read(kk + 1);
@@ -327,6 +331,7 @@ void linear_tile_kernel(const LinearKArgs a) {
         wait_lds_reads();
         __syncthreads();
         if (s + 2 < s1) issue(s + 2, (s - s0) & 1);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
             xat[kk] ^= kXBuf;
@@ -334,6 +339,12 @@ void linear_tile_kernel(const LinearKArgs a) {
         }
         read(0);   // (after the last step: what is there, and not used)
         multiply(3);
+        interleaved();
+        // (without a use here the reads would sink to the next step's first multiplication)
+#pragma unroll
+        for (int f = 0; f < 2; ++f) asm volatile("" : "+v"(wf[0][f]));
+#pragma unroll
+        for (int b = 0; b < kRB; ++b) asm volatile("" : "+v"(xf[0][b]));
     }
     wait_lds_reads();
     __syncthreads();
