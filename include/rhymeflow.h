@@ -624,7 +624,8 @@ typedef struct rf_rotary_axes {
  *   one); otherwise no output row may overlap another row of the call. Rows of
  *   one stride may interleave (q and k as views of one buffer).
  * head_dim: a multiple of 8 up to 256; with RF_ROTARY_HALVES R is a multiple of 16.
- * frame_ids, M, T: as rf_keyframe_attention. H, W: token grid, up to 65536 each.
+ * frame_ids, M, T: as rf_keyframe_attention. H, W: token grid, up to 65536 each and
+ *   2^26 tokens. Up to 65535 heads each.
  * flags: RF_ROWS_IN_FULL, RF_ROWS_OUT_FULL, RF_ROTARY_HALVES, RF_ROTARY_INVERSE.
  * Errors: RF_ERR_INVALID_ARG (NULL, sizes <= 0, ids, unknown flags, axes, a
  *   stride below the row, overlap), RF_ERR_RANGE (ids, T, H, W, positions, sizes

@@ -8,6 +8,7 @@ the HIP kernels; there is no CPU fallback. Importing this module fails loudly
 if the library has not been built.
 """
 import ctypes
+import functools
 import os
 
 import numpy as np
@@ -727,11 +728,11 @@ def rf_async_schedule(T: int, T_w: int, T_mid: int, n_small: int, n_large: int):
 # --- a block's operators around the attention -------------------------------------
 
 def _on_device(tensors):
-    """The addresses of device tensors (a dict by name; None stays None) of any
-    strides, all on torch's current device: the device the stream and the launch
-    belong to."""
-    index, out = None, []
-    for name, t in tensors.items():
+    """The current device's index and the addresses of the device tensors
+    ((tensor or None, name) pairs; None stays None) of any strides, which all
+    have to be on it: stream and launch belong to the current device."""
+    index, out = -1, []
+    for t, name in tensors:
         if t is None:
             out.append(None)
             continue
@@ -739,31 +740,53 @@ def _on_device(tensors):
             raise TypeError(f"{name} must be a torch.Tensor")
         if not t.is_cuda:
             raise ValueError(f"{name} must be a device tensor")
-        if index is None:
+        if index < 0:
             index = torch.cuda.current_device()
-        if t.device.index != index:
+        if t.get_device() != index:
             raise ValueError(f"{name} is on {t.device}, the current device is cuda:{index}")
         out.append(t.data_ptr())
-    return out
+    return index, out
+
+
+def _stream_on(stream, index):
+    """_stream, for a caller that has the current device's index already."""
+    return _raw_stream(index) if stream is None and _raw_stream is not None else _stream(stream)
 
 
 def _same_dtype(tensors):
-    dt = next(iter(tensors.values())).dtype
-    for name, t in tensors.items():
+    dt = tensors[0][0].dtype
+    for t, name in tensors:
         if t is not None and t.dtype != dt:
             raise TypeError(f"{name} has dtype {t.dtype}, the call's is {dt}")
     return _dtype_code(dt)
 
 
-def _head_rows(t, name, heads, d):
+def _head_rows(t, name, rows, heads, d):
     """Row stride in elements of a [rows][heads][head_dim] tensor whose rows are contiguous."""
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d:
-        raise ValueError(f"{name} must be [rows][{heads}][{d}]")
-    if (d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d):
+    if t.shape != (rows, heads, d):
+        raise ValueError(f"{name} must be [{rows}][{heads}][{d}], it is {list(t.shape)}: [rows of the layout][heads][head_dim]")
+    row, head, one = t.stride()
+    if (d > 1 and one != 1) or (heads > 1 and head != d):
         raise ValueError(f"{name}: the elements of a row must be contiguous")
-    if t.shape[0] > 1 and t.stride(0) < heads * d:
+    if rows <= 1:
+        return heads * d
+    if row < heads * d:
         raise ValueError(f"{name}: rows overlap")
-    return t.stride(0) if t.shape[0] > 1 else heads * d
+    return row
+
+
+@functools.lru_cache(maxsize=64)
+def _rotary_axes(dims, theta, origin, step):
+    axes = rf_rotary_axes()
+    axes.dims[:] = [int(n) for n in dims]
+    axes.theta[:] = [float(theta)] * 3 if isinstance(theta, (int, float)) else [float(x) for x in theta]
+    axes.origin[:] = [float(x) for x in origin]
+    axes.step[:] = [float(x) for x in step]
+    return axes
+
+
+def _key(values):
+    return values if isinstance(values, (int, float, tuple)) else tuple(values)
 
 
 def rf_rotary(q, frame_ids, T: int, H: int, W: int, dims, k=None, out=None, k_out=None, theta=10000.0,
@@ -778,45 +801,36 @@ def rf_rotary(q, frame_ids, T: int, H: int, W: int, dims, k=None, out=None, k_ou
     (out, k_out) if k is given."""
     ids, ids_p = _ids(frame_ids)
     M = ids.size
-    if q.dim() != 3:
-        raise ValueError("q must be [rows][heads][head_dim]")
-    d = q.shape[2]
-    rows_in, rows_out = H * W * (T if in_full else M), H * W * (T if out_full else M)
-
-    def output(y, x, name):
-        if y is not None:
-            return y
-        if out_full and M != T:
-            raise ValueError(f"{name} must be given with out_full: rows of other frames are left as they are")
-        return _empty((rows_out, x.shape[1], d), x.dtype, x.device, stream)
-    pairs = [("q", q, "out", output(out, q, "out"))]
-    if k is not None:
-        if k.dim() != 3:
-            raise ValueError("k must be [rows][heads][head_dim]")
-        pairs.append(("k", k, "k_out", output(k_out, k, "k_out")))
-    strides, heads = [], []
-    for xn, x, yn, y in pairs:
-        for t, name, rows in ((x, xn, rows_in), (y, yn, rows_out)):
-            strides.append(_head_rows(t, name, x.shape[1], d))
-            if t.shape[0] != rows:
-                raise ValueError(f"{name} has {t.shape[0]} rows, the layout asks for {rows}")
-        heads.append(x.shape[1])
-    code = _same_dtype({n: t for xn, x, yn, y in pairs for n, t in ((xn, x), (yn, y))})
-    ptrs = _on_device({n: t for xn, x, yn, y in pairs for n, t in ((xn, x), (yn, y))})
+    if q.dim() != 3 or (k is not None and k.dim() != 3):
+        raise ValueError("q and k must be [rows][heads][head_dim]")
+    _, hq, d = q.shape
+    N = H * W
+    rows_in, rows_out = N * (T if in_full else M), N * (T if out_full else M)
+    if out_full and M != T and (out is None or (k is not None and k_out is None)):
+        raise ValueError("out must be given with out_full: rows of other frames are left as they are")
+    if out is None:
+        out = _empty((rows_out, hq, d), q.dtype, q.device, stream)
+    sq, so = _head_rows(q, "q", rows_in, hq, d), _head_rows(out, "out", rows_out, hq, d)
     if k is None:
-        strides += [0, 0]
-        heads.append(0)
+        hk = sk = sko = 0
+        tensors = ((q, "q"), (out, "out"))
+        code = _same_dtype(tensors)
+        index, ptrs = _on_device(tensors)
         ptrs += [None, None]
-    axes = rf_rotary_axes()
-    axes.dims[:] = [int(n) for n in dims]
-    axes.theta[:] = [float(theta)] * 3 if np.isscalar(theta) else [float(x) for x in theta]
-    axes.origin[:] = [float(x) for x in origin]
-    axes.step[:] = [float(x) for x in step]
+    else:
+        hk = k.shape[1]
+        if k_out is None:
+            k_out = _empty((rows_out, hk, d), k.dtype, k.device, stream)
+        sk, sko = _head_rows(k, "k", rows_in, hk, d), _head_rows(k_out, "k_out", rows_out, hk, d)
+        tensors = ((q, "q"), (out, "out"), (k, "k"), (k_out, "k_out"))
+        code = _same_dtype(tensors)
+        index, ptrs = _on_device(tensors)
+    axes = _rotary_axes(_key(dims), _key(theta), _key(origin), _key(step))
     flags = ((RF_ROWS_IN_FULL if in_full else 0) | (RF_ROWS_OUT_FULL if out_full else 0) |
              (RF_ROTARY_HALVES if halves else 0) | (RF_ROTARY_INVERSE if inverse else 0))
-    _check(lib.rf_rotary(*ptrs, ids_p, M, T, H, W, heads[0], heads[1], d, ctypes.byref(axes), *strides, flags, code,
-                         _stream(stream)))
-    return pairs[0][3] if k is None else (pairs[0][3], pairs[1][3])
+    _check(lib.rf_rotary(*ptrs, ids_p, M, T, H, W, hq, hk, d, ctypes.byref(axes), sq, so, sk, sko, flags, code,
+                         _stream_on(stream, index)))
+    return out if k is None else (out, k_out)
 
 
 def rf_cross_attention_workspace(B: int, Lq: int, Lk: int, heads: int, kv_heads: int, head_dim: int, dtype,
@@ -830,6 +844,17 @@ def rf_cross_attention_workspace(B: int, Lq: int, Lk: int, heads: int, kv_heads:
     return int(n.value)
 
 
+# What a call that brings no workspace asks for each time, by the current device and the sizes.
+@functools.lru_cache(maxsize=256)
+def _cross_need(device, B, Lq, Lk, heads, kv_heads, head_dim, code):
+    return rf_cross_attention_workspace(B, Lq, Lk, heads, kv_heads, head_dim, code)
+
+
+@functools.lru_cache(maxsize=256)
+def _linear_need(device, M, rows_per_frame, in_features, out_features, code):
+    return rf_frame_linear_workspace(M, rows_per_frame, in_features, out_features, code)
+
+
 def rf_cross_attention(q, k, v, kv_lengths=None, key_mask=None, out=None, workspace=None, stream=None):
     """q [B][Lq][heads][head_dim] attends to k, v [B][Lk][kv_heads][head_dim], of
     any strides whose head_dim elements are contiguous, -> out as q. kv_lengths:
@@ -839,32 +864,39 @@ def rf_cross_attention(q, k, v, kv_lengths=None, key_mask=None, out=None, worksp
     if q.dim() != 4 or k.dim() != 4 or v.shape != k.shape or k.shape[0] != q.shape[0] or k.shape[3] != q.shape[3]:
         raise ValueError("q must be [B][Lq][heads][head_dim], k and v [B][Lk][kv_heads][head_dim]")
     B, Lq, heads, d = q.shape
-    Lk, kvh = k.shape[1], k.shape[2]
+    _, Lk, kvh, _ = k.shape
     if out is None:
         out = _empty((B, Lq, heads, d), q.dtype, q.device, stream)
-    if out.shape != q.shape:
+    elif out.shape != q.shape:
         raise ValueError("out must have q's shape")
-    code = _same_dtype({"q": q, "k": k, "v": v, "out": out})
-    layout = rf_cross_layout()
-    for name, t in (("q", q), ("k", k), ("v", v), ("out", out)):
-        if d > 1 and t.stride(3) != 1:
+    tensors = ((q, "q"), (k, "k"), (v, "v"), (out, "out"))
+    code = _same_dtype(tensors)
+    strides = []
+    for t, name in tensors:
+        st = t.stride()
+        if d > 1 and st[3] != 1:
             raise ValueError(f"{name}: the elements of a head must be contiguous")
-        # (the stride of an axis of one element is never taken)
-        getattr(layout, name)[:] = [t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)]
+        strides.append(st[:3])
+    if B == 1 or Lq == 1 or Lk == 1 or heads == 1 or kvh == 1:
+        # (the stride of an axis of one element is any number and never taken)
+        sizes = ((B, Lq, heads), (B, Lk, kvh), (B, Lk, kvh), (B, Lq, heads))
+        strides = [tuple(x if n > 1 else 0 for x, n in zip(a, b)) for a, b in zip(strides, sizes)]
+    layout = rf_cross_layout(*strides)
     if kv_lengths is not None:
         if kv_lengths.dtype != torch.int32 or kv_lengths.shape != (B,) or not kv_lengths.is_contiguous():
             raise ValueError("kv_lengths must be contiguous int32 [B]")
     if key_mask is not None:
         if key_mask.dtype not in (torch.uint8, torch.bool) or key_mask.shape != (B, Lk) or not key_mask.is_contiguous():
             raise ValueError("key_mask must be contiguous bool or uint8 [B][Lk]")
-    ptrs = _on_device({"q": q, "k": k, "v": v, "out": out, "kv_lengths": kv_lengths, "key_mask": key_mask})
+    index, ptrs = _on_device(tensors + ((kv_lengths, "kv_lengths"), (key_mask, "key_mask")))
     if workspace is None and q.numel() > 0 and k.numel() > 0:
-        need = rf_cross_attention_workspace(B, Lq, Lk, heads, kvh, d, code)
+        need = _cross_need(index, B, Lq, Lk, heads, kvh, d, code)
         workspace = _empty(need, torch.uint8, q.device, stream) if need > 0 else None
     ws_p, wbytes = _workspace_arg(workspace)
     _check(lib.rf_cross_attention(*ptrs, B, Lq, Lk, heads, kvh, d, ctypes.byref(layout), code, ws_p, wbytes,
-                                  _stream(stream)))
+                                  _stream_on(stream, index)))
     return out
+
 
 
 def _workspace_arg(workspace):
@@ -872,7 +904,7 @@ def _workspace_arg(workspace):
         return None, 0
     if not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
-    return _on_device({"workspace": workspace})[0], workspace.numel() * workspace.element_size()
+    return _on_device(((workspace, "workspace"),))[1][0], workspace.numel() * workspace.element_size()
 
 
 def rf_frame_linear_workspace(M: int, rows_per_frame: int, in_features: int, out_features: int, dtype,
@@ -926,18 +958,18 @@ def rf_frame_linear(x, weight, bias=None, activation: str = "none", gate=None, r
         if gate.shape != (T, n_out):
             raise ValueError(f"gate must be [{n_out}] or [{T}][{n_out}]")
         flags |= RF_GATE_PER_FRAME
-    tensors = {"x": x, "weight": weight, "bias": bias, "gate": gate, "residual": residual, "out": out}
+    tensors = ((x, "x"), (weight, "weight"), (bias, "bias"), (gate, "gate"), (residual, "residual"), (out, "out"))
     code = _same_dtype(tensors)
-    for name, t in tensors.items():
+    for t, name in tensors:
         if t is not None and not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous")
-    ptrs = _on_device(tensors)
+    index, ptrs = _on_device(tensors)
     if workspace is None and M > 0 and rows_per_frame > 0 and weight.numel() > 0:
-        need = rf_frame_linear_workspace(M, rows_per_frame, K, n_out, code)
+        need = _linear_need(index, M, rows_per_frame, K, n_out, code)
         workspace = _empty(need, torch.uint8, x.device, stream) if need > 0 else None
     ws_p, wbytes = _workspace_arg(workspace)
     _check(lib.rf_frame_linear(*ptrs, ids_p, M, T, rows_per_frame, K, n_out, ACTIVATIONS[activation], flags, code,
-                               ws_p, wbytes, _stream(stream)))
+                               ws_p, wbytes, _stream_on(stream, index)))
     return out
 
 

@@ -891,7 +891,10 @@ static int rotary_call(const void *q, void *q_out, const void *k, void *k_out, c
     if (H <= 0 || W <= 0 || q_heads <= 0 || (k && k_heads <= 0) || head_dim <= 0)
         return fail(RF_ERR_INVALID_ARG, "%s: sizes must be positive (H=%d W=%d q_heads=%d k_heads=%d head_dim=%d)", fn,
                     H, W, q_heads, k_heads, head_dim);
+    if (q_heads > 65535 || (k && k_heads > 65535))
+        return fail(RF_ERR_RANGE, "%s: more than 65535 heads", fn);
     if (H > 65536 || W > 65536) return fail(RF_ERR_RANGE, "%s: H = %d or W = %d exceeds 65536", fn, H, W);
+    if (static_cast<double>(H) * W > 67108864.0) return fail(RF_ERR_RANGE, "%s: more than 2^26 tokens a frame", fn);
     int32_t ids[RF_MAX_FRAMES];
     const int rc = check_id_list(frame_ids, M, T, ids, fn);
     if (rc != RF_OK) return rc;
@@ -968,10 +971,10 @@ static int rotary_call(const void *q, void *q_out, const void *k, void *k_out, c
     for (int a = 0; a < 3; ++a) {
         p.origin[a] = axes->origin[a];
         p.step[a] = axes->step[a];
-        for (int32_t j = 0; j < axes->dims[a] / 2; ++j) {
-            const double turns = pow(axes->theta[a], -2.0 * j / axes->dims[a]) / 6.283185307179586476925;
-            p.turns[pair++] = (flags & RF_ROTARY_INVERSE) ? -turns : turns;
-        }
+        // theta^(-2j/dims) by multiplication: with 64-bit mantissas 128 of them stay right to a double's last place
+        const long double ratio = axes->dims[a] > 0 ? powl(axes->theta[a], -2.0L / axes->dims[a]) : 1.0L;
+        long double turns = ((flags & RF_ROTARY_INVERSE) ? -0.5L : 0.5L) / 3.14159265358979323846264338328L;
+        for (int32_t j = 0; j < axes->dims[a] / 2; ++j, turns *= ratio) p.turns[pair++] = static_cast<double>(turns);
     }
     for (int32_t m = 0; m < M; ++m) p.frame[m] = static_cast<int16_t>(ids[m]);
     row_frames(ids, M, in_full, p.src_frame);

@@ -65,6 +65,10 @@ __device__ __forceinline__ void buffer_lds16(__amdgpu_buffer_rsrc_t r, uint8_t *
     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t *)dst, 16, voffset, soffset, 0, 0);
 }
 
+__device__ __forceinline__ u32x4_t buffer_load16(__amdgpu_buffer_rsrc_t r, int voffset, int soffset) {
+    return __builtin_amdgcn_raw_buffer_load_b128(r, voffset, soffset, 0);
+}
+
 template <typename E>
 __device__ __forceinline__ f32x16_t mma32(u32x4_t a, u32x4_t b, f32x16_t c) {
     if constexpr (sizeof(E) == 2) {
@@ -207,10 +211,11 @@ void linear_tile_kernel(const LinearKArgs a) {
     constexpr int kWaves = kWR * kWC, kBM = 32 * kRB * kWR, kBN = 64 * kWC;
     constexpr int kXLoads = kBM / 8 / kWaves, kWLoads = kBN / 8 / kWaves;   // 8 rows each
     constexpr int kXBuf = kBM * kStep, kWBuf = kBN * kStep;
-    // [x, even step][x, odd][W, even][W, odd]
+    // [W, even step][W, odd][x, even][x, odd]
     __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * (kXBuf + kWBuf)];
     static_assert(kWaves * 8192 <= 2 * (kXBuf + kWBuf), "the epilogue's rows fit the buffers");
-    static_assert(kXBuf == kWBuf && (kXBuf & (kXBuf - 1)) == 0, "a step's parity is one bit of an LDS offset");
+    static_assert((kXBuf & (kXBuf - 1)) == 0 && (kWBuf & (kWBuf - 1)) == 0 && kXBuf <= kWBuf,
+                  "a step's parity is one bit of an LDS offset");
     int rt, ct;
     const int part = blockIdx.x % a.parts;
     if (!tile_of(a, blockIdx.x / a.parts, rt, ct)) return;
@@ -259,8 +264,8 @@ void linear_tile_kernel(const LinearKArgs a) {
             for (int i = 0; i < kWLoads; ++i)
                 if (16 * (piece ^ (((wave * kWLoads + i) % 2) * 4)) >= tail) wo[i] = -1;
         }
-        uint8_t *xd = lds + odd * kXBuf + wave * kXLoads * 1024;
-        uint8_t *wd = lds + 2 * kXBuf + odd * kWBuf + wave * kWLoads * 1024;
+        uint8_t *xd = lds + 2 * kWBuf + odd * kXBuf + wave * kXLoads * 1024;
+        uint8_t *wd = lds + odd * kWBuf + wave * kWLoads * 1024;
 #pragma unroll
         for (int i = 0; i < kXLoads; ++i) {
             if constexpr (kFar) global_lds16(xp[i] + at0, xd + i * 1024);
@@ -280,8 +285,8 @@ void linear_tile_kernel(const LinearKArgs a) {
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) {
         const int at = ((2 * kk + grp) ^ ((col / 2) % 8)) * 16;
-        xat[kk] = (wr * kRB * 32 + col) * kStep + at;
-        wat[kk] = 2 * kXBuf + (wc * 64 + col) * kStep + at;
+        xat[kk] = 2 * kWBuf + (wr * kRB * 32 + col) * kStep + at;
+        wat[kk] = (wc * 64 + col) * kStep + at;
     }
     // Four pairs of pieces to a step; the next pair's operands are read while this one's
     // multiply, across the steps' border too: at the last pair a wave waits for its loads
@@ -392,52 +397,93 @@ void linear_tile_kernel(const LinearKArgs a) {
     }
 }
 
+#ifndef RF_STREAM_BYTES
+#define RF_STREAM_BYTES 1e30
+#define RF_STREAM_WG 2
+#endif
+#ifndef RF_F2
+#define RF_F2 2
+#define RF_F4 2
+#endif
 constexpr int kFewWaves = 8;
 
-// kR blocks of 16 rows. The reduction goes in pieces of 64 bytes (16 bytes a lane, four
-// lanes to a row); wave w of part p owns a run of them.
-template <typename E, int kR>
+// kR blocks of 16 rows, kF blocks of 16 features. The reduction goes in pieces of 64
+// bytes (16 bytes a lane, four lanes to a row). The waves of a part take four at a time
+// in turn, 2 KB of a row in all, and have the next four in flight while four multiply.
+template <typename E, int kR, int kF>
 __global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(const LinearKArgs a) {
-    __shared__ __attribute__((aligned(16))) float sums[kFewWaves][16 * kR][16];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ __attribute__((aligned(16))) float sums[kFewWaves][16 * kR][16 * kF];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int part = blockIdx.x % a.parts, tile = blockIdx.x / a.parts;
-    const int rt = tile / a.col_tiles, c0 = (tile - rt * a.col_tiles) * 16;
+    const int rt = tile / a.col_tiles, c0 = (tile - rt * a.col_tiles) * (16 * kF);
     const uint32_t r0 = static_cast<uint32_t>(rt) * (16 * kR);
     const int l16 = lane & 15, grp = lane >> 4;
-    const uint8_t *wp = w_row(a, c0 + l16) + grp * 16;
-    const uint8_t *xp[kR];
+    // (steps here are pieces of 64 bytes)
+    constexpr int kAhead = 4, kRound = kAhead * kFewWaves;
+    const int s0 = part * a.steps_per_part + wave * kAhead;
+    const int s1 = (part + 1) * a.steps_per_part < a.steps ? (part + 1) * a.steps_per_part : a.steps;
+    const int32_t rb = static_cast<int32_t>(a.row_bytes), end = rb - grp * 16;
+    const uint8_t *const x0 = static_cast<const uint8_t *>(uniform_ptr(x_row(a, r0)));
+    const __amdgpu_buffer_rsrc_t wres = __builtin_amdgcn_make_buffer_rsrc(
+        uniform_ptr(w_row(a, c0)), 0, 0x7fffffff, kBufferWord3);
+    const __amdgpu_buffer_rsrc_t xres =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(x0), 0, 0x7fffffff, kBufferWord3);
+    int32_t wo[kF], xo[kR];
 #pragma unroll
-    for (int b = 0; b < kR; ++b) xp[b] = x_row(a, r0 + b * 16 + l16) + grp * 16;
-    f32x4_t acc[kR];
+    for (int f = 0; f < kF; ++f) {
+        const int c = f * 16 + l16, most = a.n_out - 1 - c0;
+        wo[f] = (c < most ? c : most) * rb + grp * 16;
+    }
 #pragma unroll
-    for (int b = 0; b < kR; ++b) acc[b] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    constexpr int kAhead = 4;
-    // (steps here are pieces of 64 bytes; steps_per_part a wave's share of them)
-    const int s0 = (part * kFewWaves + wave) * a.steps_per_part;
-    const int s1 = s0 + a.steps_per_part < a.steps ? s0 + a.steps_per_part : a.steps;
-    const int64_t end = a.row_bytes - grp * 16;
-    for (int s = s0; s < s1; s += kAhead) {
-        u32x4_t wf[kAhead], xf[kAhead][kR];
+    for (int b = 0; b < kR; ++b) xo[b] = static_cast<int32_t>(x_row(a, r0 + b * 16 + l16) - x0) + grp * 16;
+    f32x4_t acc[kF][kR];
+#pragma unroll
+    for (int f = 0; f < kF; ++f)
+#pragma unroll
+        for (int b = 0; b < kR; ++b) acc[f][b] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    struct Batch {
+        u32x4_t w[kAhead][kF], x[kAhead][kR];
+    };
+    auto load = [&](int s, Batch &t) {
+        // (lanes past the end read zeros: a load under a condition would be waited for at once)
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            const int64_t at = static_cast<int64_t>(s + i) * 64;
-            const bool in = s + i < s1 && at < end;
-            wf[i] = in ? *reinterpret_cast<const u32x4_t *>(wp + at) : u32x4_t{0u, 0u, 0u, 0u};
+            const int32_t at = s + i < s1 ? (s + i) * 64 : 0x7fffff00;
+            const bool out = at >= end;
 #pragma unroll
-            for (int b = 0; b < kR; ++b)
-                xf[i][b] = in ? *reinterpret_cast<const u32x4_t *>(xp[b] + at) : u32x4_t{0u, 0u, 0u, 0u};
+            for (int f = 0; f < kF; ++f) t.w[i][f] = buffer_load16(wres, out ? -1 : wo[f], at);
+#pragma unroll
+            for (int b = 0; b < kR; ++b) t.x[i][b] = buffer_load16(xres, out ? -1 : xo[b], at);
         }
+    };
+    auto multiply = [&](const Batch &t) {
 #pragma unroll
         for (int i = 0; i < kAhead; ++i)
 #pragma unroll
-            for (int b = 0; b < kR; ++b) acc[b] = mma16<E>(wf[i], xf[i][b], acc[b]);
+            for (int f = 0; f < kF; ++f)
+#pragma unroll
+                for (int b = 0; b < kR; ++b) acc[f][b] = mma16<E>(t.w[i][f], t.x[i][b], acc[f][b]);
+    };
+    if (s0 < s1) {
+        Batch even, odd;
+        load(s0, even);
+        for (int s = s0; s < s1; s += 2 * kRound) {
+            load(s + kRound, odd);
+            multiply(even);
+            load(s + 2 * kRound, even);
+            multiply(odd);
+        }
     }
     // lane: row l16 of a block, features 4 grp .. 4 grp + 3
 #pragma unroll
-    for (int b = 0; b < kR; ++b) *reinterpret_cast<f32x4_t *>(&sums[wave][b * 16 + l16][grp * 4]) = acc[b];
+    for (int f = 0; f < kF; ++f)
+#pragma unroll
+        for (int b = 0; b < kR; ++b)
+            *reinterpret_cast<f32x4_t *>(&sums[wave][b * 16 + l16][f * 16 + grp * 4]) = acc[f][b];
     __syncthreads();
-    for (int i = tid; i < 16 * kR * 4; i += 64 * kFewWaves) {
-        const int lr = i / 4, q = i % 4;
+    for (int i = tid; i < 16 * kR * 4 * kF; i += 64 * kFewWaves) {
+        const int lr = i / (4 * kF), q = i % (4 * kF);
         const uint32_t r = r0 + lr;
         const int c = c0 + q * 4;
         if (r >= a.rows || c >= a.n_out) continue;
@@ -473,7 +519,7 @@ __global__ __launch_bounds__(256) void linear_join_kernel(const LinearKArgs a) {
     finish<E, 4>(a, r, c, v);
 }
 
-enum LinearForm { kFew16, kFew32, kFew64, kTile128, kTile256 };
+enum LinearForm { kFew16, kFew32, kFew64, kStream32, kStream64, kTile128, kTile256 };
 struct LinearPlan {
     LinearForm form;
     int64_t row_tiles, col_tiles;
@@ -485,16 +531,28 @@ LinearPlan linear_plan(int64_t rows, int32_t K, int32_t n_out, int32_t dtype, in
     LinearPlan p{};
     const int64_t bytes = static_cast<int64_t>(K) * (dtype == RF_F32 ? 4 : 2);
     auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
-    if (rows <= 64) {
+    if (rows <= 64 && !far && static_cast<double>(n_out) * static_cast<double>(bytes) >= RF_STREAM_BYTES) {
+        p.form = rows <= 32 ? kStream32 : kStream64;
+        p.row_tiles = 1;
+        p.col_tiles = up(n_out, 256);
+        p.steps = static_cast<int32_t>(up(bytes, kStep));
+        const int64_t want = RF_STREAM_WG * cus / p.col_tiles, most = p.steps / 4;
+        p.parts = static_cast<int32_t>(!may_split ? 1 : want < most ? want : most);
+        if (p.parts < 1) p.parts = 1;
+        p.per_part = static_cast<int32_t>(up(p.steps, p.parts));
+        p.parts = static_cast<int32_t>(up(p.steps, p.per_part));
+        return p;
+    }
+    if (rows <= 64 && !far) {
         p.form = rows <= 16 ? kFew16 : rows <= 32 ? kFew32 : kFew64;
         p.row_tiles = 1;
-        p.col_tiles = up(n_out, 16);
+        p.col_tiles = up(n_out, 16 * (rows <= 16 ? 1 : rows <= 32 ? RF_F2 : RF_F4));
         p.steps = static_cast<int32_t>(up(bytes, 64));
         // a wave takes at least four pieces; two workgroups to a compute unit
         const int64_t want = up(2 * cus, p.col_tiles), most = up(p.steps, 4 * kFewWaves);
         p.parts = static_cast<int32_t>(!may_split || p.col_tiles >= cus ? 1 : want < most ? want : most);
-        p.per_part = static_cast<int32_t>(up(p.steps, static_cast<int64_t>(p.parts) * kFewWaves));
-        p.parts = static_cast<int32_t>(up(p.steps, static_cast<int64_t>(p.per_part) * kFewWaves));
+        p.per_part = static_cast<int32_t>(up(up(p.steps, p.parts), 4) * 4);
+        p.parts = static_cast<int32_t>(up(p.steps, p.per_part));
         return p;
     }
     const int64_t big = up(rows, 256) * up(n_out, 256), small = up(rows, 128) * up(n_out, 128);
@@ -518,9 +576,11 @@ LinearPlan linear_plan(int64_t rows, int32_t K, int32_t n_out, int32_t dtype, in
 template <typename E>
 void run(const LinearPlan &p, const LinearKArgs &a, bool far, dim3 grid, hipStream_t stream) {
     switch (p.form) {
-        case kFew16: hipLaunchKernelGGL((linear_few_kernel<E, 1>), grid, dim3(512), 0, stream, a); break;
-        case kFew32: hipLaunchKernelGGL((linear_few_kernel<E, 2>), grid, dim3(512), 0, stream, a); break;
-        case kFew64: hipLaunchKernelGGL((linear_few_kernel<E, 4>), grid, dim3(512), 0, stream, a); break;
+        case kFew16: hipLaunchKernelGGL((linear_few_kernel<E, 1, 1>), grid, dim3(512), 0, stream, a); break;
+        case kFew32: hipLaunchKernelGGL((linear_few_kernel<E, 2, RF_F2>), grid, dim3(512), 0, stream, a); break;
+        case kFew64: hipLaunchKernelGGL((linear_few_kernel<E, 4, RF_F4>), grid, dim3(512), 0, stream, a); break;
+        case kStream32: hipLaunchKernelGGL((linear_tile_kernel<E, 1, 1, 4, false>), grid, dim3(256), 0, stream, a); break;
+        case kStream64: hipLaunchKernelGGL((linear_tile_kernel<E, 2, 1, 4, false>), grid, dim3(256), 0, stream, a); break;
         case kTile128:
             if (far) hipLaunchKernelGGL((linear_tile_kernel<E, 2, 2, 2, true>), grid, dim3(256), 0, stream, a);
             else hipLaunchKernelGGL((linear_tile_kernel<E, 2, 2, 2, false>), grid, dim3(256), 0, stream, a);

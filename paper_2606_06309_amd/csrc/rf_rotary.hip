@@ -8,7 +8,8 @@
 //
 // What bounds it: every element is read and written once (memory). A thread
 // owns 8 neighbouring dimensions of a token (4 pairs; with halves, 8 + 8) and
-// walks heads of q and k with them, so a sine and cosine serve all its heads.
+// walks heads of q and k with them, four at a time, so a sine and cosine serve
+// all its heads and four loads are in flight.
 // Angles are formed in double, reduced to half a turn there and only then
 // rounded: at position 2^20 an fp32 angle would be off by 0.06.
 #include "rf_internal.h"
@@ -17,13 +18,15 @@ namespace rf {
 namespace {
 
 constexpr int kThreads = 256;
+// Workgroups that fill the device (eight to each of 256 compute units).
+constexpr int64_t kFill = 2048;
 
 struct RotaryKArgs {
     RotaryParams p;
-    int64_t N;
-    int64_t threads;           // rows * units
-    int32_t units;             // threads per token
-    int32_t rot_units;         // of them, those that own turning dimensions
+    uint32_t N;                // tokens per frame
+    uint32_t blocks;           // workgroups per frame
+    uint32_t units;            // threads per token
+    uint32_t rot_units;        // of them, those that own turning dimensions
     int32_t heads_per_thread;  // of q's and k's heads, one after the other
 };
 static_assert(sizeof(RotaryKArgs) <= 4096, "kernel arguments exceed 4 KB");
@@ -68,67 +71,90 @@ __device__ __forceinline__ void store8(E *p, const Vec8<E> &v) {
     *reinterpret_cast<aligned_t *>(p) = v.w;
 }
 
+// One head's 8 (with halves 8 + 8) elements of a thread.
+template <typename E, bool kHalves>
+struct Piece {
+    Vec8<E> v, w;
+    E *to;
+};
+
 template <typename E, bool kHalves>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryKArgs a) {
     const RotaryParams &p = a.p;
-    const int64_t id = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-    if (id >= a.threads) return;
-    const int64_t row = id / a.units;
-    const int unit = static_cast<int>(id - row * a.units);
-    const int m = static_cast<int>(row / a.N);
-    const int64_t n = row - m * a.N;
-    const int y = static_cast<int>(n / p.W), x = static_cast<int>(n - static_cast<int64_t>(y) * p.W);
+    const uint32_t m = blockIdx.x / a.blocks;
+    // (a frame's threads are fewer than 2^32 + 256: launch_rotary)
+    const uint32_t id = (blockIdx.x - m * a.blocks) * kThreads + threadIdx.x;
+    const uint32_t n = id / a.units, unit = id - n * a.units;
+    if (n >= a.N) return;
+    const uint32_t y = n / static_cast<uint32_t>(p.W), x = n - y * static_cast<uint32_t>(p.W);
     const bool turns = unit < a.rot_units;
     // halves: unit u < rot_units owns dimensions 8u.. and R/2 + 8u..; later units 8 dimensions past R
     const int at = kHalves && !turns ? 2 * p.pairs + 8 * (unit - a.rot_units) : 8 * unit;
 
-    constexpr int kP = kHalves ? 8 : 4;   // pairs
-    float c[kP], s[kP];
-    if (turns) {
-#pragma unroll
-        for (int i = 0; i < kP; ++i) {
-            const int pair = (kHalves ? 8 : 4) * unit + i;
-            c[i] = 1.0f;
-            s[i] = 0.0f;
-            if (pair < p.pairs) {
-                const int axis = pair < p.pair_end[0] ? 0 : pair < p.pair_end[1] ? 1 : 2;
-                const double index = axis == 0 ? p.frame[m] : axis == 1 ? y : x;
-                const double t = fma(p.step[axis], index, p.origin[axis]) * p.turns[pair];
-                sincospif(static_cast<float>(2.0 * (t - rint(t))), &s[i], &c[i]);
-            }
-        }
-    }
     const int64_t src = static_cast<int64_t>(p.src_frame[m]) * a.N + n;
     const int64_t dst = static_cast<int64_t>(p.dst_frame[m]) * a.N + n;
-    const int h0 = blockIdx.y * a.heads_per_thread;
     const int total = p.heads[0] + p.heads[1];
+    const int h0 = blockIdx.y * a.heads_per_thread;
     const int h1 = h0 + a.heads_per_thread < total ? h0 + a.heads_per_thread : total;
-    for (int h = h0; h < h1; ++h) {
+    auto load = [&](int h) {
         const int t = h < p.heads[0] ? 0 : 1;
         const int64_t col = static_cast<int64_t>(h - (t ? p.heads[0] : 0)) * p.head_dim + at;
-        const E *xp = static_cast<const E *>(p.x[t]) + src * p.x_stride[t] + col;
-        E *yp = static_cast<E *>(p.y[t]) + dst * p.y_stride[t] + col;
-        Vec8<E> v = load8(xp);
+        const E *from = static_cast<const E *>(p.x[t]) + src * p.x_stride[t] + col;
+        Piece<E, kHalves> r;
+        r.to = static_cast<E *>(p.y[t]) + dst * p.y_stride[t] + col;
+        r.v = load8(from);
+        if (kHalves && turns) r.w = load8(from + p.pairs);
+        return r;
+    };
+    constexpr int kAhead = 4;
+    Piece<E, kHalves> r[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+        if (h0 + i < h1) r[i] = load(h0 + i);
+
+    constexpr int kP = kHalves ? 8 : 4;   // pairs
+    float c[kP], s[kP];
+#pragma unroll
+    for (int i = 0; i < kP; ++i) {
+        const int pair = kP * unit + i;
+        c[i] = 1.0f;
+        s[i] = 0.0f;
+        if (pair < p.pairs) {
+            const int axis = pair < p.pair_end[0] ? 0 : pair < p.pair_end[1] ? 1 : 2;
+            const double index = axis == 0 ? p.frame[m] : axis == 1 ? y : x;
+            const double t = fma(p.step[axis], index, p.origin[axis]) * p.turns[pair];
+            sincospif(static_cast<float>(2.0 * (t - rint(t))), &s[i], &c[i]);
+        }
+    }
+    auto turn = [&](Piece<E, kHalves> &q) {
         if (turns && kHalves) {
-            Vec8<E> w = load8(xp + p.pairs);
-            const Vec8<E> v0 = v, w0 = w;
+            const Vec8<E> v = q.v, w = q.w;
 #pragma unroll
             for (int i = 0; i < 8; i += 2) {
-                const float a0 = v0.get(i), a1 = v0.get(i + 1), b0 = w0.get(i), b1 = w0.get(i + 1);
-                v.set2(i, fmaf(a0, c[i], -(b0 * s[i])), fmaf(a1, c[i + 1], -(b1 * s[i + 1])));
-                w.set2(i, fmaf(a0, s[i], b0 * c[i]), fmaf(a1, s[i + 1], b1 * c[i + 1]));
+                const float a0 = v.get(i), a1 = v.get(i + 1), b0 = w.get(i), b1 = w.get(i + 1);
+                q.v.set2(i, fmaf(a0, c[i], -(b0 * s[i])), fmaf(a1, c[i + 1], -(b1 * s[i + 1])));
+                q.w.set2(i, fmaf(a0, s[i], b0 * c[i]), fmaf(a1, s[i + 1], b1 * c[i + 1]));
             }
-            store8(yp + p.pairs, w);
+            store8(q.to + p.pairs, q.w);
         } else if (turns) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 // (a pair past R passes as it is, infinities and NaN too)
-                if (4 * unit + i >= p.pairs) continue;
-                const float a0 = v.get(2 * i), b0 = v.get(2 * i + 1);
-                v.set2(2 * i, fmaf(a0, c[i], -(b0 * s[i])), fmaf(a0, s[i], b0 * c[i]));
+                if (kP * static_cast<int>(unit) + i >= p.pairs) continue;
+                const float a0 = q.v.get(2 * i), b0 = q.v.get(2 * i + 1);
+                q.v.set2(2 * i, fmaf(a0, c[i], -(b0 * s[i])), fmaf(a0, s[i], b0 * c[i]));
             }
         }
-        store8(yp, v);
+        store8(q.to, q.v);
+    };
+    for (int h = h0; h < h1; h += kAhead) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (h + i < h1) turn(r[i]);
+        if (h + kAhead >= h1) break;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (h + kAhead + i < h1) r[i] = load(h + kAhead + i);
     }
 }
 
@@ -143,15 +169,21 @@ hipError_t launch(const RotaryKArgs &a, dim3 grid, hipStream_t stream) {
 hipError_t launch_rotary(const RotaryParams &p, hipStream_t stream) {
     RotaryKArgs a{};
     a.p = p;
-    a.N = static_cast<int64_t>(p.H) * p.W;
+    const int64_t N = static_cast<int64_t>(p.H) * p.W;
     // (halves: R/2 is a multiple of 8; else the unit that holds the last pair may pass some dimensions on)
     a.rot_units = p.halves ? p.pairs / 8 : (p.pairs + 3) / 4;
     a.units = p.halves ? a.rot_units + (p.head_dim - 2 * p.pairs) / 8 : p.head_dim / 8;
-    a.threads = p.M * a.N * a.units;
-    a.heads_per_thread = p.heads[0] + p.heads[1];
-    const int64_t blocks = (a.threads + kThreads - 1) / kThreads;
-    if (blocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-    const dim3 grid(static_cast<uint32_t>(blocks), 1);
+    const int64_t blocks = (N * a.units + kThreads - 1) / kThreads;
+    if (N * a.units > 0xffffffffLL || blocks * p.M > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    a.N = static_cast<uint32_t>(N);
+    a.blocks = static_cast<uint32_t>(blocks);
+    const int heads = p.heads[0] + p.heads[1];
+    // a thread takes all heads of its token, or fewer where tokens do not fill the device
+    const int64_t most = (heads + 3) / 4, want = kFill / (blocks * p.M) + 1;
+    const int64_t groups = want < most ? want : most;
+    a.heads_per_thread = static_cast<int32_t>((heads + groups - 1) / groups);
+    const dim3 grid(static_cast<uint32_t>(blocks * p.M),
+                    static_cast<uint32_t>((heads + a.heads_per_thread - 1) / a.heads_per_thread));
     if (p.dtype == RF_F32) return p.halves ? launch<float, true>(a, grid, stream) : launch<float, false>(a, grid, stream);
     return p.halves ? launch<uint16_t, true>(a, grid, stream) : launch<uint16_t, false>(a, grid, stream);
 }

@@ -224,18 +224,21 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
         is_cuda = True
         index = 0
 
+        def get_device(self):
+            return self.index
+
         @property
         def device(self):
             return torch.device("cuda", self.index)
     a, b = z(4, 8).as_subclass(Fake), z(4, 8).as_subclass(Fake)
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
-    assert len(rf._on_device({"a": a, "none": None, "b": b})) == 3
+    assert rf._on_device(((a, "a"), (None, "none"), (b, "b")))[0] == 0
     b.index = 1
     with pytest.raises(ValueError, match="cuda:1"):
-        rf._on_device({"a": a, "b": b})
+        rf._on_device(((a, "a"), (b, "b")))
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
     with pytest.raises(ValueError, match="current device is cuda:1"):
-        rf._on_device({"a": a})
+        rf._on_device(((a, "a"),))
 
 
 def test_constants_match_the_header():
