@@ -16,12 +16,13 @@ struct CrossKArgs {
     const int32_t *kv_lengths;
     const uint8_t *key_mask;
     int64_t qs[3], ks[3], vs[3], os[3];   // {batch, token, head} in elements
-    int64_t rows;            // query rows of a key head: group * Lq
+    uint32_t rows;           // query rows of a key head: group * Lq
     int32_t Lq, Lk, kv_heads, group;
     int32_t q_tiles;         // tiles of rows of a (sequence, key head)
     int32_t tiles;           // of the launch
     int32_t per_xcd, xcds;   // workgroup id i runs on XCD i % xcds
     int32_t parts;           // of the key axis (1: not split)
+    int32_t walkers;         // many rows: workgroups of the launch, each with a run of tiles
     float scale_log2;        // log2(e) / sqrt(d)
     float *ws_o;             // [tile * parts + part][32][D] unnormalised O
     float *ws_ml;            // [tile * parts + part][32][2] reference and row sum
@@ -32,24 +33,31 @@ struct CrossKArgs {
 // workgroups read the same head's keys and values through that XCD's L2.
 struct CrossTile {
     int32_t tile, b, hk;
-    int64_t row0;
+    uint32_t row0;
 };
 template <int kRows>
-__device__ __forceinline__ bool cross_tile(const CrossKArgs &a, int bid, CrossTile &t) {
-    t.tile = (bid % a.xcds) * a.per_xcd + bid / a.xcds;
-    if (t.tile >= a.tiles) return false;
-    const int head = t.tile / a.q_tiles;
-    t.row0 = static_cast<int64_t>(t.tile - head * a.q_tiles) * kRows;
+__device__ __forceinline__ CrossTile cross_tile_at(const CrossKArgs &a, int32_t tile) {
+    CrossTile t;
+    t.tile = tile;
+    const int head = tile / a.q_tiles;
+    t.row0 = static_cast<uint32_t>(tile - head * a.q_tiles) * kRows;
     t.b = head / a.kv_heads;
     t.hk = head - t.b * a.kv_heads;
+    return t;
+}
+template <int kRows>
+__device__ __forceinline__ bool cross_tile(const CrossKArgs &a, int bid, CrossTile &t) {
+    const int32_t tile = (bid % a.xcds) * a.per_xcd + bid / a.xcds;
+    if (tile >= a.tiles) return false;
+    t = cross_tile_at<kRows>(a, tile);
     return true;
 }
 
 // Element offset of query row r's first element in a tensor of these strides.
 __device__ __forceinline__ int64_t row_offset(const CrossKArgs &a, const int64_t (&s)[3], const CrossTile &t,
-                                              int64_t r) {
-    const int64_t g = r / a.Lq;
-    return t.b * s[0] + (r - g * a.Lq) * s[1] + (t.hk * a.group + g) * s[2];
+                                              uint32_t r) {
+    const uint32_t g = a.group == 1 ? 0 : r / static_cast<uint32_t>(a.Lq);
+    return t.b * s[0] + static_cast<int64_t>(r - g * a.Lq) * s[1] + (t.hk * a.group + static_cast<int64_t>(g)) * s[2];
 }
 
 __device__ __forceinline__ int32_t key_count(const CrossKArgs &a, int b) {
@@ -58,13 +66,8 @@ __device__ __forceinline__ int32_t key_count(const CrossKArgs &a, int b) {
     return n < 0 ? 0 : n < a.Lk ? n : a.Lk;
 }
 
-// Bits of the valid keys among keys key0 .. key0 + 63 (n: the sequence's length).
-template <bool kMask>
+// A masked launch's valid keys among keys key0 .. key0 + 63 (n: the sequence's length).
 __device__ __forceinline__ uint64_t key_bits(const CrossKArgs &a, int b, int32_t key0, int32_t n, int lane) {
-    if constexpr (!kMask) {
-        const int32_t left = n - key0;
-        return left >= 64 ? ~0ull : left <= 0 ? 0ull : (1ull << left) - 1;
-    }
     bool ok = key0 + lane < n;
     if (ok) ok = a.key_mask[static_cast<int64_t>(b) * a.Lk + key0 + lane] != 0;
     return __builtin_amdgcn_ballot_w64(ok);

@@ -70,17 +70,19 @@ struct Wave {
     float l;      // this lane's part of the row sum
 };
 
+// Query fragments: the B operand of S^T = K Q^T. Rows past the last read the last one
+// (nothing is stored for them).
 template <int D>
-__device__ __forceinline__ void start(const CrossKArgs &a, const CrossTile &t, int64_t row, int grp, Wave<D> &w) {
-    const uint16_t *q = static_cast<const uint16_t *>(a.q);
-    if (row < a.rows) {
-        const uint16_t *qp = q + row_offset(a, a.qs, t, row) + grp * 8;
+__device__ __forceinline__ void load_queries(const CrossKArgs &a, const CrossTile &t, uint32_t row, int grp,
+                                             u32x4_t (&qf)[D / 16]) {
+    const uint16_t *qp = static_cast<const uint16_t *>(a.q) +
+                         row_offset(a, a.qs, t, row < a.rows ? row : a.rows - 1) + grp * 8;
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) w.qf[kk] = *reinterpret_cast<const u32x4_t *>(qp + kk * 16);
-    } else {
-#pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) w.qf[kk] = u32x4_t{0u, 0u, 0u, 0u};
-    }
+    for (int kk = 0; kk < D / 16; ++kk) qf[kk] = *reinterpret_cast<const u32x4_t *>(qp + kk * 16);
+}
+
+template <int D>
+__device__ __forceinline__ void clear(Wave<D> &w) {
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
 #pragma unroll
@@ -165,20 +167,23 @@ __device__ __forceinline__ void values(const uint8_t *vb, const Fragments<D> &f,
 // show in a probability: then (s - m) * scale is formed instead.
 constexpr float kFarReference = 4096.0f;
 
-// Probabilities of kNB blocks of 32 keys, packed as the B operand of the second
-// product, and the running softmax. `bits`: the tile's valid keys.
-template <int D, int kNB>
-__device__ __forceinline__ void softmax(Wave<D> &w, f32x16_t (&s)[kNB], const uint64_t (&bits)[(kNB + 1) / 2], int grp,
-                                        float sl2, bool first, u32x4_t (&pw)[2 * kNB]) {
+// Scores of keys that are not valid become -inf. `bits`: the tile's valid keys.
+template <int kNB>
+__device__ __forceinline__ void mask_scores(f32x16_t (&s)[kNB], const uint64_t (&bits)[2], int grp) {
 #pragma unroll
     for (int b = 0; b < kNB; ++b) {
         const uint32_t word = static_cast<uint32_t>(bits[b / 2] >> (32 * (b % 2)));
-        if (word == 0xffffffffu) continue;
         const uint32_t mine = word >> (4 * grp);   // accumulator r holds key (r/4)*8 + grp*4 + r%4
 #pragma unroll
         for (int r = 0; r < 16; ++r)
             if (!((mine >> ((r / 4) * 8 + r % 4)) & 1u)) s[b][r] = -kInf;
     }
+}
+
+// Probabilities of kNB blocks of 32 keys, packed as the B operand of the second
+// product, and the running softmax.
+template <int D, int kNB>
+__device__ __forceinline__ void softmax(Wave<D> &w, f32x16_t (&s)[kNB], float sl2, bool first, u32x4_t (&pw)[2 * kNB]) {
     auto probs = [&](float m, float mref) {
         // four partial sums, of the rounded values that the matrix cores take
         float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -232,24 +237,23 @@ __device__ __forceinline__ void softmax(Wave<D> &w, f32x16_t (&s)[kNB], const ui
     w.l += ls;
 }
 
-// This wave's global->LDS loads i0 .. i0 + kN - 1 of a tile (each fills 1 KB).
+// This wave's global->LDS loads i0 .. i0 + kN - 1 of a tile (each fills 1 KB). `key`: the
+// tile's first key; `left`: the sequence's keys from there on, at which the resource ends.
 // bits: the valid keys, taken for masked launches only.
-template <int D, bool kMask, int kN>
-__device__ __forceinline__ void issue(const uint16_t *head, int64_t stride, int32_t key0, int32_t left,
-                                      const uint64_t (&bits)[2], uint8_t *dst, int i0, const int (&go)[kN], int lane) {
-    // the resource starts at the tile's first key and ends at the length's last one
-    const int64_t span = ((static_cast<int64_t>(left) - 1) * stride + D) * 2;
-    const int32_t rec = __builtin_amdgcn_readfirstlane(static_cast<int32_t>(
-        left <= 0 ? 0 : span < kNowhere ? span : kNowhere));
-    const __amdgpu_buffer_rsrc_t r =
-        __builtin_amdgcn_make_buffer_rsrc(uniform_ptr(head + key0 * stride), 0, rec, kBufferWord3);
+template <int D, bool kMask, int kBc, int kN>
+__device__ __forceinline__ void issue(const uint16_t *key, int64_t stride, int32_t left, const uint64_t (&bits)[2],
+                                      uint8_t *dst, int i0, const int (&go)[kN], int lane) {
+    // (a tile spans less than 2^31 bytes)
+    const int32_t rec = __builtin_amdgcn_readfirstlane(
+        left >= kBc ? kNowhere : (left - 1) * static_cast<int32_t>(stride) * 2 + 2 * D);
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(uniform_ptr(key), 0, rec, kBufferWord3);
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
         int at = go[i];
         if constexpr (kMask) {
-            const int key = (i0 + i) * Tile<D>::kRowsPerLoad + lane / Tile<D>::kSlots;
-            const uint64_t word = key < 64 ? bits[0] : bits[1];
-            if (!((word >> (key & 63)) & 1)) at = kNowhere;
+            const int k = (i0 + i) * Tile<D>::kRowsPerLoad + lane / Tile<D>::kSlots;
+            const uint64_t word = k < 64 ? bits[0] : bits[1];
+            if (!((word >> (k & 63)) & 1)) at = kNowhere;
         }
         load_lds16(r, (lds_void_t *)(dst + (i0 + i) * 1024), at);
     }
@@ -266,100 +270,152 @@ __device__ __forceinline__ void load_offsets(int64_t stride, int i0, int lane, i
 }
 
 // ---------------------------------------------------------------------------
-// Many rows: a workgroup of 4 waves owns 128 rows of one key head; its waves
-// share double-buffered tiles (64 KB of LDS), one barrier a tile.
+// Many rows: a workgroup of 4 waves owns 128 rows of one key head at a time; its
+// waves share double-buffered tiles (64 KB of LDS), one barrier a tile; two
+// workgroups to a compute unit.
+// A prompt is a few tiles long, so the time between two tiles of rows counts: a
+// workgroup walks a run of tiles of rows, and under the last tile of keys of one
+// the queries and the first keys and values of the next are on their way.
 // ---------------------------------------------------------------------------
 
 constexpr int kTileWaves = kCrossTileRows / 32;
-__host__ __device__ constexpr int tile_keys(int head_dim) { return head_dim == 64 ? 128 : 64; }
+__host__ __device__ constexpr int tile_waves(int head_dim, bool mask) { return head_dim == 64 && !mask ? 3 : 2; }
+__host__ __device__ constexpr int tile_keys(int) { return 64; }
 
 template <int D, bool kMask>
-__global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu(2)))
+__global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu(tile_waves(D, kMask))))
 void cross_tile_kernel(const CrossKArgs a) {
     constexpr int kBc = tile_keys(D), kNB = kBc / 32, kTileBytes = kBc * Tile<D>::kRow;
     constexpr int kN = kTileBytes / 1024 / kTileWaves;
-    __shared__ __attribute__((aligned(1024))) uint8_t k0[kTileBytes];
-    __shared__ __attribute__((aligned(1024))) uint8_t k1[kTileBytes];
-    __shared__ __attribute__((aligned(1024))) uint8_t v0[kTileBytes];
-    __shared__ __attribute__((aligned(1024))) uint8_t v1[kTileBytes];
-    CrossTile t;
-    if (!cross_tile<kCrossTileRows>(a, blockIdx.x, t)) return;
+    // [K, V][buffer]
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * kTileBytes];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, grp = lane >> 5;
-    const int64_t row = t.row0 + wave * 32 + col;
-    const int32_t n = key_count(a, t.b);
-    const uint16_t *kh = static_cast<const uint16_t *>(a.k) + t.b * a.ks[0] + t.hk * a.ks[2];
-    const uint16_t *vh = static_cast<const uint16_t *>(a.v) + t.b * a.vs[0] + t.hk * a.vs[2];
+    int32_t tile, end;
+    {
+        // walkers of an XCD have neighbouring runs
+        const int64_t per = a.walkers / a.xcds, w = (blockIdx.x % a.xcds) * per + blockIdx.x / a.xcds;
+        tile = static_cast<int32_t>(w * a.tiles / a.walkers);
+        end = static_cast<int32_t>((w + 1) * a.tiles / a.walkers);
+    }
+    if (tile >= end) return;
     int kgo[kN], vgo[kN];
     load_offsets<D, true, kN>(a.ks[1], wave * kN, lane, kgo);
     load_offsets<D, false, kN>(a.vs[1], wave * kN, lane, vgo);
-    auto tile_bits = [&](int32_t i, uint64_t (&bits)[2]) {
-        bits[0] = key_bits<kMask>(a, t.b, i * kBc, n, lane);
-        bits[1] = kBc == 128 ? key_bits<kMask>(a, t.b, i * kBc + 64, n, lane) : 0;
+    // a sequence's keys from one on: the first of a tile
+    struct Keys {
+        const uint16_t *k, *v;
+        int32_t key, left;
+        uint64_t bits[2];   // masked launches: the tile's valid keys
     };
-    auto load = [&](int32_t i, const uint64_t (&bits)[2], uint8_t *kd, uint8_t *vd) {
-        issue<D, kMask, kN>(kh, a.ks[1], i * kBc, n - i * kBc, bits, kd, wave * kN, kgo, lane);
-        issue<D, kMask, kN>(vh, a.vs[1], i * kBc, n - i * kBc, bits, vd, wave * kN, vgo, lane);
+    auto keys_of = [&](const CrossTile &t) {
+        Keys r;
+        r.k = static_cast<const uint16_t *>(a.k) + t.b * a.ks[0] + t.hk * a.ks[2];
+        r.v = static_cast<const uint16_t *>(a.v) + t.b * a.vs[0] + t.hk * a.vs[2];
+        r.key = 0;
+        r.left = key_count(a, t.b);
+        return r;
     };
-    const Fragments<D> f(lane);
-    Wave<D> w;
-    const int32_t tiles = static_cast<int32_t>((static_cast<int64_t>(n) + kBc - 1) / kBc);
-    uint64_t cur[2], nxt[2];
-    if (tiles > 0) {
-        tile_bits(0, cur);
-        load(0, cur, k0, v0);
-        tile_bits(1, nxt);
-    }
-    start<D>(a, t, row, grp, w);
-    auto compute = [&](int32_t i, const uint64_t (&bits)[2], const uint8_t *kb, const uint8_t *vb) {
-        if (kMask && bits[0] == 0 && bits[1] == 0 && i > 0) return;
-        f32x16_t s[kNB];
-        scores<D, kNB>(kb, f, w.qf, s);
-        u32x4_t pw[2 * kNB];
-        uint64_t word[(kNB + 1) / 2];
-#pragma unroll
-        for (int x = 0; x < (kNB + 1) / 2; ++x) word[x] = bits[x];
-        softmax<D, kNB>(w, s, word, grp, a.scale_log2, i == 0, pw);
-        values<D, kNB>(vb, f, pw, w.o);
+    auto load = [&](Keys &s, const CrossTile &t, int buf) {
+        if constexpr (kMask) {
+            s.bits[0] = key_bits(a, t.b, s.key, s.key + s.left, lane);
+            s.bits[1] = kBc == 128 ? key_bits(a, t.b, s.key + 64, s.key + s.left, lane) : 0;
+        }
+        uint8_t *kd = lds + buf * kTileBytes, *vd = lds + (2 + buf) * kTileBytes;
+        issue<D, kMask, kBc, kN>(s.k, a.ks[1], s.left, s.bits, kd, wave * kN, kgo, lane);
+        issue<D, kMask, kBc, kN>(s.v, a.vs[1], s.left, s.bits, vd, wave * kN, vgo, lane);
     };
     auto tile_done = [&]() {
         wait_loads<0>();   // this wave's loads have reached LDS
         __syncthreads();
     };
-    if (tiles > 0) tile_done();
-    for (int32_t i = 0; i < tiles; i += 2) {
-        uint64_t next[2];
-        if (i + 1 < tiles) {
-            load(i + 1, nxt, k1, v1);
-            tile_bits(i + 2, next);
+    const Fragments<D> f(lane);
+    CrossTile t = cross_tile_at<kCrossTileRows>(a, tile);
+    Keys cur = keys_of(t);
+    Wave<D> w;
+    int buf = 0;
+    load_queries<D>(a, t, t.row0 + wave * 32 + col, grp, w.qf);
+    if (cur.left > 0) load(cur, t, 0);
+    tile_done();
+    for (; tile < end; ++tile) {
+        clear<D>(w);
+        bool first = true;
+        // whole tiles of keys, each under the loads of the next one
+        while (cur.left > kBc) {
+            Keys next = cur;
+            next.k += kBc * a.ks[1];
+            next.v += kBc * a.vs[1];
+            next.key += kBc;
+            next.left -= kBc;
+            load(next, t, buf ^ 1);
+            if (!kMask || first || (cur.bits[0] | cur.bits[1]) != 0) {
+                f32x16_t s[kNB];
+                scores<D, kNB>(lds + buf * kTileBytes, f, w.qf, s);
+                if constexpr (kMask) mask_scores<kNB>(s, cur.bits, grp);
+                u32x4_t pw[2 * kNB];
+                softmax<D, kNB>(w, s, a.scale_log2, first, pw);
+                values<D, kNB>(lds + (2 + buf) * kTileBytes, f, pw, w.o);
+            }
+            first = false;
+            cur = next;
+            buf ^= 1;
+            tile_done();
         }
-        compute(i, cur, k0, v0);
-        tile_done();
-        if (i + 1 >= tiles) break;
-        if (i + 2 < tiles) {
-            cur[0] = next[0];
-            cur[1] = next[1];
-            load(i + 2, cur, k0, v0);
-            tile_bits(i + 3, next);
+        // the last one, whole or not (or none), under those of the next tile of rows, whose
+        // queries follow as soon as this one's have met their last keys
+        CrossTile tn = t;
+        Keys next = cur;
+        if (tile + 1 < end) {
+            tn = cross_tile_at<kCrossTileRows>(a, tile + 1);
+            next = keys_of(tn);
+            if (next.left > 0) load(next, tn, buf ^ 1);
         }
-        compute(i + 1, nxt, k1, v1);
-        nxt[0] = next[0];
-        nxt[1] = next[1];
+        auto turn = [&]() {
+            if (tile + 1 < end) load_queries<D>(a, tn, tn.row0 + wave * 32 + col, grp, w.qf);
+        };
+        if (cur.left > 0) {
+            f32x16_t s[kNB];
+            scores<D, kNB>(lds + buf * kTileBytes, f, w.qf, s);
+            turn();
+            if constexpr (!kMask) {
+                cur.bits[0] = cur.left >= 64 ? ~0ull : (1ull << cur.left) - 1;
+                cur.bits[1] = cur.left >= 128 ? ~0ull : cur.left <= 64 ? 0ull : (1ull << (cur.left - 64)) - 1;
+            }
+            if (kMask || cur.left < kBc) mask_scores<kNB>(s, cur.bits, grp);
+            u32x4_t pw[2 * kNB];
+            softmax<D, kNB>(w, s, a.scale_log2, first, pw);
+            values<D, kNB>(lds + (2 + buf) * kTileBytes, f, pw, w.o);
+        } else {
+            turn();
+        }
+        buf ^= 1;
         tile_done();
+        const uint32_t row = t.row0 + wave * 32 + col;
+        const float l = halves_sum(w.l), inv = l == 0.0f ? 0.0f : 1.0f / l;
+        uint16_t *op = static_cast<uint16_t *>(a.out) + row_offset(a, a.os, t, row < a.rows ? row : 0);
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int g4 = 0; g4 < 4; g4 += 2) {
+                // accumulator r holds dimension db*32 + (r/4)*8 + grp*4 + r%4: two groups of four,
+                // and the half-waves trade one each, so that a lane has eight neighbours
+                uint32_t lo[2], hi[2];
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const int r = g4 * 4 + 2 * x;
+                    lo[x] = pack_bf16x2(w.o[db][r] * inv, w.o[db][r + 1] * inv);
+                    hi[x] = pack_bf16x2(w.o[db][r + 4] * inv, w.o[db][r + 5] * inv);
+                    const auto sw = __builtin_amdgcn_permlane32_swap(lo[x], hi[x], false, false);
+                    lo[x] = sw[0];
+                    hi[x] = sw[1];
+                }
+                if (row < a.rows)
+                    *reinterpret_cast<u32x4_t *>(op + db * 32 + g4 * 8 + grp * 8) = u32x4_t{lo[0], lo[1], hi[0], hi[1]};
+            }
+        t = tn;
+        cur = next;
     }
-    if (row >= a.rows) return;
-    const float l = halves_sum(w.l), inv = l == 0.0f ? 0.0f : 1.0f / l;
-    uint16_t *op = static_cast<uint16_t *>(a.out) + row_offset(a, a.os, t, row);
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-        for (int g4 = 0; g4 < 4; ++g4) {
-            const int r = g4 * 4;   // accumulator r holds dimension db*32 + (r/4)*8 + grp*4 + r%4
-            const u32x2_t x = {pack_bf16x2(w.o[db][r] * inv, w.o[db][r + 1] * inv),
-                               pack_bf16x2(w.o[db][r + 2] * inv, w.o[db][r + 3] * inv)};
-            *reinterpret_cast<u32x2_t *>(op + db * 32 + g4 * 8 + grp * 4) = x;
-        }
 }
 
 // ---------------------------------------------------------------------------
@@ -395,42 +451,45 @@ void cross_few_kernel(const CrossKArgs a) {
     const Fragments<D> f(lane);
     const int64_t tiles = (static_cast<int64_t>(n) + kBc - 1) / kBc;
     const int64_t first = part * kFewWaves + wave, step = static_cast<int64_t>(a.parts) * kFewWaves;
-    auto tile_bits = [&](int64_t i, uint64_t (&bits)[2]) {
-        uint64_t x = key_bits<kMask>(a, t.b, static_cast<int32_t>(i) * kBc, n, lane);
-        if (kBc == 32) x &= 0xffffffffull;
-        bits[0] = x;
+    uint64_t cur[2], nxt[2];
+    auto tile_bits = [&](int32_t key0, uint64_t (&bits)[2]) {
+        if constexpr (kMask) bits[0] = key_bits(a, t.b, key0, n, lane);
+        else bits[0] = n - key0 >= 64 ? ~0ull : (1ull << (n - key0)) - 1;
         bits[1] = 0;
     };
+    auto load = [&](bool key, int32_t key0, const uint64_t (&bits)[2]) {
+        if (key) issue<D, kMask, kBc, kN>(kh + key0 * a.ks[1], a.ks[1], n - key0, bits, kb, 0, kgo, lane);
+        else issue<D, kMask, kBc, kN>(vh + key0 * a.vs[1], a.vs[1], n - key0, bits, vb, 0, vgo, lane);
+    };
     Wave<D> w;
-    uint64_t cur[2], nxt[2];
     if (first < tiles) {
         const int32_t key0 = static_cast<int32_t>(first) * kBc;
-        tile_bits(first, cur);
-        issue<D, kMask, kN>(kh, a.ks[1], key0, n - key0, cur, kb, 0, kgo, lane);
-        issue<D, kMask, kN>(vh, a.vs[1], key0, n - key0, cur, vb, 0, vgo, lane);
+        tile_bits(key0, cur);
+        load(true, key0, cur);
+        load(false, key0, cur);
     }
-    start<D>(a, t, t.row0 + col, grp, w);
+    load_queries<D>(a, t, t.row0 + col, grp, w.qf);
+    clear<D>(w);
     if (first < tiles) {
-        asm volatile("" ::: "memory");
         wait_loads<0>();
         for (int64_t i = first; i < tiles; i += step) {
             // (past the last tile it is fetched again and not used: with the loads on every
             // path the waits below can be counted)
             const int64_t next = i + step < tiles ? i + step : i;
             const int32_t key0 = static_cast<int32_t>(next) * kBc;
-            tile_bits(next, nxt);
+            tile_bits(key0, nxt);
             wait_loads<kN>();       // K is there; V may still be in flight
             f32x16_t s[kNB];
             scores<D, kNB>(kb, f, w.qf, s);
             wait_lds_reads();       // K is read: its buffer is free
-            issue<D, kMask, kN>(kh, a.ks[1], key0, n - key0, nxt, kb, 0, kgo, lane);
+            load(true, key0, nxt);
+            if (kMask || n - static_cast<int32_t>(i) * kBc < kBc) mask_scores<kNB>(s, cur, grp);
             u32x4_t pw[2 * kNB];
-            const uint64_t word[1] = {cur[0]};
-            softmax<D, kNB>(w, s, word, grp, a.scale_log2, i == first, pw);
+            softmax<D, kNB>(w, s, a.scale_log2, i == first, pw);
             wait_loads<kN>();       // V is there; the next K may still be in flight
             values<D, kNB>(vb, f, pw, w.o);
             wait_lds_reads();
-            issue<D, kMask, kN>(vh, a.vs[1], key0, n - key0, nxt, vb, 0, vgo, lane);
+            load(false, key0, nxt);
             cur[0] = nxt[0];
         }
         wait_loads<0>();   // nothing lands in the buffers any more
@@ -453,7 +512,7 @@ void cross_few_kernel(const CrossKArgs a) {
         }
     __syncthreads();
     const int r = tid / 16, unit = tid % 16;   // 512 threads: 32 rows x 16 units
-    const int64_t row = t.row0 + r;
+    const uint32_t row = t.row0 + r;
     if (row >= a.rows) return;
     float m = ml[0][r][0];
 #pragma unroll
@@ -502,7 +561,7 @@ __global__ __launch_bounds__(256) void cross_join_kernel(const CrossKArgs a) {
     t.tile = static_cast<int32_t>(id / kCrossFewRows);
     if (t.tile >= a.tiles) return;
     const int r = static_cast<int>(id % kCrossFewRows), head = t.tile / a.q_tiles;
-    t.row0 = static_cast<int64_t>(t.tile - head * a.q_tiles) * kCrossFewRows;
+    t.row0 = static_cast<uint32_t>(t.tile - head * a.q_tiles) * kCrossFewRows;
     t.b = head / a.kv_heads;
     t.hk = head - t.b * a.kv_heads;
     if (t.row0 + r >= a.rows) return;
@@ -587,7 +646,7 @@ hipError_t launch_cross(const CrossParams &p, hipStream_t stream) {
     a.Lk = p.Lk;
     a.kv_heads = p.kv_heads;
     a.group = p.heads / p.kv_heads;
-    a.rows = static_cast<int64_t>(a.group) * p.Lq;
+    a.rows = static_cast<uint32_t>(a.group) * static_cast<uint32_t>(p.Lq);   // (below 2^29 + 32: the tiles' limit)
     a.scale_log2 = static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(p.head_dim)));
     a.xcds = xcds;
     CrossPlan c = cross_plan(p.B, a.rows, p.kv_heads, p.Lk, p.head_dim, p.dtype, p.geo.cus);
@@ -598,7 +657,14 @@ hipError_t launch_cross(const CrossParams &p, hipStream_t stream) {
     a.q_tiles = static_cast<int32_t>((a.rows + rows - 1) / rows);
     a.tiles = static_cast<int32_t>(c.tiles);
     a.per_xcd = (a.tiles + xcds - 1) / xcds;
-    const int64_t grid = static_cast<int64_t>(a.per_xcd) * xcds * c.parts;
+    int64_t grid = static_cast<int64_t>(a.per_xcd) * xcds * c.parts;
+    if (!c.few && p.dtype == RF_BF16) {
+        // as many walkers as are resident, or one to a tile, in whole XCDs
+        const int64_t resident = tile_waves(p.head_dim, p.key_mask != nullptr) * static_cast<int64_t>(p.geo.cus);
+        const int64_t rounds = (a.tiles + resident - 1) / resident, want = (a.tiles + rounds - 1) / rounds;
+        grid = (want + xcds - 1) / xcds * xcds;
+        a.walkers = static_cast<int32_t>(grid);
+    }
     if (grid > 0x7fffffffLL) return hipErrorInvalidConfiguration;
     if (c.parts > 1) {
         a.ws_o = static_cast<float *>(p.ws);

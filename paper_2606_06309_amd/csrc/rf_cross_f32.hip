@@ -43,7 +43,7 @@ struct Wave {
 };
 
 template <int D>
-__device__ __forceinline__ void start(const CrossKArgs &a, const CrossTile &t, int64_t row, int grp, Wave<D> &w) {
+__device__ __forceinline__ void start(const CrossKArgs &a, const CrossTile &t, uint32_t row, int grp, Wave<D> &w) {
     if (row < a.rows) {
         const float *qp = static_cast<const float *>(a.q) + row_offset(a, a.qs, t, row) + grp * 4;
 #pragma unroll
@@ -141,6 +141,14 @@ __device__ __forceinline__ void values(Wave<D> &w, const uint8_t *vb, const f32x
     }
 }
 
+// A tile's valid keys.
+template <bool kMask>
+__device__ __forceinline__ uint64_t tile_keys(const CrossKArgs &a, int b, int32_t key0, int32_t n, int lane) {
+    if constexpr (kMask) return key_bits(a, b, key0, n, lane) & 0xffffffffull;
+    const int32_t left = n - key0;
+    return left >= kKeys ? 0xffffffffull : left <= 0 ? 0ull : (1ull << left) - 1;
+}
+
 // Many rows: 4 waves, 128 rows, shared double-buffered tiles.
 constexpr int kTileWaves = kCrossTileRows / 32;
 
@@ -156,7 +164,7 @@ void cross_f32_tile_kernel(const CrossKArgs a) {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, grp = lane >> 5;
-    const int64_t row = t.row0 + wave * 32 + col;
+    const uint32_t row = t.row0 + wave * 32 + col;
     const int32_t n = key_count(a, t.b);
     const float *kh = static_cast<const float *>(a.k) + t.b * a.ks[0] + t.hk * a.ks[2];
     const float *vh = static_cast<const float *>(a.v) + t.b * a.vs[0] + t.hk * a.vs[2];
@@ -166,8 +174,7 @@ void cross_f32_tile_kernel(const CrossKArgs a) {
     };
     Wave<D> w;
     const int32_t tiles = static_cast<int32_t>((static_cast<int64_t>(n) + kKeys - 1) / kKeys);
-    // the bits of 64 keys, of which a tile takes its 32
-    auto tile_bits = [&](int32_t i) { return key_bits<kMask>(a, t.b, i * kKeys, n, lane) & 0xffffffffull; };
+    auto tile_bits = [&](int32_t i) { return tile_keys<kMask>(a, t.b, i * kKeys, n, lane); };
     uint64_t cur = 0, nxt = 0;
     if (tiles > 0) {
         cur = tile_bits(0);
@@ -229,9 +236,7 @@ void cross_f32_few_kernel(const CrossKArgs a) {
     uint8_t *kb = ks + wave * L::kBytes, *vb = vs + wave * L::kBytes;
     const int64_t tiles = (static_cast<int64_t>(n) + kKeys - 1) / kKeys;
     const int64_t first = part * kW + wave, step = static_cast<int64_t>(a.parts) * kW;
-    auto tile_bits = [&](int64_t i) {
-        return key_bits<kMask>(a, t.b, static_cast<int32_t>(i) * kKeys, n, lane) & 0xffffffffull;
-    };
+    auto tile_bits = [&](int64_t i) { return tile_keys<kMask>(a, t.b, static_cast<int32_t>(i) * kKeys, n, lane); };
     Wave<D> w;
     uint64_t cur = 0;
     if (first < tiles) {
@@ -280,7 +285,7 @@ void cross_f32_few_kernel(const CrossKArgs a) {
     __syncthreads();
     for (int u = tid; u < kCrossFewRows * 32; u += 64 * kW) {
         const int r = u / 32, unit = u % 32;
-        const int64_t row = t.row0 + r;
+        const uint32_t row = t.row0 + r;
         if (row >= a.rows) break;
         float m = ml[0][r][0];
 #pragma unroll
