@@ -550,80 +550,134 @@ void cross_few_kernel(const CrossKArgs a) {
 // ---------------------------------------------------------------------------
 // Join of a split key axis: for each row the parts' references m_p (raw scores),
 // sums l_p and unnormalised outputs O_p give, with w_p = 2^((m_p - max m) scale),
-// sum w_p O_p / sum w_p l_p. A wave owns a row; parts are added in their order.
+// sum w_p O_p / sum w_p l_p. A workgroup owns a row: thread (p, c) takes four
+// dimensions of parts p, p + 256 / (D/4), ..., all loaded before their weights are
+// known; its sums meet in LDS in a fixed order.
 // ---------------------------------------------------------------------------
+
+constexpr int kMaxParts = 64;
 
 template <int D, typename E>
 __global__ __launch_bounds__(256) void cross_join_kernel(const CrossKArgs a) {
-    const int64_t id = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
-    CrossTile t;
-    t.tile = static_cast<int32_t>(id / kCrossFewRows);
-    if (t.tile >= a.tiles) return;
-    const int r = static_cast<int>(id % kCrossFewRows), head = t.tile / a.q_tiles;
-    t.row0 = static_cast<uint32_t>(t.tile - head * a.q_tiles) * kCrossFewRows;
-    t.b = head / a.kv_heads;
-    t.hk = head - t.b * a.kv_heads;
+    constexpr int kCols = D / 4, kGroups = 256 / kCols, kEach = (kMaxParts + kGroups - 1) / kGroups;
+    __shared__ float ml[kMaxParts][2];
+    __shared__ __attribute__((aligned(16))) float sums[kGroups][D];
+    const CrossTile t = cross_tile_at<kCrossFewRows>(a, blockIdx.x / kCrossFewRows);
+    const int r = blockIdx.x % kCrossFewRows, tid = threadIdx.x;
     if (t.row0 + r >= a.rows) return;
     const int64_t slot0 = static_cast<int64_t>(t.tile) * a.parts * kCrossFewRows + r;
-    float m = -kInf;
-    for (int p = lane; p < a.parts; p += 64) m = fmaxf(m, a.ws_ml[(slot0 + static_cast<int64_t>(p) * kCrossFewRows) * 2]);
+    const int g = tid / kCols, c = tid % kCols;
+    f32x4_t x[kEach];
 #pragma unroll
-    for (int x = 32; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
+    for (int i = 0; i < kEach; ++i) {
+        const int p = g + i * kGroups;
+        x[i] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        if (p < a.parts)
+            x[i] = *reinterpret_cast<const f32x4_t *>(a.ws_o + (slot0 + static_cast<int64_t>(p) * kCrossFewRows) * D + c * 4);
+    }
+    if (tid < a.parts) {
+        const f32x2_t y = *reinterpret_cast<const f32x2_t *>(a.ws_ml + (slot0 + static_cast<int64_t>(tid) * kCrossFewRows) * 2);
+        ml[tid][0] = y[0];
+        ml[tid][1] = y[1];
+    }
+    __syncthreads();
+    float m = ml[0][0];
+    for (int p = 1; p < a.parts; ++p) m = fmaxf(m, ml[p][0]);
     const float ref = m == -kInf ? 0.0f : m;
-    constexpr int kE = D / 64;
-    float l = 0.0f, o[kE] = {};
-#pragma unroll 4
-    for (int p = 0; p < a.parts; ++p) {
-        const int64_t slot = slot0 + static_cast<int64_t>(p) * kCrossFewRows;
-        const f32x2_t ml = *reinterpret_cast<const f32x2_t *>(a.ws_ml + slot * 2);
-        const float wgt = fast_exp2((ml[0] - ref) * a.scale_log2);
-        l = fmaf(wgt, ml[1], l);
+    float l = 0.0f;
+    for (int p = 0; p < a.parts; ++p) l = fmaf(fast_exp2((ml[p][0] - ref) * a.scale_log2), ml[p][1], l);
+    f32x4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int e = 0; e < kE; ++e) o[e] = fmaf(wgt, a.ws_o[slot * D + lane * kE + e], o[e]);
+    for (int i = 0; i < kEach; ++i) {
+        const int p = g + i * kGroups;
+        if (p >= a.parts) break;
+        const float wgt = fast_exp2((ml[p][0] - ref) * a.scale_log2);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = fmaf(wgt, x[i][e], o[e]);
+    }
+    *reinterpret_cast<f32x4_t *>(&sums[g][c * 4]) = o;
+    __syncthreads();
+    if (tid >= D / 2) return;
+    float v[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int p = 0; p < kGroups; ++p) {
+        v[0] += sums[p][2 * tid];
+        v[1] += sums[p][2 * tid + 1];
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    E *op = static_cast<E *>(a.out) + row_offset(a, a.os, t, t.row0 + r) + lane * kE;
-#pragma unroll
-    for (int e = 0; e < kE; ++e) {
-        if constexpr (sizeof(E) == 4) op[e] = o[e] * inv;
-        else op[e] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(o[e] * inv));
-    }
+    E *op = static_cast<E *>(a.out) + row_offset(a, a.os, t, t.row0 + r) + 2 * tid;
+    if constexpr (sizeof(E) == 4) *reinterpret_cast<f32x2_t *>(op) = f32x2_t{v[0] * inv, v[1] * inv};
+    else *reinterpret_cast<uint32_t *>(op) = pack_bf16x2(v[0] * inv, v[1] * inv);
 }
 
 // How a launch is cut: tiles of 128 rows, or of 32 with the keys shared out and
 // `parts` workgroups to a tile.
+//
+// The choice goes by the forms' times in us, counted in rounds of the device: a round
+// has a fixed part and the tiles of keys that a workgroup (of the few-row form: its
+// busiest wave) walks; a split has the join. Tiles of keys cost more where more
+// workgroups share a compute unit. Counts and measured times, us (tile / few):
+//   1,560 x 512 keys, 12 heads x 128: 14 / 25     9,360 x 77, 12 x 128: 21 / 66
+//   2 x 500 x 1,000, 8 x 128: 22 / 12             300 x 5,000, 8 x 128: 83 / 20 (3 parts)
+//   128 x 20,000, 8 x 64: 224 / 21 (8 parts)      3 x 1,581 x 334, 5 x 64: 10 / 17
+// and in fp32 1,560 x 512, 12 x 128: 76 / 72; 512 x 512, 12 x 64: 41 / 15;
+// 4,680 x 512, 12 x 128: 140 / 166.
 struct CrossPlan {
     bool few;
     int32_t parts;
     int64_t tiles;
 };
 
+struct CrossCost {
+    double tile[3];            // a tile of keys with one, two, three workgroups to a compute unit
+    double few;                // a wave's tile of keys in the few-row form
+    int32_t keys, few_keys;    // keys of a tile
+    int32_t few_waves;
+};
+constexpr double kRound = 4.0, kFewRound = 4.5, kJoin = 4.0;
+
 CrossPlan cross_plan(int32_t B, int64_t rows, int32_t kv_heads, int32_t Lk, int32_t head_dim, int32_t dtype,
-                     int32_t cus) {
-    CrossPlan c{};
+                     bool mask, bool may_split, int32_t cus) {
+    static const CrossCost costs[2][2] = {
+        {{{0.7, 1.06, 1.44}, 1.9, tile_keys(64), few_keys(64), kFewWaves},
+         {{1.0, 1.9, 1.9}, 1.9, tile_keys(128), few_keys(128), kFewWaves}},
+        {{{2.4, 4.8, 4.8}, 4.5, 32, 32, 8}, {{4.5, 9.0, 9.0}, 4.9, 32, 32, 4}}};
+    const CrossCost &c = costs[dtype == RF_F32][head_dim == 128];
+    auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
     const int64_t heads = static_cast<int64_t>(B) * kv_heads;
-    const int64_t whole = (rows + kCrossTileRows - 1) / kCrossTileRows * heads, few = (rows + kCrossFewRows - 1) / kCrossFewRows * heads;
-    c.few = whole < 2 * cus;
-    c.tiles = c.few ? few : whole;
-    c.parts = 1;
-    if (c.few) {
-        const int64_t keys = dtype == RF_F32 ? 32 : few_keys(head_dim);
-        const int64_t waves = dtype == RF_F32 && head_dim == 128 ? 4 : kFewWaves;
-        const int64_t key_tiles = (static_cast<int64_t>(Lk) + keys - 1) / keys;
-        const int64_t most = (key_tiles + 2 * waves - 1) / (2 * waves);   // two tiles a wave
-        const int64_t want = cus / few;
-        c.parts = static_cast<int32_t>(want < 1 ? 1 : want < most ? want : most);
+    const int64_t whole = up(rows, kCrossTileRows) * heads, few = up(rows, kCrossFewRows) * heads;
+    const int64_t most = dtype == RF_F32 ? 2 : tile_waves(head_dim, mask);   // workgroups to a compute unit
+    const int64_t share = up(whole, cus) < most ? up(whole, cus) : most;
+    const double t_whole = static_cast<double>(up(whole, cus * most)) *
+                           (kRound + static_cast<double>(up(Lk, c.keys)) * c.tile[share - 1]);
+    CrossPlan p{false, 1, whole};
+    double best = 0.95 * t_whole;   // (the few-row form reads keys four times as often)
+    const int64_t key_tiles = up(Lk, c.few_keys);
+    for (int64_t parts = 1; parts <= kMaxParts; ++parts) {
+        if (parts > 1 && (!may_split || parts * c.few_waves > key_tiles || few * (parts - 1) >= 2 * cus)) break;
+        const double t = static_cast<double>(up(few * parts, cus)) *
+                             (kFewRound + static_cast<double>(up(key_tiles, parts * c.few_waves)) * c.few) +
+                         (parts > 1 ? kJoin : 0.0);
+        if (t < best) {
+            best = t;
+            p = CrossPlan{true, static_cast<int32_t>(parts), few};
+        }
     }
-    return c;
+    return p;
 }
 
 }  // namespace
 
 int64_t cross_workspace(int32_t B, int32_t Lq, int32_t Lk, int32_t heads, int32_t kv_heads, int32_t head_dim,
                         int32_t dtype, int32_t cus) {
-    const CrossPlan c = cross_plan(B, static_cast<int64_t>(heads / kv_heads) * Lq, kv_heads, Lk, head_dim, dtype, cus);
-    return c.parts > 1 ? c.tiles * c.parts * kCrossFewRows * (static_cast<int64_t>(head_dim) * 4 + 8) : 0;
+    int64_t bytes = 0;   // (masked or not: room for either)
+    for (const bool mask : {false, true}) {
+        const CrossPlan c = cross_plan(B, static_cast<int64_t>(heads / kv_heads) * Lq, kv_heads, Lk, head_dim, dtype,
+                                       mask, true, cus);
+        const int64_t need = c.parts > 1 ? c.tiles * c.parts * kCrossFewRows * (static_cast<int64_t>(head_dim) * 4 + 8) : 0;
+        bytes = need > bytes ? need : bytes;
+    }
+    return bytes;
 }
 
 hipError_t launch_cross(const CrossParams &p, hipStream_t stream) {
@@ -649,8 +703,8 @@ hipError_t launch_cross(const CrossParams &p, hipStream_t stream) {
     a.rows = static_cast<uint32_t>(a.group) * static_cast<uint32_t>(p.Lq);   // (below 2^29 + 32: the tiles' limit)
     a.scale_log2 = static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(p.head_dim)));
     a.xcds = xcds;
-    CrossPlan c = cross_plan(p.B, a.rows, p.kv_heads, p.Lk, p.head_dim, p.dtype, p.geo.cus);
-    if (!p.ws) c.parts = 1;
+    const CrossPlan c = cross_plan(p.B, a.rows, p.kv_heads, p.Lk, p.head_dim, p.dtype, p.key_mask != nullptr,
+                                   p.ws != nullptr, p.geo.cus);
     a.parts = c.parts;
     const int64_t rows = c.few ? kCrossFewRows : kCrossTileRows;
     if (c.tiles > 0x7fffffffLL / 64) return hipErrorInvalidConfiguration;
@@ -688,7 +742,7 @@ hipError_t launch_cross(const CrossParams &p, hipStream_t stream) {
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || c.parts == 1) return e;
-    const dim3 jg(static_cast<uint32_t>(c.tiles * kCrossFewRows / 4));
+    const dim3 jg(static_cast<uint32_t>(c.tiles * kCrossFewRows));
     if (p.dtype == RF_F32 && p.head_dim == 128)
         hipLaunchKernelGGL((cross_join_kernel<128, float>), jg, dim3(256), 0, stream, a);
     else if (p.dtype == RF_F32) hipLaunchKernelGGL((cross_join_kernel<64, float>), jg, dim3(256), 0, stream, a);
