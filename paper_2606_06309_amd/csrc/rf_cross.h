@@ -17,7 +17,7 @@ struct CrossKArgs {
     const uint8_t *key_mask;
     int64_t qs[3], ks[3], vs[3], os[3];   // {batch, token, head} in elements
     uint32_t rows;           // query rows of a key head: group * Lq
-    int32_t Lq, Lk, kv_heads, group;
+    int32_t B, Lq, Lk, group;
     int32_t q_tiles;         // tiles of rows of a (sequence, key head)
     int32_t tiles;           // of the launch
     int32_t per_xcd, xcds;   // workgroup id i runs on XCD i % xcds
@@ -28,9 +28,11 @@ struct CrossKArgs {
     float *ws_ml;            // [tile * parts + part][32][2] reference and row sum
 };
 
-// A workgroup's tile: its sequence, key head and first row. Consecutive ids go
-// round-robin to the XCDs, so each XCD gets a contiguous range of tiles whose
-// workgroups read the same head's keys and values through that XCD's L2.
+// A tile: its sequence, key head and first row. Tiles are counted by key head, then
+// rows, then sequence: sequences may differ much in length (a prompt's and an empty
+// one's, in guidance), and this way neighbours share out the long ones. Consecutive
+// workgroup ids go round-robin to the XCDs, so each XCD gets a contiguous range of
+// tiles whose workgroups read the same heads' keys and values through that XCD's L2.
 struct CrossTile {
     int32_t tile, b, hk;
     uint32_t row0;
@@ -39,10 +41,10 @@ template <int kRows>
 __device__ __forceinline__ CrossTile cross_tile_at(const CrossKArgs &a, int32_t tile) {
     CrossTile t;
     t.tile = tile;
-    const int head = tile / a.q_tiles;
-    t.row0 = static_cast<uint32_t>(tile - head * a.q_tiles) * kRows;
-    t.b = head / a.kv_heads;
-    t.hk = head - t.b * a.kv_heads;
+    const int32_t r = tile / a.B;
+    t.b = tile - r * a.B;
+    t.hk = r / a.q_tiles;
+    t.row0 = static_cast<uint32_t>(r - t.hk * a.q_tiles) * kRows;
     return t;
 }
 template <int kRows>
@@ -60,9 +62,12 @@ __device__ __forceinline__ int64_t row_offset(const CrossKArgs &a, const int64_t
     return t.b * s[0] + static_cast<int64_t>(r - g * a.Lq) * s[1] + (t.hk * a.group + static_cast<int64_t>(g)) * s[2];
 }
 
-__device__ __forceinline__ int32_t key_count(const CrossKArgs &a, int b) {
-    if (!a.kv_lengths) return a.Lk;
-    const int32_t n = __builtin_amdgcn_readfirstlane(a.kv_lengths[b]);
+// A sequence's length as it stands, and as it counts.
+__device__ __forceinline__ int32_t given_count(const CrossKArgs &a, int b) {
+    return a.kv_lengths ? a.kv_lengths[b] : a.Lk;
+}
+__device__ __forceinline__ int32_t key_count(const CrossKArgs &a, int32_t given) {
+    const int32_t n = __builtin_amdgcn_readfirstlane(given);
     return n < 0 ? 0 : n < a.Lk ? n : a.Lk;
 }
 

@@ -309,12 +309,12 @@ void cross_tile_kernel(const CrossKArgs a) {
         int32_t key, left;
         uint64_t bits[2];   // masked launches: the tile's valid keys
     };
-    auto keys_of = [&](const CrossTile &t) {
+    auto keys_of = [&](const CrossTile &t, int32_t given) {
         Keys r;
         r.k = static_cast<const uint16_t *>(a.k) + t.b * a.ks[0] + t.hk * a.ks[2];
         r.v = static_cast<const uint16_t *>(a.v) + t.b * a.vs[0] + t.hk * a.vs[2];
         r.key = 0;
-        r.left = key_count(a, t.b);
+        r.left = key_count(a, given);
         return r;
     };
     auto load = [&](Keys &s, const CrossTile &t, int buf) {
@@ -332,7 +332,7 @@ void cross_tile_kernel(const CrossKArgs a) {
     };
     const Fragments<D> f(lane);
     CrossTile t = cross_tile_at<kCrossTileRows>(a, tile);
-    Keys cur = keys_of(t);
+    Keys cur = keys_of(t, given_count(a, t.b));
     Wave<D> w;
     int buf = 0;
     load_queries<D>(a, t, t.row0 + wave * 32 + col, grp, w.qf);
@@ -341,6 +341,9 @@ void cross_tile_kernel(const CrossKArgs a) {
     for (; tile < end; ++tile) {
         clear<D>(w);
         bool first = true;
+        CrossTile tn = t;
+        if (tile + 1 < end) tn = cross_tile_at<kCrossTileRows>(a, tile + 1);
+        const int32_t given = given_count(a, tn.b);   // (asked for early, waited for below)
         // whole tiles of keys, each under the loads of the next one
         while (cur.left > kBc) {
             Keys next = cur;
@@ -364,11 +367,9 @@ void cross_tile_kernel(const CrossKArgs a) {
         }
         // the last one, whole or not (or none), under those of the next tile of rows, whose
         // queries follow as soon as this one's have met their last keys
-        CrossTile tn = t;
         Keys next = cur;
         if (tile + 1 < end) {
-            tn = cross_tile_at<kCrossTileRows>(a, tile + 1);
-            next = keys_of(tn);
+            next = keys_of(tn, given);
             if (next.left > 0) load(next, tn, buf ^ 1);
         }
         auto turn = [&]() {
@@ -441,7 +442,7 @@ void cross_few_kernel(const CrossKArgs a) {
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, grp = lane >> 5;
-    const int32_t n = key_count(a, t.b);
+    const int32_t n = key_count(a, given_count(a, t.b));
     const uint16_t *kh = static_cast<const uint16_t *>(a.k) + t.b * a.ks[0] + t.hk * a.ks[2];
     const uint16_t *vh = static_cast<const uint16_t *>(a.v) + t.b * a.vs[0] + t.hk * a.vs[2];
     uint8_t *kb = ks + wave * kTileBytes, *vb = vs + wave * kTileBytes;
@@ -698,7 +699,7 @@ hipError_t launch_cross(const CrossParams &p, hipStream_t stream) {
     }
     a.Lq = p.Lq;
     a.Lk = p.Lk;
-    a.kv_heads = p.kv_heads;
+    a.B = p.B;
     a.group = p.heads / p.kv_heads;
     a.rows = static_cast<uint32_t>(a.group) * static_cast<uint32_t>(p.Lq);   // (below 2^29 + 32: the tiles' limit)
     a.scale_log2 = static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(p.head_dim)));

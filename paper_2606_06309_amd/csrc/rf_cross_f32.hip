@@ -165,7 +165,7 @@ void cross_f32_tile_kernel(const CrossKArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, grp = lane >> 5;
     const uint32_t row = t.row0 + wave * 32 + col;
-    const int32_t n = key_count(a, t.b);
+    const int32_t n = key_count(a, given_count(a, t.b));
     const float *kh = static_cast<const float *>(a.k) + t.b * a.ks[0] + t.hk * a.ks[2];
     const float *vh = static_cast<const float *>(a.v) + t.b * a.vs[0] + t.hk * a.vs[2];
     auto load = [&](int32_t i, uint64_t bits, int buf) {
@@ -230,7 +230,7 @@ void cross_f32_few_kernel(const CrossKArgs a) {
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, grp = lane >> 5;
-    const int32_t n = key_count(a, t.b);
+    const int32_t n = key_count(a, given_count(a, t.b));
     const float *kh = static_cast<const float *>(a.k) + t.b * a.ks[0] + t.hk * a.ks[2];
     const float *vh = static_cast<const float *>(a.v) + t.b * a.vs[0] + t.hk * a.vs[2];
     uint8_t *kb = ks + wave * L::kBytes, *vb = vs + wave * L::kBytes;
