@@ -397,14 +397,6 @@ void linear_tile_kernel(const LinearKArgs a) {
     }
 }
 
-#ifndef RF_STREAM_BYTES
-#define RF_STREAM_BYTES 1e30
-#define RF_STREAM_WG 2
-#endif
-#ifndef RF_F2
-#define RF_F2 2
-#define RF_F4 2
-#endif
 constexpr int kFewWaves = 8;
 
 // kR blocks of 16 rows, kF blocks of 16 features. The reduction goes in pieces of 64
@@ -531,22 +523,30 @@ LinearPlan linear_plan(int64_t rows, int32_t K, int32_t n_out, int32_t dtype, in
     LinearPlan p{};
     const int64_t bytes = static_cast<int64_t>(K) * (dtype == RF_F32 ? 4 : 2);
     auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
-    if (rows <= 64 && !far && static_cast<double>(n_out) * static_cast<double>(bytes) >= RF_STREAM_BYTES) {
-        p.form = rows <= 32 ? kStream32 : kStream64;
-        p.row_tiles = 1;
-        p.col_tiles = up(n_out, 256);
-        p.steps = static_cast<int32_t>(up(bytes, kStep));
-        const int64_t want = RF_STREAM_WG * cus / p.col_tiles, most = p.steps / 4;
-        p.parts = static_cast<int32_t>(!may_split ? 1 : want < most ? want : most);
-        if (p.parts < 1) p.parts = 1;
-        p.per_part = static_cast<int32_t>(up(p.steps, p.parts));
-        p.parts = static_cast<int32_t>(up(p.steps, p.per_part));
-        return p;
-    }
     if (rows <= 64 && !far) {
+        // Straight to registers, or through LDS in tiles of 256 features: by the bytes of W
+        // from which the latter is faster. us of a product, registers / LDS, bf16: 16 rows x
+        // 4,096 x 4,096 10.6 / 11.5, 8 x 5,120 x 5,120 19.2 / 16.2, 16 x 20,480 x 5,120 73 / 41;
+        // 17 x 1,536 x 1,536 8.3 / 8.3, 17 x 1,536 x 6,144 12.3 / 9.7; 64 x 1,536 x 1,536 11.4 /
+        // 10.8, 64 x 20,480 x 5,120 97 / 48; fp32: 16 x 4,096 x 4,096 18.5 / 18.8, 8 x 5,120 x
+        // 5,120 33 / 29, 17 x 1,536 x 6,144 24.7 / 14.8.
+        const double w_mb = static_cast<double>(n_out) * static_cast<double>(bytes) * 1e-6;
+        if (w_mb >= (dtype == RF_F32 ? 2 : 1) * (rows <= 16 ? 40 : rows <= 32 ? 8 : 4)) {
+            p.form = rows <= 32 ? kStream32 : kStream64;
+            p.row_tiles = 1;
+            p.col_tiles = up(n_out, 256);
+            p.steps = static_cast<int32_t>(up(bytes, kStep));
+            // two workgroups to a compute unit, of six steps at least
+            const int64_t want = 2 * cus / p.col_tiles, most = p.steps / 6;
+            p.parts = static_cast<int32_t>(!may_split ? 1 : want < most ? want : most);
+            if (p.parts < 1) p.parts = 1;
+            p.per_part = static_cast<int32_t>(up(p.steps, p.parts));
+            p.parts = static_cast<int32_t>(up(p.steps, p.per_part));
+            return p;
+        }
         p.form = rows <= 16 ? kFew16 : rows <= 32 ? kFew32 : kFew64;
         p.row_tiles = 1;
-        p.col_tiles = up(n_out, 16 * (rows <= 16 ? 1 : rows <= 32 ? RF_F2 : RF_F4));
+        p.col_tiles = up(n_out, rows <= 16 ? 16 : 32);
         p.steps = static_cast<int32_t>(up(bytes, 64));
         // a wave takes at least four pieces; two workgroups to a compute unit
         const int64_t want = up(2 * cus, p.col_tiles), most = up(p.steps, 4 * kFewWaves);
@@ -577,8 +577,8 @@ template <typename E>
 void run(const LinearPlan &p, const LinearKArgs &a, bool far, dim3 grid, hipStream_t stream) {
     switch (p.form) {
         case kFew16: hipLaunchKernelGGL((linear_few_kernel<E, 1, 1>), grid, dim3(512), 0, stream, a); break;
-        case kFew32: hipLaunchKernelGGL((linear_few_kernel<E, 2, RF_F2>), grid, dim3(512), 0, stream, a); break;
-        case kFew64: hipLaunchKernelGGL((linear_few_kernel<E, 4, RF_F4>), grid, dim3(512), 0, stream, a); break;
+        case kFew32: hipLaunchKernelGGL((linear_few_kernel<E, 2, 2>), grid, dim3(512), 0, stream, a); break;
+        case kFew64: hipLaunchKernelGGL((linear_few_kernel<E, 4, 2>), grid, dim3(512), 0, stream, a); break;
         case kStream32: hipLaunchKernelGGL((linear_tile_kernel<E, 1, 1, 4, false>), grid, dim3(256), 0, stream, a); break;
         case kStream64: hipLaunchKernelGGL((linear_tile_kernel<E, 2, 1, 4, false>), grid, dim3(256), 0, stream, a); break;
         case kTile128:
