@@ -511,7 +511,7 @@ __global__ __launch_bounds__(256) void linear_join_kernel(const LinearKArgs a) {
     finish<E, 4>(a, r, c, v);
 }
 
-enum LinearForm { kFew16, kFew32, kFew64, kStream32, kStream64, kTile128, kTile256 };
+enum LinearForm { kFew16, kFew32, kFew64, kStream32, kStream64, kTile64, kTile128, kTile256 };
 struct LinearPlan {
     LinearForm form;
     int64_t row_tiles, col_tiles;
@@ -555,21 +555,57 @@ LinearPlan linear_plan(int64_t rows, int32_t K, int32_t n_out, int32_t dtype, in
         p.parts = static_cast<int32_t>(up(p.steps, p.per_part));
         return p;
     }
-    const int64_t big = up(rows, 256) * up(n_out, 256), small = up(rows, 128) * up(n_out, 128);
-    p.form = big * 8 >= cus * 6 && !far ? kTile256 : kTile128;
-    const int64_t t = p.form == kTile256 ? 256 : 128, tiles = p.form == kTile256 ? big : small;
-    p.row_tiles = up(rows, t);
-    p.col_tiles = up(n_out, t);
+    // Tiles of 64 x 128, 128 x 128 or 256 x 256 (rows x features) and parts of the reduction,
+    // by the time in us that they come to, counted in rounds of the device: a round has a
+    // fixed part and its steps, which take the longer the more workgroups share a compute
+    // unit; a split adds the second kernel and its parts, written and read again. The
+    // counts are fitted to products of 70 to 21,600 rows, 8 to 20,480 inputs and 256 to
+    // 6,144 features. us, 64 x 128 / 128 x 128 / 256 x 256 (* split), bf16: 512 x 1,536 x 1,536
+    // 11.6 / 17.5 / 41; 500 x 8,960 x 1,536 29.5* / 29.8* / 36*; 3,600 x 1,536 x 1,536 27 / 26 /
+    // 41; 9,360 x 1,536 x 1,536 64 / 53 / 47; fp32: 512 x 1,536 x 1,536 31* / 41* / 74*; 7,800 x
+    // 1,536 x 1,536 279 / 353 / 363; 9,360 x 1,536 x 6,144 - / 1,247 / 1,438.
+    struct Form {
+        LinearForm form;
+        int64_t rows, cols;
+        int32_t most;        // workgroups to a compute unit
+        double round;
+        double step[3];      // with one, two, three workgroups to a compute unit
+    };
+    static const Form forms[2][3] = {{{kTile64, 64, 128, 3, 3.0, {0.38, 0.68, 1.0}},
+                                      {kTile128, 128, 128, 2, 4.0, {0.62, 0.95, 0.95}},
+                                      {kTile256, 256, 256, 1, 8.0, {1.55, 1.55, 1.55}}},
+                                     {{kTile64, 64, 128, 3, 3.0, {1.03, 1.95, 2.93}},
+                                      {kTile128, 128, 128, 2, 4.0, {2.05, 3.65, 3.65}},
+                                      {kTile256, 256, 256, 1, 8.0, {7.4, 7.4, 7.4}}}};
+    constexpr int64_t kLeastSteps = 4, kMostParts = 16;
+    constexpr double kJoin = 3.0;
+    const double join_mb = dtype == RF_F32 ? 0.6 : 0.45;
     p.steps = static_cast<int32_t>(up(bytes, kStep));
-    p.parts = 1;
-    if (may_split && p.form == kTile128 && tiles < cus) {
-        const int64_t want = 2 * cus / tiles, most = p.steps / 8;
-        p.parts = static_cast<int32_t>(want < most ? want : most);
-        if (p.parts < 1) p.parts = 1;
-        if (p.parts > 16) p.parts = 16;
+    double best = 0.0;
+    for (const Form &f : forms[dtype == RF_F32]) {
+        if (far && f.form != kTile128) continue;
+        const int64_t row_tiles = up(rows, f.rows), col_tiles = up(n_out, f.cols);
+        for (int64_t parts = 1; parts <= kMostParts; ++parts) {
+            if (parts > 1 && (!may_split || p.steps / parts < kLeastSteps)) break;
+            const int64_t per = up(p.steps, parts), tiles = row_tiles * col_tiles * parts;
+            if (parts > 1 && up(p.steps, per) != parts) continue;
+            const int64_t share = up(tiles, cus) < f.most ? up(tiles, cus) : f.most;
+            const double full = static_cast<double>(tiles) / static_cast<double>(cus * share);
+            // (workgroups of the smallest tile follow each other closely enough to fill a broken round)
+            const double rounds = f.form == kTile64 ? (full > 0.8 ? full + 0.2 : 1.0) : ceil(full);
+            double t = rounds * (f.round + static_cast<double>(per) * f.step[share - 1]);
+            if (parts > 1)
+                t += kJoin + join_mb * 4e-6 * static_cast<double>(parts) * static_cast<double>(rows) * n_out;
+            if (best == 0.0 || t < best) {
+                best = t;
+                p.form = f.form;
+                p.row_tiles = row_tiles;
+                p.col_tiles = col_tiles;
+                p.parts = static_cast<int32_t>(parts);
+                p.per_part = static_cast<int32_t>(per);
+            }
+        }
     }
-    p.per_part = static_cast<int32_t>(up(p.steps, p.parts));
-    p.parts = static_cast<int32_t>(up(p.steps, p.per_part));
     return p;
 }
 
@@ -581,6 +617,7 @@ void run(const LinearPlan &p, const LinearKArgs &a, bool far, dim3 grid, hipStre
         case kFew64: hipLaunchKernelGGL((linear_few_kernel<E, 4, 2>), grid, dim3(512), 0, stream, a); break;
         case kStream32: hipLaunchKernelGGL((linear_tile_kernel<E, 1, 1, 4, false>), grid, dim3(256), 0, stream, a); break;
         case kStream64: hipLaunchKernelGGL((linear_tile_kernel<E, 2, 1, 4, false>), grid, dim3(256), 0, stream, a); break;
+        case kTile64: hipLaunchKernelGGL((linear_tile_kernel<E, 1, 2, 2, false>), grid, dim3(256), 0, stream, a); break;
         case kTile128:
             if (far) hipLaunchKernelGGL((linear_tile_kernel<E, 2, 2, 2, true>), grid, dim3(256), 0, stream, a);
             else hipLaunchKernelGGL((linear_tile_kernel<E, 2, 2, 2, false>), grid, dim3(256), 0, stream, a);
