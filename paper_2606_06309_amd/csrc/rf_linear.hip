@@ -153,25 +153,53 @@ __device__ __forceinline__ void activate(int kind, float (&v)[kN]) {
     }
 }
 
+__device__ __forceinline__ void widen8(u32x4_t x, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        v[2 * e] = __uint_as_float(x[e] << 16);
+        v[2 * e + 1] = __uint_as_float(x[e] & 0xffff0000u);
+    }
+}
+
+// Bias and gate of kN neighbouring features c.., in fp32 as everything between the
+// products' sums and the result's one rounding.
+template <int kN>
+struct Epilogue {
+    float bias[kN], gate[kN];
+    // frame: whose gate (-1: gate_of will say)
+    template <typename E>
+    __device__ __forceinline__ void load(const LinearKArgs &a, int c, int frame) {
+        if (a.bias) load_n<E, kN>(a.bias, c, bias);
+        if (frame >= 0) gate_of<E>(a, c, frame);
+    }
+    template <typename E>
+    __device__ __forceinline__ void gate_of(const LinearKArgs &a, int c, int frame) {
+        if (a.gate) load_n<E, kN>(a.gate, a.gate_rows ? static_cast<int64_t>(frame) * a.n_out + c : c, gate);
+    }
+    __device__ __forceinline__ void apply(const LinearKArgs &a, float (&v)[kN]) const {
+        if (a.bias) {
+#pragma unroll
+            for (int e = 0; e < kN; ++e) v[e] += bias[e];
+        }
+        if (a.activation != RF_ACT_NONE) activate(a.activation, v);
+        if (a.gate) {
+#pragma unroll
+            for (int e = 0; e < kN; ++e) v[e] *= gate[e];
+        }
+    }
+};
+
 // The epilogue of kN neighbouring features c.. of product row r.
 template <typename E, int kN>
 __device__ __forceinline__ void finish(const LinearKArgs &a, uint32_t r, int c, float (&v)[kN]) {
     const uint32_t m = r / a.N;
     const int64_t dst = static_cast<int64_t>(a.dst_frame[m]) * a.N + (r - m * a.N);
+    Epilogue<kN> ep;
+    ep.template load<E>(a, c, a.frame[m]);
     float t[kN];
-    if (a.bias) {
-        load_n<E, kN>(a.bias, c, t);
-#pragma unroll
-        for (int e = 0; e < kN; ++e) v[e] += t[e];
-    }
-    if (a.activation != RF_ACT_NONE) activate(a.activation, v);
-    if (a.gate) {
-        load_n<E, kN>(a.gate, a.gate_rows ? static_cast<int64_t>(a.frame[m]) * a.n_out + c : c, t);
-#pragma unroll
-        for (int e = 0; e < kN; ++e) v[e] *= t[e];
-    }
+    if (a.residual) load_n<E, kN>(a.residual, dst * a.n_out + c, t);
+    ep.apply(a, v);
     if (a.residual) {
-        load_n<E, kN>(a.residual, dst * a.n_out + c, t);
 #pragma unroll
         for (int e = 0; e < kN; ++e) v[e] += t[e];
     }
@@ -213,7 +241,6 @@ void linear_tile_kernel(const LinearKArgs a) {
     constexpr int kXBuf = kBM * kStep, kWBuf = kBN * kStep;
     // [W, even step][W, odd][x, even][x, odd]
     __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * (kXBuf + kWBuf)];
-    static_assert(kWaves * 8192 <= 2 * (kXBuf + kWBuf), "the epilogue's rows fit the buffers");
     static_assert((kXBuf & (kXBuf - 1)) == 0 && (kWBuf & (kWBuf - 1)) == 0 && kXBuf <= kWBuf,
                   "a step's parity is one bit of an LDS offset");
     int rt, ct;
@@ -357,8 +384,34 @@ void linear_tile_kernel(const LinearKArgs a) {
     // ---- epilogue: 32 rows x 64 features at a time through 8 KB of the wave's own, 256
     // bytes a row, 16-byte units permuted by row % 16; a lane then has 8 neighbouring
     // features of a row, and eight lanes whole lines of y ----
-    uint8_t *mine = lds + wave * 8192;
+    // Residual rows come into LDS too, a block ahead (bf16: 4 KB of a lane's 16 bytes, four
+    // times; in fp32 the products outlast their latency). Loaded where they are added, one
+    // row after the other, they cost 23 us of 69 at 9,360 x 1,536 x 1,536. ----
+    constexpr bool kStage = sizeof(E) == 2;
+    constexpr int kArea = 8192 + (kStage ? (kRB > 1 ? 8192 : 4096) : 0);
+    static_assert(kWaves * kArea <= 2 * (kXBuf + kWBuf), "the epilogue's rows fit the buffers");
+    uint8_t *mine = lds + wave * kArea;
     const int c = ct * kBN + wc * 64 + (lane % 8) * 8;
+    const bool stage = kStage && a.residual && a.parts == 1;
+    // (a row past the last, or features past the last, load those)
+    const int cs = c < a.n_out ? c : a.n_out - 8;
+    auto residual = [&](int b) {
+        uint8_t *to = mine + 8192 + (b & 1) * 4096;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t r = row0 + (wr * kRB + b) * 32 + i * 8 + sub;
+            if (r >= a.rows) r = a.rows - 1;
+            const uint32_t m = r / a.N;
+            const int64_t dst = static_cast<int64_t>(a.dst_frame[m]) * a.N + (r - m * a.N);
+            global_lds16(static_cast<const uint8_t *>(a.residual) + (dst * a.n_out + cs) * 2, to + i * 1024);
+        }
+    };
+    // bias and gate of this lane's features, where all the tile's rows have one gate
+    const uint32_t last = row0 + kBM - 1 < a.rows ? row0 + kBM - 1 : a.rows - 1;
+    const bool one_gate = !a.gate_rows || row0 / a.N == last / a.N;
+    Epilogue<8> ep;
+    if (a.parts == 1 && c + 8 <= a.n_out) ep.template load<E>(a, c, one_gate ? a.frame[row0 / a.N] : -1);
+    if (stage) residual(0);
 #pragma unroll
     for (int b = 0; b < kRB; ++b) {
 #pragma unroll
@@ -370,6 +423,10 @@ void linear_tile_kernel(const LinearKArgs a) {
                     f32x4_t{acc[f][b][g4 * 4], acc[f][b][g4 * 4 + 1], acc[f][b][g4 * 4 + 2], acc[f][b][g4 * 4 + 3]};
             }
         wait_lds_reads();   // (a wave's LDS accesses run in order; this orders the compiler's)
+        if (stage) {
+            wait_loads<0>();
+            if (b + 1 < kRB) residual(b + 1);
+        }
 #pragma unroll 1
         for (int i = 0; i < 4; ++i) {
             const int lr = i * 8 + sub;
@@ -390,8 +447,22 @@ void linear_tile_kernel(const LinearKArgs a) {
                 else finish<E, 4>(a, r, c, lo);
                 continue;
             }
-            if (a.parts > 1) store_n<float, 8>(a.ws, (static_cast<int64_t>(part) * a.rows + r) * a.n_out + c, v);
-            else finish<E, 8>(a, r, c, v);
+            if (a.parts > 1) {
+                store_n<float, 8>(a.ws, (static_cast<int64_t>(part) * a.rows + r) * a.n_out + c, v);
+                continue;
+            }
+            const uint32_t m = r / a.N;
+            const int64_t dst = static_cast<int64_t>(a.dst_frame[m]) * a.N + (r - m * a.N);
+            if (!one_gate) ep.template gate_of<E>(a, c, a.frame[m]);
+            ep.apply(a, v);
+            if (a.residual) {
+                float t[8];
+                if constexpr (kStage) widen8(*reinterpret_cast<const u32x4_t *>(mine + 8192 + (b & 1) * 4096 + i * 1024 + lane * 16), t);
+                else load_n<E, 8>(a.residual, dst * a.n_out + c, t);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] += t[e];
+            }
+            store_n<E, 8>(a.y, dst * a.n_out + c, v);
         }
         wait_lds_reads();
     }
