@@ -738,11 +738,12 @@ def _on_device(tensors):
             continue
         if not isinstance(t, torch.Tensor):
             raise TypeError(f"{name} must be a torch.Tensor")
-        if not t.is_cuda:
+        on = t.get_device()
+        if on < 0:
             raise ValueError(f"{name} must be a device tensor")
         if index < 0:
             index = torch.cuda.current_device()
-        if t.get_device() != index:
+        if on != index:
             raise ValueError(f"{name} is on {t.device}, the current device is cuda:{index}")
         out.append(t.data_ptr())
     return index, out

@@ -862,9 +862,11 @@ int rf_async_schedule(int32_t T, int32_t T_w, int32_t T_mid, int32_t n_small, in
 
 // --- a block's operators around the attention ---
 
-// Where the rows of the M listed frames are: compact (frame m) or full (frame ids[m]).
-static void row_frames(const int32_t *ids, int32_t M, bool full, int16_t *dst) {
-    for (int32_t m = 0; m < M; ++m) dst[m] = static_cast<int16_t>(full ? ids[m] : m);
+static_assert(RF_MAX_FRAMES <= 256, "a frame index is a byte");
+static void row_frames(const int32_t *ids, int32_t M, bool in_full, bool out_full, rf::RowFrames *f) {
+    for (int32_t m = 0; m < M; ++m) f->frame[m] = static_cast<uint8_t>(ids[m]);
+    f->in_full = in_full;
+    f->out_full = out_full;
 }
 
 static int64_t abs_diff(uintptr_t a, uintptr_t b) { return static_cast<int64_t>(a > b ? a - b : b - a); }
@@ -976,9 +978,7 @@ static int rotary_call(const void *q, void *q_out, const void *k, void *k_out, c
         long double turns = ((flags & RF_ROTARY_INVERSE) ? -0.5L : 0.5L) / 3.14159265358979323846264338328L;
         for (int32_t j = 0; j < axes->dims[a] / 2; ++j, turns *= ratio) p.turns[pair++] = static_cast<double>(turns);
     }
-    for (int32_t m = 0; m < M; ++m) p.frame[m] = static_cast<int16_t>(ids[m]);
-    row_frames(ids, M, in_full, p.src_frame);
-    row_frames(ids, M, out_full, p.dst_frame);
+    row_frames(ids, M, in_full, out_full, &p.frames);
     return launched(rf::launch_rotary(p, static_cast<hipStream_t>(stream)), fn);
 }
 
@@ -1246,9 +1246,7 @@ int rf_frame_linear(const void *x, const void *weight, const void *bias, const v
     p.activation = activation;
     p.dtype = dtype;
     p.gate_rows = (flags & RF_GATE_PER_FRAME) != 0;
-    for (int32_t m = 0; m < M; ++m) p.frame[m] = static_cast<int16_t>(ids[m]);
-    row_frames(ids, M, (flags & RF_ROWS_IN_FULL) != 0, p.src_frame);
-    row_frames(ids, M, (flags & RF_ROWS_OUT_FULL) != 0, p.dst_frame);
+    row_frames(ids, M, (flags & RF_ROWS_IN_FULL) != 0, (flags & RF_ROWS_OUT_FULL) != 0, &p.frames);
     return launched(rf::launch_linear(p, static_cast<hipStream_t>(stream)), fn);
 }
 

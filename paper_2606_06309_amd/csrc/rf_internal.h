@@ -159,9 +159,18 @@ struct SimParams {
 
 hipError_t launch_similarity(const SimParams &p, hipStream_t stream);
 
+// The listed frames, and where their rows are: row n of listed frame m is row
+// in(m) * N + n of what is read and out(m) * N + n of what is written. In bytes:
+// kernel arguments are written to device memory at every launch.
+struct RowFrames {
+    uint8_t frame[kMaxFrames];
+    uint8_t in_full, out_full;
+    __host__ __device__ int32_t in(int32_t m) const { return in_full ? frame[m] : m; }
+    __host__ __device__ int32_t out(int32_t m) const { return out_full ? frame[m] : m; }
+};
+
 // Rotary positions: tensor 0 is q, tensor 1 is k (heads[1] = 0: none). Strides
-// in elements; row r of the call is row src_frame[m] * N + n of x and
-// dst_frame[m] * N + n of y (m = r / N).
+// in elements.
 constexpr int kMaxRotaryPairs = 128;
 struct RotaryParams {
     const void *x[2];
@@ -177,9 +186,7 @@ struct RotaryParams {
     int32_t pair_end[2];                 // pairs of axis 0, and of axes 0 and 1
     double origin[3], step[3];
     double turns[kMaxRotaryPairs];       // each pair's turns per unit of position, negative for the inverse
-    int16_t frame[kMaxFrames];           // frame index, the position on the time axis
-    int16_t src_frame[kMaxFrames];
-    int16_t dst_frame[kMaxFrames];
+    RowFrames frames;                    // (a frame's index is its position on the time axis)
 };
 
 hipError_t launch_rotary(const RotaryParams &p, hipStream_t stream);
@@ -203,8 +210,8 @@ int64_t cross_workspace(int32_t B, int32_t Lq, int32_t Lk, int32_t heads, int32_
 hipError_t launch_cross(const CrossParams &p, hipStream_t stream);
 
 // Matrix product with epilogue: y = residual + gate * act(x weight^T + bias).
-// Row r of the product is row src_frame[m] * N + n of x and dst_frame[m] * N + n of
-// y and residual (m = r / N); gate row frame[m] with gate_rows, else row 0.
+// Row r of the product is row n of listed frame m = r / N, for x as read, for y and the
+// residual as written; gate row frame[m] with gate_rows, else row 0.
 struct LinearParams {
     const void *x, *weight, *bias, *gate, *residual;
     void *y;
@@ -213,9 +220,7 @@ struct LinearParams {
     int32_t activation;
     int32_t dtype;
     int32_t gate_rows;
-    int16_t frame[kMaxFrames];
-    int16_t src_frame[kMaxFrames];
-    int16_t dst_frame[kMaxFrames];
+    RowFrames frames;
     void *ws;                    // NULL: no split
     DeviceGeometry geo;
 };

@@ -47,7 +47,7 @@ struct LinearKArgs {
     int32_t steps_per_part, parts;
     int32_t row_tiles, col_tiles, tiles, per_xcd, xcds;
     int32_t activation, gate_rows;
-    int16_t frame[kMaxFrames], src_frame[kMaxFrames], dst_frame[kMaxFrames];
+    RowFrames frames;
 };
 
 // What lanes past the end of a row load.
@@ -189,28 +189,48 @@ struct Epilogue {
     }
 };
 
-// The epilogue of kN neighbouring features c.. of product row r.
+// The epilogue of kN neighbouring features c.. of product row r: what it takes from
+// memory, early, and the rest.
+template <typename E, int kN>
+struct Finish {
+    Epilogue<kN> ep;
+    float residual[kN];
+    int64_t dst;
+    int frame, out;
+    // (the frames' loads and what depends on them apart: loads return in order, so a wait
+    // for a frame is one for all loads before it)
+    __device__ __forceinline__ void frames(const LinearKArgs &a, uint32_t r) {
+        const uint32_t m = r / a.N;
+        frame = a.frames.frame[m];
+        out = a.frames.out(m);
+    }
+    __device__ __forceinline__ void load(const LinearKArgs &a, uint32_t r, int c) {
+        dst = (static_cast<int64_t>(out) * a.N + r % a.N) * a.n_out;
+        ep.template load<E>(a, c, frame);
+        if (a.residual) load_n<E, kN>(a.residual, dst + c, residual);
+    }
+    __device__ __forceinline__ void store(const LinearKArgs &a, int c, float (&v)[kN]) const {
+        ep.apply(a, v);
+        if (a.residual) {
+#pragma unroll
+            for (int e = 0; e < kN; ++e) v[e] += residual[e];
+        }
+        store_n<E, kN>(a.y, dst + c, v);
+    }
+};
 template <typename E, int kN>
 __device__ __forceinline__ void finish(const LinearKArgs &a, uint32_t r, int c, float (&v)[kN]) {
-    const uint32_t m = r / a.N;
-    const int64_t dst = static_cast<int64_t>(a.dst_frame[m]) * a.N + (r - m * a.N);
-    Epilogue<kN> ep;
-    ep.template load<E>(a, c, a.frame[m]);
-    float t[kN];
-    if (a.residual) load_n<E, kN>(a.residual, dst * a.n_out + c, t);
-    ep.apply(a, v);
-    if (a.residual) {
-#pragma unroll
-        for (int e = 0; e < kN; ++e) v[e] += t[e];
-    }
-    store_n<E, kN>(a.y, dst * a.n_out + c, v);
+    Finish<E, kN> f;
+    f.frames(a, r);
+    f.load(a, r, c);
+    f.store(a, c, v);
 }
 
 // Product row r's (clamped to the last one) first byte in x.
 __device__ __forceinline__ const uint8_t *x_row(const LinearKArgs &a, uint32_t r) {
     if (r >= a.rows) r = a.rows - 1;
     const uint32_t m = r / a.N;
-    return a.x + (static_cast<int64_t>(a.src_frame[m]) * a.N + (r - m * a.N)) * a.row_bytes;
+    return a.x + (static_cast<int64_t>(a.frames.in(m)) * a.N + (r - m * a.N)) * a.row_bytes;
 }
 __device__ __forceinline__ const uint8_t *w_row(const LinearKArgs &a, int c) {
     return a.w + static_cast<int64_t>(c < a.n_out ? c : a.n_out - 1) * a.row_bytes;
@@ -256,13 +276,36 @@ void linear_tile_kernel(const LinearKArgs a) {
     const int sub = lane / 8, piece = (lane % 8) ^ (sub / 2);
     const uint32_t row0 = static_cast<uint32_t>(rt) * kBM;
     const int32_t rb = static_cast<int32_t>(a.row_bytes);
-    const uint8_t *const x0 = static_cast<const uint8_t *>(uniform_ptr(x_row(a, row0)));
     const __amdgpu_buffer_rsrc_t wres = __builtin_amdgcn_make_buffer_rsrc(
         uniform_ptr(w_row(a, ct * kBN)), 0, 0x7fffffff, kBufferWord3);
+    int32_t wo[kWLoads];
+#pragma unroll
+    for (int i = 0; i < kWLoads; ++i) {
+        const int at = wave * kWLoads + i, c = at * 8 + sub, most = a.n_out - 1 - ct * kBN;
+        wo[i] = (c < most ? c : most) * rb + 16 * (piece ^ ((at % 2) * 4));
+    }
+    // Loads of a step, W's and x's, into the buffers of its parity. The reduction's last
+    // step may be short: from then on lanes past the row's end load zeros.
+    const int32_t tail = rb % kStep;
+    auto issue_w = [&](int step, int odd) {
+        const int32_t at0 = step * kStep;
+        if (tail != 0 && at0 + kStep > rb) {
+#pragma unroll
+            for (int i = 0; i < kWLoads; ++i)
+                if (16 * (piece ^ (((wave * kWLoads + i) % 2) * 4)) >= tail) wo[i] = -1;
+        }
+        uint8_t *wd = lds + odd * kWBuf + wave * kWLoads * 1024;
+#pragma unroll
+        for (int i = 0; i < kWLoads; ++i) buffer_lds16(wres, wd + i * 1024, wo[i], at0);
+    };
+    const int s0 = part * a.steps_per_part;
+    const int s1 = s0 + a.steps_per_part < a.steps ? s0 + a.steps_per_part : a.steps;
+    issue_w(s0, 0);   // W does not wait for where x's rows are
+    const uint8_t *const x0 = static_cast<const uint8_t *>(uniform_ptr(x_row(a, row0)));
     const __amdgpu_buffer_rsrc_t xres =
         __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(x0), 0, 0x7fffffff, kBufferWord3);
     [[maybe_unused]] const uint8_t *xp[kXLoads];
-    [[maybe_unused]] int32_t xo[kXLoads], wo[kWLoads];
+    [[maybe_unused]] int32_t xo[kXLoads];
 #pragma unroll
     for (int i = 0; i < kXLoads; ++i) {
         const int at = wave * kXLoads + i;
@@ -270,15 +313,7 @@ void linear_tile_kernel(const LinearKArgs a) {
         if constexpr (kFar) xp[i] = p;
         else xo[i] = static_cast<int32_t>(p - x0);
     }
-#pragma unroll
-    for (int i = 0; i < kWLoads; ++i) {
-        const int at = wave * kWLoads + i, c = at * 8 + sub, most = a.n_out - 1 - ct * kBN;
-        wo[i] = (c < most ? c : most) * rb + 16 * (piece ^ ((at % 2) * 4));
-    }
-    // Loads of a step, x's and W's, into the buffers of its parity. The reduction's last
-    // step may be short: from then on lanes past the row's end load zeros.
-    const int32_t tail = rb % kStep;
-    auto issue = [&](int step, int odd) {
+    auto issue_x = [&](int step, int odd) {
         const int32_t at0 = step * kStep;
         if (tail != 0 && at0 + kStep > rb) {
 #pragma unroll
@@ -287,19 +322,18 @@ void linear_tile_kernel(const LinearKArgs a) {
                     if constexpr (kFar) xp[i] = reinterpret_cast<const uint8_t *>(&kZeros) - at0;
                     else xo[i] = -1;
                 }
-#pragma unroll
-            for (int i = 0; i < kWLoads; ++i)
-                if (16 * (piece ^ (((wave * kWLoads + i) % 2) * 4)) >= tail) wo[i] = -1;
         }
         uint8_t *xd = lds + 2 * kWBuf + odd * kXBuf + wave * kXLoads * 1024;
-        uint8_t *wd = lds + odd * kWBuf + wave * kWLoads * 1024;
 #pragma unroll
         for (int i = 0; i < kXLoads; ++i) {
             if constexpr (kFar) global_lds16(xp[i] + at0, xd + i * 1024);
             else buffer_lds16(xres, xd + i * 1024, xo[i], at0);
         }
-#pragma unroll
-        for (int i = 0; i < kWLoads; ++i) buffer_lds16(wres, wd + i * 1024, wo[i], at0);
+    };
+    issue_x(s0, 0);
+    auto issue = [&](int step, int odd) {
+        issue_x(step, odd);
+        issue_w(step, odd);
     };
 
     f32x16_t acc[2][kRB];
@@ -344,9 +378,6 @@ void linear_tile_kernel(const LinearKArgs a) {
         __builtin_amdgcn_sched_group_barrier(0x008, kMma - kMma / kReads * kReads, 0);
         __builtin_amdgcn_sched_barrier(0);
     };
-    const int s0 = part * a.steps_per_part;
-    const int s1 = s0 + a.steps_per_part < a.steps ? s0 + a.steps_per_part : a.steps;
-    issue(s0, 0);
     wait_loads<0>();
     __syncthreads();
     if (s0 + 1 < s1) issue(s0 + 1, 1);
@@ -402,7 +433,7 @@ void linear_tile_kernel(const LinearKArgs a) {
             uint32_t r = row0 + (wr * kRB + b) * 32 + i * 8 + sub;
             if (r >= a.rows) r = a.rows - 1;
             const uint32_t m = r / a.N;
-            const int64_t dst = static_cast<int64_t>(a.dst_frame[m]) * a.N + (r - m * a.N);
+            const int64_t dst = static_cast<int64_t>(a.frames.out(m)) * a.N + (r - m * a.N);
             global_lds16(static_cast<const uint8_t *>(a.residual) + (dst * a.n_out + cs) * 2, to + i * 1024);
         }
     };
@@ -410,7 +441,7 @@ void linear_tile_kernel(const LinearKArgs a) {
     const uint32_t last = row0 + kBM - 1 < a.rows ? row0 + kBM - 1 : a.rows - 1;
     const bool one_gate = !a.gate_rows || row0 / a.N == last / a.N;
     Epilogue<8> ep;
-    if (a.parts == 1 && c + 8 <= a.n_out) ep.template load<E>(a, c, one_gate ? a.frame[row0 / a.N] : -1);
+    if (a.parts == 1 && c + 8 <= a.n_out) ep.template load<E>(a, c, one_gate ? a.frames.frame[row0 / a.N] : -1);
     if (stage) residual(0);
 #pragma unroll
     for (int b = 0; b < kRB; ++b) {
@@ -452,8 +483,8 @@ void linear_tile_kernel(const LinearKArgs a) {
                 continue;
             }
             const uint32_t m = r / a.N;
-            const int64_t dst = static_cast<int64_t>(a.dst_frame[m]) * a.N + (r - m * a.N);
-            if (!one_gate) ep.template gate_of<E>(a, c, a.frame[m]);
+            const int64_t dst = static_cast<int64_t>(a.frames.out(m)) * a.N + (r - m * a.N);
+            if (!one_gate) ep.template gate_of<E>(a, c, a.frames.frame[m]);
             ep.apply(a, v);
             if (a.residual) {
                 float t[8];
@@ -487,19 +518,14 @@ __global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(const Linear
     const int s0 = part * a.steps_per_part + wave * kAhead;
     const int s1 = (part + 1) * a.steps_per_part < a.steps ? (part + 1) * a.steps_per_part : a.steps;
     const int32_t rb = static_cast<int32_t>(a.row_bytes), end = rb - grp * 16;
-    const uint8_t *const x0 = static_cast<const uint8_t *>(uniform_ptr(x_row(a, r0)));
     const __amdgpu_buffer_rsrc_t wres = __builtin_amdgcn_make_buffer_rsrc(
         uniform_ptr(w_row(a, c0)), 0, 0x7fffffff, kBufferWord3);
-    const __amdgpu_buffer_rsrc_t xres =
-        __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(x0), 0, 0x7fffffff, kBufferWord3);
     int32_t wo[kF], xo[kR];
 #pragma unroll
     for (int f = 0; f < kF; ++f) {
         const int c = f * 16 + l16, most = a.n_out - 1 - c0;
         wo[f] = (c < most ? c : most) * rb + grp * 16;
     }
-#pragma unroll
-    for (int b = 0; b < kR; ++b) xo[b] = static_cast<int32_t>(x_row(a, r0 + b * 16 + l16) - x0) + grp * 16;
     f32x4_t acc[kF][kR];
 #pragma unroll
     for (int f = 0; f < kF; ++f)
@@ -508,18 +534,55 @@ __global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(const Linear
     struct Batch {
         u32x4_t w[kAhead][kF], x[kAhead][kR];
     };
-    auto load = [&](int s, Batch &t) {
-        // (lanes past the end read zeros: a load under a condition would be waited for at once)
+    // (lanes past the end read zeros: a load under a condition would be waited for at once)
+    auto place = [&](int s, int i) { return s + i < s1 ? (s + i) * 64 : 0x7fffff00; };
+    auto load_w = [&](int s, Batch &t) {
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            const int32_t at = s + i < s1 ? (s + i) * 64 : 0x7fffff00;
-            const bool out = at >= end;
+            const int32_t at = place(s, i);
 #pragma unroll
-            for (int f = 0; f < kF; ++f) t.w[i][f] = buffer_load16(wres, out ? -1 : wo[f], at);
-#pragma unroll
-            for (int b = 0; b < kR; ++b) t.x[i][b] = buffer_load16(xres, out ? -1 : xo[b], at);
+            for (int f = 0; f < kF; ++f) t.w[i][f] = buffer_load16(wres, at >= end ? -1 : wo[f], at);
         }
     };
+    // where x's and y's rows are is asked for first, W next, which does not wait for it
+    uint32_t xr[kR];
+    int32_t xf[kR];
+#pragma unroll
+    for (int b = 0; b < kR; ++b) {
+        const uint32_t r = r0 + b * 16 + l16;
+        xr[b] = r < a.rows ? r : a.rows - 1;
+        xf[b] = a.frames.in(xr[b] / a.N);
+    }
+    const int32_t f0 = a.frames.in(r0 / a.N);
+    // this thread's four results and what the epilogue takes from memory for them
+    static_assert(16 * kR * 4 * kF <= 64 * kFewWaves, "a thread finishes one run of four features");
+    const int lr = tid / (4 * kF), q = tid % (4 * kF), c = c0 + q * 4;
+    const uint32_t r = r0 + lr;
+    const bool mine = tid < 16 * kR * 4 * kF && r < a.rows && c < a.n_out;
+    Finish<E, 4> fin;
+    if (mine) fin.frames(a, r);
+    Batch even, odd;
+    load_w(s0, even);
+    auto row_at = [&](int32_t frame, uint32_t row) {
+        return (static_cast<int64_t>(frame) * a.N + row % a.N) * a.row_bytes;
+    };
+    const int64_t x0 = row_at(f0, r0);
+    const __amdgpu_buffer_rsrc_t xres =
+        __builtin_amdgcn_make_buffer_rsrc(uniform_ptr(a.x + x0), 0, 0x7fffffff, kBufferWord3);
+#pragma unroll
+    for (int b = 0; b < kR; ++b)
+        // (lanes of rows past the last read zeros: no line is fetched for them)
+        xo[b] = r0 + b * 16 + l16 < a.rows ? static_cast<int32_t>(row_at(xf[b], xr[b]) - x0) + grp * 16 : -1;
+    auto load_x = [&](int s, Batch &t) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int32_t at = place(s, i);
+#pragma unroll
+            for (int b = 0; b < kR; ++b) t.x[i][b] = buffer_load16(xres, at >= end ? -1 : xo[b], at);
+        }
+    };
+    load_x(s0, even);
+    if (mine && a.parts == 1) fin.load(a, r, c);
     auto multiply = [&](const Batch &t) {
 #pragma unroll
         for (int i = 0; i < kAhead; ++i)
@@ -528,15 +591,13 @@ __global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(const Linear
 #pragma unroll
                 for (int b = 0; b < kR; ++b) acc[f][b] = mma16<E>(t.w[i][f], t.x[i][b], acc[f][b]);
     };
-    if (s0 < s1) {
-        Batch even, odd;
-        load(s0, even);
-        for (int s = s0; s < s1; s += 2 * kRound) {
-            load(s + kRound, odd);
-            multiply(even);
-            load(s + 2 * kRound, even);
-            multiply(odd);
-        }
+    for (int s = s0; s < s1; s += 2 * kRound) {
+        load_w(s + kRound, odd);
+        load_x(s + kRound, odd);
+        multiply(even);
+        load_w(s + 2 * kRound, even);
+        load_x(s + 2 * kRound, even);
+        multiply(odd);
     }
     // lane: row l16 of a block, features 4 grp .. 4 grp + 3
 #pragma unroll
@@ -545,22 +606,17 @@ __global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(const Linear
         for (int b = 0; b < kR; ++b)
             *reinterpret_cast<f32x4_t *>(&sums[wave][b * 16 + l16][f * 16 + grp * 4]) = acc[f][b];
     __syncthreads();
-    for (int i = tid; i < 16 * kR * 4 * kF; i += 64 * kFewWaves) {
-        const int lr = i / (4 * kF), q = i % (4 * kF);
-        const uint32_t r = r0 + lr;
-        const int c = c0 + q * 4;
-        if (r >= a.rows || c >= a.n_out) continue;
-        f32x4_t x = *reinterpret_cast<const f32x4_t *>(&sums[0][lr][q * 4]);
+    if (!mine) return;
+    f32x4_t x = *reinterpret_cast<const f32x4_t *>(&sums[0][lr][q * 4]);
 #pragma unroll
-        for (int w = 1; w < kFewWaves; ++w) {
-            const f32x4_t y = *reinterpret_cast<const f32x4_t *>(&sums[w][lr][q * 4]);
+    for (int w = 1; w < kFewWaves; ++w) {
+        const f32x4_t y = *reinterpret_cast<const f32x4_t *>(&sums[w][lr][q * 4]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] += y[e];
-        }
-        float v[4] = {x[0], x[1], x[2], x[3]};
-        if (a.parts > 1) store_n<float, 4>(a.ws, (static_cast<int64_t>(part) * a.rows + r) * a.n_out + c, v);
-        else finish<E, 4>(a, r, c, v);
+        for (int e = 0; e < 4; ++e) x[e] += y[e];
     }
+    float v[4] = {x[0], x[1], x[2], x[3]};
+    if (a.parts > 1) store_n<float, 4>(a.ws, (static_cast<int64_t>(part) * a.rows + r) * a.n_out + c, v);
+    else fin.store(a, c, v);
 }
 
 template <typename E>
@@ -569,6 +625,9 @@ __global__ __launch_bounds__(256) void linear_join_kernel(const LinearKArgs a) {
     if (id >= per_row * a.rows) return;
     const uint32_t r = static_cast<uint32_t>(id / per_row);
     const int c = static_cast<int>(id - r * per_row) * 4;
+    Finish<E, 4> fin;
+    fin.frames(a, r);
+    fin.load(a, r, c);
     f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f};
     const float *p = a.ws + static_cast<int64_t>(r) * a.n_out + c;
     const int64_t step = static_cast<int64_t>(a.rows) * a.n_out;
@@ -579,7 +638,7 @@ __global__ __launch_bounds__(256) void linear_join_kernel(const LinearKArgs a) {
         for (int e = 0; e < 4; ++e) x[e] += y[e];
     }
     float v[4] = {x[0], x[1], x[2], x[3]};
-    finish<E, 4>(a, r, c, v);
+    fin.store(a, c, v);
 }
 
 enum LinearForm { kFew16, kFew32, kFew64, kStream32, kStream64, kTile64, kTile128, kTile256 };
@@ -719,7 +778,7 @@ hipError_t launch_linear(const LinearParams &p, hipStream_t stream) {
     int64_t gaps = 0;
     for (int i = 0, j = 0; i < p.M; ++i) {
         while ((i - j) * p.N > 256) ++j;   // frames j..i may meet in one tile
-        const int64_t gap = (p.src_frame[i] - p.src_frame[j] - (i - j)) * p.N;
+        const int64_t gap = (p.frames.in(i) - p.frames.in(j) - (i - j)) * p.N;
         gaps = gap > gaps ? gap : gaps;
     }
     const bool far = static_cast<double>(gaps + 257) * static_cast<double>(row_bytes) >= 2147483647.0;
@@ -741,11 +800,7 @@ hipError_t launch_linear(const LinearParams &p, hipStream_t stream) {
     a.parts = plan.parts;
     a.activation = p.activation;
     a.gate_rows = p.gate_rows;
-    for (int i = 0; i < p.M; ++i) {
-        a.frame[i] = p.frame[i];
-        a.src_frame[i] = p.src_frame[i];
-        a.dst_frame[i] = p.dst_frame[i];
-    }
+    a.frames = p.frames;
     const int64_t tiles = plan.row_tiles * plan.col_tiles;
     if (tiles > 0x7fffffffLL / 64) return hipErrorInvalidConfiguration;
     a.row_tiles = static_cast<int32_t>(plan.row_tiles);

@@ -101,8 +101,8 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryKArgs a) {
     // halves: unit u < rot_units owns dimensions 8u.. and R/2 + 8u..; later units 8 dimensions past R
     const int at = kHalves && !turns ? 2 * p.pairs + 8 * (unit - a.rot_units) : 8 * unit;
 
-    const int64_t src = static_cast<int64_t>(p.src_frame[m]) * a.N + n;
-    const int64_t dst = static_cast<int64_t>(p.dst_frame[m]) * a.N + n;
+    const int64_t src = static_cast<int64_t>(p.frames.in(m)) * a.N + n;
+    const int64_t dst = static_cast<int64_t>(p.frames.out(m)) * a.N + n;
     const int total = p.heads[0] + p.heads[1];
     const int h0 = blockIdx.y * a.heads_per_thread;
     const int h1 = h0 + a.heads_per_thread < total ? h0 + a.heads_per_thread : total;
@@ -131,7 +131,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryKArgs a) {
         s[i] = 0.0f;
         if (pair < p.pairs) {
             const int axis = pair < p.pair_end[0] ? 0 : pair < p.pair_end[1] ? 1 : 2;
-            const double index = axis == 0 ? p.frame[m] : axis == 1 ? y : x;
+            const double index = axis == 0 ? p.frames.frame[m] : axis == 1 ? y : x;
             const double t = fma(p.step[axis], index, p.origin[axis]) * p.turns[pair];
             sincospif(static_cast<float>(2.0 * (t - rint(t))), &s[i], &c[i]);
         }
