@@ -1006,7 +1006,7 @@ static int cross_sizes(int32_t B, int32_t Lq, int32_t Lk, int32_t heads, int32_t
         static_cast<double>(B) * Lk * kv_heads * head_dim * 4.0 > kMaxBytes)
         return fail(RF_ERR_RANGE, "%s: sizes overflow 64-bit byte counts", fn);
     if (Lk > (1 << 30)) return fail(RF_ERR_RANGE, "%s: Lk = %d exceeds 2^30", fn, Lk);
-    if ((static_cast<double>(Lq) / 32 + 1) * B * heads > 16777216.0)
+    if (static_cast<double>((static_cast<int64_t>(Lq) + 31) / 32) * B * heads > 16777216.0)
         return fail(RF_ERR_RANGE, "%s: more than 2^24 tiles of 32 queries", fn);
     return RF_OK;
 }

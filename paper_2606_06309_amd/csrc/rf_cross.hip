@@ -701,7 +701,7 @@ hipError_t launch_cross(const CrossParams &p, hipStream_t stream) {
     a.Lk = p.Lk;
     a.B = p.B;
     a.group = p.heads / p.kv_heads;
-    a.rows = static_cast<uint32_t>(a.group) * static_cast<uint32_t>(p.Lq);   // (below 2^29 + 32: the tiles' limit)
+    a.rows = static_cast<uint32_t>(a.group) * static_cast<uint32_t>(p.Lq);   // (2^29 at most: the tiles' limit)
     a.scale_log2 = static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(p.head_dim)));
     a.xcds = xcds;
     const CrossPlan c = cross_plan(p.B, a.rows, p.kv_heads, p.Lk, p.head_dim, p.dtype, p.key_mask != nullptr,

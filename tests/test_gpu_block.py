@@ -80,3 +80,76 @@ def test_block(T, H, W, ids, heads, d, dims, dtype):
     half = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -20}[dtype]
     rel = float(torch.linalg.norm(got - want) / torch.linalg.norm(want))
     assert rel <= 16 * half, rel
+
+
+def test_two_streams_at_once():
+    """Calls on two streams, each with a workspace of its own, give what they give one after the other."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+
+    def draw(*shape):
+        return torch.randn(shape, generator=g, device="cuda").to(torch.bfloat16)
+    sets = []
+    for i in range(2):
+        q, k, v = draw(2, 3, 8, 128), draw(2, 9000 + i, 2, 128), draw(2, 9000 + i, 2, 128)
+        x, w = draw(200, 4096), draw(256, 4096)
+        sets.append((q, k, v, x, w))
+
+    def both(s, stream=None):
+        q, k, v, x, w = s
+        return (rf.rf_cross_attention(q, k, v, stream=stream), rf.rf_frame_linear(x, w, stream=stream))
+    alone = [both(s) for s in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(5):
+        for i in range(2):
+            got[i].append(both(sets[i], streams[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for pair in got[i]:
+            for a, b in zip(pair, alone[i]):
+                assert torch.equal(a, b)
+
+
+def test_two_graphs_with_workspaces_of_their_own():
+    """Two captured graphs replayed in turn and on two streams at once."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(6)
+
+    def draw(*shape):
+        return torch.randn(shape, generator=g, device="cuda").to(torch.bfloat16)
+    graphs, outs, want, alive = [], [], [], []
+    for i in range(2):
+        q, k, v = draw(1, 2, 4, 64), draw(1, 12000, 4, 64), draw(1, 12000, 4, 64)
+        x, w = draw(100, 6000), draw(128, 6000)
+        ws = [torch.empty(max(16, n), dtype=torch.uint8, device="cuda")
+              for n in (rf.rf_cross_attention_workspace(1, 2, 12000, 4, 4, 64, torch.bfloat16),
+                        rf.rf_frame_linear_workspace(1, 100, 6000, 128, torch.bfloat16))]
+        out = (torch.empty_like(q), torch.empty((100, 128), dtype=torch.bfloat16, device="cuda"))
+        alive.append((q, k, v, x, w, ws))      # a graph holds addresses, not tensors
+
+        def call(out):
+            rf.rf_cross_attention(q, k, v, out=out[0], workspace=ws[0])
+            rf.rf_frame_linear(x, w, out=out[1], workspace=ws[1])
+        eager = tuple(torch.empty_like(o) for o in out)
+        call(eager)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call(out)
+        graphs.append(graph)
+        outs.append(out)
+        want.append(eager)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for turn in range(4):
+        for out in outs:
+            for o in out:
+                o.fill_(turn)
+        torch.cuda.synchronize()
+        for i in range(2):
+            with torch.cuda.stream(streams[i] if turn % 2 else torch.cuda.current_stream()):
+                graphs[i].replay()
+        torch.cuda.synchronize()
+        for out, eager in zip(outs, want):
+            assert all(torch.equal(a, b) for a, b in zip(out, eager))
