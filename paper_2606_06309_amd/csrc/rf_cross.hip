@@ -294,10 +294,16 @@ void cross_tile_kernel(const CrossKArgs a) {
     const int col = lane & 31, grp = lane >> 5;
     int32_t tile, end;
     {
-        // walkers of an XCD have neighbouring runs
-        const int64_t per = a.walkers / a.xcds, w = (blockIdx.x % a.xcds) * per + blockIdx.x / a.xcds;
-        tile = static_cast<int32_t>(w * a.tiles / a.walkers);
-        end = static_cast<int32_t>((w + 1) * a.tiles / a.walkers);
+        // An XCD's walkers have neighbouring runs, alike to one tile; the first ones, which go to
+        // a compute unit each, have the longer (fewer walkers, of runs alike, where tiles do not
+        // share out evenly: 224 against 188 us at 8,000 x 4,000 keys, 12 heads x 128, 82 against
+        // 75 at 2 x 9,360 x 512).
+        const int32_t x = blockIdx.x % a.xcds, w = blockIdx.x / a.xcds, per = a.walkers / a.xcds;
+        const int32_t x0 = static_cast<int32_t>(static_cast<int64_t>(x) * a.tiles / a.xcds);
+        const int32_t n = static_cast<int32_t>(static_cast<int64_t>(x + 1) * a.tiles / a.xcds) - x0;
+        const int32_t each = n / per, more = n - each * per;
+        tile = x0 + w * each + (w < more ? w : more);
+        end = tile + each + (w < more);
     }
     if (tile >= end) return;
     int kgo[kN], vgo[kN];
@@ -716,7 +722,7 @@ hipError_t launch_cross(const CrossParams &p, hipStream_t stream) {
     if (!c.few && p.dtype == RF_BF16) {
         // as many walkers as are resident, or one to a tile, in whole XCDs
         const int64_t resident = tile_waves(p.head_dim, p.key_mask != nullptr) * static_cast<int64_t>(p.geo.cus);
-        const int64_t rounds = (a.tiles + resident - 1) / resident, want = (a.tiles + rounds - 1) / rounds;
+        const int64_t want = a.tiles < resident ? a.tiles : resident;
         grid = (want + xcds - 1) / xcds * xcds;
         a.walkers = static_cast<int32_t>(grid);
     }
