@@ -645,12 +645,13 @@ __global__ __launch_bounds__(256) void cross_join_kernel(const CrossKArgs a) {
 // The choice goes by the forms' times in us, counted in rounds of the device: a round
 // has a fixed part and the tiles of keys that a workgroup (of the few-row form: its
 // busiest wave) walks; a split has the join. Tiles of keys cost more where more
-// workgroups share a compute unit. Counts and measured times, us (tile / few):
+// workgroups share a compute unit, and a round that few of them share counts for as
+// much less. Counts and measured times, us (tile / few):
 //   1,560 x 512 keys, 12 heads x 128: 14 / 25     9,360 x 77, 12 x 128: 21 / 66
 //   2 x 500 x 1,000, 8 x 128: 22 / 12             300 x 5,000, 8 x 128: 83 / 20 (3 parts)
 //   128 x 20,000, 8 x 64: 224 / 21 (8 parts)      3 x 1,581 x 334, 5 x 64: 10 / 17
 // and in fp32 1,560 x 512, 12 x 128: 76 / 72; 512 x 512, 12 x 64: 41 / 15;
-// 4,680 x 512, 12 x 128: 140 / 166.
+// 4,680 x 512, 12 x 128: 140 / 166; 6,400 x 512, 12 x 64: 114 / 137.
 struct CrossPlan {
     bool few;
     int32_t parts;
@@ -677,7 +678,7 @@ CrossPlan cross_plan(int32_t B, int64_t rows, int32_t kv_heads, int32_t Lk, int3
     const int64_t whole = up(rows, kCrossTileRows) * heads, few = up(rows, kCrossFewRows) * heads;
     const int64_t most = dtype == RF_F32 ? 2 : tile_waves(head_dim, mask);   // workgroups to a compute unit
     const int64_t share = up(whole, cus) < most ? up(whole, cus) : most;
-    const double t_whole = static_cast<double>(up(whole, cus * most)) *
+    const double t_whole = static_cast<double>(up(whole, cus)) / static_cast<double>(share) *
                            (kRound + static_cast<double>(up(Lk, c.keys)) * c.tile[share - 1]);
     CrossPlan p{false, 1, whole};
     double best = 0.95 * t_whole;   // (the few-row form reads keys four times as often)
