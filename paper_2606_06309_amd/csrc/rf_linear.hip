@@ -132,6 +132,25 @@ __device__ __forceinline__ void store_n(void *p, int64_t at, const float (&v)[kN
     }
 }
 
+// The same past the caches: for results, which are written once and as whole lines.
+template <typename E>
+__device__ __forceinline__ void stream_8(void *p, int64_t at, const float (&v)[8]) {
+    if constexpr (sizeof(E) == 4) {
+#pragma unroll
+        for (int i = 0; i < 8; i += 4)
+            __builtin_nontemporal_store((f32x4_t{v[i], v[i + 1], v[i + 2], v[i + 3]}),
+                                        reinterpret_cast<f32x4_t *>(static_cast<float *>(p) + at + i));
+    } else {
+        u32x4_t x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bf16x2_t b = {static_cast<__bf16>(v[2 * e]), static_cast<__bf16>(v[2 * e + 1])};
+            x[e] = __builtin_bit_cast(uint32_t, b);
+        }
+        __builtin_nontemporal_store(x, reinterpret_cast<u32x4_t *>(static_cast<uint16_t *>(p) + at));
+    }
+}
+
 // x / (1 + 2^t): both sigmoid forms. 2^t = inf gives 0.
 __device__ __forceinline__ float gated(float x, float t) {
     return x * __builtin_amdgcn_rcpf(1.0f + fast_exp2(t));
@@ -378,9 +397,46 @@ void linear_tile_kernel(const LinearKArgs a) {
         __builtin_amdgcn_sched_group_barrier(0x008, kMma - kMma / kReads * kReads, 0);
         __builtin_amdgcn_sched_barrier(0);
     };
+    // The residual's rows come into LDS ahead of the epilogue, 32 rows x 64 features of a
+    // wave at a time, 4 KB, block b in one of two places (bf16; in fp32 the products outlast
+    // their latency). The buffers of the last step but one are free under the last step: the
+    // first two blocks go there then, the others as their places get free. Loaded where they
+    // are added, one row after the other, they cost 23 us of 69 at 9,360 x 1,536 x 1,536; a
+    // block ahead within the epilogue 2 us more than so.
+    constexpr bool kStage = sizeof(E) == 2;
+    const bool stage = kStage && a.residual && a.parts == 1;
+    const int free_odd = (s1 - s0) & 1;
+    constexpr int kBlocks = kWaves * 4096;
+    static_assert(kBlocks <= kWBuf && (kRB == 1 || kBlocks <= kXBuf || 2 * kBlocks <= kWBuf), "they fit");
+    const int c = ct * kBN + wc * 64 + (lane % 8) * 8;
+    // (a row past the last, or features past the last, load those)
+    const int cs = c < a.n_out ? c : a.n_out - 8;
+    auto block = [&](int b) {
+        constexpr bool kBoth = 2 * kBlocks <= kWBuf;   // in W's buffer; else one in W's, one in x's
+        const int at = b % 2 == 0 ? free_odd * kWBuf
+                       : kBoth    ? free_odd * kWBuf + kBlocks
+                                  : 2 * kWBuf + free_odd * kXBuf;
+        return lds + at + wave * 4096;
+    };
+    auto residual = [&](int b) {
+        uint8_t *to = block(b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t r = row0 + (wr * kRB + b) * 32 + i * 8 + sub;
+            if (r >= a.rows) r = a.rows - 1;
+            const uint32_t m = r / a.N;
+            const int64_t dst = static_cast<int64_t>(a.frames.out(m)) * a.N + (r - m * a.N);
+            global_lds16(static_cast<const uint8_t *>(a.residual) + (dst * a.n_out + cs) * 2, to + i * 1024);
+        }
+    };
+    auto residuals = [&]() {
+        residual(0);
+        if constexpr (kRB > 1) residual(1);
+    };
     wait_loads<0>();
     __syncthreads();
     if (s0 + 1 < s1) issue(s0 + 1, 1);
+    else if (stage) residuals();
     read(0);
     for (int s = s0; s < s1; ++s) {
         __builtin_amdgcn_sched_barrier(0);
@@ -394,6 +450,7 @@ void linear_tile_kernel(const LinearKArgs a) {
         wait_lds_reads();
         __syncthreads();
         if (s + 2 < s1) issue(s + 2, (s - s0) & 1);
+        else if (s + 2 == s1 && stage) residuals();
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
@@ -414,35 +471,16 @@ void linear_tile_kernel(const LinearKArgs a) {
 
     // ---- epilogue: 32 rows x 64 features at a time through 8 KB of the wave's own, 256
     // bytes a row, 16-byte units permuted by row % 16; a lane then has 8 neighbouring
-    // features of a row, and eight lanes whole lines of y ----
-    // Residual rows come into LDS too, a block ahead (bf16: 4 KB of a lane's 16 bytes, four
-    // times; in fp32 the products outlast their latency). Loaded where they are added, one
-    // row after the other, they cost 23 us of 69 at 9,360 x 1,536 x 1,536. ----
-    constexpr bool kStage = sizeof(E) == 2;
-    constexpr int kArea = 8192 + (kStage ? (kRB > 1 ? 8192 : 4096) : 0);
-    static_assert(kWaves * kArea <= 2 * (kXBuf + kWBuf), "the epilogue's rows fit the buffers");
-    uint8_t *mine = lds + wave * kArea;
-    const int c = ct * kBN + wc * 64 + (lane % 8) * 8;
-    const bool stage = kStage && a.residual && a.parts == 1;
-    // (a row past the last, or features past the last, load those)
-    const int cs = c < a.n_out ? c : a.n_out - 8;
-    auto residual = [&](int b) {
-        uint8_t *to = mine + 8192 + (b & 1) * 4096;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t r = row0 + (wr * kRB + b) * 32 + i * 8 + sub;
-            if (r >= a.rows) r = a.rows - 1;
-            const uint32_t m = r / a.N;
-            const int64_t dst = static_cast<int64_t>(a.frames.out(m)) * a.N + (r - m * a.N);
-            global_lds16(static_cast<const uint8_t *>(a.residual) + (dst * a.n_out + cs) * 2, to + i * 1024);
-        }
-    };
+    // features of a row, and eight lanes whole lines of y, which leave past the caches (52 ->
+    // 49 us at 9,360 x 1,536 x 1,536 without residual) ----
     // bias and gate of this lane's features, where all the tile's rows have one gate
     const uint32_t last = row0 + kBM - 1 < a.rows ? row0 + kBM - 1 : a.rows - 1;
     const bool one_gate = !a.gate_rows || row0 / a.N == last / a.N;
     Epilogue<8> ep;
     if (a.parts == 1 && c + 8 <= a.n_out) ep.template load<E>(a, c, one_gate ? a.frames.frame[row0 / a.N] : -1);
-    if (stage) residual(0);
+    // (8 KB of a wave, in the buffers of the last step, and in 64-row tiles all of x's)
+    uint8_t *mine = lds + (wave < kWC ? (free_odd ^ 1) * kWBuf + wave * 8192
+                                      : 2 * kWBuf + (kRB == 1 ? 0 : (free_odd ^ 1) * kXBuf) + (wave - kWC) * 8192);
 #pragma unroll
     for (int b = 0; b < kRB; ++b) {
 #pragma unroll
@@ -455,8 +493,11 @@ void linear_tile_kernel(const LinearKArgs a) {
             }
         wait_lds_reads();   // (a wave's LDS accesses run in order; this orders the compiler's)
         if (stage) {
-            wait_loads<0>();
-            if (b + 1 < kRB) residual(b + 1);
+            // (block b's loads are older than the stores of the block before, four of them
+            // if any row of this block is stored, and the next block's loads)
+            if (b == 0) wait_loads<0>();
+            else if (b + 1 < kRB) wait_loads<8>();
+            else wait_loads<4>();
         }
 #pragma unroll 1
         for (int i = 0; i < 4; ++i) {
@@ -488,14 +529,15 @@ void linear_tile_kernel(const LinearKArgs a) {
             ep.apply(a, v);
             if (a.residual) {
                 float t[8];
-                if constexpr (kStage) widen8(*reinterpret_cast<const u32x4_t *>(mine + 8192 + (b & 1) * 4096 + i * 1024 + lane * 16), t);
+                if constexpr (kStage) widen8(*reinterpret_cast<const u32x4_t *>(block(b) + i * 1024 + lane * 16), t);
                 else load_n<E, 8>(a.residual, dst * a.n_out + c, t);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] += t[e];
             }
-            store_n<E, 8>(a.y, dst * a.n_out + c, v);
+            stream_8<E>(a.y, dst * a.n_out + c, v);
         }
         wait_lds_reads();
+        if (stage && b + 2 < kRB) residual(b + 2);
     }
 }
 
