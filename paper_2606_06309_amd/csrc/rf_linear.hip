@@ -56,11 +56,8 @@ __device__ const u32x4_t kZeros = {0u, 0u, 0u, 0u};
 // 16 bytes per lane from memory straight into LDS: lane l's bytes land at dst + 16 l.
 // (Kept out of the kernel templates: the host pass drops the launch stub of a
 // template that names this builtin.)
-// kOnce: as data that is not met again (the nt bit of the cache policy).
-template <bool kOnce>
 __device__ __forceinline__ void global_lds16(const uint8_t *p, uint8_t *dst) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)p, (lds_void_t *)dst, 16, 0,
-                                     kOnce ? 2 : 0);
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)p, (lds_void_t *)dst, 16, 0, 0);
 }
 
 // The same from a buffer resource; an offset of -1 reads as zero.
@@ -348,7 +345,7 @@ void linear_tile_kernel(const LinearKArgs a) {
         uint8_t *xd = lds + 2 * kWBuf + odd * kXBuf + wave * kXLoads * 1024;
 #pragma unroll
         for (int i = 0; i < kXLoads; ++i) {
-            if constexpr (kFar) global_lds16<false>(xp[i] + at0, xd + i * 1024);
+            if constexpr (kFar) global_lds16(xp[i] + at0, xd + i * 1024);
             else buffer_lds16(xres, xd + i * 1024, xo[i], at0);
         }
     };
@@ -429,9 +426,7 @@ void linear_tile_kernel(const LinearKArgs a) {
             if (r >= a.rows) r = a.rows - 1;
             const uint32_t m = r / a.N;
             const int64_t dst = static_cast<int64_t>(a.frames.out(m)) * a.N + (r - m * a.N);
-            // (past the caches in 256-row tiles, 1,001 -> 978 us at 21,600 x 5,120 x 5,120; in
-            // 128-row ones, two to a compute unit, that costs 28.6 -> 30.2 at 3,600 x 1,536 x 1,536)
-            global_lds16<kRB == 4>(static_cast<const uint8_t *>(a.residual) + (dst * a.n_out + cs) * 2, to + i * 1024);
+            global_lds16(static_cast<const uint8_t *>(a.residual) + (dst * a.n_out + cs) * 2, to + i * 1024);
         }
     };
     auto residuals = [&]() {
