@@ -471,8 +471,10 @@ void linear_tile_kernel(const LinearKArgs a) {
 
     // ---- epilogue: 32 rows x 64 features at a time through 8 KB of the wave's own, 256
     // bytes a row, 16-byte units permuted by row % 16; a lane then has 8 neighbouring
-    // features of a row, and eight lanes whole lines of y, which leave past the caches (52 ->
-    // 49 us at 9,360 x 1,536 x 1,536 without residual) ----
+    // features of a row, and eight lanes whole lines of y. 256-row tiles, taken where y is
+    // large, send them past the caches: 50.5 -> 46 us at 9,360 x 1,536 x 1,536 without
+    // residual, and with a product that reads y next 1,990 -> 1,963 at 21,600 x 5,120 x 5,120
+    // (128-row tiles so: 54 -> 56 at 3,600 x 1,536 x 1,536). ----
     // bias and gate of this lane's features, where all the tile's rows have one gate
     const uint32_t last = row0 + kBM - 1 < a.rows ? row0 + kBM - 1 : a.rows - 1;
     const bool one_gate = !a.gate_rows || row0 / a.N == last / a.N;
@@ -534,7 +536,8 @@ void linear_tile_kernel(const LinearKArgs a) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] += t[e];
             }
-            stream_8<E>(a.y, dst * a.n_out + c, v);
+            if constexpr (kRB == 4) stream_8<E>(a.y, dst * a.n_out + c, v);
+            else store_n<E, 8>(a.y, dst * a.n_out + c, v);
         }
         wait_lds_reads();
         if (stage && b + 2 < kRB) residual(b + 2);
