@@ -399,9 +399,9 @@ void cross_tile_kernel(const CrossKArgs a) {
         buf ^= 1;
         tile_done();
         // The result goes through this wave's part of the buffer just freed (the part that
-        // only its own loads fill next) and leaves in whole rows, past the caches: 57 -> 52 us
-        // at 2 x 9,360 x 512 and 30 keys, 12 heads x 128, 21.4 -> 19.2 at 9,360 x 77; stores of
-        // 32 bytes a row as they come want the caches (75 us without).
+        // only its own loads fill next) and leaves in whole rows. (Past the caches it would be
+        // gone sooner, 21.9 -> 17.9 us at 9,360 x 77, 12 heads x 128, but the projection that reads
+        // it next would wait for it: 73.9 -> 78.0 for the two, 151 -> 160 at 2 x 9,360 x 512.)
         // (What follows from the lane is formed here, not held in registers through the loop.)
         using L = Tile<D>;
         int ln = lane;
@@ -439,7 +439,7 @@ void cross_tile_kernel(const CrossKArgs a) {
                                                                  ((slot ^ L::kswz(r)) * 16));
             const uint32_t row = t.row0 + wave * 32 + r;
             uint16_t *op = static_cast<uint16_t *>(a.out) + row_offset(a, a.os, t, row < a.rows ? row : 0) + slot * 8;
-            if (row < a.rows) __builtin_nontemporal_store(x, reinterpret_cast<u32x4_t *>(op));
+            if (row < a.rows) *reinterpret_cast<u32x4_t *>(op) = x;
         }
         wait_lds_reads();
         t = tn;
