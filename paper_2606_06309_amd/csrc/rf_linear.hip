@@ -47,6 +47,7 @@ struct LinearKArgs {
     int32_t steps_per_part, parts;
     int32_t row_tiles, col_tiles, tiles, per_xcd, xcds;
     int32_t activation, gate_rows;
+    int32_t stream;            // 256-row tiles: y goes past the caches
     RowFrames frames;
 };
 
@@ -472,9 +473,10 @@ void linear_tile_kernel(const LinearKArgs a) {
     // ---- epilogue: 32 rows x 64 features at a time through 8 KB of the wave's own, 256
     // bytes a row, 16-byte units permuted by row % 16; a lane then has 8 neighbouring
     // features of a row, and eight lanes whole lines of y. 256-row tiles, taken where y is
-    // large, send them past the caches: 50.5 -> 46 us at 9,360 x 1,536 x 1,536 without
-    // residual, and with a product that reads y next 1,990 -> 1,963 at 21,600 x 5,120 x 5,120
-    // (128-row tiles so: 54 -> 56 at 3,600 x 1,536 x 1,536). ----
+    // large, send it past the caches if it is no wider than x: 50 -> 45 us at 9,360 x 1,536 x
+    // 1,536 without residual, 1,977 -> 1,896 at 21,600 x 5,120 x 5,120 and a product that reads
+    // it next; wider ones so, a feed-forward's, 1,536 to 6,144 and back: 323 -> 340; 128-row tiles
+    // so, the two at 3,600 x 1,536 x 1,536: 54 -> 56. ----
     // bias and gate of this lane's features, where all the tile's rows have one gate
     const uint32_t last = row0 + kBM - 1 < a.rows ? row0 + kBM - 1 : a.rows - 1;
     const bool one_gate = !a.gate_rows || row0 / a.N == last / a.N;
@@ -536,8 +538,13 @@ void linear_tile_kernel(const LinearKArgs a) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] += t[e];
             }
-            if constexpr (kRB == 4) stream_8<E>(a.y, dst * a.n_out + c, v);
-            else store_n<E, 8>(a.y, dst * a.n_out + c, v);
+            if (kRB == 4 && a.stream) {
+                asm volatile("" ::: "memory");   // (without these two the compiler makes one store of both)
+                stream_8<E>(a.y, dst * a.n_out + c, v);
+                asm volatile("" ::: "memory");
+            } else {
+                store_n<E, 8>(a.y, dst * a.n_out + c, v);
+            }
         }
         wait_lds_reads();
         if (stage && b + 2 < kRB) residual(b + 2);
@@ -846,6 +853,7 @@ hipError_t launch_linear(const LinearParams &p, hipStream_t stream) {
     a.parts = plan.parts;
     a.activation = p.activation;
     a.gate_rows = p.gate_rows;
+    a.stream = p.n_out <= p.K;
     a.frames = p.frames;
     const int64_t tiles = plan.row_tiles * plan.col_tiles;
     if (tiles > 0x7fffffffLL / 64) return hipErrorInvalidConfiguration;
