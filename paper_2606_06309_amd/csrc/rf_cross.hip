@@ -18,7 +18,22 @@
 //    holds there (NaN, infinities) has no effect, and its score becomes -inf.
 //  * Softmax in the log2 domain against a reference that is a past row maximum,
 //    replaced when a row's probabilities of a tile sum to more than 256 (the sum
-//    bounds each of them). A walk's first tile takes its own maximum.
+//    bounds each of them). A walk's first tile takes its own maximum. Probabilities
+//    are rounded to bf16 for the second product, and the row sum adds the rounded
+//    ones, so their errors (2^-8 of each at most) are weighted alike.
+//
+// What bounds them, and what they measure:
+//  * Many rows, many keys (8,000 x 4,000, 12 heads x 128: 185 us, 1,060 TFLOP/s): issue of
+//    the matrix instructions and the softmax's vector instructions, as in self attention.
+//  * Many rows, a prompt (21,600 x 512, 40 heads x 128: 262 us, 864 TFLOP/s; at heads of
+//    64 157 us): the same, and each 128 rows' queries and results, 64 KB, which the
+//    other workgroup of the compute unit covers in part. Tiles of 32 keys with three
+//    workgroups to a compute unit at 128 (279 us where this had 267), the next queries
+//    held in registers (313) or touched ahead (288), a wait that leaves them out (no
+//    change) did not cover more.
+//  * Short prompts (2 x 9,360 rows, 12 heads x 128, 116 MB: 38 us): memory, q in and out.
+//  * One token over 20,280 keys, 4 key heads x 128: 17 us, 4.9 TB/s of K and V, and 4 of
+//    the join.
 #include "rf_cross.h"
 
 namespace rf {
@@ -271,11 +286,12 @@ __device__ __forceinline__ void load_offsets(int64_t stride, int i0, int lane, i
 
 // ---------------------------------------------------------------------------
 // Many rows: a workgroup of 4 waves owns 128 rows of one key head at a time; its
-// waves share double-buffered tiles (64 KB of LDS), one barrier a tile; two
-// workgroups to a compute unit.
+// waves share double-buffered tiles of 64 keys (64 KB of LDS at head dimension 128, 32
+// at 64), one barrier a tile; two workgroups to a compute unit, three at 64 without mask.
 // A prompt is a few tiles long, so the time between two tiles of rows counts: a
 // workgroup walks a run of tiles of rows, and under the last tile of keys of one
-// the queries and the first keys and values of the next are on their way.
+// the first keys and values of the next are on their way, its queries from where the
+// last scores are done.
 // ---------------------------------------------------------------------------
 
 constexpr int kTileWaves = kCrossTileRows / 32;

@@ -12,15 +12,29 @@
 // of y and runs of four features.
 //
 //  * linear_tile_kernel: a workgroup owns kBM rows x kBN features, 8 or 4 waves of
-//    32 kRB x 64. Steps go from memory straight into LDS, double-buffered, one
-//    barrier a step. Rows of 128 bytes are stored without padding, their eight
-//    16-byte slots permuted by (row / 2) % 8, so the 16 lanes of a read pass meet 16
-//    different slots of the 256-byte bank window.
-//  * linear_few_kernel: up to 64 rows, where reading W is all that costs: a workgroup
-//    owns 16 features, its 8 waves share out the reduction index, operands go
-//    straight to registers, and the waves' sums meet in LDS.
+//    32 kRB x 64: 256 x 256, 128 x 128 and 64 x 128, and 64 x 256 and 32 x 256 where
+//    rows are few and W large. Steps go from memory straight into LDS,
+//    double-buffered, one barrier a step. Rows of 128 bytes are stored without
+//    padding, their eight 16-byte slots permuted by (row / 2) % 8, so the 16 lanes of
+//    a read pass meet 16 different slots of the 256-byte bank window.
+//  * linear_few_kernel: up to 64 rows of a small W, where reading W is all that
+//    costs: a workgroup owns 16 or 32 features, its 8 waves share out the reduction
+//    index, operands go straight to registers, and the waves' sums meet in LDS.
 //  * A reduction index may also be split over workgroups, whose fp32 parts go to the
 //    workspace; linear_join_kernel adds them in order and runs the epilogue.
+//
+// What bounds them, and what they measure:
+//  * Large bf16 products (21,600 x 20,480 x 5,120 with gate and residual: 3.79 ms,
+//    1,197 TFLOP/s): matrix instructions are busy 65 % of the cycles. Per step a
+//    256 x 256 tile reads 192 KB of LDS while 64 KB of loads are written into it; the
+//    same loop without the loads runs at 1,570. Four waves of 128 x 128 (1,225 TFLOP/s
+//    where this had 1,323), a ring of four half steps (1,218) and loads between the
+//    matrix instructions (1,248) were slower.
+//  * One round of tiles (9,360 x 1,536 x 1,536: 45 us, 52 with gate and residual): 24
+//    steps of 1.55 us, the first loads and the epilogue's memory time.
+//  * fp32 (7,800 x 1,536 x 1,536: 280 us, 131 TFLOP/s): the matrix instructions, busy 82 %.
+//  * Few rows (6 x 1,536 x 9,216: 10.0 us, 2.9 TB/s): the latency of a launch, of two
+//    loads one after the other, and of the waves' sums.
 #include "rf_device.h"
 
 namespace rf {
