@@ -260,3 +260,22 @@ def test_offsets_past_32_bits():
     kv.copy_(draw(kv.shape, BF16, 19))
     k, v = kv[:1].expand(B, -1, -1, -1), kv[1:].expand(B, -1, -1, -1)
     ref.assert_within(rf.rf_cross_attention(q, k, v), *ref.cross(q, k, v))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("masked", [False, True])
+def test_runs_of_row_tiles(masked, d, dtype):
+    """More tiles of rows than workgroups stay on the device, so each walks several, of sequences of unlike length (one
+    without any key) and of rows that end inside a tile; the results' rows stand apart and nothing between them is
+    written."""
+    B, Lq, Lk, heads = 3, 5000, 130, 7
+    q, k, v = make(B, Lq, Lk, heads, heads, d, dtype, seed=30)
+    lengths = [Lk, 0, 65]
+    mask = (draw((B, Lk), F32, 33) > -0.5) if masked else None
+    wide = torch.full((B, Lq, heads, d + 8), 7.0, dtype=dtype, device="cuda")
+    out = wide[..., :d]
+    rf.rf_cross_attention(q, k, v, i32(lengths), mask, out=out)
+    ref.assert_within(out, *ref.cross(q, k, v, i32(lengths), mask))
+    assert bool((wide[..., d:] == 7.0).all())
+    assert torch.equal(rf.rf_cross_attention(q, k, v, i32(lengths), mask), out)

@@ -171,3 +171,25 @@ def test_offsets_past_32_bits():
     y = rf.rf_frame_linear(x, w)
     ref.assert_within(y[at], *ref.linear(x[at], w))
     assert not bool(y[2:1000].any())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("K", [8, 64, 72, 136, 200, 2048])
+def test_large_tiles_in_place(K, dtype):
+    """Many rows: the largest tiles, from one step of the reduction on, the last rows and features in part; the
+    residual is the result's own buffer, and each frame has a gate."""
+    T, N, n = 131, 127, 2008
+    ids = [t for t in range(T) if t not in (3, 64)]
+    x, w, b = draw((len(ids) * N, K), dtype, 50), draw((n, K), dtype, 51, K ** -0.5), draw((n,), dtype, 52)
+    gate, full = draw((T, n), dtype, 53), draw((T * N, n), dtype, 54)
+    pos = ref.positions(ids, N, "cuda")
+    want, bound = ref.linear(x, w, b, "silu", gate[torch.tensor(ids, device="cuda")].repeat_interleave(N, 0), full[pos])
+    old = full.clone()
+    kw = dict(frame_ids=ids, T=T, rows_per_frame=N, out_full=True)
+    rf.rf_frame_linear(x, w, b, "silu", gate, full, out=full, **kw)
+    ref.assert_within(full[pos], want, bound, f"{K}")
+    for t in (3, 64):
+        assert torch.equal(full[t * N:(t + 1) * N], old[t * N:(t + 1) * N])
+    again = old.clone()
+    rf.rf_frame_linear(x, w, b, "silu", gate, again, out=again, **kw)
+    assert torch.equal(again, full)
