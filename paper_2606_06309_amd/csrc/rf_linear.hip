@@ -12,8 +12,8 @@
 // of y and runs of four features.
 //
 //  * linear_tile_kernel: a workgroup owns kBM rows x kBN features, 8 or 4 waves of
-//    32 kRB x 64: 256 x 256, 128 x 128 and 64 x 128, and 64 x 256 and 32 x 256 where
-//    rows are few and W large. Steps go from memory straight into LDS,
+//    32 kRB x 64: 256 x 256, 128 x 128 and 64 x 128, and 32 x 256 and (bf16) 64 x 256
+//    where rows are few and W large. Steps go from memory straight into LDS,
 //    double-buffered, one barrier a step. Rows of 128 bytes are stored without
 //    padding, their eight 16-byte slots permuted by (row / 2) % 8, so the 16 lanes of
 //    a read pass meet 16 different slots of the 256-byte bank window.
@@ -721,14 +721,20 @@ LinearPlan linear_plan(int64_t rows, int32_t K, int32_t n_out, int32_t dtype, in
     const int64_t bytes = static_cast<int64_t>(K) * (dtype == RF_F32 ? 4 : 2);
     auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
     if (rows <= 64 && !far) {
-        // Straight to registers, or through LDS in tiles of 256 features: by the bytes of W
-        // from which the latter is faster. us of a product, registers / LDS, bf16: 16 rows x
-        // 4,096 x 4,096 10.6 / 11.5, 8 x 5,120 x 5,120 19.2 / 16.2, 16 x 20,480 x 5,120 73 / 41;
-        // 17 x 1,536 x 1,536 8.3 / 8.3, 17 x 1,536 x 6,144 12.3 / 9.7; 64 x 1,536 x 1,536 11.4 /
-        // 10.8, 64 x 20,480 x 5,120 97 / 48; fp32: 16 x 4,096 x 4,096 18.5 / 18.8, 8 x 5,120 x
-        // 5,120 33 / 29, 17 x 1,536 x 6,144 24.7 / 14.8.
+        // Straight to registers, through LDS in tiles of 256 features, or (33 rows on) as
+        // products of more rows: by the bytes of W from which the latter are faster. us of a
+        // product, registers / LDS, bf16: 16 rows x 4,096 x 4,096 10.6 / 11.5, 8 x 5,120 x 5,120
+        // 19.2 / 16.2, 16 x 20,480 x 5,120 73 / 41; 17 x 1,536 x 1,536 8.3 / 8.3, 17 x 1,536 x
+        // 6,144 12.3 / 9.7; fp32: 16 x 4,096 x 4,096 18.5 / 18.8, 8 x 5,120 x 5,120 33 / 29, 17 x
+        // 1,536 x 6,144 24.7 / 14.8. Registers / tiles of 64 x 128, bf16: 64 x 1,536 x 1,024 9.3 /
+        // 10.0, 64 x 1,536 x 1,536 11.4 / 10.9; fp32: 64 x 1,024 x 1,536 11.1 / 14.4, 64 x 1,536 x
+        // 1,536 - / 15.7. LDS, 256 features / tiles of 64 x 128, 64 rows: 1,536 x 1,536 13.2 / 10.9,
+        // 4,096 x 4,096 18.5 / 16.2, 10,240 x 5,120 36 / 29, 20,480 x 5,120 61 / 73; 24 rows: 1,536 x
+        // 6,144 12.5 / 12.0, in fp32 17 / 21.
         const double w_mb = static_cast<double>(n_out) * static_cast<double>(bytes) * 1e-6;
-        if (w_mb >= (dtype == RF_F32 ? 2 : 1) * (rows <= 16 ? 40 : rows <= 32 ? 8 : 4)) {
+        const bool few = w_mb < (dtype == RF_F32 ? 2 : 1) * (rows <= 16 ? 40 : rows <= 32 ? 8 : 4);
+        const bool stream = !few && (rows <= 32 || (dtype == RF_BF16 && w_mb >= 150));
+        if (stream) {
             p.form = rows <= 32 ? kStream32 : kStream64;
             p.row_tiles = 1;
             p.col_tiles = up(n_out, 256);
@@ -741,16 +747,18 @@ LinearPlan linear_plan(int64_t rows, int32_t K, int32_t n_out, int32_t dtype, in
             p.parts = static_cast<int32_t>(up(p.steps, p.per_part));
             return p;
         }
-        p.form = rows <= 16 ? kFew16 : rows <= 32 ? kFew32 : kFew64;
-        p.row_tiles = 1;
-        p.col_tiles = up(n_out, rows > 16 && rows <= 32 ? 32 : 16);
-        p.steps = static_cast<int32_t>(up(bytes, 64));
-        // a wave takes four pieces at least; two workgroups to a compute unit
-        const int64_t want = up(2 * cus, p.col_tiles), most = up(p.steps, 4 * kFewWaves);
-        p.parts = static_cast<int32_t>(!may_split || p.col_tiles >= cus ? 1 : want < most ? want : most);
-        p.per_part = static_cast<int32_t>(up(up(p.steps, p.parts), 4) * 4);
-        p.parts = static_cast<int32_t>(up(p.steps, p.per_part));
-        return p;
+        if (few) {
+            p.form = rows <= 16 ? kFew16 : rows <= 32 ? kFew32 : kFew64;
+            p.row_tiles = 1;
+            p.col_tiles = up(n_out, rows > 16 && rows <= 32 ? 32 : 16);
+            p.steps = static_cast<int32_t>(up(bytes, 64));
+            // a wave takes four pieces at least; two workgroups to a compute unit
+            const int64_t want = up(2 * cus, p.col_tiles), most = up(p.steps, 4 * kFewWaves);
+            p.parts = static_cast<int32_t>(!may_split || p.col_tiles >= cus ? 1 : want < most ? want : most);
+            p.per_part = static_cast<int32_t>(up(up(p.steps, p.parts), 4) * 4);
+            p.parts = static_cast<int32_t>(up(p.steps, p.per_part));
+            return p;
+        }
     }
     // Tiles of 64 x 128, 128 x 128 or 256 x 256 (rows x features) and parts of the reduction,
     // by the time in us that they come to, counted in rounds of the device: a round has a
@@ -813,7 +821,10 @@ void run(const LinearPlan &p, const LinearKArgs &a, bool far, dim3 grid, hipStre
         case kFew32: hipLaunchKernelGGL((linear_few_kernel<E, 2, 2>), grid, dim3(512), 0, stream, a); break;
         case kFew64: hipLaunchKernelGGL((linear_few_kernel<E, 4, 1>), grid, dim3(512), 0, stream, a); break;
         case kStream32: hipLaunchKernelGGL((linear_tile_kernel<E, 1, 1, 4, false>), grid, dim3(256), 0, stream, a); break;
-        case kStream64: hipLaunchKernelGGL((linear_tile_kernel<E, 2, 1, 4, false>), grid, dim3(256), 0, stream, a); break;
+        case kStream64:   // (bf16 only)
+            if constexpr (sizeof(E) == 2)
+                hipLaunchKernelGGL((linear_tile_kernel<E, 2, 1, 4, false>), grid, dim3(256), 0, stream, a);
+            break;
         case kTile64: hipLaunchKernelGGL((linear_tile_kernel<E, 1, 2, 2, false>), grid, dim3(256), 0, stream, a); break;
         case kTile128:
             if (far) hipLaunchKernelGGL((linear_tile_kernel<E, 2, 2, 2, true>), grid, dim3(256), 0, stream, a);

@@ -193,3 +193,16 @@ def test_large_tiles_in_place(K, dtype):
     again = old.clone()
     rf.rf_frame_linear(x, w, b, "silu", gate, again, out=again, **kw)
     assert torch.equal(again, full)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,K,n", [(9, 4104, 5000), (20, 1536, 2728), (32, 1544, 2728), (33, 1544, 1400),
+                                      (64, 520, 4104), (33, 15000, 5128), (50, 15008, 5120), (64, 15000, 5128)])
+def test_few_rows_of_large_weights(rows, K, n, dtype):
+    """Where the weights' size decides how few rows are taken; with a residual, in place, and again bit for bit."""
+    x, w = draw((rows, K), dtype, 60), draw((n, K), dtype, 61, K ** -0.5)
+    b, g, r = draw((n,), dtype, 62), draw((n,), dtype, 63), draw((rows, n), dtype, 64)
+    want, bound = ref.linear(x, w, b, "gelu", g, r)
+    y = rf.rf_frame_linear(x, w, b, "gelu", g, r)
+    ref.assert_within(y, want, bound, f"{rows} {K} {n}")
+    assert torch.equal(rf.rf_frame_linear(x, w, b, "gelu", g, r, out=r), y)
