@@ -765,8 +765,12 @@ LinearPlan linear_plan(int64_t rows, int32_t K, int32_t n_out, int32_t dtype, in
     // fixed part and its steps, which take the longer the more workgroups share a compute
     // unit; a split adds the second kernel and its parts, written and read again. The
     // counts are fitted to products of 70 to 21,600 rows, 8 to 20,480 inputs and 256 to
-    // 6,144 features. us, 64 x 128 / 128 x 128 / 256 x 256 (* split), bf16: 512 x 1,536 x 1,536
-    // 11.6 / 17.5 / 41; 500 x 8,960 x 1,536 29.5* / 29.8* / 36*; 3,600 x 1,536 x 1,536 27 / 26 /
+    // 6,144 features, whose weights come from beyond the L2s, as from one layer to the
+    // next: a workgroup alone on a compute unit then takes 0.53 us for a step of the
+    // smallest tile where it takes 0.38 with the weights at hand. (Unsplit / split so: 512 x
+    // 1,536 x 1,536 18.6 / 16.0, 1,000 x 6,144 x 1,536 58 / 35, 2,000 x 6,144 x 1,536 72 / 54;
+    // fp32 1,500 x 4,096 x 320 84 / 53.) us, 64 x 128 / 128 x 128 / 256 x 256 (* split), bf16, weights
+    // at hand: 512 x 1,536 x 1,536 11.6 / 17.5 / 41; 500 x 8,960 x 1,536 29.5* / 29.8* / 36*; 3,600 x 1,536 x 1,536 27 / 26 /
     // 41; 9,360 x 1,536 x 1,536 64 / 53 / 47; fp32: 512 x 1,536 x 1,536 31* / 41* / 74*; 7,800 x
     // 1,536 x 1,536 279 / 353 / 363; 9,360 x 1,536 x 6,144 - / 1,247 / 1,438.
     struct Form {
@@ -776,11 +780,11 @@ LinearPlan linear_plan(int64_t rows, int32_t K, int32_t n_out, int32_t dtype, in
         double round;
         double step[3];      // with one, two, three workgroups to a compute unit
     };
-    static const Form forms[2][3] = {{{kTile64, 64, 128, 3, 3.0, {0.38, 0.68, 1.0}},
-                                      {kTile128, 128, 128, 2, 4.0, {0.62, 0.95, 0.95}},
+    static const Form forms[2][3] = {{{kTile64, 64, 128, 3, 3.0, {0.53, 0.68, 1.0}},
+                                      {kTile128, 128, 128, 2, 4.0, {0.80, 0.95, 0.95}},
                                       {kTile256, 256, 256, 1, 8.0, {1.55, 1.55, 1.55}}},
-                                     {{kTile64, 64, 128, 3, 3.0, {1.03, 1.95, 2.93}},
-                                      {kTile128, 128, 128, 2, 4.0, {2.05, 3.65, 3.65}},
+                                     {{kTile64, 64, 128, 3, 3.0, {1.1, 1.95, 2.93}},
+                                      {kTile128, 128, 128, 2, 4.0, {2.4, 3.65, 3.65}},
                                       {kTile256, 256, 256, 1, 8.0, {7.4, 7.4, 7.4}}}};
     constexpr int64_t kLeastSteps = 4, kMostParts = 16;
     constexpr double kJoin = 3.0;
