@@ -25,14 +25,14 @@
 //
 // What bounds them, and what they measure:
 //  * Large bf16 products (21,600 x 20,480 x 5,120 with gate and residual: 3.79 ms,
-//    1,197 TFLOP/s): matrix instructions are busy 65 % of the cycles. Per step a
+//    1,197 TFLOP/s): matrix instructions are busy 64 % of the cycles. Per step a
 //    256 x 256 tile reads 192 KB of LDS while 64 KB of loads are written into it; the
 //    same loop without the loads runs at 1,570. Four waves of 128 x 128 (1,225 TFLOP/s
 //    where this had 1,323), a ring of four half steps (1,218) and loads between the
 //    matrix instructions (1,248) were slower.
 //  * One round of tiles (9,360 x 1,536 x 1,536: 45 us, 52 with gate and residual): 24
 //    steps of 1.55 us, the first loads and the epilogue's memory time.
-//  * fp32 (7,800 x 1,536 x 1,536: 280 us, 131 TFLOP/s): the matrix instructions, busy 82 %.
+//  * fp32 (7,800 x 1,536 x 1,536: 280 us, 131 TFLOP/s): the matrix instructions, busy 81 %.
 //  * Few rows (6 x 1,536 x 9,216: 10.0 us, 2.9 TB/s): the latency of a launch, of two
 //    loads one after the other, and of the waves' sums.
 #include "rf_device.h"
