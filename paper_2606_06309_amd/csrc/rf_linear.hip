@@ -36,6 +36,7 @@
 //  * Few rows (6 x 1,536 x 9,216: 10.0 us, 2.9 TB/s): the latency of a launch, of two
 //    loads one after the other, and of the waves' sums.
 #include "rf_device.h"
+#include "rf_linear_plan.h"
 
 namespace rf {
 namespace {
@@ -856,14 +857,7 @@ hipError_t launch_linear(const LinearParams &p, hipStream_t stream) {
     if (p.geo.cus < 1 || xcds < 1 || xcds > 64) return hipErrorInvalidValue;
     const int64_t rows = p.M * p.N;
     const int64_t row_bytes = static_cast<int64_t>(p.K) * (p.dtype == RF_F32 ? 4 : 2);
-    // a tile's rows span 256 rows and what lies between the frames that it meets
-    int64_t gaps = 0;
-    for (int i = 0, j = 0; i < p.M; ++i) {
-        while ((i - j) * p.N > 256) ++j;   // frames j..i may meet in one tile
-        const int64_t gap = (p.frames.in(i) - p.frames.in(j) - (i - j)) * p.N;
-        gaps = gap > gaps ? gap : gaps;
-    }
-    const bool far = static_cast<double>(gaps + 257) * static_cast<double>(row_bytes) >= 2147483647.0;
+    const bool far = linear_far(p.frames, p.M, p.N, row_bytes);
     const LinearPlan plan = linear_plan(rows, p.K, p.n_out, p.dtype, p.geo.cus, far, p.ws != nullptr);
     LinearKArgs a{};
     a.x = static_cast<const uint8_t *>(p.x);

@@ -1,0 +1,78 @@
+/* Host rules of the frame matrix product's launch against plain walks over rows. Prints "ok <checks>"; exits 1 at the
+   first mismatch. */
+#include <cstdio>
+#include <random>
+#include <vector>
+
+#include "rf_linear_plan.h"
+
+static int checks;
+#define CHECK(cond)                                                                     \
+    do {                                                                                \
+        ++checks;                                                                       \
+        if (!(cond)) return std::printf("line %d: %s\n", __LINE__, #cond), 1;           \
+    } while (0)
+
+static rf::RowFrames list(const std::vector<int> &ids, bool full) {
+    rf::RowFrames f{};
+    for (size_t i = 0; i < ids.size(); ++i) f.frame[i] = static_cast<uint8_t>(ids[i]);
+    f.in_full = full;
+    return f;
+}
+
+// The widest distance in x, in rows, of two rows that any 256 consecutive rows of the product hold: the
+// first and the last of them, as positions grow. (All that matter of a frame are 256 rows at either end.)
+static int64_t widest(const std::vector<int> &ids, int64_t N, bool full) {
+    const int64_t rows = static_cast<int64_t>(ids.size()) * N;
+    auto at = [&](int64_t r) { return full ? ids[r / N] * N + r % N : r; };
+    int64_t most = 0;
+    for (int64_t m = 0; m < static_cast<int64_t>(ids.size()); ++m)
+        for (int64_t n = N > 600 ? N - 300 : 0; n < N; ++n) {
+            const int64_t r = m * N + n, last = r + 255 < rows ? r + 255 : rows - 1;
+            most = at(last) - at(r) > most ? at(last) - at(r) : most;
+        }
+    return most;
+}
+
+static int meeting(const std::vector<int> &ids, int64_t N) {
+    const int32_t M = static_cast<int32_t>(ids.size());
+    for (const bool full : {false, true}) {
+        const rf::RowFrames f = list(ids, full);
+        const int64_t gap = rf::linear_gap(f, M, N), far = widest(ids, N, full);
+        CHECK(gap <= far && far <= gap + 255);   // (no tile is wider, and one is as wide)
+        CHECK(full || gap == 0);
+        // 32-bit offsets exactly where the widest tile's fit, for rows of 16 bytes to just below 8 MB
+        for (int64_t row = 16; row < (1 << 23); row = row * 3 + 16) {
+            CHECK(rf::linear_far(f, M, N, row) || (far + 1) * row <= 2147483647);
+            CHECK(!rf::linear_far(f, M, N, row) || (far + 258) * row >= 2147483647);
+        }
+    }
+    return 0;
+}
+
+static int frames_that_meet() {
+    const int64_t sizes[] = {1, 2, 37, 84, 85, 86, 127, 128, 129, 200, 253, 254, 255, 256, 257, 300, 511, 1560, 3600};
+    std::mt19937 rng(7);
+    for (const int64_t N : sizes) {
+        for (const std::vector<int> &ids : {std::vector<int>{0}, {255}, {0, 1}, {0, 255}, {0, 20}, {0, 1, 255}, {0, 254, 255},
+                                            {0, 127, 255}, {3, 4, 5, 200, 201, 255}})
+            if (meeting(ids, N)) return 1;
+        for (int i = 0; i < 40; ++i) {
+            std::vector<int> ids;
+            const int keep = 1 + static_cast<int>(rng() % 100);
+            for (int t = 0; t < 256; ++t)
+                if (static_cast<int>(rng() % 100) < keep) ids.push_back(t);
+            if (!ids.empty() && meeting(ids, N)) return 1;
+        }
+    }
+    // keyframes of a 720p video and a wide feed-forward's rows: 3,600 rows of 40,960 bytes, 19 frames apart
+    CHECK(rf::linear_far(list({0, 20}, true), 2, 3600, 40960));
+    CHECK(!rf::linear_far(list({0, 20}, false), 2, 3600, 40960));
+    return 0;
+}
+
+int main() {
+    if (frames_that_meet()) return 1;
+    std::printf("ok %d\n", checks);
+    return 0;
+}
