@@ -778,16 +778,32 @@ def _head_rows(t, name, rows, heads, d):
 
 @functools.lru_cache(maxsize=64)
 def _rotary_axes(dims, theta, origin, step):
+    """The struct of plain numbers (tuples of int and float; theta also one for all axes)."""
+    for n in dims:
+        if n != n or abs(n) >= 2 ** 31 or n != int(n):
+            raise ValueError(f"dims must be whole numbers, not {n}")
     axes = rf_rotary_axes()
     axes.dims[:] = [int(n) for n in dims]
-    axes.theta[:] = [float(theta)] * 3 if isinstance(theta, (int, float)) else [float(x) for x in theta]
-    axes.origin[:] = [float(x) for x in origin]
-    axes.step[:] = [float(x) for x in step]
+    axes.theta[:] = [theta] * 3 if isinstance(theta, (int, float)) else theta
+    axes.origin[:], axes.step[:] = origin, step
     return axes
 
 
-def _key(values):
-    return values if isinstance(values, (int, float, tuple)) else tuple(values)
+_PLAIN = frozenset((int, float))
+
+
+def _axes(dims, theta, origin, step):
+    """_rotary_axes of numbers of any kind, by their values now: what is kept goes by
+    plain numbers only, as a tensor among them may hold another one at the next call."""
+    if (type(dims) is type(origin) is type(step) is tuple and type(theta) in _PLAIN
+            and _PLAIN.issuperset(map(type, dims + origin + step))):
+        return _rotary_axes(dims, theta, origin, step)
+    try:
+        theta = tuple([float(x) for x in theta])
+    except TypeError:   # one for all axes
+        theta = float(theta)
+    dims, origin, step = (tuple([float(x) for x in v]) for v in (dims, origin, step))
+    return _rotary_axes(dims, theta, origin, step)
 
 
 def rf_rotary(q, frame_ids, T: int, H: int, W: int, dims, k=None, out=None, k_out=None, theta=10000.0,
@@ -826,7 +842,7 @@ def rf_rotary(q, frame_ids, T: int, H: int, W: int, dims, k=None, out=None, k_ou
         tensors = ((q, "q"), (out, "out"), (k, "k"), (k_out, "k_out"))
         code = _same_dtype(tensors)
         index, ptrs = _on_device(tensors)
-    axes = _rotary_axes(_key(dims), _key(theta), _key(origin), _key(step))
+    axes = _axes(dims, theta, origin, step)
     flags = ((RF_ROWS_IN_FULL if in_full else 0) | (RF_ROWS_OUT_FULL if out_full else 0) |
              (RF_ROTARY_HALVES if halves else 0) | (RF_ROTARY_INVERSE if inverse else 0))
     _check(lib.rf_rotary(*ptrs, ids_p, M, T, H, W, hq, hk, d, ctypes.byref(axes), sq, so, sk, sko, flags, code,
