@@ -30,7 +30,6 @@ constexpr int64_t kFill = 8192;
 struct RotaryKArgs {
     RotaryParams p;
     uint32_t N;                // tokens per frame
-    uint32_t blocks;           // workgroups per frame
     uint32_t units;            // threads per token
     uint32_t rot_units;        // of them, those that own turning dimensions
     int32_t heads_per_thread;  // of q's and k's heads, one after the other
@@ -94,9 +93,9 @@ struct Piece {
 template <typename E, bool kHalves>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryKArgs a) {
     const RotaryParams &p = a.p;
-    const uint32_t m = blockIdx.x / a.blocks;
-    // (a frame's threads are fewer than 2^32 + 256: launch_rotary)
-    const uint32_t id = (blockIdx.x - m * a.blocks) * kThreads + threadIdx.x;
+    const uint32_t m = blockIdx.z;
+    // (a frame has at most 2^26 tokens of 32 threads)
+    const uint32_t id = blockIdx.x * kThreads + threadIdx.x;
     const uint32_t n = id / a.units, unit = id - n * a.units;
     if (n >= a.N) return;
     const uint32_t y = n / static_cast<uint32_t>(p.W), x = n - y * static_cast<uint32_t>(p.W);
@@ -187,16 +186,17 @@ hipError_t launch_rotary(const RotaryParams &p, hipStream_t stream) {
     a.rot_units = p.halves ? p.pairs / 8 : (p.pairs + 3) / 4;
     a.units = p.halves ? a.rot_units + (p.head_dim - 2 * p.pairs) / 8 : p.head_dim / 8;
     const int64_t blocks = (N * a.units + kThreads - 1) / kThreads;
-    if (N * a.units > 0xffffffffLL || blocks * p.M > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    // (a launch has fewer than 2^32 threads along an axis: each frame is one step of the third)
+    if (N * a.units > 0x7fffffffLL + 1) return hipErrorInvalidConfiguration;
     a.N = static_cast<uint32_t>(N);
-    a.blocks = static_cast<uint32_t>(blocks);
     const int heads = p.heads[0] + p.heads[1];
     // a thread takes all heads of its token, or fewer where tokens do not fill the device
     const int64_t most = (heads + 3) / 4, want = kFill / (blocks * p.M) + 1;
     const int64_t groups = want < most ? want : most;
     a.heads_per_thread = static_cast<int32_t>((heads + groups - 1) / groups);
-    const dim3 grid(static_cast<uint32_t>(blocks * p.M),
-                    static_cast<uint32_t>((heads + a.heads_per_thread - 1) / a.heads_per_thread));
+    const dim3 grid(static_cast<uint32_t>(blocks),
+                    static_cast<uint32_t>((heads + a.heads_per_thread - 1) / a.heads_per_thread),
+                    static_cast<uint32_t>(p.M));
     if (p.dtype == RF_F32) return p.halves ? launch<float, true>(a, grid, stream) : launch<float, false>(a, grid, stream);
     return p.halves ? launch<uint16_t, true>(a, grid, stream) : launch<uint16_t, false>(a, grid, stream);
 }
