@@ -663,7 +663,8 @@ typedef struct rf_cross_layout {
  *   between the first and last element of q, k or v.
  * kv_lengths: device int32 [B], or NULL (Lk for all); read by the kernel, values
  *   outside [0, Lk] count as the nearer end. key_mask: device bytes [B][Lk], or NULL.
- * B, Lq, Lk, heads: >= 1, Lk <= 2^30, ceil(Lq / 32) * B * heads up to 2^24;
+ * B, Lq, Lk, heads: >= 1, Lk <= 2^30, ceil(Lq / 32) * B * heads up to 2^24 (and in
+ *   RF_F32 ceil(Lq * (heads / kv_heads) / 128) * B * kv_heads up to 2^24 - 64);
  *   heads a multiple of kv_heads. head_dim: 64 or 128.
  * dtype: RF_BF16 (products on the bf16 matrix cores, probabilities rounded to
  *   bf16 for the second one, fp32 softmax and sums, one rounding of the output) or

@@ -5,6 +5,7 @@
 #include <stdio.h>
 #include <string.h>
 
+#include "rf_cross_plan.h"
 #include "rf_internal.h"
 
 namespace {
@@ -1008,6 +1009,8 @@ static int cross_sizes(int32_t B, int32_t Lq, int32_t Lk, int32_t heads, int32_t
     if (Lk > (1 << 30)) return fail(RF_ERR_RANGE, "%s: Lk = %d exceeds 2^30", fn, Lk);
     if (static_cast<double>((static_cast<int64_t>(Lq) + 31) / 32) * B * heads > 16777216.0)
         return fail(RF_ERR_RANGE, "%s: more than 2^24 tiles of 32 queries", fn);
+    if (!rf::cross_whole_fits(B, static_cast<int64_t>(heads / kv_heads) * Lq, kv_heads, dtype))
+        return fail(RF_ERR_RANGE, "%s: more than 2^24 - 64 tiles of 128 queries in fp32", fn);
     return RF_OK;
 }
 

@@ -6,6 +6,7 @@
 // holds several heads where queries are few.
 #pragma once
 
+#include "rf_cross_plan.h"
 #include "rf_device.h"
 
 namespace rf {
@@ -80,10 +81,6 @@ __device__ __forceinline__ uint64_t key_bits(const CrossKArgs &a, int b, int32_t
 
 // An offset past every buffer resource: a load from it gives zero.
 constexpr int kNowhere = 0x7fffffff - 15;
-
-// Both types' tiles: rows of a workgroup where rows are many, and where they are few.
-constexpr int kCrossTileRows = 128;
-constexpr int kCrossFewRows = 32;
 
 hipError_t launch_cross_f32(const CrossKArgs &a, int32_t head_dim, bool few, uint32_t grid, hipStream_t stream);
 

@@ -295,13 +295,11 @@ __device__ __forceinline__ void load_offsets(int64_t stride, int i0, int lane, i
 // ---------------------------------------------------------------------------
 
 constexpr int kTileWaves = kCrossTileRows / 32;
-__host__ __device__ constexpr int tile_waves(int head_dim, bool mask) { return head_dim == 64 && !mask ? 3 : 2; }
-__host__ __device__ constexpr int tile_keys(int) { return 64; }
 
 template <int D, bool kMask>
-__global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu(tile_waves(D, kMask))))
+__global__ __launch_bounds__(64 * kTileWaves) __attribute__((amdgpu_waves_per_eu(cross_tile_waves(D, kMask))))
 void cross_tile_kernel(const CrossKArgs a) {
-    constexpr int kBc = tile_keys(D), kNB = kBc / 32, kTileBytes = kBc * Tile<D>::kRow;
+    constexpr int kBc = kCrossTileKeys, kNB = kBc / 32, kTileBytes = kBc * Tile<D>::kRow;
     constexpr int kN = kTileBytes / 1024 / kTileWaves;
     // [K, V][buffer]
     __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * kTileBytes];
@@ -470,13 +468,13 @@ void cross_tile_kernel(const CrossKArgs a) {
 // are merged through LDS, the parts' by the join kernel.
 // ---------------------------------------------------------------------------
 
-constexpr int kFewWaves = 8;
-__host__ __device__ constexpr int few_keys(int head_dim) { return head_dim == 64 ? 64 : 32; }
+constexpr int kFewWaves = cross_few_waves(64, RF_BF16);
+static_assert(kFewWaves == cross_few_waves(128, RF_BF16), "one for both");
 
 template <int D, bool kMask>
 __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(2)))
 void cross_few_kernel(const CrossKArgs a) {
-    constexpr int kBc = few_keys(D), kNB = kBc / 32, kTileBytes = kBc * Tile<D>::kRow, kN = kTileBytes / 1024;
+    constexpr int kBc = cross_few_keys(D), kNB = kBc / 32, kTileBytes = kBc * Tile<D>::kRow, kN = kTileBytes / 1024;
     __shared__ __attribute__((aligned(1024))) uint8_t ks[kFewWaves * kTileBytes];
     __shared__ __attribute__((aligned(1024))) uint8_t vs[kFewWaves * kTileBytes];
     __shared__ float ml[kFewWaves][kCrossFewRows][2];
@@ -600,12 +598,10 @@ void cross_few_kernel(const CrossKArgs a) {
 // known; its sums meet in LDS in a fixed order.
 // ---------------------------------------------------------------------------
 
-constexpr int kMaxParts = 64;
-
 template <int D, typename E>
 __global__ __launch_bounds__(256) void cross_join_kernel(const CrossKArgs a) {
-    constexpr int kCols = D / 4, kGroups = 256 / kCols, kEach = (kMaxParts + kGroups - 1) / kGroups;
-    __shared__ float ml[kMaxParts][2];
+    constexpr int kCols = D / 4, kGroups = 256 / kCols, kEach = (kCrossMaxParts + kGroups - 1) / kGroups;
+    __shared__ float ml[kCrossMaxParts][2];
     __shared__ __attribute__((aligned(16))) float sums[kGroups][D];
     const CrossTile t = cross_tile_at<kCrossFewRows>(a, blockIdx.x / kCrossFewRows);
     const int r = blockIdx.x % kCrossFewRows, tid = threadIdx.x;
@@ -653,63 +649,6 @@ __global__ __launch_bounds__(256) void cross_join_kernel(const CrossKArgs a) {
     E *op = static_cast<E *>(a.out) + row_offset(a, a.os, t, t.row0 + r) + 2 * tid;
     if constexpr (sizeof(E) == 4) *reinterpret_cast<f32x2_t *>(op) = f32x2_t{v[0] * inv, v[1] * inv};
     else *reinterpret_cast<uint32_t *>(op) = pack_bf16x2(v[0] * inv, v[1] * inv);
-}
-
-// How a launch is cut: tiles of 128 rows, or of 32 with the keys shared out and
-// `parts` workgroups to a tile.
-//
-// The choice goes by the forms' times in us, counted in rounds of the device: a round
-// has a fixed part and the tiles of keys that a workgroup (of the few-row form: its
-// busiest wave) walks; a split has the join. Tiles of keys cost more where more
-// workgroups share a compute unit, and a round that few of them share counts for as
-// much less. Counts and measured times, us (tile / few):
-//   1,560 x 512 keys, 12 heads x 128: 14 / 25     9,360 x 77, 12 x 128: 21 / 66
-//   2 x 500 x 1,000, 8 x 128: 22 / 12             300 x 5,000, 8 x 128: 83 / 20 (3 parts)
-//   128 x 20,000, 8 x 64: 224 / 21 (8 parts)      3 x 1,581 x 334, 5 x 64: 10 / 17
-// and in fp32 1,560 x 512, 12 x 128: 76 / 72; 512 x 512, 12 x 64: 41 / 15;
-// 4,680 x 512, 12 x 128: 140 / 166; 6,400 x 512, 12 x 64: 114 / 137.
-struct CrossPlan {
-    bool few;
-    int32_t parts;
-    int64_t tiles;
-};
-
-struct CrossCost {
-    double tile[3];            // a tile of keys with one, two, three workgroups to a compute unit
-    double few;                // a wave's tile of keys in the few-row form
-    int32_t keys, few_keys;    // keys of a tile
-    int32_t few_waves;
-};
-constexpr double kRound = 4.0, kFewRound = 4.5, kJoin = 4.0;
-
-CrossPlan cross_plan(int32_t B, int64_t rows, int32_t kv_heads, int32_t Lk, int32_t head_dim, int32_t dtype,
-                     bool mask, bool may_split, int32_t cus) {
-    static const CrossCost costs[2][2] = {
-        {{{0.7, 1.06, 1.44}, 1.9, tile_keys(64), few_keys(64), kFewWaves},
-         {{1.0, 1.9, 1.9}, 1.9, tile_keys(128), few_keys(128), kFewWaves}},
-        {{{2.4, 4.8, 4.8}, 4.5, 32, 32, 8}, {{4.5, 9.0, 9.0}, 4.9, 32, 32, 4}}};
-    const CrossCost &c = costs[dtype == RF_F32][head_dim == 128];
-    auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
-    const int64_t heads = static_cast<int64_t>(B) * kv_heads;
-    const int64_t whole = up(rows, kCrossTileRows) * heads, few = up(rows, kCrossFewRows) * heads;
-    const int64_t most = dtype == RF_F32 ? 2 : tile_waves(head_dim, mask);   // workgroups to a compute unit
-    const int64_t share = up(whole, cus) < most ? up(whole, cus) : most;
-    const double t_whole = static_cast<double>(up(whole, cus)) / static_cast<double>(share) *
-                           (kRound + static_cast<double>(up(Lk, c.keys)) * c.tile[share - 1]);
-    CrossPlan p{false, 1, whole};
-    double best = 0.95 * t_whole;   // (the few-row form reads keys four times as often)
-    const int64_t key_tiles = up(Lk, c.few_keys);
-    for (int64_t parts = 1; parts <= kMaxParts; ++parts) {
-        if (parts > 1 && (!may_split || parts * c.few_waves > key_tiles || few * (parts - 1) >= 2 * cus)) break;
-        const double t = static_cast<double>(up(few * parts, cus)) *
-                             (kFewRound + static_cast<double>(up(key_tiles, parts * c.few_waves)) * c.few) +
-                         (parts > 1 ? kJoin : 0.0);
-        if (t < best) {
-            best = t;
-            p = CrossPlan{true, static_cast<int32_t>(parts), few};
-        }
-    }
-    return p;
 }
 
 }  // namespace
@@ -760,7 +699,7 @@ hipError_t launch_cross(const CrossParams &p, hipStream_t stream) {
     int64_t grid = static_cast<int64_t>(a.per_xcd) * xcds * c.parts;
     if (!c.few && p.dtype == RF_BF16) {
         // as many walkers as are resident, or one to a tile, in whole XCDs
-        const int64_t resident = tile_waves(p.head_dim, p.key_mask != nullptr) * static_cast<int64_t>(p.geo.cus);
+        const int64_t resident = cross_tile_waves(p.head_dim, p.key_mask != nullptr) * static_cast<int64_t>(p.geo.cus);
         const int64_t want = a.tiles < resident ? a.tiles : resident;
         grid = (want + xcds - 1) / xcds * xcds;
         a.walkers = static_cast<int32_t>(grid);

@@ -215,7 +215,7 @@ void cross_f32_tile_kernel(const CrossKArgs a) {
 }
 
 // Few rows: 32 rows, the keys of a part shared out among the waves, merged through LDS.
-template <int D> constexpr int kWaves = D == 128 ? 4 : 8;
+template <int D> constexpr int kWaves = cross_few_waves(D, RF_F32);
 
 template <int D, bool kMask>
 __global__ __launch_bounds__(64 * kWaves<D>) __attribute__((amdgpu_waves_per_eu(kWaves<D> / 4)))
