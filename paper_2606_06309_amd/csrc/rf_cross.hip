@@ -184,10 +184,11 @@ constexpr float kFarReference = 4096.0f;
 
 // Scores of keys that are not valid become -inf. `bits`: the tile's valid keys.
 template <int kNB>
-__device__ __forceinline__ void mask_scores(f32x16_t (&s)[kNB], const uint64_t (&bits)[2], int grp) {
+__device__ __forceinline__ void mask_scores(f32x16_t (&s)[kNB], uint64_t bits, int grp) {
+    static_assert(kNB <= 2, "a tile's keys fit a word");
 #pragma unroll
     for (int b = 0; b < kNB; ++b) {
-        const uint32_t word = static_cast<uint32_t>(bits[b / 2] >> (32 * (b % 2)));
+        const uint32_t word = static_cast<uint32_t>(bits >> (32 * b));
         const uint32_t mine = word >> (4 * grp);   // accumulator r holds key (r/4)*8 + grp*4 + r%4
 #pragma unroll
         for (int r = 0; r < 16; ++r)
@@ -256,7 +257,7 @@ __device__ __forceinline__ void softmax(Wave<D> &w, f32x16_t (&s)[kNB], float sl
 // tile's first key; `left`: the sequence's keys from there on, at which the resource ends.
 // bits: the valid keys, taken for masked launches only.
 template <int D, bool kMask, int kBc, int kN>
-__device__ __forceinline__ void issue(const uint16_t *key, int64_t stride, int32_t left, const uint64_t (&bits)[2],
+__device__ __forceinline__ void issue(const uint16_t *key, int64_t stride, int32_t left, uint64_t bits,
                                       uint8_t *dst, int i0, const int (&go)[kN], int lane) {
     // (a tile spans less than 2^31 bytes)
     const int32_t rec = __builtin_amdgcn_readfirstlane(
@@ -267,8 +268,7 @@ __device__ __forceinline__ void issue(const uint16_t *key, int64_t stride, int32
         int at = go[i];
         if constexpr (kMask) {
             const int k = (i0 + i) * Tile<D>::kRowsPerLoad + lane / Tile<D>::kSlots;
-            const uint64_t word = k < 64 ? bits[0] : bits[1];
-            if (!((word >> (k & 63)) & 1)) at = kNowhere;
+            if (!((bits >> k) & 1)) at = kNowhere;
         }
         load_lds16(r, (lds_void_t *)(dst + (i0 + i) * 1024), at);
     }
@@ -327,7 +327,7 @@ void cross_tile_kernel(const CrossKArgs a) {
     struct Keys {
         const uint16_t *k, *v;
         int32_t key, left;
-        uint64_t bits[2];   // masked launches: the tile's valid keys
+        uint64_t bits;   // masked launches: the tile's valid keys
     };
     auto keys_of = [&](const CrossTile &t, int32_t given) {
         Keys r;
@@ -338,10 +338,7 @@ void cross_tile_kernel(const CrossKArgs a) {
         return r;
     };
     auto load = [&](Keys &s, const CrossTile &t, int buf) {
-        if constexpr (kMask) {
-            s.bits[0] = key_bits(a, t.b, s.key, s.key + s.left, lane);
-            s.bits[1] = kBc == 128 ? key_bits(a, t.b, s.key + 64, s.key + s.left, lane) : 0;
-        }
+        if constexpr (kMask) s.bits = key_bits(a, t.b, s.key, s.key + s.left, lane);
         uint8_t *kd = lds + buf * kTileBytes, *vd = lds + (2 + buf) * kTileBytes;
         issue<D, kMask, kBc, kN>(s.k, a.ks[1], s.left, s.bits, kd, wave * kN, kgo, lane);
         issue<D, kMask, kBc, kN>(s.v, a.vs[1], s.left, s.bits, vd, wave * kN, vgo, lane);
@@ -372,7 +369,7 @@ void cross_tile_kernel(const CrossKArgs a) {
             next.key += kBc;
             next.left -= kBc;
             load(next, t, buf ^ 1);
-            if (!kMask || first || (cur.bits[0] | cur.bits[1]) != 0) {
+            if (!kMask || first || cur.bits != 0) {
                 f32x16_t s[kNB];
                 scores<D, kNB>(lds + buf * kTileBytes, f, w.qf, s);
                 if constexpr (kMask) mask_scores<kNB>(s, cur.bits, grp);
@@ -399,10 +396,7 @@ void cross_tile_kernel(const CrossKArgs a) {
             f32x16_t s[kNB];
             scores<D, kNB>(lds + buf * kTileBytes, f, w.qf, s);
             turn();
-            if constexpr (!kMask) {
-                cur.bits[0] = cur.left >= 64 ? ~0ull : (1ull << cur.left) - 1;
-                cur.bits[1] = cur.left >= 128 ? ~0ull : cur.left <= 64 ? 0ull : (1ull << (cur.left - 64)) - 1;
-            }
+            if constexpr (!kMask) cur.bits = cur.left >= kBc ? ~0ull : (1ull << cur.left) - 1;
             if (kMask || cur.left < kBc) mask_scores<kNB>(s, cur.bits, grp);
             u32x4_t pw[2 * kNB];
             softmax<D, kNB>(w, s, a.scale_log2, first, pw);
@@ -494,20 +488,19 @@ void cross_few_kernel(const CrossKArgs a) {
     const Fragments<D> f(lane);
     const int64_t tiles = (static_cast<int64_t>(n) + kBc - 1) / kBc;
     const int64_t first = part * kFewWaves + wave, step = static_cast<int64_t>(a.parts) * kFewWaves;
-    uint64_t cur[2], nxt[2];
-    auto tile_bits = [&](int32_t key0, uint64_t (&bits)[2]) {
-        if constexpr (kMask) bits[0] = key_bits(a, t.b, key0, n, lane);
-        else bits[0] = n - key0 >= 64 ? ~0ull : (1ull << (n - key0)) - 1;
-        bits[1] = 0;
+    uint64_t cur = 0, nxt;
+    auto tile_bits = [&](int32_t key0) -> uint64_t {
+        if constexpr (kMask) return key_bits(a, t.b, key0, n, lane);
+        else return n - key0 >= 64 ? ~0ull : (1ull << (n - key0)) - 1;
     };
-    auto load = [&](bool key, int32_t key0, const uint64_t (&bits)[2]) {
+    auto load = [&](bool key, int32_t key0, uint64_t bits) {
         if (key) issue<D, kMask, kBc, kN>(kh + key0 * a.ks[1], a.ks[1], n - key0, bits, kb, 0, kgo, lane);
         else issue<D, kMask, kBc, kN>(vh + key0 * a.vs[1], a.vs[1], n - key0, bits, vb, 0, vgo, lane);
     };
     Wave<D> w;
     if (first < tiles) {
         const int32_t key0 = static_cast<int32_t>(first) * kBc;
-        tile_bits(key0, cur);
+        cur = tile_bits(key0);
         load(true, key0, cur);
         load(false, key0, cur);
     }
@@ -520,7 +513,7 @@ void cross_few_kernel(const CrossKArgs a) {
             // path the waits below can be counted)
             const int64_t next = i + step < tiles ? i + step : i;
             const int32_t key0 = static_cast<int32_t>(next) * kBc;
-            tile_bits(key0, nxt);
+            nxt = tile_bits(key0);
             wait_loads<kN>();       // K is there; V may still be in flight
             f32x16_t s[kNB];
             scores<D, kNB>(kb, f, w.qf, s);
@@ -533,7 +526,7 @@ void cross_few_kernel(const CrossKArgs a) {
             values<D, kNB>(vb, f, pw, w.o);
             wait_lds_reads();
             load(false, key0, nxt);
-            cur[0] = nxt[0];
+            cur = nxt;
         }
         wait_loads<0>();   // nothing lands in the buffers any more
     }
