@@ -12,8 +12,8 @@
 // of y and runs of four features.
 //
 //  * linear_tile_kernel: a workgroup owns kBM rows x kBN features, 8 or 4 waves of
-//    32 kRB x 64: 256 x 256, 128 x 128 and 64 x 128, and 32 x 256 and (bf16) 64 x 256
-//    where rows are few and W large. Steps go from memory straight into LDS,
+//    32 kRB x 64: (bf16) 256 x 256, 128 x 128 and 64 x 128, and 32 x 256 and (bf16) 64 x
+//    256 where rows are few and W large. Steps go from memory straight into LDS,
 //    double-buffered, one barrier a step. Rows of 128 bytes are stored without
 //    padding, their eight 16-byte slots permuted by (row / 2) % 8, so the 16 lanes of
 //    a read pass meet 16 different slots of the 256-byte bank window.
@@ -48,7 +48,7 @@ typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
-constexpr int kStep = 128;   // bytes of a row that a step takes
+constexpr int kStep = kLinearStep;
 
 struct LinearKArgs {
     const uint8_t *x, *w;
@@ -566,7 +566,7 @@ void linear_tile_kernel(const LinearKArgs a) {
     }
 }
 
-constexpr int kFewWaves = 8;
+constexpr int kFewWaves = kLinearFewWaves;
 
 // kR blocks of 16 rows, kF blocks of 16 features. The reduction goes in pieces of 64
 // bytes (16 bytes a lane, four lanes to a row). The waves of a part take two at a time
@@ -709,116 +709,6 @@ __global__ __launch_bounds__(256) void linear_join_kernel(const LinearKArgs a) {
     fin.store(a, c, v);
 }
 
-enum LinearForm { kFew16, kFew32, kFew64, kStream32, kStream64, kTile64, kTile128, kTile256 };
-struct LinearPlan {
-    LinearForm form;
-    int64_t row_tiles, col_tiles;
-    int32_t steps, per_part, parts;
-};
-
-// far: rows of a tile may lie 2 GB apart (only the smaller tile's kernel takes them).
-LinearPlan linear_plan(int64_t rows, int32_t K, int32_t n_out, int32_t dtype, int32_t cus, bool far, bool may_split) {
-    LinearPlan p{};
-    const int64_t bytes = static_cast<int64_t>(K) * (dtype == RF_F32 ? 4 : 2);
-    auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
-    if (rows <= 64 && !far) {
-        // Straight to registers, through LDS in tiles of 256 features, or (33 rows on) as
-        // products of more rows: by the bytes of W from which the latter are faster. us of a
-        // product, registers / LDS, bf16: 16 rows x 4,096 x 4,096 10.6 / 11.5, 8 x 5,120 x 5,120
-        // 19.2 / 16.2, 16 x 20,480 x 5,120 73 / 41; 17 x 1,536 x 1,536 8.3 / 8.3, 17 x 1,536 x
-        // 6,144 12.3 / 9.7; fp32: 16 x 4,096 x 4,096 18.5 / 18.8, 8 x 5,120 x 5,120 33 / 29, 17 x
-        // 1,536 x 6,144 24.7 / 14.8. Registers / tiles of 64 x 128, bf16: 64 x 1,536 x 1,024 9.3 /
-        // 10.0, 64 x 1,536 x 1,536 11.4 / 10.9; fp32: 64 x 1,024 x 1,536 11.1 / 14.4, 64 x 1,536 x
-        // 1,536 - / 15.7. LDS, 256 features / tiles of 64 x 128, 64 rows: 1,536 x 1,536 13.2 / 10.9,
-        // 4,096 x 4,096 18.5 / 16.2, 10,240 x 5,120 36 / 29, 20,480 x 5,120 61 / 73; 24 rows: 1,536 x
-        // 6,144 12.5 / 12.0, in fp32 17 / 21.
-        const double w_mb = static_cast<double>(n_out) * static_cast<double>(bytes) * 1e-6;
-        const bool few = w_mb < (dtype == RF_F32 ? 2 : 1) * (rows <= 16 ? 40 : rows <= 32 ? 8 : 4);
-        const bool stream = !few && (rows <= 32 || (dtype == RF_BF16 && w_mb >= 150));
-        if (stream) {
-            p.form = rows <= 32 ? kStream32 : kStream64;
-            p.row_tiles = 1;
-            p.col_tiles = up(n_out, 256);
-            p.steps = static_cast<int32_t>(up(bytes, kStep));
-            // two workgroups to a compute unit, of six steps at least
-            const int64_t want = 2 * cus / p.col_tiles, most = p.steps / 6;
-            p.parts = static_cast<int32_t>(!may_split ? 1 : want < most ? want : most);
-            if (p.parts < 1) p.parts = 1;
-            p.per_part = static_cast<int32_t>(up(p.steps, p.parts));
-            p.parts = static_cast<int32_t>(up(p.steps, p.per_part));
-            return p;
-        }
-        if (few) {
-            p.form = rows <= 16 ? kFew16 : rows <= 32 ? kFew32 : kFew64;
-            p.row_tiles = 1;
-            p.col_tiles = up(n_out, rows > 16 && rows <= 32 ? 32 : 16);
-            p.steps = static_cast<int32_t>(up(bytes, 64));
-            // a wave takes four pieces at least; two workgroups to a compute unit
-            const int64_t want = up(2 * cus, p.col_tiles), most = up(p.steps, 4 * kFewWaves);
-            p.parts = static_cast<int32_t>(!may_split || p.col_tiles >= cus ? 1 : want < most ? want : most);
-            p.per_part = static_cast<int32_t>(up(up(p.steps, p.parts), 4) * 4);
-            p.parts = static_cast<int32_t>(up(p.steps, p.per_part));
-            return p;
-        }
-    }
-    // Tiles of 64 x 128, 128 x 128 or 256 x 256 (rows x features) and parts of the reduction,
-    // by the time in us that they come to, counted in rounds of the device: a round has a
-    // fixed part and its steps, which take the longer the more workgroups share a compute
-    // unit; a split adds the second kernel and its parts, written and read again. The
-    // counts are fitted to products of 70 to 21,600 rows, 8 to 20,480 inputs and 256 to
-    // 6,144 features, whose weights come from beyond the L2s, as from one layer to the
-    // next: a workgroup alone on a compute unit then takes 0.53 us for a step of the
-    // smallest tile where it takes 0.38 with the weights at hand. (Unsplit / split so: 512 x
-    // 1,536 x 1,536 18.6 / 16.0, 1,000 x 6,144 x 1,536 58 / 35, 2,000 x 6,144 x 1,536 72 / 54;
-    // fp32 1,500 x 4,096 x 320 84 / 53.) us, 64 x 128 / 128 x 128 / 256 x 256 (* split), bf16, weights
-    // at hand: 512 x 1,536 x 1,536 11.6 / 17.5 / 41; 500 x 8,960 x 1,536 29.5* / 29.8* / 36*; 3,600 x 1,536 x 1,536 27 / 26 /
-    // 41; 9,360 x 1,536 x 1,536 64 / 53 / 47; fp32: 512 x 1,536 x 1,536 31* / 41* / 74*; 7,800 x
-    // 1,536 x 1,536 279 / 353 / 363; 9,360 x 1,536 x 6,144 - / 1,247 / 1,438.
-    struct Form {
-        LinearForm form;
-        int64_t rows, cols;
-        int32_t most;        // workgroups to a compute unit
-        double round;
-        double step[3];      // with one, two, three workgroups to a compute unit
-    };
-    static const Form forms[2][3] = {{{kTile64, 64, 128, 3, 3.0, {0.53, 0.68, 1.0}},
-                                      {kTile128, 128, 128, 2, 4.0, {0.80, 0.95, 0.95}},
-                                      {kTile256, 256, 256, 1, 8.0, {1.55, 1.55, 1.55}}},
-                                     {{kTile64, 64, 128, 3, 3.0, {1.1, 1.95, 2.93}},
-                                      {kTile128, 128, 128, 2, 4.0, {2.4, 3.65, 3.65}},
-                                      {kTile256, 256, 256, 1, 8.0, {7.4, 7.4, 7.4}}}};
-    constexpr int64_t kLeastSteps = 4, kMostParts = 16;
-    constexpr double kJoin = 3.0;
-    const double join_mb = dtype == RF_F32 ? 0.6 : 0.45;
-    p.steps = static_cast<int32_t>(up(bytes, kStep));
-    double best = 0.0;
-    for (const Form &f : forms[dtype == RF_F32]) {
-        if (far && f.form != kTile128) continue;
-        const int64_t row_tiles = up(rows, f.rows), col_tiles = up(n_out, f.cols);
-        for (int64_t parts = 1; parts <= kMostParts; ++parts) {
-            if (parts > 1 && (!may_split || p.steps / parts < kLeastSteps)) break;
-            const int64_t per = up(p.steps, parts), tiles = row_tiles * col_tiles * parts;
-            if (parts > 1 && up(p.steps, per) != parts) continue;
-            const int64_t share = up(tiles, cus) < f.most ? up(tiles, cus) : f.most;
-            const double full = static_cast<double>(tiles) / static_cast<double>(cus * share);
-            // (workgroups of the smallest tile follow each other closely enough to fill a broken round)
-            const double rounds = f.form == kTile64 ? (full > 0.8 ? full + 0.2 : 1.0) : ceil(full);
-            double t = rounds * (f.round + static_cast<double>(per) * f.step[share - 1]);
-            if (parts > 1)
-                t += kJoin + join_mb * 4e-6 * static_cast<double>(parts) * static_cast<double>(rows) * n_out;
-            if (best == 0.0 || t < best) {
-                best = t;
-                p.form = f.form;
-                p.row_tiles = row_tiles;
-                p.col_tiles = col_tiles;
-                p.parts = static_cast<int32_t>(parts);
-                p.per_part = static_cast<int32_t>(per);
-            }
-        }
-    }
-    return p;
-}
-
 template <typename E>
 void run(const LinearPlan &p, const LinearKArgs &a, bool far, dim3 grid, hipStream_t stream) {
     switch (p.form) {
@@ -835,7 +725,11 @@ void run(const LinearPlan &p, const LinearKArgs &a, bool far, dim3 grid, hipStre
             if (far) hipLaunchKernelGGL((linear_tile_kernel<E, 2, 2, 2, true>), grid, dim3(256), 0, stream, a);
             else hipLaunchKernelGGL((linear_tile_kernel<E, 2, 2, 2, false>), grid, dim3(256), 0, stream, a);
             break;
-        case kTile256: hipLaunchKernelGGL((linear_tile_kernel<E, 4, 2, 4, false>), grid, dim3(512), 0, stream, a); break;
+        case kTile256:    // (bf16 only)
+            if constexpr (sizeof(E) == 2)
+                hipLaunchKernelGGL((linear_tile_kernel<E, 4, 2, 4, false>), grid, dim3(512), 0, stream, a);
+            break;
+        case kLinearForms: break;
     }
 }
 

@@ -1,5 +1,6 @@
 /* Host rules of the frame matrix product's launch against plain walks over rows. Prints "ok <checks>"; exits 1 at the
    first mismatch. */
+#include <cmath>
 #include <cstdio>
 #include <random>
 #include <vector>
@@ -71,8 +72,38 @@ static int frames_that_meet() {
     return 0;
 }
 
+// A plan covers its product, and every form is some product's best in each type that has it.
+static int forms_in_use() {
+    std::mt19937_64 rng(3);
+    auto upto = [&](double most) { return static_cast<int64_t>(std::exp(std::uniform_real_distribution<>(0, std::log(most))(rng))); };
+    int64_t seen[2][2][rf::kLinearForms] = {};
+    for (int i = 0; i < 200000; ++i) {
+        const int dtype = i & 1 ? RF_F32 : RF_BF16;
+        const int64_t rows = i % 3 ? upto(100000) : upto(64), K = 8 * upto(4000), n = 8 * upto(4000);
+        const bool far = i % 5 == 0, ws = i % 4 != 0;
+        const rf::LinearPlan p = rf::linear_plan(rows, static_cast<int32_t>(K), static_cast<int32_t>(n), dtype, 256, far, ws);
+        CHECK(p.form >= 0 && p.form < rf::kLinearForms);
+        CHECK(!far || p.form == rf::kTile128);
+        CHECK(dtype == RF_BF16 || (p.form != rf::kStream64 && p.form != rf::kTile256));
+        const int64_t tile_rows[] = {16, 32, 64, 32, 64, 64, 128, 256}, tile_cols[] = {16, 32, 16, 256, 256, 128, 128, 256};
+        CHECK(p.row_tiles == (rows + tile_rows[p.form] - 1) / tile_rows[p.form]);
+        CHECK(p.col_tiles == (n + tile_cols[p.form] - 1) / tile_cols[p.form]);
+        const int64_t step = p.form <= rf::kFew64 ? 64 : rf::kLinearStep, bytes = K * (dtype == RF_F32 ? 4 : 2);
+        CHECK(p.steps == (bytes + step - 1) / step);
+        CHECK(p.parts >= 1 && (ws || p.parts == 1));
+        // every part has a step, and the last one ends the reduction
+        CHECK(static_cast<int64_t>(p.parts) * p.per_part >= p.steps && static_cast<int64_t>(p.parts - 1) * p.per_part < p.steps);
+        ++seen[dtype][p.parts > 1][p.form];
+    }
+    for (int form = 0; form < rf::kLinearForms; ++form) {
+        CHECK(seen[RF_BF16][0][form] + seen[RF_BF16][1][form] > 0);
+        if (form != rf::kStream64 && form != rf::kTile256) CHECK(seen[RF_F32][0][form] + seen[RF_F32][1][form] > 0);
+    }
+    return 0;
+}
+
 int main() {
-    if (frames_that_meet()) return 1;
+    if (frames_that_meet() || forms_in_use()) return 1;
     std::printf("ok %d\n", checks);
     return 0;
 }
