@@ -719,7 +719,8 @@ int rf_cross_attention_workspace(int32_t B, int32_t Lq, int32_t Lk, int32_t head
  *   activation, gate and residual in fp32, one rounding at the end) or RF_F32
  *   (fp32 throughout).
  * in_features, out_features: rows of a multiple of 16 bytes. rows_per_frame >= 1,
- *   M * rows_per_frame < 2^31.
+ *   M * rows_per_frame < 2^31, ceil(M * rows_per_frame / 128) * ceil(out_features / 128)
+ *   up to 2^24 - 64.
  * workspace: NULL, or device scratch, 16-byte aligned, of at least
  *   rf_frame_linear_workspace bytes, overlapping no tensor of the call: products
  *   of few output tiles then split in_features over workgroups, whose parts a second

@@ -7,6 +7,7 @@
 
 #include "rf_cross_plan.h"
 #include "rf_internal.h"
+#include "rf_linear_plan.h"
 
 namespace {
 
@@ -1226,6 +1227,8 @@ int rf_frame_linear(const void *x, const void *weight, const void *bias, const v
             if (hit) return fail(RF_ERR_INVALID_ARG, "%s: workspace overlaps a tensor", fn);
         }
     }
+    if (!rf::linear_whole_fits(M * rows_per_frame, out_features))
+        return fail(RF_ERR_RANGE, "%s: more than 2^24 - 64 tiles of 128 rows and 128 features", fn);
     rf::LinearParams p{};
     rc = query_geometry(&p.geo, fn);
     if (rc != RF_OK) return rc;

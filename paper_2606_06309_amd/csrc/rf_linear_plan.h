@@ -41,6 +41,15 @@ struct LinearPlan {
     int32_t steps, per_part, parts;
 };
 
+// A launch of this many workgroups (a multiple of the XCDs, 64 at most, of them) has fewer than 2^32
+// threads.
+inline bool linear_fits(int64_t groups, int64_t threads) { return (groups + 63) * threads <= 0xffffffffLL; }
+
+// Whether tiles of 128 x 128, the form that every product may take, can be launched.
+inline bool linear_whole_fits(int64_t rows, int64_t n_out) {
+    return linear_fits(((rows + 127) / 128) * ((n_out + 127) / 128), 256);
+}
+
 // far: rows of a tile may lie 2 GB apart (only the smaller tile's kernel takes them).
 inline LinearPlan linear_plan(int64_t rows, int32_t K, int32_t n_out, int32_t dtype, int32_t cus, bool far, bool may_split) {
     LinearPlan p{};
@@ -126,6 +135,7 @@ inline LinearPlan linear_plan(int64_t rows, int32_t K, int32_t n_out, int32_t dt
             if (parts > 1 && (!may_split || p.steps / parts < kLeastSteps)) break;
             const int64_t per = up(p.steps, parts), tiles = row_tiles * col_tiles * parts;
             if (parts > 1 && up(p.steps, per) != parts) continue;
+            if (!linear_fits(tiles, f.form == kTile256 ? 512 : 256)) break;
             const int64_t share = up(tiles, cus) < f.most ? up(tiles, cus) : f.most;
             const double full = static_cast<double>(tiles) / static_cast<double>(cus * share);
             // (workgroups of the smallest tile follow each other closely enough to fill a broken round)

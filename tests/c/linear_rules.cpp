@@ -102,8 +102,33 @@ static int forms_in_use() {
     return 0;
 }
 
+// What is not refused can be launched: threads of the launch, and of the join's, below 2^32.
+static int launches_fit() {
+    std::mt19937_64 rng(5);
+    auto upto = [&](double most) { return static_cast<int64_t>(std::exp(std::uniform_real_distribution<>(0, std::log(most))(rng))); };
+    int near = 0, refused = 0;
+    for (int i = 0; i < 300000; ++i) {
+        const int dtype = i & 1 ? RF_F32 : RF_BF16;
+        const int64_t rows = i % 3 ? 1 + static_cast<int64_t>(rng() % 2147483647) : upto(2147483647.0);
+        const int64_t K = 8 * upto(200000), n = i % 4 ? 8 * upto(16) : 8 * upto(268435455);
+        const int cus = i % 5 ? 256 : 1 + static_cast<int>(upto(RF_MAX_COMPUTE_UNITS - 1)), xcds = i % 7 ? 8 : 1 + static_cast<int>(rng() % 64);
+        if (!rf::linear_whole_fits(rows, n)) {
+            ++refused;
+            continue;
+        }
+        const rf::LinearPlan p = rf::linear_plan(rows, static_cast<int32_t>(K), static_cast<int32_t>(n), dtype, cus, i % 11 == 0, i % 2);
+        const int64_t tiles = p.row_tiles * p.col_tiles, rounded = p.form <= rf::kFew64 ? tiles : (tiles + xcds - 1) / xcds * xcds;
+        const int64_t threads = rounded * p.parts * (p.form <= rf::kFew64 || p.form == rf::kTile256 ? 512 : 256);
+        CHECK(tiles > 0 && threads <= 0xffffffffLL);
+        CHECK(p.parts == 1 || (rows * (n / 4) + 255) / 256 * 256 <= 0xffffffffLL);
+        near += threads > (1LL << 30);
+    }
+    CHECK(near > 100 && refused > 100);
+    return 0;
+}
+
 int main() {
-    if (frames_that_meet() || forms_in_use()) return 1;
+    if (frames_that_meet() || forms_in_use() || launches_fit()) return 1;
     std::printf("ok %d\n", checks);
     return 0;
 }
