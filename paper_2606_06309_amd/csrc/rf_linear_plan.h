@@ -15,11 +15,12 @@ constexpr int kLinearFewWaves = 8;
 
 // Rows of x that lie between two rows of one tile besides those that the product has there: where
 // rows are read at full positions, those of the frames that are not listed. Frames j < i of the list
-// meet in a tile when the frames between them and a row of each fit into it, so neighbours always may.
+// meet in a tile when the last row of one and the first of the other do (each tile of every form lies
+// in one of the largest), so neighbours may unless it divides their rows.
 inline int64_t linear_gap(const RowFrames &f, int32_t M, int64_t N) {
     int64_t widest = 0;
     for (int32_t i = 1, j = 0; i < M; ++i) {
-        while ((i - j - 1) * N + 2 > kLinearTileRows) ++j;
+        while (((j + 1) * N - 1) / kLinearTileRows < i * N / kLinearTileRows) ++j;   // (ends at j = i)
         const int64_t gap = (f.in(i) - f.in(j) - (i - j)) * N;
         widest = gap > widest ? gap : widest;
     }
@@ -27,7 +28,8 @@ inline int64_t linear_gap(const RowFrames &f, int32_t M, int64_t N) {
 }
 
 // Rows of x in one tile may lie 2 GB apart: their offsets from the tile's first row then do not fit
-// the 31 bits of a buffer resource's range.
+// the 31 bits of a buffer resource's range, and only the 128 x 128 form has 64-bit ones (two frames of
+// 3,600 rows x 20,480 x 5,120 bf16, 2.8 GB apart: 1,840 us, where the same rows side by side take 1,480).
 inline bool linear_far(const RowFrames &f, int32_t M, int64_t N, int64_t row_bytes) {
     return static_cast<double>(linear_gap(f, M, N) + kLinearTileRows + 1) * static_cast<double>(row_bytes) >= 2147483647.0;
 }

@@ -21,17 +21,16 @@ static rf::RowFrames list(const std::vector<int> &ids, bool full) {
     return f;
 }
 
-// The widest distance in x, in rows, of two rows that any 256 consecutive rows of the product hold: the
-// first and the last of them, as positions grow. (All that matter of a frame are 256 rows at either end.)
+// The widest distance in x, in rows, of two rows that a tile of 256 rows of the product holds: its
+// first and last one, as positions grow.
 static int64_t widest(const std::vector<int> &ids, int64_t N, bool full) {
     const int64_t rows = static_cast<int64_t>(ids.size()) * N;
     auto at = [&](int64_t r) { return full ? ids[r / N] * N + r % N : r; };
     int64_t most = 0;
-    for (int64_t m = 0; m < static_cast<int64_t>(ids.size()); ++m)
-        for (int64_t n = N > 600 ? N - 300 : 0; n < N; ++n) {
-            const int64_t r = m * N + n, last = r + 255 < rows ? r + 255 : rows - 1;
-            most = at(last) - at(r) > most ? at(last) - at(r) : most;
-        }
+    for (int64_t r = 0; r < rows; r += 256) {
+        const int64_t last = r + 255 < rows ? r + 255 : rows - 1;
+        most = at(last) - at(r) > most ? at(last) - at(r) : most;
+    }
     return most;
 }
 
@@ -52,7 +51,7 @@ static int meeting(const std::vector<int> &ids, int64_t N) {
 }
 
 static int frames_that_meet() {
-    const int64_t sizes[] = {1, 2, 37, 84, 85, 86, 127, 128, 129, 200, 253, 254, 255, 256, 257, 300, 511, 1560, 3600};
+    const int64_t sizes[] = {1, 2, 37, 84, 85, 86, 127, 128, 129, 200, 253, 254, 255, 256, 257, 300, 511, 512, 1024, 1560, 3600};
     std::mt19937 rng(7);
     for (const int64_t N : sizes) {
         for (const std::vector<int> &ids : {std::vector<int>{0}, {255}, {0, 1}, {0, 255}, {0, 20}, {0, 1, 255}, {0, 254, 255},
@@ -69,6 +68,8 @@ static int frames_that_meet() {
     // keyframes of a 720p video and a wide feed-forward's rows: 3,600 rows of 40,960 bytes, 19 frames apart
     CHECK(rf::linear_far(list({0, 20}, true), 2, 3600, 40960));
     CHECK(!rf::linear_far(list({0, 20}, false), 2, 3600, 40960));
+    // frames of whole tiles never meet in one
+    CHECK(!rf::linear_far(list({0, 20}, true), 2, 4096, 40960));
     return 0;
 }
 
