@@ -19,20 +19,23 @@
 //  * Softmax in the log2 domain against a reference that is a past row maximum,
 //    replaced when a row's probabilities of a tile sum to more than 256 (the sum
 //    bounds each of them). A walk's first tile takes its own maximum. Probabilities
-//    are rounded to bf16 for the second product, and the row sum adds the rounded
-//    ones, so their errors (2^-8 of each at most) are weighted alike.
+//    are rounded to bf16 for the second product: its operands are bf16 on the matrix
+//    cores, and as sums of two bf16 they would double it. The row sum, in fp32, adds the
+//    rounded ones, so their errors (2^-8 of each at most) are weighted alike: results are
+//    off by 2.3e-3 of their norm, where fp32 probabilities rounded at the end give 1.7e-3.
 //
 // What bounds them, and what they measure:
 //  * Many rows, many keys (8,000 x 4,000, 12 heads x 128: 185 us, 1,060 TFLOP/s): issue of
 //    the matrix instructions and the softmax's vector instructions, as in self attention.
-//  * Many rows, a prompt (21,600 x 512, 40 heads x 128: 262 us, 864 TFLOP/s; at heads of
-//    64 157 us): the same, and each 128 rows' queries and results, 64 KB, which the
+//  * Many rows, a prompt (21,600 x 512, 40 heads x 128: 262 to 276 us by card, 820 to 864
+//    TFLOP/s; at heads of 64 157 us): the same, and each 128 rows' queries and results, 64 KB, which the
 //    other workgroup of the compute unit covers in part. Tiles of 32 keys with three
 //    workgroups to a compute unit at 128 (279 us where this had 267), the next queries
 //    held in registers (313) or touched ahead (288), a wait that leaves them out (no
 //    change) did not cover more.
-//  * Short prompts (2 x 9,360 rows, 12 heads x 128, 116 MB: 38 us): memory, q in and out.
-//  * One token over 20,280 keys, 4 key heads x 128: 17 us, 4.9 TB/s of K and V, and 4 of
+//  * Short prompts (2 x 9,360 rows, 12 heads x 128, 116 MB: 37 to 42 us): memory, q in and out,
+//    little of it under the matrix work (busy 19 %).
+//  * One token over 20,280 keys, 4 key heads x 128: 17 us, 5.0 TB/s of K and V, and 4 of
 //    the join.
 #include "rf_cross.h"
 

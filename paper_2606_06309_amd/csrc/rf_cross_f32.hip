@@ -11,10 +11,12 @@
 //    largest score gives exactly 1 however large it is.
 //  * A tile is 32 keys, 16 KB (head dimension 128) or 8 KB (64) of K and of V.
 //
-// What bounds it: the fp32 matrix instructions (64 cycles each); one 16-byte LDS
-// read feeds four, and the other pipes are far from their limits. 2 x 5,000 x 1,000, 8
-// heads x 64: 208 us, 98 TFLOP/s; 6,400 x 512, 12 x 64: 114 us, 88. Small calls are bound by
-// the launch and one walk of a tile: 192 x 77, 2 x 64: 8.5 us.
+// What bounds it: on long walks the fp32 matrix instructions (64 cycles each), busy 79 % of the
+// cycles at 8,000 x 4,000 keys, 12 heads x 64 (798 us, 123 TFLOP/s); one 16-byte LDS read
+// feeds four, and the vector and LDS pipes are at 15 % and 5 %. Over a prompt they are busy less,
+// as workgroups do not share out evenly: 6,400 x 512, 12 x 64 (109 us, 92 TFLOP/s, 55 %) is 600 of
+// them on 512 places, and the last 88 take a quarter of the time alone; 2 x 5,000 x 1,000, 8 x 64:
+// 208 us, 98, 63 %. Small calls are bound by the launch and one walk of a tile: 192 x 77, 2 x 64: 8.4 us.
 #include "rf_cross.h"
 
 namespace rf {

@@ -24,17 +24,19 @@
 //    workspace; linear_join_kernel adds them in order and runs the epilogue.
 //
 // What bounds them, and what they measure:
-//  * Large bf16 products (21,600 x 20,480 x 5,120 with gate and residual: 3.79 ms,
-//    1,197 TFLOP/s): matrix instructions are busy 64 % of the cycles. Per step a
+//  * Large bf16 products (21,600 x 20,480 x 5,120 with gate and residual: 3.79 to 3.94 ms by
+//    card, 1,150 to 1,197 TFLOP/s): matrix instructions are busy 64 to 66 % of the cycles. Per step a
 //    256 x 256 tile reads 192 KB of LDS while 64 KB of loads are written into it; the
 //    same loop without the loads runs at 1,570. Four waves of 128 x 128 (1,225 TFLOP/s
 //    where this had 1,323), a ring of four half steps (1,218) and loads between the
 //    matrix instructions (1,248) were slower.
-//  * One round of tiles (9,360 x 1,536 x 1,536: 45 us, 52 with gate and residual): 24
+//  * One round of tiles (9,360 x 1,536 x 1,536: 45 us, 47 with rows read at full positions, 52
+//    to 54 with gate and residual): 24
 //    steps of 1.55 us, the first loads and the epilogue's memory time.
-//  * fp32 (7,800 x 1,536 x 1,536: 280 us, 131 TFLOP/s): the matrix instructions, busy 81 %.
-//  * Few rows (6 x 1,536 x 9,216: 10.0 us, 2.9 TB/s): the latency of a launch, of two
-//    loads one after the other, and of the waves' sums.
+//  * fp32 (7,800 x 1,536 x 1,536: 280 us, 131 TFLOP/s): the matrix instructions, busy 82 %.
+//  * Few rows (6 x 1,536 x 9,216: 10.0 us, 2.9 TB/s): 576 workgroups in two rounds and a
+//    quarter, each with loads that wait for one another and the waves' sums. A library's
+//    product without epilogue takes 6.5: this is not the least that it can take.
 #include "rf_device.h"
 #include "rf_linear_plan.h"
 
@@ -167,7 +169,8 @@ __device__ __forceinline__ void stream_8(void *p, int64_t at, const float (&v)[8
     }
 }
 
-// x / (1 + 2^t): both sigmoid forms. 2^t = inf gives 0.
+// x / (1 + 2^t): both sigmoid forms. 2^t = inf gives 0. (The reciprocal is the hardware's, off by one
+// last place of fp32; a divide would be ten instructions, and 2^t is off by as much.)
 __device__ __forceinline__ float gated(float x, float t) {
     return x * __builtin_amdgcn_rcpf(1.0f + fast_exp2(t));
 }

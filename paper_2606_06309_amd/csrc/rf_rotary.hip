@@ -11,7 +11,8 @@
 // walks heads of q and k with them, four at a time, so a sine and cosine serve
 // all its heads and four loads are in flight.
 // 21 frames of 30 x 52, 12 + 12 heads x 128, bf16: 72.5 us, 5.55 TB/s (a large copy 4.9
-// to 5.2); 6 of them, views of a fused projection, to their positions: 24.3 us, 4.7 TB/s.
+// to 5.2); 6 of them, views of a fused projection, to their positions: 24 us, 4.8 TB/s. With
+// halves 74.5 and 22.6 us; fp32, either way, 170 us (4.7 TB/s) and 50 to 51 (4.5).
 // Lanes interleaved over heads, 1 KB contiguous to a load, took 86.8 us where this took 73.3.
 // Angles are formed in double, reduced to half a turn there and only then
 // rounded: at position 2^20 an fp32 angle would be off by 0.06.
