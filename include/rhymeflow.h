@@ -573,8 +573,9 @@ int rf_async_schedule(int32_t T, int32_t T_w, int32_t T_mid, int32_t n_small, in
 /* ---- A block's operators around the attention ----
  * What a DiT block does with the rows of the listed frames directly before and
  * after keyframe-query attention: rotary positions of queries and keys,
- * attention to an encoder's states (the prompt), and the matrix products with
- * their bias, activation, gate and residual.
+ * attention to an encoder's states (the prompt), the matrix products with their
+ * bias, activation, gate and residual, also of 8-bit integers, and the group norm
+ * before them.
  *
  * Rows of frames come and go in one of two layouts, per call and side:
  *   compact: M*N rows, row m*N + n is row n of the m-th listed frame (what a
@@ -587,6 +588,7 @@ int rf_async_schedule(int32_t T, int32_t T_w, int32_t T_mid, int32_t n_small, in
 #define RF_ROWS_IN_FULL 1u      /* input rows are read at full positions (default: compact) */
 #define RF_ROWS_OUT_FULL 2u     /* output rows (and the residual's) are at full positions (default: compact) */
 #define RF_GATE_PER_FRAME 4u    /* rf_frame_linear: gate is [T][out_features], frames have their own */
+#define RF_AFFINE_PER_FRAME 8u  /* rf_frame_group_norm: weight and bias are [T][channels], frames have their own */
 #define RF_ROTARY_HALVES 16u    /* rf_rotary: pair p is dimensions p and p + R/2 (default: 2p and 2p + 1) */
 #define RF_ROTARY_INVERSE 32u   /* rf_rotary: rotate by the negative angles */
 
@@ -694,7 +696,7 @@ int rf_cross_attention(const void *q, const void *k, const void *v, void *out, c
 int rf_cross_attention_workspace(int32_t B, int32_t Lq, int32_t Lk, int32_t heads, int32_t kv_heads,
                                  int32_t head_dim, int32_t dtype, int32_t compute_units, int64_t *bytes_out);
 
-/* Activations of rf_frame_linear. */
+/* Activations of rf_frame_linear, rf_frame_linear_i8 and rf_frame_group_norm. */
 #define RF_ACT_NONE 0
 #define RF_ACT_GELU 1        /* x/2 (1 + erf(x / sqrt 2)) */
 #define RF_ACT_GELU_TANH 2   /* x/2 (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))) */
@@ -745,6 +747,107 @@ int rf_frame_linear(const void *x, const void *weight, const void *bias, const v
    compute_units), RF_ERR_UNSUPPORTED (dtype, row sizes), RF_ERR_HIP. */
 int rf_frame_linear_workspace(int32_t M, int64_t rows_per_frame, int32_t in_features, int32_t out_features,
                               int32_t dtype, int32_t compute_units, int64_t *bytes_out);
+
+/*
+ * Rows in 8 bits, for rf_frame_linear_i8: with a the row's largest magnitude,
+ *   scale = a / 127,   q = x * (127 / a) to the nearest integer, ties to even,
+ * both quotients and the product rounded to fp32 each. q lies in [-127, 127] and
+ * stands for q * scale. A row whose a is below 2^-100 is a row of zeros (scale 0);
+ * one that holds an infinity or a NaN has scale NaN and q 0, so that its products
+ * are NaN. Rows of a weight [out_features][in_features], which are output features,
+ * are rounded by the same call.
+ *
+ * x: device rows of `features` elements, x_stride elements from row to row (0: the
+ *   rows are contiguous), compact or full with RF_ROWS_IN_FULL. q: device rows of
+ *   `features` bytes, contiguous, and scale: device fp32, one a row (4-byte aligned):
+ *   compact, or full with RF_ROWS_OUT_FULL. Neither overlaps another tensor of the call.
+ * features: a multiple of 16 up to RF_I8_FEATURES. rows_per_frame >= 1,
+ *   M * rows_per_frame < 2^31. dtype: x's, RF_BF16 or RF_F32.
+ * frame_ids, M, T: as rf_keyframe_attention. flags: RF_ROWS_IN_FULL, RF_ROWS_OUT_FULL.
+ * Errors: RF_ERR_INVALID_ARG (NULL, sizes <= 0, ids, unknown flags, x_stride below
+ *   the row, overlap), RF_ERR_RANGE (ids, T, rows, sizes whose byte counts would pass
+ *   4e18), RF_ERR_UNSUPPORTED (dtype, features, alignment), RF_ERR_HIP.
+ */
+#define RF_I8_FEATURES 65536
+int rf_frame_quantize(const void *x, int8_t *q, float *scale, const int32_t *frame_ids, int32_t M, int32_t T,
+                      int64_t rows_per_frame, int32_t features, int64_t x_stride, uint32_t flags, int32_t dtype,
+                      void *stream);
+
+/*
+ * Matrix product in 8-bit integers, with a scale for each row and each output
+ * feature, on the rows of the listed frames:
+ *   y[r][c] = residual[r][c] + gate[c] * act(sum_k x[r][k] weight[c][k] * x_scale[r] * weight_scale[c] + bias[c]).
+ * The sum is exact (32-bit integers; in_features is bounded so that none passes
+ * them), everything after it fp32, with one rounding to y's type at the end; results
+ * do not depend on the workspace. Any int8 value may occur in x and weight, -128
+ * among them.
+ *
+ * x: device int8 rows of in_features, contiguous, and x_scale: device fp32, one a
+ *   row (4-byte aligned): both compact, or both full with RF_ROWS_IN_FULL. weight:
+ *   device int8 [out_features][in_features]; weight_scale: device fp32 [out_features].
+ * bias, gate, residual, y, frame_ids, M, T, rows_per_frame, activation, flags,
+ *   workspace: as rf_frame_linear; dtype is theirs: RF_BF16 or RF_F32.
+ * in_features: a multiple of 16 up to RF_I8_FEATURES. out_features: rows of y of a
+ *   multiple of 16 bytes.
+ * Errors: as rf_frame_linear.
+ */
+int rf_frame_linear_i8(const int8_t *x, const float *x_scale, const int8_t *weight, const float *weight_scale,
+                       const void *bias, const void *gate, const void *residual, void *y, const int32_t *frame_ids,
+                       int32_t M, int32_t T, int64_t rows_per_frame, int32_t in_features, int32_t out_features,
+                       int32_t activation, uint32_t flags, int32_t dtype, void *workspace, int64_t workspace_bytes,
+                       void *stream);
+
+/* Bytes of workspace rf_frame_linear_i8 uses; arguments and errors as rf_frame_linear_workspace. */
+int rf_frame_linear_i8_workspace(int32_t M, int64_t rows_per_frame, int32_t in_features, int32_t out_features,
+                                 int32_t dtype, int32_t compute_units, int64_t *bytes_out);
+
+/*
+ * Group norm with an activation, channels last, on the rows of the listed frames:
+ *   y = act((x - mean) / sqrt(var + eps) * weight + bias),
+ * mean and (biased) variance over the rows of frames_together consecutive frames of
+ * the list and the channels / groups channels of a group: 1 is a norm of each frame
+ * by itself, M one over the whole clip. An infinity or a NaN makes its group's results
+ * of those frames NaN. Deviations are squared and summed in fp32: magnitudes up to
+ * 2^60.
+ *
+ * x: device rows of `channels` elements, x_stride elements from row to row (0: the
+ *   rows are contiguous), compact, or full with RF_ROWS_IN_FULL.
+ * y_scale == NULL: y: device rows of x's type, y_stride elements apart (0: contiguous),
+ *   compact, or full with RF_ROWS_OUT_FULL. y may be exactly x with the same stride and
+ *   layout (with M == T both layouts are one); otherwise it overlaps no row of x.
+ * y_scale != NULL: rows in 8 bits as rf_frame_quantize makes them of the fp32 results:
+ *   y: device int8 rows, contiguous (y_stride 0 or channels), y_scale: device fp32, one
+ *   a row (4-byte aligned), both compact or full; channels a multiple of 16.
+ * weight, bias: device [channels], or with RF_AFFINE_PER_FRAME [T][channels] (frames
+ *   denoised at times of their own have modulations of their own), each or NULL (1, 0).
+ * channels: rows of a multiple of 16 bytes, up to RF_NORM_CHANNELS; groups divides it.
+ *   rows_per_frame >= 1, M * rows_per_frame < 2^31. eps: 1e-30 to 1e30. activation: RF_ACT_*.
+ * workspace: device scratch, 16-byte aligned, of rf_frame_group_norm_workspace bytes
+ *   (NULL where that is 0), overlapping no tensor of the call. Its contents mean nothing
+ *   afterwards; two calls, or two captured graphs, that may run at the same time need
+ *   one each.
+ * frame_ids, M, T: as rf_keyframe_attention.
+ * flags: RF_ROWS_IN_FULL, RF_ROWS_OUT_FULL, RF_AFFINE_PER_FRAME (which needs a weight or bias).
+ * Errors: RF_ERR_INVALID_ARG (NULL x, y; sizes <= 0, ids, groups, frames_together that
+ *   does not divide M, eps, unknown flags or activation, a stride below the row, overlap,
+ *   workspace too small), RF_ERR_RANGE (ids, T, rows, sizes whose byte counts would pass
+ *   4e18), RF_ERR_UNSUPPORTED (dtype, channels, alignment), RF_ERR_HIP.
+ */
+#define RF_NORM_CHANNELS 8192
+int rf_frame_group_norm(const void *x, const void *weight, const void *bias, void *y, float *y_scale,
+                        const int32_t *frame_ids, int32_t M, int32_t T, int64_t rows_per_frame, int32_t channels,
+                        int32_t groups, int32_t frames_together, double eps, int32_t activation, int64_t x_stride,
+                        int64_t y_stride, uint32_t flags, int32_t dtype, void *workspace, int64_t workspace_bytes,
+                        void *stream);
+
+/* Bytes of workspace rf_frame_group_norm needs for M frames (0: none) whose results are
+   in 8 bits (rows_8bit nonzero) or in dtype, on a device of compute_units compute units,
+   or 0 for the current device's count (queried once per device).
+   Errors: RF_ERR_INVALID_ARG (NULL, sizes <= 0, groups, frames_together), RF_ERR_RANGE
+   (rows, compute_units), RF_ERR_UNSUPPORTED (dtype, channels), RF_ERR_HIP. */
+int rf_frame_group_norm_workspace(int32_t M, int64_t rows_per_frame, int32_t channels, int32_t groups,
+                                  int32_t frames_together, int32_t rows_8bit, int32_t dtype, int32_t compute_units,
+                                  int64_t *bytes_out);
 
 /* ---- Device probes (measurement support, not part of the method) ----
  * Sustained whole-chip rates of this device under a pure load of one kind, to

@@ -18,7 +18,8 @@ LIB = os.path.join(PKG, "librhymeflow.so")
 ARCH = "gfx950"
 
 SOURCES = ["rf_abi.cpp", "rf_attention.hip", "rf_attention_f32.hip", "rf_project.hip", "rf_gather.hip", "rf_similarity.hip",
-           "rf_cache.hip", "rf_probe.hip", "rf_noalloc.hip", "rf_rotary.hip", "rf_cross.hip", "rf_cross_f32.hip", "rf_linear.hip"]
+           "rf_cache.hip", "rf_probe.hip", "rf_noalloc.hip", "rf_rotary.hip", "rf_cross.hip", "rf_cross_f32.hip", "rf_linear.hip",
+           "rf_norm.hip"]
 
 HIPCC_FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC",

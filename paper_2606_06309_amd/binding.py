@@ -27,9 +27,12 @@ RF_F32 = 1
 RF_SEL_NO_FORCE_FIRST = 1
 RF_SEL_INTENT_SIGN = 1
 RF_MAX_FRAMES = 256
+RF_I8_FEATURES = 65536
+RF_NORM_CHANNELS = 8192
 RF_ROWS_IN_FULL = 1
 RF_ROWS_OUT_FULL = 2
 RF_GATE_PER_FRAME = 4
+RF_AFFINE_PER_FRAME = 8
 RF_ROTARY_HALVES = 16
 RF_ROTARY_INVERSE = 32
 ACTIVATIONS = {"none": 0, "gelu": 1, "gelu_tanh": 2, "silu": 3}
@@ -46,6 +49,8 @@ EXPORTED = [
     "rf_cache_project_kv", "rf_keyframe_attention_cached", "rf_async_schedule",
     "rf_rotary", "rf_cross_attention", "rf_cross_attention_workspace",
     "rf_frame_linear", "rf_frame_linear_workspace",
+    "rf_frame_quantize", "rf_frame_linear_i8", "rf_frame_linear_i8_workspace",
+    "rf_frame_group_norm", "rf_frame_group_norm_workspace",
     "rf_probe_mfma_bf16", "rf_probe_hbm_read", "rf_probe_lds_read",
 ]
 
@@ -212,6 +217,18 @@ lib.rf_frame_linear.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _
 lib.rf_frame_linear.restype = ctypes.c_int
 lib.rf_frame_linear_workspace.argtypes = [_i32, _i64, _i32, _i32, _i32, _i32, ctypes.POINTER(_i64)]
 lib.rf_frame_linear_workspace.restype = ctypes.c_int
+lib.rf_frame_quantize.argtypes = [_vp, _vp, _vp, _vp, _i32, _i32, _i64, _i32, _i64, ctypes.c_uint32, _i32, _vp]
+lib.rf_frame_quantize.restype = ctypes.c_int
+lib.rf_frame_linear_i8.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i64, _i32, _i32, _i32,
+                                   ctypes.c_uint32, _i32, _vp, _i64, _vp]
+lib.rf_frame_linear_i8.restype = ctypes.c_int
+lib.rf_frame_linear_i8_workspace.argtypes = lib.rf_frame_linear_workspace.argtypes
+lib.rf_frame_linear_i8_workspace.restype = ctypes.c_int
+lib.rf_frame_group_norm.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i64, _i32, _i32, _i32, ctypes.c_double,
+                                    _i32, _i64, _i64, ctypes.c_uint32, _i32, _vp, _i64, _vp]
+lib.rf_frame_group_norm.restype = ctypes.c_int
+lib.rf_frame_group_norm_workspace.argtypes = [_i32, _i64, _i32, _i32, _i32, _i32, _i32, _i32, ctypes.POINTER(_i64)]
+lib.rf_frame_group_norm_workspace.restype = ctypes.c_int
 lib.rf_probe_mfma_bf16.argtypes = [_vp, _i32, _i32, _vp, _vp]
 lib.rf_probe_mfma_bf16.restype = ctypes.c_int
 lib.rf_probe_hbm_read.argtypes = [_vp, _i64, _i32, _vp, _vp]
@@ -872,6 +889,16 @@ def _linear_need(device, M, rows_per_frame, in_features, out_features, code):
     return rf_frame_linear_workspace(M, rows_per_frame, in_features, out_features, code)
 
 
+@functools.lru_cache(maxsize=256)
+def _linear_i8_need(device, M, rows_per_frame, in_features, out_features, code):
+    return rf_frame_linear_i8_workspace(M, rows_per_frame, in_features, out_features, code)
+
+
+@functools.lru_cache(maxsize=256)
+def _norm_need(device, M, rows_per_frame, channels, groups, frames_together, rows_8bit, code):
+    return rf_frame_group_norm_workspace(M, rows_per_frame, channels, groups, code, rows_8bit, frames_together)
+
+
 def rf_cross_attention(q, k, v, kv_lengths=None, key_mask=None, out=None, workspace=None, stream=None):
     """q [B][Lq][heads][head_dim] attends to k, v [B][Lk][kv_heads][head_dim], of
     any strides whose head_dim elements are contiguous, -> out as q. kv_lengths:
@@ -991,6 +1018,200 @@ def rf_frame_linear(x, weight, bias=None, activation: str = "none", gate=None, r
 
 
 _FRAME0 = np.zeros(1, dtype=np.int32)
+
+
+def _frame_rows(frame_ids, T, rows_per_frame, in_full, out_full, rows):
+    """(ids, their address, M, T, rows_per_frame, rows read, rows written) of a call on the rows of listed frames, or
+    without a list on all `rows` rows as one frame."""
+    if frame_ids is None:
+        if T is not None or rows_per_frame is not None or in_full or out_full:
+            raise ValueError("T, rows_per_frame, in_full and out_full go with frame_ids")
+        frame_ids, T, rows_per_frame = _FRAME0, 1, rows
+    elif T is None or rows_per_frame is None:
+        raise ValueError("frame_ids needs T and rows_per_frame")
+    ids, ids_p = _ids(frame_ids)
+    M = ids.size
+    rows_in, rows_out = rows_per_frame * (T if in_full else M), rows_per_frame * (T if out_full else M)
+    if rows != rows_in:
+        raise ValueError(f"x has {rows} rows, the layout asks for {rows_in}")
+    return ids, ids_p, M, T, rows_per_frame, rows_in, rows_out
+
+
+def _row_stride(t, name, rows, features):
+    """Row stride in elements of a [rows][features] tensor whose rows are contiguous."""
+    if t.shape != (rows, features):
+        raise ValueError(f"{name} must be [{rows}][{features}], it is {list(t.shape)}")
+    row, one = t.stride()
+    if features > 1 and one != 1:
+        raise ValueError(f"{name}: the elements of a row must be contiguous")
+    if rows <= 1:
+        return features
+    if row < features:
+        raise ValueError(f"{name}: rows overlap")
+    return row
+
+
+def _rows_8bit(out, out_scale, rows, features, x, whole, stream):
+    """out and out_scale of rows in 8 bits, checked or allocated (`whole`: every row of the layout is written)."""
+    if not whole and (out is None or out_scale is None):
+        raise ValueError("out and out_scale must be given with out_full: rows of other frames are left as they are")
+    if out is None:
+        out = _empty((rows, features), torch.int8, x.device, stream)
+    if out_scale is None:
+        out_scale = _empty((rows,), torch.float32, x.device, stream)
+    if out.dtype != torch.int8 or out.shape != (rows, features) or not out.is_contiguous():
+        raise ValueError(f"out must be contiguous int8 [{rows}][{features}]")
+    if out_scale.dtype != torch.float32 or out_scale.shape != (rows,) or not out_scale.is_contiguous():
+        raise ValueError(f"out_scale must be contiguous float32 [{rows}]")
+    return out, out_scale
+
+
+def rf_frame_quantize(x, frame_ids=None, T=None, rows_per_frame=None, in_full: bool = False, out_full: bool = False,
+                      out=None, out_scale=None, stream=None):
+    """Rows of x in 8 bits with a scale each, (int8 [rows][features], float32 [rows]),
+    for rf_frame_linear_i8: the rows of the listed frames, without frame_ids all of
+    x's. x [rows][features], compact or, with in_full, full (a view with a longer row
+    stride is taken as it is); out and out_scale compact or, with out_full, full
+    (required then unless M = T). A weight [out_features][in_features] is rounded so too."""
+    if x.dim() != 2:
+        raise ValueError("x must be [rows][features]")
+    K = x.shape[1]
+    ids, ids_p, M, T, N, rows_in, rows_out = _frame_rows(frame_ids, T, rows_per_frame, in_full, out_full, x.shape[0])
+    stride = _row_stride(x, "x", rows_in, K)
+    out, out_scale = _rows_8bit(out, out_scale, rows_out, K, x, not out_full or M == T, stream)
+    code = _dtype_code(x.dtype)
+    index, ptrs = _on_device(((x, "x"), (out, "out"), (out_scale, "out_scale")))
+    flags = (RF_ROWS_IN_FULL if in_full else 0) | (RF_ROWS_OUT_FULL if out_full else 0)
+    _check(lib.rf_frame_quantize(*ptrs, ids_p, M, T, N, K, stride, flags, code, _stream_on(stream, index)))
+    return out, out_scale
+
+
+def rf_frame_linear_i8_workspace(M: int, rows_per_frame: int, in_features: int, out_features: int, dtype,
+                                 compute_units: int = 0) -> int:
+    """Bytes of workspace rf_frame_linear_i8 uses for M frames (0: in_features are not split) on a device of
+    compute_units compute units (0: the current device); dtype: the result's."""
+    n = _i64(0)
+    code = dtype if isinstance(dtype, int) else _dtype_code(dtype)
+    _check(lib.rf_frame_linear_i8_workspace(M, rows_per_frame, in_features, out_features, code, compute_units,
+                                            ctypes.byref(n)))
+    return int(n.value)
+
+
+def rf_frame_linear_i8(x, x_scale, weight, weight_scale, bias=None, activation: str = "none", gate=None, residual=None,
+                       frame_ids=None, T=None, rows_per_frame=None, in_full: bool = False, out_full: bool = False,
+                       out=None, dtype=None, workspace=None, stream=None):
+    """residual + gate * act(x weight^T * x_scale * weight_scale + bias) of 8-bit integers
+    on the rows of the listed frames; without frame_ids on all of x's rows. x int8
+    [rows][in] and x_scale float32 [rows] (compact or, with in_full, full), weight int8
+    [out][in] and weight_scale float32 [out], as rf_frame_quantize makes them; bias, gate,
+    residual and out as rf_frame_linear, all of the result's type: dtype, or out's or
+    theirs if given, else bfloat16. The workspace is allocated here if not given."""
+    if x.dim() != 2 or weight.dim() != 2 or weight.shape[1] != x.shape[1]:
+        raise ValueError("x must be [rows][in_features], weight [out_features][in_features]")
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"unknown activation {activation!r}: one of {sorted(ACTIVATIONS)}")
+    n_out, K = weight.shape
+    ids, ids_p, M, T, N, rows_in, rows_out = _frame_rows(frame_ids, T, rows_per_frame, in_full, out_full, x.shape[0])
+    if dtype is None:
+        dtype = next((t.dtype for t in (out, residual, bias, gate) if t is not None), torch.bfloat16)
+    if out is None:
+        if out_full and M != T:
+            raise ValueError("out must be given with out_full: rows of other frames are left as they are")
+        out = _empty((rows_out, n_out), dtype, x.device, stream)
+    for t, name in ((out, "out"), (residual, "residual")):
+        if t is not None and t.shape != (rows_out, n_out):
+            raise ValueError(f"{name} must be [{rows_out}][{n_out}]")
+    if bias is not None and bias.shape != (n_out,):
+        raise ValueError(f"bias must be [{n_out}]")
+    if x_scale.shape != (rows_in,) or weight_scale.shape != (n_out,):
+        raise ValueError(f"x_scale must be [{rows_in}], weight_scale [{n_out}]")
+    for t, name, want in ((x, "x", torch.int8), (weight, "weight", torch.int8), (x_scale, "x_scale", torch.float32),
+                          (weight_scale, "weight_scale", torch.float32)):
+        if t.dtype != want:
+            raise TypeError(f"{name} has dtype {t.dtype}, not {want}")
+    flags = (RF_ROWS_IN_FULL if in_full else 0) | (RF_ROWS_OUT_FULL if out_full else 0)
+    if gate is not None and gate.shape != (n_out,):
+        if gate.shape != (T, n_out):
+            raise ValueError(f"gate must be [{n_out}] or [{T}][{n_out}]")
+        flags |= RF_GATE_PER_FRAME
+    tensors = ((x, "x"), (x_scale, "x_scale"), (weight, "weight"), (weight_scale, "weight_scale"), (bias, "bias"),
+               (gate, "gate"), (residual, "residual"), (out, "out"))
+    code = _dtype_code(dtype)
+    for t, name in tensors[4:]:
+        if t is not None and t.dtype != dtype:
+            raise TypeError(f"{name} has dtype {t.dtype}, the result's is {dtype}")
+    for t, name in tensors:
+        if t is not None and not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+    index, ptrs = _on_device(tensors)
+    if workspace is None and M > 0 and N > 0 and weight.numel() > 0:
+        need = _linear_i8_need(index, M, N, K, n_out, code)
+        workspace = _empty(need, torch.uint8, x.device, stream) if need > 0 else None
+    ws_p, wbytes = _workspace_arg(workspace)
+    _check(lib.rf_frame_linear_i8(*ptrs, ids_p, M, T, N, K, n_out, ACTIVATIONS[activation], flags, code, ws_p, wbytes,
+                                  _stream_on(stream, index)))
+    return out
+
+
+def rf_frame_group_norm_workspace(M: int, rows_per_frame: int, channels: int, groups: int, dtype, int8: bool = False,
+                                  frames_together: int = 1, compute_units: int = 0) -> int:
+    """Bytes of workspace rf_frame_group_norm needs for M frames (0: none), its results in dtype or in 8 bits, on a
+    device of compute_units compute units (0: the current device)."""
+    n = _i64(0)
+    code = dtype if isinstance(dtype, int) else _dtype_code(dtype)
+    _check(lib.rf_frame_group_norm_workspace(M, rows_per_frame, channels, groups, frames_together, 1 if int8 else 0, code,
+                                             compute_units, ctypes.byref(n)))
+    return int(n.value)
+
+
+def rf_frame_group_norm(x, groups: int, weight=None, bias=None, eps: float = 1e-5, activation: str = "none",
+                        frame_ids=None, T=None, rows_per_frame=None, frames_together: int = 1, in_full: bool = False,
+                        out_full: bool = False, out=None, out_scale=None, int8: bool = False, workspace=None,
+                        stream=None):
+    """act((x - mean) / sqrt(var + eps) * weight + bias), channels last, on the rows of the
+    listed frames (without frame_ids all of x's rows are one frame): mean and variance
+    over the rows of frames_together consecutive listed frames and the channels of one of
+    `groups` groups. x [rows][channels], compact or, with in_full, full; weight and bias
+    [channels] or [T][channels] (each frame its own). The result is x's type, in out if
+    given (x itself: in place), or with int8 (or an out_scale, or an out of int8) rows in 8
+    bits as of rf_frame_quantize, (out, out_scale); compact or, with out_full, full (out is
+    required then unless M = T). Views with a longer row stride are taken as they are,
+    but for rows in 8 bits. The workspace is allocated here if not given."""
+    if x.dim() != 2:
+        raise ValueError("x must be [rows][channels]")
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"unknown activation {activation!r}: one of {sorted(ACTIVATIONS)}")
+    C = x.shape[1]
+    ids, ids_p, M, T, N, rows_in, rows_out = _frame_rows(frame_ids, T, rows_per_frame, in_full, out_full, x.shape[0])
+    xs, ys = _row_stride(x, "x", rows_in, C), 0
+    int8 = int8 or out_scale is not None or (out is not None and out.dtype == torch.int8)
+    if int8:
+        out, out_scale = _rows_8bit(out, out_scale, rows_out, C, x, not out_full or M == T, stream)
+    else:
+        if out is None:
+            if out_full and M != T:
+                raise ValueError("out must be given with out_full: rows of other frames are left as they are")
+            out = _empty((rows_out, C), x.dtype, x.device, stream)
+        ys = _row_stride(out, "out", rows_out, C)
+    flags = (RF_ROWS_IN_FULL if in_full else 0) | (RF_ROWS_OUT_FULL if out_full else 0)
+    per_frame = {t.shape == (T, C) for t in (weight, bias) if t is not None}
+    for t, name in ((weight, "weight"), (bias, "bias")):
+        if t is not None and ((t.shape != (C,) and t.shape != (T, C)) or not t.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous [{C}] or [{T}][{C}]")
+    if len(per_frame) > 1:
+        raise ValueError("weight and bias must both be of each frame, or neither")
+    if True in per_frame:
+        flags |= RF_AFFINE_PER_FRAME
+    code = _same_dtype(((x, "x"), (weight, "weight"), (bias, "bias"), (None if int8 else out, "out")))
+    index, ptrs = _on_device(((x, "x"), (weight, "weight"), (bias, "bias"), (out, "out"), (out_scale, "out_scale")))
+    if workspace is None and M > 0 and N > 0 and C > 0 and groups > 0 and frames_together > 0:
+        need = _norm_need(index, M, N, C, groups, frames_together, int8, code)
+        workspace = _empty(need, torch.uint8, x.device, stream) if need > 0 else None
+    ws_p, wbytes = _workspace_arg(workspace)
+    _check(lib.rf_frame_group_norm(*ptrs, ids_p, M, T, N, C, groups, frames_together, eps, ACTIVATIONS[activation], xs, ys,
+                                   flags, code, ws_p, wbytes, _stream_on(stream, index)))
+    return (out, out_scale) if int8 else out
+
 
 
 # --- device probes (measurement support) ------------------------------------------

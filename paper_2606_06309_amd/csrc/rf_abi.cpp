@@ -26,6 +26,7 @@ int ok() {
     return RF_OK;
 }
 
+bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // Byte counts are 64-bit: sizes whose product (computed in double) passes this
@@ -1167,6 +1168,23 @@ static int linear_sizes(int32_t M, int64_t N, int32_t K, int32_t n_out, int32_t 
     return RF_OK;
 }
 
+// Those of a product of 8-bit integers.
+static int linear_i8_sizes(int32_t M, int64_t N, int32_t K, int32_t n_out, int32_t dtype, const char *fn) {
+    if (M <= 0 || N <= 0 || K <= 0 || n_out <= 0)
+        return fail(RF_ERR_INVALID_ARG, "%s: sizes must be positive (M=%d rows_per_frame=%lld in=%d out=%d)", fn, M,
+                    static_cast<long long>(N), K, n_out);
+    if (static_cast<double>(M) * static_cast<double>(N) > 2147483647.0)
+        return fail(RF_ERR_RANGE, "%s: %d frames of %lld rows exceed 2^31 - 1 rows", fn, M, static_cast<long long>(N));
+    if (dtype != RF_BF16 && dtype != RF_F32) return fail(RF_ERR_UNSUPPORTED, "%s: unknown dtype %d", fn, dtype);
+    // (a sum's terms are 2^14 at most: 2^16 of them stay in 32 bits)
+    static_assert(RF_I8_FEATURES * int64_t(128) * 128 < INT32_MAX, "sums of 8-bit products fit");
+    if (K % 16 != 0 || K > RF_I8_FEATURES)
+        return fail(RF_ERR_UNSUPPORTED, "%s: %d in_features are no multiple of 16 up to %d", fn, K, RF_I8_FEATURES);
+    if (n_out % (dtype == RF_F32 ? 4 : 8) != 0)
+        return fail(RF_ERR_UNSUPPORTED, "%s: %d out_features make no rows of 16-byte multiples", fn, n_out);
+    return RF_OK;
+}
+
 int rf_frame_linear_workspace(int32_t M, int64_t rows_per_frame, int32_t in_features, int32_t out_features,
                               int32_t dtype, int32_t compute_units, int64_t *bytes_out) {
     const char *fn = "rf_frame_linear_workspace";
@@ -1180,29 +1198,38 @@ int rf_frame_linear_workspace(int32_t M, int64_t rows_per_frame, int32_t in_feat
     return ok();
 }
 
-int rf_frame_linear(const void *x, const void *weight, const void *bias, const void *gate, const void *residual,
-                    void *y, const int32_t *frame_ids, int32_t M, int32_t T, int64_t rows_per_frame,
-                    int32_t in_features, int32_t out_features, int32_t activation, uint32_t flags, int32_t dtype,
-                    void *workspace, int64_t workspace_bytes, void *stream) {
-    const char *fn = "rf_frame_linear";
-    if (!x || !weight || !y) return fail(RF_ERR_INVALID_ARG, "%s: NULL tensor", fn);
+// What a matrix product reads; with i8 set x and weight are int8 and have scales.
+struct LinearIn {
+    const void *x, *weight, *bias, *gate, *residual;
+    bool i8;
+    const float *x_scale, *w_scale;
+};
+
+static int linear_call(const LinearIn &in, void *y, const int32_t *frame_ids, int32_t M, int32_t T,
+                       int64_t rows_per_frame, int32_t in_features, int32_t out_features, int32_t activation,
+                       uint32_t flags, int32_t dtype, void *workspace, int64_t workspace_bytes, void *stream,
+                       const char *fn) {
+    if (!in.x || !in.weight || !y || (in.i8 && (!in.x_scale || !in.w_scale)))
+        return fail(RF_ERR_INVALID_ARG, "%s: NULL tensor", fn);
     if (flags & ~(RF_ROWS_IN_FULL | RF_ROWS_OUT_FULL | RF_GATE_PER_FRAME))
         return fail(RF_ERR_INVALID_ARG, "%s: unknown flags 0x%x", fn, flags);
-    if ((flags & RF_GATE_PER_FRAME) && !gate) return fail(RF_ERR_INVALID_ARG, "%s: a gate per frame needs a gate", fn);
+    if ((flags & RF_GATE_PER_FRAME) && !in.gate) return fail(RF_ERR_INVALID_ARG, "%s: a gate per frame needs a gate", fn);
     if (activation < RF_ACT_NONE || activation > RF_ACT_SILU)
         return fail(RF_ERR_INVALID_ARG, "%s: unknown activation %d", fn, activation);
     int32_t ids[RF_MAX_FRAMES];
     int rc = check_id_list(frame_ids, M, T, ids, fn);
     if (rc != RF_OK) return rc;
-    rc = linear_sizes(M, rows_per_frame, in_features, out_features, dtype, fn);
+    rc = in.i8 ? linear_i8_sizes(M, rows_per_frame, in_features, out_features, dtype, fn)
+               : linear_sizes(M, rows_per_frame, in_features, out_features, dtype, fn);
     if (rc != RF_OK) return rc;
     if (static_cast<double>(T) * static_cast<double>(rows_per_frame) * (in_features > out_features ? in_features : out_features) * 4.0 >
         kMaxBytes)
         return fail(RF_ERR_RANGE, "%s: sizes overflow 64-bit byte counts", fn);
-    if (!aligned16(x) || !aligned16(weight) || !aligned16(y) || !aligned16(bias) || !aligned16(gate) ||
-        !aligned16(residual))
+    if (!aligned16(in.x) || !aligned16(in.weight) || !aligned16(y) || !aligned16(in.bias) || !aligned16(in.gate) ||
+        !aligned16(in.residual) || !aligned16(in.w_scale))
         return fail(RF_ERR_UNSUPPORTED, "%s: pointers must be 16-byte aligned", fn);
-    const int64_t esize = dtype == RF_F32 ? 4 : 2;
+    if (!aligned4(in.x_scale)) return fail(RF_ERR_UNSUPPORTED, "%s: x_scale must be 4-byte aligned", fn);
+    const int64_t esize = dtype == RF_F32 ? 4 : 2, in_size = in.i8 ? 1 : esize;
     const int64_t in_rows = rows_per_frame * ((flags & RF_ROWS_IN_FULL) ? T : M);
     const int64_t out_rows = rows_per_frame * ((flags & RF_ROWS_OUT_FULL) ? T : M);
     const int64_t out_row = out_features * esize;
@@ -1210,11 +1237,13 @@ int rf_frame_linear(const void *x, const void *weight, const void *bias, const v
         const void *p;
         int64_t n;
     };
-    const Range ins[5] = {{x, in_rows * in_features * esize},
-                          {weight, static_cast<int64_t>(out_features) * in_features * esize},
-                          {bias, out_row},
-                          {gate, out_row * ((flags & RF_GATE_PER_FRAME) ? T : 1)},
-                          {residual == y ? nullptr : residual, out_rows * out_row}};
+    const Range ins[7] = {{in.x, in_rows * in_features * in_size},
+                          {in.weight, static_cast<int64_t>(out_features) * in_features * in_size},
+                          {in.bias, out_row},
+                          {in.gate, out_row * ((flags & RF_GATE_PER_FRAME) ? T : 1)},
+                          {in.residual == y ? nullptr : in.residual, out_rows * out_row},
+                          {in.x_scale, in_rows * 4},
+                          {in.w_scale, static_cast<int64_t>(out_features) * 4}};
     for (const Range &r : ins)
         if (r.p && overlaps(y, out_rows * out_row, r.p, r.n))
             return fail(RF_ERR_INVALID_ARG, "%s: y overlaps an input", fn);
@@ -1233,17 +1262,18 @@ int rf_frame_linear(const void *x, const void *weight, const void *bias, const v
     rc = query_geometry(&p.geo, fn);
     if (rc != RF_OK) return rc;
     if (workspace) {
-        const int64_t need = rf::linear_workspace(M * rows_per_frame, in_features, out_features, dtype, p.geo.cus);
+        const int64_t need = in.i8 ? rf::linear_i8_workspace(M * rows_per_frame, in_features, out_features, dtype, p.geo.cus)
+                                   : rf::linear_workspace(M * rows_per_frame, in_features, out_features, dtype, p.geo.cus);
         if (workspace_bytes < need)
             return fail(RF_ERR_INVALID_ARG, "%s: workspace of %lld bytes, %lld needed on %d compute units", fn,
                         static_cast<long long>(workspace_bytes), static_cast<long long>(need), p.geo.cus);
         p.ws = need > 0 ? workspace : nullptr;
     }
-    p.x = x;
-    p.weight = weight;
-    p.bias = bias;
-    p.gate = gate;
-    p.residual = residual;
+    p.x = in.x;
+    p.weight = in.weight;
+    p.bias = in.bias;
+    p.gate = in.gate;
+    p.residual = in.residual;
     p.y = y;
     p.N = rows_per_frame;
     p.M = M;
@@ -1253,7 +1283,198 @@ int rf_frame_linear(const void *x, const void *weight, const void *bias, const v
     p.dtype = dtype;
     p.gate_rows = (flags & RF_GATE_PER_FRAME) != 0;
     row_frames(ids, M, (flags & RF_ROWS_IN_FULL) != 0, (flags & RF_ROWS_OUT_FULL) != 0, &p.frames);
-    return launched(rf::launch_linear(p, static_cast<hipStream_t>(stream)), fn);
+    hipStream_t hs = static_cast<hipStream_t>(stream);
+    return launched(in.i8 ? rf::launch_linear_i8(p, in.x_scale, in.w_scale, hs) : rf::launch_linear(p, hs), fn);
+}
+
+int rf_frame_linear(const void *x, const void *weight, const void *bias, const void *gate, const void *residual,
+                    void *y, const int32_t *frame_ids, int32_t M, int32_t T, int64_t rows_per_frame,
+                    int32_t in_features, int32_t out_features, int32_t activation, uint32_t flags, int32_t dtype,
+                    void *workspace, int64_t workspace_bytes, void *stream) {
+    const LinearIn in = {x, weight, bias, gate, residual, false, nullptr, nullptr};
+    return linear_call(in, y, frame_ids, M, T, rows_per_frame, in_features, out_features, activation, flags, dtype,
+                       workspace, workspace_bytes, stream, "rf_frame_linear");
+}
+
+int rf_frame_linear_i8_workspace(int32_t M, int64_t rows_per_frame, int32_t in_features, int32_t out_features,
+                                 int32_t dtype, int32_t compute_units, int64_t *bytes_out) {
+    const char *fn = "rf_frame_linear_i8_workspace";
+    if (!bytes_out) return fail(RF_ERR_INVALID_ARG, "%s: NULL output", fn);
+    int rc = linear_i8_sizes(M, rows_per_frame, in_features, out_features, dtype, fn);
+    if (rc != RF_OK) return rc;
+    int32_t cus = 0;
+    rc = plan_units(compute_units, &cus, fn);
+    if (rc != RF_OK) return rc;
+    *bytes_out = rf::linear_i8_workspace(M * rows_per_frame, in_features, out_features, dtype, cus);
+    return ok();
+}
+
+int rf_frame_linear_i8(const int8_t *x, const float *x_scale, const int8_t *weight, const float *weight_scale,
+                       const void *bias, const void *gate, const void *residual, void *y, const int32_t *frame_ids,
+                       int32_t M, int32_t T, int64_t rows_per_frame, int32_t in_features, int32_t out_features,
+                       int32_t activation, uint32_t flags, int32_t dtype, void *workspace, int64_t workspace_bytes,
+                       void *stream) {
+    const LinearIn in = {x, weight, bias, gate, residual, true, x_scale, weight_scale};
+    return linear_call(in, y, frame_ids, M, T, rows_per_frame, in_features, out_features, activation, flags, dtype,
+                       workspace, workspace_bytes, stream, "rf_frame_linear_i8");
+}
+
+int rf_frame_quantize(const void *x, int8_t *q, float *scale, const int32_t *frame_ids, int32_t M, int32_t T,
+                      int64_t rows_per_frame, int32_t features, int64_t x_stride, uint32_t flags, int32_t dtype,
+                      void *stream) {
+    const char *fn = "rf_frame_quantize";
+    if (!x || !q || !scale) return fail(RF_ERR_INVALID_ARG, "%s: NULL tensor", fn);
+    if (flags & ~(RF_ROWS_IN_FULL | RF_ROWS_OUT_FULL)) return fail(RF_ERR_INVALID_ARG, "%s: unknown flags 0x%x", fn, flags);
+    int32_t ids[RF_MAX_FRAMES];
+    int rc = check_id_list(frame_ids, M, T, ids, fn);
+    if (rc != RF_OK) return rc;
+    if (rows_per_frame <= 0 || features <= 0)
+        return fail(RF_ERR_INVALID_ARG, "%s: sizes must be positive (rows_per_frame=%lld features=%d)", fn,
+                    static_cast<long long>(rows_per_frame), features);
+    if (static_cast<double>(M) * static_cast<double>(rows_per_frame) > 2147483647.0)
+        return fail(RF_ERR_RANGE, "%s: more than 2^31 - 1 rows", fn);
+    if (dtype != RF_BF16 && dtype != RF_F32) return fail(RF_ERR_UNSUPPORTED, "%s: unknown dtype %d", fn, dtype);
+    if (features % 16 != 0 || features > RF_I8_FEATURES)
+        return fail(RF_ERR_UNSUPPORTED, "%s: %d features are no multiple of 16 up to %d", fn, features, RF_I8_FEATURES);
+    const int64_t esize = dtype == RF_F32 ? 4 : 2, stride = x_stride == 0 ? features : x_stride;
+    if (stride < features)
+        return fail(RF_ERR_INVALID_ARG, "%s: x_stride is below the row's %d elements", fn, features);
+    if (static_cast<double>(T) * static_cast<double>(rows_per_frame) * static_cast<double>(stride) * 4.0 > kMaxBytes)
+        return fail(RF_ERR_RANGE, "%s: sizes overflow 64-bit byte counts", fn);
+    if (!aligned16(x) || !aligned16(q) || (stride * esize) % 16 != 0)
+        return fail(RF_ERR_UNSUPPORTED, "%s: x, q and the row stride must be multiples of 16 bytes", fn);
+    if (!aligned4(scale)) return fail(RF_ERR_UNSUPPORTED, "%s: scale must be 4-byte aligned", fn);
+    const int64_t in_rows = rows_per_frame * ((flags & RF_ROWS_IN_FULL) ? T : M);
+    const int64_t out_rows = rows_per_frame * ((flags & RF_ROWS_OUT_FULL) ? T : M);
+    const int64_t in_bytes = ((in_rows - 1) * stride + features) * esize;
+    if (overlaps(q, out_rows * features, x, in_bytes) || overlaps(scale, out_rows * 4, x, in_bytes) ||
+        overlaps(scale, out_rows * 4, q, out_rows * features))
+        return fail(RF_ERR_INVALID_ARG, "%s: an output overlaps a tensor", fn);
+    rf::QuantizeParams p{};
+    p.x = x;
+    p.q = q;
+    p.scale = scale;
+    p.N = rows_per_frame;
+    p.x_stride = stride;
+    p.M = M;
+    p.K = features;
+    p.dtype = dtype;
+    row_frames(ids, M, (flags & RF_ROWS_IN_FULL) != 0, (flags & RF_ROWS_OUT_FULL) != 0, &p.frames);
+    return launched(rf::launch_quantize(p, static_cast<hipStream_t>(stream)), fn);
+}
+
+// Sizes common to a group norm and its workspace query.
+static int norm_sizes(int32_t M, int64_t N, int32_t C, int32_t groups, int32_t together, bool rows8, int32_t dtype,
+                      const char *fn) {
+    if (M <= 0 || N <= 0 || C <= 0 || groups <= 0 || together <= 0)
+        return fail(RF_ERR_INVALID_ARG, "%s: sizes must be positive (M=%d rows_per_frame=%lld channels=%d groups=%d "
+                    "frames_together=%d)", fn, M, static_cast<long long>(N), C, groups, together);
+    if (M > RF_MAX_FRAMES) return fail(RF_ERR_RANGE, "%s: M = %d exceeds %d frames", fn, M, RF_MAX_FRAMES);
+    if (static_cast<double>(M) * static_cast<double>(N) > 2147483647.0)
+        return fail(RF_ERR_RANGE, "%s: more than 2^31 - 1 rows", fn);
+    if (dtype != RF_BF16 && dtype != RF_F32) return fail(RF_ERR_UNSUPPORTED, "%s: unknown dtype %d", fn, dtype);
+    const int32_t vec = rows8 ? 16 : dtype == RF_F32 ? 4 : 8;
+    if (C % vec != 0 || C > RF_NORM_CHANNELS)
+        return fail(RF_ERR_UNSUPPORTED, "%s: %d channels are no multiple of %d up to %d", fn, C, vec, RF_NORM_CHANNELS);
+    if (C % groups != 0) return fail(RF_ERR_INVALID_ARG, "%s: %d groups do not divide %d channels", fn, groups, C);
+    if (M % together != 0)
+        return fail(RF_ERR_INVALID_ARG, "%s: frames_together = %d does not divide %d frames", fn, together, M);
+    return RF_OK;
+}
+
+int rf_frame_group_norm_workspace(int32_t M, int64_t rows_per_frame, int32_t channels, int32_t groups,
+                                  int32_t frames_together, int32_t rows_8bit, int32_t dtype, int32_t compute_units,
+                                  int64_t *bytes_out) {
+    const char *fn = "rf_frame_group_norm_workspace";
+    if (!bytes_out) return fail(RF_ERR_INVALID_ARG, "%s: NULL output", fn);
+    int rc = norm_sizes(M, rows_per_frame, channels, groups, frames_together, rows_8bit != 0, dtype, fn);
+    if (rc != RF_OK) return rc;
+    int32_t cus = 0;
+    rc = plan_units(compute_units, &cus, fn);
+    if (rc != RF_OK) return rc;
+    *bytes_out = rf::norm_workspace(M, rows_per_frame, channels, groups, frames_together, rows_8bit != 0, dtype, cus);
+    return ok();
+}
+
+int rf_frame_group_norm(const void *x, const void *weight, const void *bias, void *y, float *y_scale,
+                        const int32_t *frame_ids, int32_t M, int32_t T, int64_t rows_per_frame, int32_t channels,
+                        int32_t groups, int32_t frames_together, double eps, int32_t activation, int64_t x_stride,
+                        int64_t y_stride, uint32_t flags, int32_t dtype, void *workspace, int64_t workspace_bytes,
+                        void *stream) {
+    const char *fn = "rf_frame_group_norm";
+    if (!x || !y) return fail(RF_ERR_INVALID_ARG, "%s: NULL tensor", fn);
+    if (flags & ~(RF_ROWS_IN_FULL | RF_ROWS_OUT_FULL | RF_AFFINE_PER_FRAME))
+        return fail(RF_ERR_INVALID_ARG, "%s: unknown flags 0x%x", fn, flags);
+    if ((flags & RF_AFFINE_PER_FRAME) && !weight && !bias)
+        return fail(RF_ERR_INVALID_ARG, "%s: a weight and bias per frame need one of them", fn);
+    if (activation < RF_ACT_NONE || activation > RF_ACT_SILU)
+        return fail(RF_ERR_INVALID_ARG, "%s: unknown activation %d", fn, activation);
+    if (!(eps >= 1e-30 && eps <= 1e30)) return fail(RF_ERR_INVALID_ARG, "%s: eps outside 1e-30..1e30", fn);
+    int32_t ids[RF_MAX_FRAMES];
+    int rc = check_id_list(frame_ids, M, T, ids, fn);
+    if (rc != RF_OK) return rc;
+    const bool rows8 = y_scale != nullptr;
+    rc = norm_sizes(M, rows_per_frame, channels, groups, frames_together, rows8, dtype, fn);
+    if (rc != RF_OK) return rc;
+    const int64_t N = rows_per_frame, C = channels, esize = dtype == RF_F32 ? 4 : 2, out_size = rows8 ? 1 : esize;
+    const int64_t xs = x_stride == 0 ? C : x_stride, ys = y_stride == 0 ? C : y_stride;
+    if (xs < C || ys < C) return fail(RF_ERR_INVALID_ARG, "%s: a row stride is below the row's %d elements", fn, channels);
+    if (rows8 && ys != C) return fail(RF_ERR_INVALID_ARG, "%s: rows in 8 bits are contiguous", fn);
+    if (static_cast<double>(T) * static_cast<double>(N) * static_cast<double>(xs > ys ? xs : ys) * 4.0 > kMaxBytes)
+        return fail(RF_ERR_RANGE, "%s: sizes overflow 64-bit byte counts", fn);
+    if (!aligned16(x) || !aligned16(y) || !aligned16(weight) || !aligned16(bias) || (xs * esize) % 16 != 0 ||
+        (ys * out_size) % 16 != 0)
+        return fail(RF_ERR_UNSUPPORTED, "%s: pointers and row strides must be multiples of 16 bytes", fn);
+    if (!aligned4(y_scale)) return fail(RF_ERR_UNSUPPORTED, "%s: y_scale must be 4-byte aligned", fn);
+    const bool in_full = (flags & RF_ROWS_IN_FULL) != 0 || M == T, out_full = (flags & RF_ROWS_OUT_FULL) != 0 || M == T;
+    const int64_t in_rows = N * (in_full ? T : M), out_rows = N * (out_full ? T : M);
+    const bool in_place = !rows8 && y == x && xs == ys && in_full == out_full;
+    if (!in_place && rows_overlap(y, out_rows, ys * out_size, C * out_size, x, in_rows, xs * esize, C * esize))
+        return fail(RF_ERR_INVALID_ARG, "%s: y overlaps x", fn);
+    const int64_t in_bytes = ((in_rows - 1) * xs + C) * esize, out_bytes = ((out_rows - 1) * ys + C) * out_size;
+    const int64_t affine = C * esize * ((flags & RF_AFFINE_PER_FRAME) ? T : 1);
+    if ((weight && overlaps(y, out_bytes, weight, affine)) || (bias && overlaps(y, out_bytes, bias, affine)))
+        return fail(RF_ERR_INVALID_ARG, "%s: y overlaps an input", fn);
+    if (rows8 && (overlaps(y_scale, out_rows * 4, x, in_bytes) || overlaps(y_scale, out_rows * 4, y, out_bytes) ||
+                  (weight && overlaps(y_scale, out_rows * 4, weight, affine)) ||
+                  (bias && overlaps(y_scale, out_rows * 4, bias, affine))))
+        return fail(RF_ERR_INVALID_ARG, "%s: y_scale overlaps a tensor", fn);
+    if (workspace) {
+        if (workspace_bytes < 0) return fail(RF_ERR_INVALID_ARG, "%s: workspace_bytes < 0", fn);
+        if (!aligned16(workspace)) return fail(RF_ERR_UNSUPPORTED, "%s: workspace must be 16-byte aligned", fn);
+        if (workspace_bytes > 0 &&
+            (overlaps(workspace, workspace_bytes, x, in_bytes) || overlaps(workspace, workspace_bytes, y, out_bytes) ||
+             (weight && overlaps(workspace, workspace_bytes, weight, affine)) ||
+             (bias && overlaps(workspace, workspace_bytes, bias, affine)) ||
+             (rows8 && overlaps(workspace, workspace_bytes, y_scale, out_rows * 4))))
+            return fail(RF_ERR_INVALID_ARG, "%s: workspace overlaps a tensor", fn);
+    }
+    rf::NormParams p{};
+    rc = query_geometry(&p.geo, fn);
+    if (rc != RF_OK) return rc;
+    const int64_t need = rf::norm_workspace(M, N, channels, groups, frames_together, rows8, dtype, p.geo.cus);
+    if (need > 0 && (!workspace || workspace_bytes < need))
+        return fail(RF_ERR_INVALID_ARG, "%s: workspace of %lld bytes, %lld needed on %d compute units", fn,
+                    static_cast<long long>(workspace ? workspace_bytes : 0), static_cast<long long>(need), p.geo.cus);
+    p.x = x;
+    p.weight = weight;
+    p.bias = bias;
+    p.y = y;
+    p.y_scale = y_scale;
+    p.N = N;
+    p.x_stride = xs;
+    p.y_stride = ys;
+    p.eps = eps;
+    p.M = M;
+    p.C = channels;
+    p.groups = groups;
+    p.together = frames_together;
+    p.activation = activation;
+    p.dtype = dtype;
+    p.affine_rows = (flags & RF_AFFINE_PER_FRAME) != 0;
+    p.ws = workspace;
+    row_frames(ids, M, in_full, out_full, &p.frames);
+    return launched(rf::launch_norm(p, static_cast<hipStream_t>(stream)), fn);
 }
 
 int rf_probe_mfma_bf16(const void *operands, int32_t workgroups, int32_t rounds, float *sink, void *stream) {

@@ -228,6 +228,46 @@ struct LinearParams {
 int64_t linear_workspace(int64_t rows, int32_t K, int32_t n_out, int32_t dtype, int32_t cus);
 hipError_t launch_linear(const LinearParams &p, hipStream_t stream);
 
+// The same of 8-bit integers: y = residual + gate * act(sum x weight * x_scale * w_scale + bias);
+// p.dtype is that of bias, gate, residual and y.
+hipError_t launch_linear_i8(const LinearParams &p, const float *x_scale, const float *w_scale, hipStream_t stream);
+int64_t linear_i8_workspace(int64_t rows, int32_t K, int32_t n_out, int32_t dtype, int32_t cus);
+
+// Rows in 8 bits with a scale each. x_stride in elements.
+struct QuantizeParams {
+    const void *x;
+    int8_t *q;
+    float *scale;
+    int64_t N;                   // rows per frame
+    int64_t x_stride;
+    int32_t M, K;
+    int32_t dtype;
+    RowFrames frames;
+};
+
+hipError_t launch_quantize(const QuantizeParams &p, hipStream_t stream);
+
+// Group norm: y = act((x - mean) / sqrt(var + eps) * weight + bias). Strides in elements.
+struct NormParams {
+    const void *x, *weight, *bias;
+    void *y;
+    float *y_scale;              // y's rows are in 8 bits; NULL: in dtype
+    int64_t N;                   // rows per frame
+    int64_t x_stride, y_stride;
+    double eps;
+    int32_t M, C, groups, together;
+    int32_t activation;
+    int32_t dtype;
+    int32_t affine_rows;         // weight and bias are [T][C]
+    RowFrames frames;
+    void *ws;
+    DeviceGeometry geo;
+};
+
+int64_t norm_workspace(int32_t M, int64_t N, int32_t C, int32_t groups, int32_t together, bool rows8, int32_t dtype,
+                       int32_t cus);
+hipError_t launch_norm(const NormParams &p, hipStream_t stream);
+
 // Device probes (measurement support): threads per workgroup of the matrix and
 // LDS probes, and of the HBM read probe.
 constexpr int kProbeThreads = 256;

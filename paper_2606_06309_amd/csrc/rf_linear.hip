@@ -39,16 +39,13 @@
 //    product without epilogue takes 6.5: this is not the least that it can take.
 #include "rf_device.h"
 #include "rf_linear_plan.h"
+#include "rf_rows.h"
 
 namespace rf {
 namespace {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
-typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
 constexpr int kStep = kLinearStep;
 
@@ -65,6 +62,7 @@ struct LinearKArgs {
     int32_t row_tiles, col_tiles, tiles, per_xcd, xcds;
     int32_t activation, gate_rows;
     int32_t stream;            // 256-row tiles: y goes past the caches
+    const float *x_scale, *w_scale;   // of 8-bit rows and features
     RowFrames frames;
 };
 
@@ -109,93 +107,6 @@ __device__ __forceinline__ f32x4_t mma16(u32x4_t a, u32x4_t b, f32x4_t c) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[e], fb[e], c, 0, 0, 0);
         return c;
-    }
-}
-
-// kN (4 or 8) consecutive elements, widened / rounded once to nearest even.
-template <typename E, int kN>
-__device__ __forceinline__ void load_n(const void *p, int64_t at, float (&v)[kN]) {
-    if constexpr (sizeof(E) == 4) {
-#pragma unroll
-        for (int i = 0; i < kN; i += 4) {
-            const f32x4_t x = *reinterpret_cast<const f32x4_t *>(static_cast<const float *>(p) + at + i);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[i + e] = x[e];
-        }
-    } else {
-        typedef uint32_t raw_t __attribute__((ext_vector_type(kN / 2)));
-        const raw_t x = *reinterpret_cast<const raw_t *>(static_cast<const uint16_t *>(p) + at);
-#pragma unroll
-        for (int e = 0; e < kN / 2; ++e) {
-            v[2 * e] = __uint_as_float(x[e] << 16);
-            v[2 * e + 1] = __uint_as_float(x[e] & 0xffff0000u);
-        }
-    }
-}
-template <typename E, int kN>
-__device__ __forceinline__ void store_n(void *p, int64_t at, const float (&v)[kN]) {
-    if constexpr (sizeof(E) == 4) {
-#pragma unroll
-        for (int i = 0; i < kN; i += 4)
-            *reinterpret_cast<f32x4_t *>(static_cast<float *>(p) + at + i) = f32x4_t{v[i], v[i + 1], v[i + 2], v[i + 3]};
-    } else {
-        typedef uint32_t raw_t __attribute__((ext_vector_type(kN / 2)));
-        raw_t x;
-#pragma unroll
-        for (int e = 0; e < kN / 2; ++e) {
-            const bf16x2_t b = {static_cast<__bf16>(v[2 * e]), static_cast<__bf16>(v[2 * e + 1])};
-            x[e] = __builtin_bit_cast(uint32_t, b);
-        }
-        *reinterpret_cast<raw_t *>(static_cast<uint16_t *>(p) + at) = x;
-    }
-}
-
-// The same past the caches: for results, which are written once and as whole lines.
-template <typename E>
-__device__ __forceinline__ void stream_8(void *p, int64_t at, const float (&v)[8]) {
-    if constexpr (sizeof(E) == 4) {
-#pragma unroll
-        for (int i = 0; i < 8; i += 4)
-            __builtin_nontemporal_store((f32x4_t{v[i], v[i + 1], v[i + 2], v[i + 3]}),
-                                        reinterpret_cast<f32x4_t *>(static_cast<float *>(p) + at + i));
-    } else {
-        u32x4_t x;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const bf16x2_t b = {static_cast<__bf16>(v[2 * e]), static_cast<__bf16>(v[2 * e + 1])};
-            x[e] = __builtin_bit_cast(uint32_t, b);
-        }
-        __builtin_nontemporal_store(x, reinterpret_cast<u32x4_t *>(static_cast<uint16_t *>(p) + at));
-    }
-}
-
-// x / (1 + 2^t): both sigmoid forms. 2^t = inf gives 0. (The reciprocal is the hardware's, off by one
-// last place of fp32; a divide would be ten instructions, and 2^t is off by as much.)
-__device__ __forceinline__ float gated(float x, float t) {
-    return x * __builtin_amdgcn_rcpf(1.0f + fast_exp2(t));
-}
-template <int kN>
-__device__ __forceinline__ void activate(int kind, float (&v)[kN]) {
-    constexpr float kLog2e = 1.4426950408889634f;
-    if (kind == RF_ACT_GELU) {
-#pragma unroll
-        for (int e = 0; e < kN; ++e) v[e] = 0.5f * v[e] * (1.0f + erff(v[e] * 0.70710678118654752f));
-    } else if (kind == RF_ACT_GELU_TANH) {
-        // x/2 (1 + tanh u) = x / (1 + e^(-2u))
-#pragma unroll
-        for (int e = 0; e < kN; ++e)
-            v[e] = gated(v[e], (-2.0f * 0.79788456080286536f * kLog2e) * (v[e] + 0.044715f * (v[e] * v[e] * v[e])));
-    } else {
-#pragma unroll
-        for (int e = 0; e < kN; ++e) v[e] = gated(v[e], -kLog2e * v[e]);
-    }
-}
-
-__device__ __forceinline__ void widen8(u32x4_t x, float (&v)[8]) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        v[2 * e] = __uint_as_float(x[e] << 16);
-        v[2 * e + 1] = __uint_as_float(x[e] & 0xffff0000u);
     }
 }
 
@@ -712,6 +623,39 @@ __global__ __launch_bounds__(256) void linear_join_kernel(const LinearKArgs a) {
     fin.store(a, c, v);
 }
 
+typedef int32_t i32x4_t __attribute__((ext_vector_type(4)));
+typedef int32_t i32x16_t __attribute__((ext_vector_type(16)));
+
+// 8-bit integers: a wave has 32 rows x 32 features, straight from memory.
+template <typename E>
+__global__ __launch_bounds__(256) void linear_i8_kernel(const LinearKArgs a) {
+    const int lane = threadIdx.x & 63, col = lane & 31, grp = lane >> 5;
+    const int64_t id = static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / 64;
+    if (id >= static_cast<int64_t>(a.row_tiles) * a.col_tiles) return;
+    const int rt = static_cast<int>(id / a.col_tiles), ct = static_cast<int>(id - static_cast<int64_t>(rt) * a.col_tiles);
+    const uint32_t r = static_cast<uint32_t>(rt) * 32 + col;
+    const uint8_t *x = x_row(a, r), *w = w_row(a, ct * 32 + col);
+    i32x16_t acc = i32x16_t{};
+    for (int64_t at = grp * 16; at - grp * 16 < a.row_bytes; at += 32) {
+        const bool in = at < a.row_bytes;
+        i32x4_t wf = *reinterpret_cast<const i32x4_t *>(in ? w + at : w), xf = *reinterpret_cast<const i32x4_t *>(in ? x + at : x);
+        if (!in) wf = xf = i32x4_t{0, 0, 0, 0};
+        acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf, xf, acc, 0, 0, 0);
+    }
+    if (r >= a.rows) return;
+    const uint32_t m = r / a.N;
+    const float xs = a.x_scale[static_cast<int64_t>(a.frames.in(m)) * a.N + (r - m * a.N)];
+#pragma unroll
+    for (int g4 = 0; g4 < 4; ++g4) {
+        const int c = ct * 32 + g4 * 8 + grp * 4;
+        if (c >= a.n_out) continue;
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = static_cast<float>(acc[g4 * 4 + e]) * xs * a.w_scale[c + e];
+        finish<E, 4>(a, r, c, v);
+    }
+}
+
 template <typename E>
 void run(const LinearPlan &p, const LinearKArgs &a, bool far, dim3 grid, hipStream_t stream) {
     switch (p.form) {
@@ -795,6 +739,36 @@ hipError_t launch_linear(const LinearParams &p, hipStream_t stream) {
     const dim3 jg(static_cast<uint32_t>(blocks));
     if (p.dtype == RF_F32) hipLaunchKernelGGL(linear_join_kernel<float>, jg, dim3(256), 0, stream, a);
     else hipLaunchKernelGGL(linear_join_kernel<uint16_t>, jg, dim3(256), 0, stream, a);
+    return hipGetLastError();
+}
+
+int64_t linear_i8_workspace(int64_t, int32_t, int32_t, int32_t, int32_t) { return 0; }
+
+hipError_t launch_linear_i8(const LinearParams &p, const float *x_scale, const float *w_scale, hipStream_t stream) {
+    LinearKArgs a{};
+    a.x = static_cast<const uint8_t *>(p.x);
+    a.w = static_cast<const uint8_t *>(p.weight);
+    a.bias = p.bias;
+    a.gate = p.gate;
+    a.residual = p.residual;
+    a.y = p.y;
+    a.x_scale = x_scale;
+    a.w_scale = w_scale;
+    a.row_bytes = p.K;
+    a.rows = static_cast<uint32_t>(p.M * p.N);
+    a.N = static_cast<uint32_t>(p.N);
+    a.n_out = p.n_out;
+    a.parts = 1;
+    a.row_tiles = static_cast<int32_t>((p.M * p.N + 31) / 32);
+    a.col_tiles = (p.n_out + 31) / 32;
+    a.activation = p.activation;
+    a.gate_rows = p.gate_rows;
+    a.frames = p.frames;
+    const int64_t blocks = (static_cast<int64_t>(a.row_tiles) * a.col_tiles + 3) / 4;
+    if (blocks > 0xffffff) return hipErrorInvalidConfiguration;
+    const dim3 g(static_cast<uint32_t>(blocks));
+    if (p.dtype == RF_F32) hipLaunchKernelGGL(linear_i8_kernel<float>, g, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL(linear_i8_kernel<uint16_t>, g, dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 

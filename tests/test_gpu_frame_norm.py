@@ -1,0 +1,195 @@
+"""Group norm with an activation, channels last, and its rows in 8 bits against the definition in 64 bits."""
+import pytest
+import torch
+
+import block_reference as block
+import rows_reference as ref
+
+rf = pytest.importorskip("paper_2606_06309_amd.binding")
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def draw(shape, dtype, seed, scale=1.0, mean=0.0):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return (torch.randn(shape, generator=g, device="cuda", dtype=F32) * scale + mean).to(dtype)
+
+
+def check(x, groups, w=None, b=None, eps=1e-5, act="none", M=1, T=None, together=1, what="", **kw):
+    """x [M * N][C]: rows in its type, and in 8 bits where its channels allow."""
+    N, C = x.shape[0] // M, x.shape[1]
+    frames = {} if M == 1 and T is None else dict(frame_ids=list(range(M)), T=M, rows_per_frame=N, frames_together=together)
+    y, err = ref.group_norm(x.view(M, N, C), groups, w, b, eps, act, together)
+    y, err = y.view(-1, C), err.view(-1, C)
+    got = rf.rf_frame_group_norm(x, groups, w, b, eps, act, **frames, **kw)
+    block.assert_within(got, *ref.rounded(y, err, x.dtype), what)
+    if C % 16 == 0:
+        check8(rf.rf_frame_group_norm(x, groups, w, b, eps, act, int8=True, **frames), y, err, what)
+
+
+def check8(got, y, err, what=""):
+    """A row's scale is its largest magnitude / 127, off as that is; a value is half a step off besides."""
+    q, s = got
+    top, slack = y.abs().amax(1), err.amax(1)
+    assert bool(((s.double() - top / 127).abs() <= slack / 127 + 2 * ref.U * top / 127 + 1e-38).all()), what
+    block.assert_within(q.double() * s.double()[:, None], y, err + (0.5 + 127 * 3 * ref.U) * s.double()[:, None], what)
+
+
+# rows of a frame, channels, groups: one row and many, groups of one channel and of all, that straddle 16 bytes, and
+# more channels than a workgroup has columns
+SIZES = [(1, 8, 1), (1, 16, 16), (2, 48, 3), (64, 128, 32), (527, 320, 32), (33, 336, 7), (100, 72, 9), (1000, 64, 64),
+         (257, 1536, 32), (70, 2048, 1), (40, 2064, 43), (9, 4112, 257), (5, 8192, 32), (3, 8176, 8176), (1560, 640, 32),
+         (6000, 512, 32), (20000, 128, 32), (30011, 24, 2), (4099, 8, 8), (700, 5120, 40)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("size", SIZES)
+def test_sizes(size, dtype):
+    N, C, G = size
+    if dtype == F32 and (C == 8 and G == 1):
+        C = 4
+    x = draw((N, C), dtype, 1) * torch.exp(draw((C,), F32, 2, 0.5)).to(dtype) + draw((C,), dtype, 3)
+    check(x, G, what=f"{size} plain")
+    w, b = draw((C,), dtype, 4, 0.3, 1.0), draw((C,), dtype, 5, 0.4)
+    check(x, G, w, b, act="silu", what=f"{size} affine silu")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("act", ["none", "gelu", "gelu_tanh", "silu"])
+def test_activations_and_affine(act, dtype):
+    M, N, C, G = 2, 150, 96, 6
+    x = draw((M * N, C), dtype, 6, 3.0)
+    w, b = draw((C,), dtype, 7, 4.0), draw((C,), dtype, 8, 5.0)
+    for weight in (None, w):
+        for bias in (None, b):
+            check(x, G, weight, bias, 1e-6, act, M, M, what=f"{act} {weight is None} {bias is None}")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("together", [1, 2, 3, 6])
+@pytest.mark.parametrize("N", [1, 40, 900])
+def test_frames_together(N, together, dtype):
+    M, C, G = 6, 160, 5
+    x = draw((M * N, C), dtype, 9) + torch.arange(M, device="cuda").repeat_interleave(N)[:, None].to(dtype)
+    check(x, G, draw((C,), dtype, 10), draw((C,), dtype, 11), act="silu", M=M, T=M, together=together)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N,C,G", [(300, 64, 4), (5000, 320, 32), (7, 32, 32)])
+def test_small_deviations_around_a_large_mean(N, C, G, dtype):
+    """A mean of 500 deviations; the first row is not like the others."""
+    x = draw((N, C), F32, 12, 1.0, 500.0)
+    x[0] = 0.0
+    check(x.to(dtype), G, draw((C,), dtype, 13), None)
+    x[0] = -40000.0
+    check(x.to(dtype), G)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_constant_groups(dtype):
+    """No deviation at all: the bias, whatever the constant."""
+    N, C, G = 70, 64, 8
+    x = torch.empty((N, C), dtype=dtype, device="cuda")
+    x[:] = torch.tensor([0.0, 1.0, -3.0, 1e-30, 2.0 ** 60, 100.0, 0.375, -2.0 ** 30], device="cuda").repeat_interleave(8).to(dtype)
+    b = draw((C,), dtype, 14)
+    y = rf.rf_frame_group_norm(x, G, None, b)
+    assert torch.equal(y, b.expand(N, C))
+    zero = rf.rf_frame_group_norm(x, G, int8=True)
+    assert not bool(zero[0].any()) and not bool(zero[1].any())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("N,C,G", [(60, 128, 8), (3000, 2080, 5)])
+def test_not_finite_spoils_only_its_group(N, C, G, value, dtype):
+    M, per = 2, C // G
+    x = draw((M * N, C), dtype, 15)
+    want, err = ref.rounded(*ref.group_norm(x.view(M, N, C), G), dtype)
+    x[N + N // 2, per] = value            # frame 1, group 1
+    y = rf.rf_frame_group_norm(x, G, frame_ids=[0, 1], T=2, rows_per_frame=N).view(M, N, C)
+    assert bool(torch.isnan(y[1, :, per:2 * per]).all())
+    ok = torch.ones((M, N, C), dtype=torch.bool, device="cuda")
+    ok[1, :, per:2 * per] = False
+    block.assert_within(torch.where(ok, y.double(), 0), torch.where(ok, want, 0), torch.where(ok, err, 0))
+    q, s = rf.rf_frame_group_norm(x, G, frame_ids=[0, 1], T=2, rows_per_frame=N, int8=True)
+    assert bool(torch.isfinite(s[:N]).all()) and bool(torch.isnan(s[N:]).all()) and not bool(q[N:].any())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N", [1, 9, 640])
+@pytest.mark.parametrize("in_full,out_full", [(False, False), (False, True), (True, False), (True, True)])
+def test_frames(N, in_full, out_full, dtype):
+    """Listed frames, their own weight and bias, strided rows on both sides; other frames are neither read nor written."""
+    T, ids, C, G = 7, [0, 3, 4, 6], 96, 12
+    M, pos = len(ids), block.positions(ids, N, "cuda")
+    at = torch.tensor(ids, device="cuda")
+    listed = torch.zeros(T * N, dtype=torch.bool, device="cuda")
+    listed[pos] = True
+    wide = draw((T * N, C + 32), dtype, 16)
+    wide[~listed] = float("nan")
+    w, b = draw((T, C), dtype, 17), draw((T, C), dtype, 18)
+    w[[1, 2, 5]] = float("nan")
+    x = wide[:, 8:8 + C]
+    xin = x if in_full else wide[pos][:, 8:8 + C]
+    y, err = ref.group_norm(x[pos].reshape(M, N, C), G, w[at], b[at], 1e-5, "silu", 2)
+    y, err = y.view(-1, C), err.view(-1, C)
+    kw = dict(frame_ids=ids, T=T, rows_per_frame=N, in_full=in_full, out_full=out_full, frames_together=2)
+    buf = draw((T * N if out_full else M * N, C + 16), dtype, 19)
+    old = buf.clone()
+    out = buf[:, 16:]
+    assert rf.rf_frame_group_norm(xin, G, w, b, 1e-5, "silu", out=out, **kw) is out
+    block.assert_within(out[pos] if out_full else out, *ref.rounded(y, err, dtype))
+    assert torch.equal(buf[:, :16], old[:, :16])
+    n = out.shape[0]
+    q, s = torch.full((n, C), 77, dtype=torch.int8, device="cuda"), torch.full((n,), 5.0, device="cuda")
+    rf.rf_frame_group_norm(xin, G, w, b, 1e-5, "silu", out=q, out_scale=s, **kw)
+    check8((q[pos], s[pos]) if out_full else (q, s), y, err)
+    if out_full:
+        assert torch.equal(buf[~listed], old[~listed])
+        assert bool((q[~listed] == 77).all()) and bool((s[~listed] == 5.0).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N,C", [(50, 64), (2000, 320), (40000, 128)])
+def test_in_place(N, C, dtype):
+    x = draw((2 * N, C), dtype, 20)
+    kw = dict(frame_ids=[0, 1], T=2, rows_per_frame=N, activation="silu")
+    want = rf.rf_frame_group_norm(x, 16, **kw)
+    y = x.clone()
+    assert rf.rf_frame_group_norm(y, 16, out=y, **kw) is y
+    assert torch.equal(y, want)
+    wide = draw((4 * N, C), dtype, 21)      # full rows in place: two of four frames
+    wide[:N], wide[3 * N:] = x[:N], x[N:]
+    old = wide.clone()
+    kw = dict(frame_ids=[0, 3], T=4, rows_per_frame=N, activation="silu", in_full=True, out_full=True)
+    rf.rf_frame_group_norm(wide, 16, out=wide, **kw)
+    assert torch.equal(wide[:N], want[:N]) and torch.equal(wide[3 * N:], want[N:])
+    assert torch.equal(wide[N:3 * N], old[N:3 * N])
+
+
+def test_rows_far_apart():
+    """Rows 1.5 GB apart on both sides."""
+    N, C, stride = 4, 64, (1 << 30) * 3 // 4
+    x = torch.empty(3 * stride + C, dtype=BF16, device="cuda").as_strided((N, C), (stride, 1))
+    y = torch.empty(3 * stride + C, dtype=BF16, device="cuda").as_strided((N, C), (stride, 1))
+    x.copy_(draw((N, C), BF16, 22))
+    rf.rf_frame_group_norm(x, 4, out=y)
+    block.assert_within(y, *ref.rounded(*(t[0] for t in ref.group_norm(x.contiguous()[None], 4)), BF16))
+
+
+def test_many_frames():
+    """256 frames, every other one of 512 groups of one channel."""
+    T, N, C = 256, 3, 512
+    x = draw((T * N, C), F32, 23)
+    y, err = ref.rounded(*ref.group_norm(x.view(T, N, C), C), F32)
+    got = rf.rf_frame_group_norm(x, C, frame_ids=range(T), T=T, rows_per_frame=N)
+    block.assert_within(got.view(T, N, C), y, err)
+
+
+def test_results_repeat():
+    """The parts of a group are joined in one order."""
+    x = draw((3 * 7000, 192), BF16, 24)
+    runs = [rf.rf_frame_group_norm(x, 24, activation="silu", frame_ids=[0, 1, 2], T=3, rows_per_frame=7000, frames_together=3)
+            for _ in range(4)]
+    assert all(torch.equal(runs[0], r) for r in runs[1:])
