@@ -46,6 +46,8 @@ namespace {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef int32_t i32x4_t __attribute__((ext_vector_type(4)));
+typedef int32_t i32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr int kStep = kLinearStep;
 
@@ -85,9 +87,32 @@ __device__ __forceinline__ u32x4_t buffer_load16(__amdgpu_buffer_rsrc_t r, int v
     return __builtin_amdgcn_raw_buffer_load_b128(r, voffset, soffset, 0);
 }
 
-template <typename E>
-__device__ __forceinline__ f32x16_t mma32(u32x4_t a, u32x4_t b, f32x16_t c) {
-    if constexpr (sizeof(E) == 2) {
+// What a product's operands (bf16, fp32 or 8-bit integers) are summed in.
+template <typename In>
+struct Value {
+    typedef float type;
+};
+template <>
+struct Value<int8_t> {
+    typedef int32_t type;
+};
+template <typename In>
+struct Sums {
+    typedef f32x16_t of32;
+    typedef f32x4_t of16;
+};
+template <>
+struct Sums<int8_t> {
+    typedef i32x16_t of32;
+    typedef i32x4_t of16;
+};
+
+template <typename In>
+__device__ __forceinline__ typename Sums<In>::of32 mma32(u32x4_t a, u32x4_t b, typename Sums<In>::of32 c) {
+    if constexpr (sizeof(In) == 1) {
+        return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4_t, a), __builtin_bit_cast(i32x4_t, b), c, 0,
+                                                     0, 0);
+    } else if constexpr (sizeof(In) == 2) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b),
                                                        c, 0, 0, 0);
     } else {
@@ -97,9 +122,12 @@ __device__ __forceinline__ f32x16_t mma32(u32x4_t a, u32x4_t b, f32x16_t c) {
         return c;
     }
 }
-template <typename E>
-__device__ __forceinline__ f32x4_t mma16(u32x4_t a, u32x4_t b, f32x4_t c) {
-    if constexpr (sizeof(E) == 2) {
+template <typename In>
+__device__ __forceinline__ typename Sums<In>::of16 mma16(u32x4_t a, u32x4_t b, typename Sums<In>::of16 c) {
+    if constexpr (sizeof(In) == 1) {
+        return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4_t, a), __builtin_bit_cast(i32x4_t, b), c, 0,
+                                                     0, 0);
+    } else if constexpr (sizeof(In) == 2) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b),
                                                        c, 0, 0, 0);
     } else {
@@ -110,16 +138,25 @@ __device__ __forceinline__ f32x4_t mma16(u32x4_t a, u32x4_t b, f32x4_t c) {
     }
 }
 
-// Bias and gate of kN neighbouring features c.., in fp32 as everything between the
-// products' sums and the result's one rounding.
-template <int kN>
+// Scales (of 8-bit integers), bias and gate of kN neighbouring features c.., in fp32 as everything
+// between the products' sums and the result's one rounding.
+template <typename In, int kN>
 struct Epilogue {
-    float bias[kN], gate[kN];
+    float bias[kN], gate[kN], scale[kN];
     // frame: whose gate (-1: gate_of will say)
     template <typename E>
     __device__ __forceinline__ void load(const LinearKArgs &a, int c, int frame) {
+        if constexpr (sizeof(In) == 1) load_n<float, kN>(a.w_scale, c, scale);
         if (a.bias) load_n<E, kN>(a.bias, c, bias);
         if (frame >= 0) gate_of<E>(a, c, frame);
+    }
+    // sums of integers as the products that they stand for (x_scale: their row's; a sum above 2^24 is
+    // rounded). Nothing after exact sums may depend on how they were split, so no product is fused with
+    // a later addition in one kernel and not in another.
+    __device__ __forceinline__ void scaled(float x_scale, const int32_t (&sums)[kN], float (&v)[kN]) const {
+#pragma clang fp contract(off)
+#pragma unroll
+        for (int e = 0; e < kN; ++e) v[e] = static_cast<float>(sums[e]) * x_scale * scale[e];
     }
     template <typename E>
     __device__ __forceinline__ void gate_of(const LinearKArgs &a, int c, int frame) {
@@ -132,29 +169,43 @@ struct Epilogue {
         }
         if (a.activation != RF_ACT_NONE) activate(a.activation, v);
         if (a.gate) {
+            if constexpr (sizeof(In) == 1) {
+#pragma clang fp contract(off)
 #pragma unroll
-            for (int e = 0; e < kN; ++e) v[e] *= gate[e];
+                for (int e = 0; e < kN; ++e) v[e] *= gate[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < kN; ++e) v[e] *= gate[e];
+            }
         }
     }
 };
 
+// A row of the product among the rows read: that of its scale.
+__device__ __forceinline__ int64_t row_in(const LinearKArgs &a, uint32_t r) {
+    const uint32_t m = r / a.N;
+    return static_cast<int64_t>(a.frames.in(m)) * a.N + (r - m * a.N);
+}
+
 // The epilogue of kN neighbouring features c.. of product row r: what it takes from
 // memory, early, and the rest.
-template <typename E, int kN>
+template <typename In, typename E, int kN>
 struct Finish {
-    Epilogue<kN> ep;
-    float residual[kN];
+    Epilogue<In, kN> ep;
+    float residual[kN], x_scale;
     int64_t dst;
-    int frame, out;
+    int frame, in, out;
     // (the frames' loads and what depends on them apart: loads return in order, so a wait
     // for a frame is one for all loads before it)
     __device__ __forceinline__ void frames(const LinearKArgs &a, uint32_t r) {
         const uint32_t m = r / a.N;
         frame = a.frames.frame[m];
+        in = a.frames.in(m);
         out = a.frames.out(m);
     }
     __device__ __forceinline__ void load(const LinearKArgs &a, uint32_t r, int c) {
         dst = (static_cast<int64_t>(out) * a.N + r % a.N) * a.n_out;
+        if constexpr (sizeof(In) == 1) x_scale = a.x_scale[static_cast<int64_t>(in) * a.N + r % a.N];
         ep.template load<E>(a, c, frame);
         if (a.residual) load_n<E, kN>(a.residual, dst + c, residual);
     }
@@ -166,13 +217,27 @@ struct Finish {
         }
         store_n<E, kN>(a.y, dst + c, v);
     }
+    __device__ __forceinline__ void store(const LinearKArgs &a, int c, const int32_t (&sums)[kN]) const {
+        float v[kN];
+        ep.scaled(x_scale, sums, v);
+        store(a, c, v);
+    }
 };
-template <typename E, int kN>
-__device__ __forceinline__ void finish(const LinearKArgs &a, uint32_t r, int c, float (&v)[kN]) {
-    Finish<E, kN> f;
+template <typename In, typename E, int kN, typename V>
+__device__ __forceinline__ void finish(const LinearKArgs &a, uint32_t r, int c, V (&v)[kN]) {
+    Finish<In, E, kN> f;
     f.frames(a, r);
     f.load(a, r, c);
     f.store(a, c, v);
+}
+
+// kN neighbouring sums of a part of the reduction, to the workspace.
+template <int kN, typename V>
+__device__ __forceinline__ void store_part(const LinearKArgs &a, int part, uint32_t r, int c, const V (&v)[kN]) {
+    typedef V v4_t __attribute__((ext_vector_type(4)));
+    V *to = reinterpret_cast<V *>(a.ws) + (static_cast<int64_t>(part) * a.rows + r) * a.n_out + c;
+#pragma unroll
+    for (int i = 0; i < kN; i += 4) *reinterpret_cast<v4_t *>(to + i) = v4_t{v[i], v[i + 1], v[i + 2], v[i + 3]};
 }
 
 // Product row r's (clamped to the last one) first byte in x.
@@ -202,7 +267,8 @@ __device__ __forceinline__ bool tile_of(const LinearKArgs &a, int bid, int &rt, 
 
 // kRB blocks of 32 rows to a wave, kWR x kWC waves of (32 kRB rows x 64 features).
 // kFar: rows of x may lie further than 2 GB from the tile's first (64-bit addresses).
-template <typename E, int kRB, int kWR, int kWC, bool kFar>
+// In: the operands' type, E: y's.
+template <typename In, typename E, int kRB, int kWR, int kWC, bool kFar>
 __global__ __launch_bounds__(64 * kWR * kWC) __attribute__((amdgpu_waves_per_eu(2)))
 void linear_tile_kernel(const LinearKArgs a) {
     constexpr int kWaves = kWR * kWC, kBM = 32 * kRB * kWR, kBN = 64 * kWC;
@@ -210,6 +276,7 @@ void linear_tile_kernel(const LinearKArgs a) {
     constexpr int kXBuf = kBM * kStep, kWBuf = kBN * kStep;
     // [W, even step][W, odd][x, even][x, odd]
     __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * (kXBuf + kWBuf)];
+    constexpr bool kI8 = sizeof(In) == 1;
     static_assert((kXBuf & (kXBuf - 1)) == 0 && (kWBuf & (kWBuf - 1)) == 0 && kXBuf <= kWBuf,
                   "a step's parity is one bit of an LDS offset");
     int rt, ct;
@@ -250,6 +317,16 @@ void linear_tile_kernel(const LinearKArgs a) {
     const int s0 = part * a.steps_per_part;
     const int s1 = s0 + a.steps_per_part < a.steps ? s0 + a.steps_per_part : a.steps;
     issue_w(s0, 0);   // W does not wait for where x's rows are
+    // the scales of the wave's rows, a lane each
+    constexpr int kScales = (kRB + 1) / 2;
+    [[maybe_unused]] float x_scale[kScales];
+    if constexpr (kI8) {
+#pragma unroll
+        for (int i = 0; i < kScales; ++i) {
+            const uint32_t r = row0 + wr * kRB * 32 + i * 64 + lane;
+            x_scale[i] = a.x_scale[row_in(a, r < a.rows ? r : a.rows - 1)];
+        }
+    }
     const uint8_t *const x0 = static_cast<const uint8_t *>(uniform_ptr(x_row(a, row0)));
     const __amdgpu_buffer_rsrc_t xres =
         __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(x0), 0, 0x7fffffff, kBufferWord3);
@@ -285,11 +362,13 @@ void linear_tile_kernel(const LinearKArgs a) {
         issue_w(step, odd);
     };
 
-    f32x16_t acc[2][kRB];
+    typedef typename Sums<In>::of32 sums_t;
+    typedef typename Sums<In>::of16 sums4_t;
+    sums_t acc[2][kRB];
 #pragma unroll
     for (int f = 0; f < 2; ++f)
 #pragma unroll
-        for (int b = 0; b < kRB; ++b) acc[f][b] = f32x16_t{};
+        for (int b = 0; b < kRB; ++b) acc[f][b] = sums_t{};
     // this lane's pieces 2 kk + grp of its row in each block
     int xat[4], wat[4];
 #pragma unroll
@@ -309,12 +388,12 @@ void linear_tile_kernel(const LinearKArgs a) {
 #pragma unroll
         for (int b = 0; b < kRB; ++b) xf[kk % 2][b] = *reinterpret_cast<const u32x4_t *>(lds + xat[kk] + b * 32 * kStep);
     };
-    constexpr int kReads = 2 + kRB, kMma = 2 * kRB * (sizeof(E) == 2 ? 1 : 4);
+    constexpr int kReads = 2 + kRB, kMma = 2 * kRB * (sizeof(In) == 4 ? 4 : 1);
     auto multiply = [&](int kk) {
 #pragma unroll
         for (int b = 0; b < kRB; ++b)
 #pragma unroll
-            for (int f = 0; f < 2; ++f) acc[f][b] = mma32<E>(wf[kk % 2][f], xf[kk % 2][b], acc[f][b]);
+            for (int f = 0; f < 2; ++f) acc[f][b] = mma32<In>(wf[kk % 2][f], xf[kk % 2][b], acc[f][b]);
     };
     // The order that the compiler keeps: one read after every kMma / kReads matrix
     // instructions (left alone it reads a pair's operands right before they multiply).
@@ -409,7 +488,7 @@ void linear_tile_kernel(const LinearKArgs a) {
     // bias and gate of this lane's features, where all the tile's rows have one gate
     const uint32_t last = row0 + kBM - 1 < a.rows ? row0 + kBM - 1 : a.rows - 1;
     const bool one_gate = !a.gate_rows || row0 / a.N == last / a.N;
-    Epilogue<8> ep;
+    Epilogue<In, 8> ep;
     if (a.parts == 1 && c + 8 <= a.n_out) ep.template load<E>(a, c, one_gate ? a.frames.frame[row0 / a.N] : -1);
     // (8 KB of a wave, in the buffers of the last step, and in 64-row tiles all of x's)
     uint8_t *mine = lds + (wave < kWC ? (free_odd ^ 1) * kWBuf + wave * 8192
@@ -421,8 +500,8 @@ void linear_tile_kernel(const LinearKArgs a) {
 #pragma unroll
             for (int g4 = 0; g4 < 4; ++g4) {
                 const int unit = (f * 8 + g4 * 2 + grp) ^ (col & 15);
-                *reinterpret_cast<f32x4_t *>(mine + col * 256 + unit * 16) =
-                    f32x4_t{acc[f][b][g4 * 4], acc[f][b][g4 * 4 + 1], acc[f][b][g4 * 4 + 2], acc[f][b][g4 * 4 + 3]};
+                *reinterpret_cast<sums4_t *>(mine + col * 256 + unit * 16) =
+                    sums4_t{acc[f][b][g4 * 4], acc[f][b][g4 * 4 + 1], acc[f][b][g4 * 4 + 2], acc[f][b][g4 * 4 + 3]};
             }
         wait_lds_reads();   // (a wave's LDS accesses run in order; this orders the compiler's)
         if (stage) {
@@ -436,25 +515,35 @@ void linear_tile_kernel(const LinearKArgs a) {
         for (int i = 0; i < 4; ++i) {
             const int lr = i * 8 + sub;
             const uint32_t r = row0 + (wr * kRB + b) * 32 + lr;
-            float v[8];
+            typename Value<In>::type sums[8];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const f32x4_t x =
-                    *reinterpret_cast<const f32x4_t *>(mine + lr * 256 + ((((lane % 8) * 2 + h) ^ (lr & 15)) * 16));
+                const sums4_t x =
+                    *reinterpret_cast<const sums4_t *>(mine + lr * 256 + ((((lane % 8) * 2 + h) ^ (lr & 15)) * 16));
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[h * 4 + e] = x[e];
+                for (int e = 0; e < 4; ++e) sums[h * 4 + e] = x[e];
             }
+            // (the row's scale is in lane 32 (b % 2) + lr)
+            [[maybe_unused]] float row_scale = 0.0f;
+            if constexpr (kI8) row_scale = __shfl(x_scale[b / 2], b % 2 * 32 + lr);
             if (r >= a.rows || c >= a.n_out) continue;
             // (fp32 may end in the middle of eight features)
             if (sizeof(E) == 4 && c + 8 > a.n_out) {
-                float lo[4] = {v[0], v[1], v[2], v[3]};
-                if (a.parts > 1) store_n<float, 4>(a.ws, (static_cast<int64_t>(part) * a.rows + r) * a.n_out + c, lo);
-                else finish<E, 4>(a, r, c, lo);
+                typename Value<In>::type lo[4] = {sums[0], sums[1], sums[2], sums[3]};
+                if (a.parts > 1) store_part<4>(a, part, r, c, lo);
+                else finish<In, E, 4>(a, r, c, lo);
                 continue;
             }
             if (a.parts > 1) {
-                store_n<float, 8>(a.ws, (static_cast<int64_t>(part) * a.rows + r) * a.n_out + c, v);
+                store_part<8>(a, part, r, c, sums);
                 continue;
+            }
+            float v[8];
+            if constexpr (kI8) {
+                ep.scaled(row_scale, sums, v);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = sums[e];
             }
             const uint32_t m = r / a.N;
             const int64_t dst = static_cast<int64_t>(a.frames.out(m)) * a.N + (r - m * a.N);
@@ -486,9 +575,11 @@ constexpr int kFewWaves = kLinearFewWaves;
 // bytes (16 bytes a lane, four lanes to a row). The waves of a part take two at a time
 // in turn, 1 KB of a row in all, and have the next two in flight while two multiply (four
 // at a time: 11.0 against 10.0 us at 6 x 1,536 x 9,216, 9.1 against 7.7 at 8 x 3,000 x 2,000).
-template <typename E, int kR, int kF>
+template <typename In, typename E, int kR, int kF>
 __global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(const LinearKArgs a) {
-    __shared__ __attribute__((aligned(16))) float sums[kFewWaves][16 * kR][16 * kF];
+    typedef typename Value<In>::type value_t;
+    typedef typename Sums<In>::of16 sums4_t;
+    __shared__ __attribute__((aligned(16))) value_t sums[kFewWaves][16 * kR][16 * kF];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int part = blockIdx.x % a.parts, tile = blockIdx.x / a.parts;
@@ -508,11 +599,11 @@ __global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(const Linear
         const int c = f * 16 + l16, most = a.n_out - 1 - c0;
         wo[f] = (c < most ? c : most) * rb + grp * 16;
     }
-    f32x4_t acc[kF][kR];
+    sums4_t acc[kF][kR];
 #pragma unroll
     for (int f = 0; f < kF; ++f)
 #pragma unroll
-        for (int b = 0; b < kR; ++b) acc[f][b] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int b = 0; b < kR; ++b) acc[f][b] = sums4_t{};
     struct Batch {
         u32x4_t w[kAhead][kF], x[kAhead][kR];
     };
@@ -541,7 +632,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(const Linear
     const int lr = tid / (4 * kF), q = tid % (4 * kF), c = c0 + q * 4;
     const uint32_t r = r0 + lr;
     const bool mine = tid < 16 * kR * 4 * kF && r < a.rows && c < a.n_out;
-    Finish<E, 4> fin;
+    Finish<In, E, 4> fin;
     if (mine) fin.frames(a, r);
     Batch even, odd;
     load_w(s0, even);
@@ -571,7 +662,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(const Linear
 #pragma unroll
             for (int f = 0; f < kF; ++f)
 #pragma unroll
-                for (int b = 0; b < kR; ++b) acc[f][b] = mma16<E>(t.w[i][f], t.x[i][b], acc[f][b]);
+                for (int b = 0; b < kR; ++b) acc[f][b] = mma16<In>(t.w[i][f], t.x[i][b], acc[f][b]);
     };
     for (int s = s0; s < s1; s += 2 * kRound) {
         load_w(s + kRound, odd);
@@ -586,123 +677,98 @@ __global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(const Linear
     for (int f = 0; f < kF; ++f)
 #pragma unroll
         for (int b = 0; b < kR; ++b)
-            *reinterpret_cast<f32x4_t *>(&sums[wave][b * 16 + l16][f * 16 + grp * 4]) = acc[f][b];
+            *reinterpret_cast<sums4_t *>(&sums[wave][b * 16 + l16][f * 16 + grp * 4]) = acc[f][b];
     __syncthreads();
     if (!mine) return;
-    f32x4_t x = *reinterpret_cast<const f32x4_t *>(&sums[0][lr][q * 4]);
+    sums4_t x = *reinterpret_cast<const sums4_t *>(&sums[0][lr][q * 4]);
 #pragma unroll
     for (int w = 1; w < kFewWaves; ++w) {
-        const f32x4_t y = *reinterpret_cast<const f32x4_t *>(&sums[w][lr][q * 4]);
+        const sums4_t y = *reinterpret_cast<const sums4_t *>(&sums[w][lr][q * 4]);
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] += y[e];
     }
-    float v[4] = {x[0], x[1], x[2], x[3]};
-    if (a.parts > 1) store_n<float, 4>(a.ws, (static_cast<int64_t>(part) * a.rows + r) * a.n_out + c, v);
+    value_t v[4] = {x[0], x[1], x[2], x[3]};
+    if (a.parts > 1) store_part<4>(a, part, r, c, v);
     else fin.store(a, c, v);
 }
 
-template <typename E>
+template <typename In, typename E>
 __global__ __launch_bounds__(256) void linear_join_kernel(const LinearKArgs a) {
+    typedef typename Value<In>::type value_t;
+    typedef typename Sums<In>::of16 sums4_t;
     const int64_t per_row = a.n_out / 4, id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
     if (id >= per_row * a.rows) return;
     const uint32_t r = static_cast<uint32_t>(id / per_row);
     const int c = static_cast<int>(id - r * per_row) * 4;
-    Finish<E, 4> fin;
+    Finish<In, E, 4> fin;
     fin.frames(a, r);
     fin.load(a, r, c);
-    f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f};
-    const float *p = a.ws + static_cast<int64_t>(r) * a.n_out + c;
+    sums4_t x = {};
+    const value_t *p = reinterpret_cast<const value_t *>(a.ws) + static_cast<int64_t>(r) * a.n_out + c;
     const int64_t step = static_cast<int64_t>(a.rows) * a.n_out;
 #pragma unroll 8
     for (int i = 0; i < a.parts; ++i) {
-        const f32x4_t y = *reinterpret_cast<const f32x4_t *>(p + i * step);
+        const sums4_t y = *reinterpret_cast<const sums4_t *>(p + i * step);
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] += y[e];
     }
-    float v[4] = {x[0], x[1], x[2], x[3]};
+    value_t v[4] = {x[0], x[1], x[2], x[3]};
     fin.store(a, c, v);
 }
 
-typedef int32_t i32x4_t __attribute__((ext_vector_type(4)));
-typedef int32_t i32x16_t __attribute__((ext_vector_type(16)));
-
-// 8-bit integers: a wave has 32 rows x 32 features, straight from memory.
-template <typename E>
-__global__ __launch_bounds__(256) void linear_i8_kernel(const LinearKArgs a) {
-    const int lane = threadIdx.x & 63, col = lane & 31, grp = lane >> 5;
-    const int64_t id = static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / 64;
-    if (id >= static_cast<int64_t>(a.row_tiles) * a.col_tiles) return;
-    const int rt = static_cast<int>(id / a.col_tiles), ct = static_cast<int>(id - static_cast<int64_t>(rt) * a.col_tiles);
-    const uint32_t r = static_cast<uint32_t>(rt) * 32 + col;
-    const uint8_t *x = x_row(a, r), *w = w_row(a, ct * 32 + col);
-    i32x16_t acc = i32x16_t{};
-    for (int64_t at = grp * 16; at - grp * 16 < a.row_bytes; at += 32) {
-        const bool in = at < a.row_bytes;
-        i32x4_t wf = *reinterpret_cast<const i32x4_t *>(in ? w + at : w), xf = *reinterpret_cast<const i32x4_t *>(in ? x + at : x);
-        if (!in) wf = xf = i32x4_t{0, 0, 0, 0};
-        acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf, xf, acc, 0, 0, 0);
-    }
-    if (r >= a.rows) return;
-    const uint32_t m = r / a.N;
-    const float xs = a.x_scale[static_cast<int64_t>(a.frames.in(m)) * a.N + (r - m * a.N)];
-#pragma unroll
-    for (int g4 = 0; g4 < 4; ++g4) {
-        const int c = ct * 32 + g4 * 8 + grp * 4;
-        if (c >= a.n_out) continue;
-        float v[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = static_cast<float>(acc[g4 * 4 + e]) * xs * a.w_scale[c + e];
-        finish<E, 4>(a, r, c, v);
-    }
-}
-
-template <typename E>
+template <typename In, typename E>
 void run(const LinearPlan &p, const LinearKArgs &a, bool far, dim3 grid, hipStream_t stream) {
+    constexpr bool kLarge = sizeof(In) < 4;   // (fp32 has neither of the largest forms)
     switch (p.form) {
-        case kFew16: hipLaunchKernelGGL((linear_few_kernel<E, 1, 1>), grid, dim3(512), 0, stream, a); break;
-        case kFew32: hipLaunchKernelGGL((linear_few_kernel<E, 2, 2>), grid, dim3(512), 0, stream, a); break;
-        case kFew64: hipLaunchKernelGGL((linear_few_kernel<E, 4, 1>), grid, dim3(512), 0, stream, a); break;
-        case kStream32: hipLaunchKernelGGL((linear_tile_kernel<E, 1, 1, 4, false>), grid, dim3(256), 0, stream, a); break;
-        case kStream64:   // (bf16 only)
-            if constexpr (sizeof(E) == 2)
-                hipLaunchKernelGGL((linear_tile_kernel<E, 2, 1, 4, false>), grid, dim3(256), 0, stream, a);
+        case kFew16: hipLaunchKernelGGL((linear_few_kernel<In, E, 1, 1>), grid, dim3(512), 0, stream, a); break;
+        case kFew32: hipLaunchKernelGGL((linear_few_kernel<In, E, 2, 2>), grid, dim3(512), 0, stream, a); break;
+        case kFew64: hipLaunchKernelGGL((linear_few_kernel<In, E, 4, 1>), grid, dim3(512), 0, stream, a); break;
+        case kStream32: hipLaunchKernelGGL((linear_tile_kernel<In, E, 1, 1, 4, false>), grid, dim3(256), 0, stream, a); break;
+        case kStream64:
+            if constexpr (kLarge)
+                hipLaunchKernelGGL((linear_tile_kernel<In, E, 2, 1, 4, false>), grid, dim3(256), 0, stream, a);
             break;
-        case kTile64: hipLaunchKernelGGL((linear_tile_kernel<E, 1, 2, 2, false>), grid, dim3(256), 0, stream, a); break;
+        case kTile64: hipLaunchKernelGGL((linear_tile_kernel<In, E, 1, 2, 2, false>), grid, dim3(256), 0, stream, a); break;
         case kTile128:
-            if (far) hipLaunchKernelGGL((linear_tile_kernel<E, 2, 2, 2, true>), grid, dim3(256), 0, stream, a);
-            else hipLaunchKernelGGL((linear_tile_kernel<E, 2, 2, 2, false>), grid, dim3(256), 0, stream, a);
+            if (far) hipLaunchKernelGGL((linear_tile_kernel<In, E, 2, 2, 2, true>), grid, dim3(256), 0, stream, a);
+            else hipLaunchKernelGGL((linear_tile_kernel<In, E, 2, 2, 2, false>), grid, dim3(256), 0, stream, a);
             break;
-        case kTile256:    // (bf16 only)
-            if constexpr (sizeof(E) == 2)
-                hipLaunchKernelGGL((linear_tile_kernel<E, 4, 2, 4, false>), grid, dim3(512), 0, stream, a);
+        case kTile256:
+            if constexpr (kLarge)
+                hipLaunchKernelGGL((linear_tile_kernel<In, E, 4, 2, 4, false>), grid, dim3(512), 0, stream, a);
             break;
         case kLinearForms: break;
     }
 }
 
-}  // namespace
-
-int64_t linear_workspace(int64_t rows, int32_t K, int32_t n_out, int32_t dtype, int32_t cus) {
-    // (far or not is the frame list's: room for either)
-    int64_t bytes = 0;
-    for (const bool far : {false, true}) {
-        const LinearPlan p = linear_plan(rows, K, n_out, dtype, cus, far, true);
-        const int64_t need = p.parts > 1 ? p.parts * rows * n_out * 4 : 0;
-        bytes = need > bytes ? need : bytes;
-    }
-    return bytes;
+template <typename In, typename E>
+hipError_t launch(const LinearPlan &plan, const LinearKArgs &a, bool far, hipStream_t stream) {
+    const bool few = plan.form <= kFew64;
+    const int64_t grid = (few ? static_cast<int64_t>(a.tiles) : static_cast<int64_t>(a.per_xcd) * a.xcds) * plan.parts;
+    if (grid > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    run<In, E>(plan, a, far, dim3(static_cast<uint32_t>(grid)), stream);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || plan.parts == 1) return e;
+    const int64_t blocks = (static_cast<int64_t>(a.rows) * (a.n_out / 4) + 255) / 256;
+    if (blocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL((linear_join_kernel<In, E>), dim3(static_cast<uint32_t>(blocks)), dim3(256), 0, stream, a);
+    return hipGetLastError();
 }
 
-hipError_t launch_linear(const LinearParams &p, hipStream_t stream) {
+// in: RF_BF16, RF_F32 or kI8, the operands' type.
+hipError_t launch_product(const LinearParams &p, int32_t in, const float *x_scale, const float *w_scale,
+                          hipStream_t stream) {
     const int32_t xcds = p.geo.xcds;
     if (p.geo.cus < 1 || xcds < 1 || xcds > 64) return hipErrorInvalidValue;
     const int64_t rows = p.M * p.N;
-    const int64_t row_bytes = static_cast<int64_t>(p.K) * (p.dtype == RF_F32 ? 4 : 2);
+    const int64_t row_bytes = static_cast<int64_t>(p.K) * linear_size(in);
     const bool far = linear_far(p.frames, p.M, p.N, row_bytes);
-    const LinearPlan plan = linear_plan(rows, p.K, p.n_out, p.dtype, p.geo.cus, far, p.ws != nullptr);
+    const LinearPlan plan = linear_plan(rows, p.K, p.n_out, in, p.geo.cus, far, p.ws != nullptr);
     LinearKArgs a{};
     a.x = static_cast<const uint8_t *>(p.x);
     a.w = static_cast<const uint8_t *>(p.weight);
+    a.x_scale = x_scale;
+    a.w_scale = w_scale;
     a.bias = p.bias;
     a.gate = p.gate;
     a.residual = p.residual;
@@ -726,50 +792,35 @@ hipError_t launch_linear(const LinearParams &p, hipStream_t stream) {
     a.tiles = static_cast<int32_t>(tiles);
     a.xcds = xcds;
     a.per_xcd = (a.tiles + xcds - 1) / xcds;
-    const bool few = plan.form <= kFew64;
-    const int64_t grid = (few ? tiles : static_cast<int64_t>(a.per_xcd) * xcds) * plan.parts;
-    if (grid > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-    const dim3 g(static_cast<uint32_t>(grid));
-    if (p.dtype == RF_F32) run<float>(plan, a, far, g, stream);
-    else run<uint16_t>(plan, a, far, g, stream);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || plan.parts == 1) return e;
-    const int64_t blocks = (rows * (p.n_out / 4) + 255) / 256;
-    if (blocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-    const dim3 jg(static_cast<uint32_t>(blocks));
-    if (p.dtype == RF_F32) hipLaunchKernelGGL(linear_join_kernel<float>, jg, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL(linear_join_kernel<uint16_t>, jg, dim3(256), 0, stream, a);
-    return hipGetLastError();
+    if (in == kI8) return p.dtype == RF_F32 ? launch<int8_t, float>(plan, a, far, stream) : launch<int8_t, uint16_t>(plan, a, far, stream);
+    return in == RF_F32 ? launch<float, float>(plan, a, far, stream) : launch<uint16_t, uint16_t>(plan, a, far, stream);
 }
 
-int64_t linear_i8_workspace(int64_t, int32_t, int32_t, int32_t, int32_t) { return 0; }
+// Workspace of a product's split reduction; far or not is the frame list's: room for either.
+int64_t product_workspace(int64_t rows, int32_t K, int32_t n_out, int32_t in, int32_t cus) {
+    int64_t bytes = 0;
+    for (const bool far : {false, true}) {
+        const LinearPlan p = linear_plan(rows, K, n_out, in, cus, far, true);
+        const int64_t need = p.parts > 1 ? p.parts * rows * n_out * 4 : 0;
+        bytes = need > bytes ? need : bytes;
+    }
+    return bytes;
+}
 
+}  // namespace
+
+int64_t linear_workspace(int64_t rows, int32_t K, int32_t n_out, int32_t dtype, int32_t cus) {
+    return product_workspace(rows, K, n_out, dtype, cus);
+}
+hipError_t launch_linear(const LinearParams &p, hipStream_t stream) {
+    return launch_product(p, p.dtype, nullptr, nullptr, stream);
+}
+
+int64_t linear_i8_workspace(int64_t rows, int32_t K, int32_t n_out, int32_t, int32_t cus) {
+    return product_workspace(rows, K, n_out, kI8, cus);
+}
 hipError_t launch_linear_i8(const LinearParams &p, const float *x_scale, const float *w_scale, hipStream_t stream) {
-    LinearKArgs a{};
-    a.x = static_cast<const uint8_t *>(p.x);
-    a.w = static_cast<const uint8_t *>(p.weight);
-    a.bias = p.bias;
-    a.gate = p.gate;
-    a.residual = p.residual;
-    a.y = p.y;
-    a.x_scale = x_scale;
-    a.w_scale = w_scale;
-    a.row_bytes = p.K;
-    a.rows = static_cast<uint32_t>(p.M * p.N);
-    a.N = static_cast<uint32_t>(p.N);
-    a.n_out = p.n_out;
-    a.parts = 1;
-    a.row_tiles = static_cast<int32_t>((p.M * p.N + 31) / 32);
-    a.col_tiles = (p.n_out + 31) / 32;
-    a.activation = p.activation;
-    a.gate_rows = p.gate_rows;
-    a.frames = p.frames;
-    const int64_t blocks = (static_cast<int64_t>(a.row_tiles) * a.col_tiles + 3) / 4;
-    if (blocks > 0xffffff) return hipErrorInvalidConfiguration;
-    const dim3 g(static_cast<uint32_t>(blocks));
-    if (p.dtype == RF_F32) hipLaunchKernelGGL(linear_i8_kernel<float>, g, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL(linear_i8_kernel<uint16_t>, g, dim3(256), 0, stream, a);
-    return hipGetLastError();
+    return launch_product(p, kI8, x_scale, w_scale, stream);
 }
 
 }  // namespace rf

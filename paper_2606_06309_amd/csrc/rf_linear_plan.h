@@ -8,6 +8,10 @@
 
 namespace rf {
 
+// The operands' type besides RF_BF16 and RF_F32, and an operand's bytes.
+constexpr int32_t kI8 = 2;
+inline int32_t linear_size(int32_t in) { return in == RF_F32 ? 4 : in == kI8 ? 1 : 2; }
+
 // Bytes of a row that a step takes; rows of the largest tile; waves of a workgroup where rows are few.
 constexpr int kLinearStep = 128;
 constexpr int64_t kLinearTileRows = 256;
@@ -55,7 +59,7 @@ inline bool linear_whole_fits(int64_t rows, int64_t n_out) {
 // far: rows of a tile may lie 2 GB apart (only the smaller tile's kernel takes them).
 inline LinearPlan linear_plan(int64_t rows, int32_t K, int32_t n_out, int32_t dtype, int32_t cus, bool far, bool may_split) {
     LinearPlan p{};
-    const int64_t bytes = static_cast<int64_t>(K) * (dtype == RF_F32 ? 4 : 2);
+    const int64_t bytes = static_cast<int64_t>(K) * linear_size(dtype);
     auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
     if (rows <= 64 && !far) {
         // Straight to registers, through LDS in tiles of 256 features, or (33 rows on) as
@@ -70,7 +74,7 @@ inline LinearPlan linear_plan(int64_t rows, int32_t K, int32_t n_out, int32_t dt
         // 6,144 12.5 / 12.0, in fp32 17 / 21.
         const double w_mb = static_cast<double>(n_out) * static_cast<double>(bytes) * 1e-6;
         const bool few = w_mb < (dtype == RF_F32 ? 2 : 1) * (rows <= 16 ? 40 : rows <= 32 ? 8 : 4);
-        const bool stream = !few && (rows <= 32 || (dtype == RF_BF16 && w_mb >= 150));
+        const bool stream = !few && (rows <= 32 || (dtype != RF_F32 && w_mb >= 150));
         if (stream) {
             p.form = rows <= 32 ? kStream32 : kStream64;
             p.row_tiles = 1;
