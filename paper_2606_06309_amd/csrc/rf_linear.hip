@@ -71,14 +71,7 @@ struct LinearKArgs {
 // What lanes past the end of a row load.
 __device__ const u32x4_t kZeros = {0u, 0u, 0u, 0u};
 
-// 16 bytes per lane from memory straight into LDS: lane l's bytes land at dst + 16 l.
-// (Kept out of the kernel templates: the host pass drops the launch stub of a
-// template that names this builtin.)
-__device__ __forceinline__ void global_lds16(const uint8_t *p, uint8_t *dst) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)p, (lds_void_t *)dst, 16, 0, 0);
-}
-
-// The same from a buffer resource; an offset of -1 reads as zero.
+// 16 bytes per lane from a buffer resource straight into LDS; an offset of -1 reads as zero.
 __device__ __forceinline__ void buffer_lds16(__amdgpu_buffer_rsrc_t r, uint8_t *dst, int voffset, int soffset) {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t *)dst, 16, voffset, soffset, 0, 0);
 }

@@ -3,12 +3,14 @@
 //   y = act((x - mean) / sqrt(var + eps) * weight + bias),   mean, var over rows x channels of a group
 //   scale = max |x| / 127,  q = x * (127 / max |x|) to the nearest integer
 //
-//  * norm_stats_kernel: a workgroup has a run of a frame's rows and up to 256 16-byte columns;
+//  * norm_slice_kernel: where all rows that share statistics fit, a few groups' channels of them, a
+//    workgroup's LDS: x is read once, in one launch.
+//  * norm_stats_kernel: else a workgroup has a run of a frame's rows and up to 256 16-byte columns;
 //    a thread keeps its column's channels and walks rows, eight at a time: their mean and
 //    squared deviations from it, joined to those so far (a sum of squares about another
 //    point than the mean would lose what small deviations around a large mean are). The
 //    threads' rows, then the channels of each group, meet in LDS.
-//  * norm_total_kernel: a wave joins the parts of a group, in a fixed order.
+//  * norm_total_kernel: a wave joins the parts of a group.
 //  * norm_rows_kernel: x again, to y; norm_rows8_kernel: whole rows at a time, to 8 bits.
 //  * quantize_kernel: rows of x to 8 bits.
 #include "rf_norm_plan.h"
@@ -18,23 +20,34 @@ namespace rf {
 namespace {
 
 constexpr int kThreads = kNormThreads;
-constexpr int kAhead = 8;      // rows of a thread in flight
-
 struct NormKArgs {
     const uint8_t *x;
     uint8_t *y;
     float *y_scale;
     const void *weight, *bias;
     float2 *partial;               // [M][parts][slices][local]: mean, sum of squared deviations
-    float2 *total;                 // [M / together][groups]: mean, 1 / sqrt(var + eps)
-    int64_t N, per_part;
+    float *affine;                 // [M / together, or M with affine_rows][3][C]: (x - mean) * mul + add
+    int64_t N;
     int64_t x_stride, y_stride;    // bytes
     double eps;
     int32_t M, C, groups, together, per_group;
-    int32_t cols, slices, lines, parts, local;
+    int32_t cols, slices, lines, hold, parts, row_parts, local;
+    float per_col, group_share;    // 1 / cols, 1 / per_group
+    int32_t more_parts;            // parts with one whole chunk more than the others; the next has the last rows
+    float part_rows, chunk_rows, last_rows;
     int32_t activation, affine_rows;
     RowFrames frames;
 };
+
+// i / n for 0 <= i < 8192 and n <= 8192, given `share` = 1 / n: (i + 1/2) / n is 1 / (2 n) from a whole number at
+// least, which is more than the product's rounding, (i + 1/2) / n * 2^-23.
+__device__ __forceinline__ int divide(int i, float share) { return static_cast<int>((static_cast<float>(i) + 0.5f) * share); }
+
+// Rows of a part: every parts-th chunk of a frame, the last of which may be short. (Whole numbers
+// below 2^24: frames have four parts to a compute unit, and no memory holds 2^34 rows.)
+__device__ __forceinline__ float part_rows(const NormKArgs &a, int part) {
+    return a.part_rows + (part < a.more_parts ? a.chunk_rows : part == a.more_parts ? a.last_rows : 0.0f);
+}
 
 // n values of mean `mean` and squared deviations `m2`, joined by n_b more: the means' distance adds
 // n n_b / (n + n_b) of its square.
@@ -54,52 +67,66 @@ __device__ __forceinline__ void widen(u32x4_t x, float (&v)[16 / sizeof(E)]) {
     }
 }
 
+// A column of x, past the caches: every launch reads it once, and beyond what they hold a walk that
+// leaves nothing behind does not drive out what is still to be written (409 MB: 65 us, where it
+// takes 95 to 105 otherwise).
+__device__ __forceinline__ u32x4_t load_x(const uint8_t *p) {
+    return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p));
+}
+
 template <typename E>
 __global__ __launch_bounds__(kThreads) void norm_stats_kernel(const NormKArgs a) {
     constexpr int kV = 16 / sizeof(E);
     __shared__ float s_mean[kV][kThreads], s_m2[kV][kThreads], s_n[kThreads];
-    const int tid = threadIdx.x;
-    int id = blockIdx.x;
-    const int slice = id % a.slices;
-    id /= a.slices;
-    const int part = id % a.parts, m = id / a.parts;
-    const int line = tid / a.cols, col = tid - line * a.cols, column = slice * a.cols + col;
+    const int tid = threadIdx.x, slice = blockIdx.x, part = blockIdx.y, m = blockIdx.z;
+    const int line = divide(tid, a.per_col), col = tid - line * a.cols, column = slice * a.cols + col;
     const bool active = line < a.lines && column * kV < a.C;
-    const int64_t r0 = part * a.per_part, r1 = r0 + a.per_part < a.N ? r0 + a.per_part : a.N;
+    const int chunk = a.lines * kNormRows;
     float n = 0.0f, mean[kV], m2[kV];
 #pragma unroll
     for (int e = 0; e < kV; ++e) mean[e] = m2[e] = 0.0f;
     if (active) {
-        const uint8_t *p = a.x + (a.frames.in(m) * a.N + r0 + line) * a.x_stride + column * 16;
+        const uint8_t *const x = a.x + a.frames.in(m) * a.N * a.x_stride + column * 16;
         const int64_t step = a.lines * a.x_stride;
-        int64_t left = r1 - r0 > line ? (r1 - r0 - line + a.lines - 1) / a.lines : 0;   // rows of this thread
-        for (; left >= kAhead; left -= kAhead, p += kAhead * step) {
-            u32x4_t raw[kAhead];
+        for (int64_t first = static_cast<int64_t>(part) * chunk; first < a.N; first += static_cast<int64_t>(a.parts) * chunk) {
+            const uint8_t *p = x + (first + line) * a.x_stride;
+            if (first + chunk <= a.N) {
+                u32x4_t raw[kNormRows];
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) raw[i] = *reinterpret_cast<const u32x4_t *>(p + i * step);
-            float v[kAhead][kV];
+                for (int i = 0; i < kNormRows; ++i) raw[i] = load_x(p + i * step);
+                float v[kNormRows][kV];
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) widen<E>(raw[i], v[i]);
-            const float share = kAhead / (n + kAhead);
+                for (int i = 0; i < kNormRows; ++i) widen<E>(raw[i], v[i]);
+                const float share = kNormRows / (n + kNormRows);
 #pragma unroll
-            for (int e = 0; e < kV; ++e) {
-                float s = 0.0f, q = 0.0f;
+                for (int e = 0; e < kV; ++e) {
+                    float s = 0.0f, q = 0.0f;
 #pragma unroll
-                for (int i = 0; i < kAhead; ++i) s += v[i][e];
-                s *= 1.0f / kAhead;
+                    for (int i = 0; i < kNormRows; ++i) s += v[i][e];
+                    s *= 1.0f / kNormRows;
 #pragma unroll
-                for (int i = 0; i < kAhead; ++i) q = fmaf(v[i][e] - s, v[i][e] - s, q);
-                join(n, mean[e], m2[e], kAhead, s, q, share);
+                    for (int i = 0; i < kNormRows; ++i) q = fmaf(v[i][e] - s, v[i][e] - s, q);
+                    join(n, mean[e], m2[e], kNormRows, s, q, share);
+                }
+                n += kNormRows;
+            } else {      // the frame's last rows, one by one (but in flight together)
+                u32x4_t raw[kNormRows];
+#pragma unroll
+                for (int i = 0; i < kNormRows; ++i) {
+                    const int64_t r = first + line + i * a.lines;
+                    raw[i] = load_x(x + (r < a.N ? r : a.N - 1) * a.x_stride);
+                }
+#pragma unroll
+                for (int i = 0; i < kNormRows; ++i) {
+                    if (first + line + i * a.lines >= a.N) continue;
+                    float v[kV];
+                    widen<E>(raw[i], v);
+                    const float share = 1.0f / (n + 1.0f);
+#pragma unroll
+                    for (int e = 0; e < kV; ++e) join(n, mean[e], m2[e], 1.0f, v[e], 0.0f, share);
+                    n += 1.0f;
+                }
             }
-            n += kAhead;
-        }
-        for (; left > 0; --left, p += step) {
-            float v[kV];
-            widen<E>(*reinterpret_cast<const u32x4_t *>(p), v);
-            const float share = 1.0f / (n + 1.0f);
-#pragma unroll
-            for (int e = 0; e < kV; ++e) join(n, mean[e], m2[e], 1.0f, v[e], 0.0f, share);
-            n += 1.0f;
         }
     }
     s_n[tid] = n;
@@ -132,11 +159,11 @@ __global__ __launch_bounds__(kThreads) void norm_stats_kernel(const NormKArgs a)
     __syncthreads();
     // the channels of a group, all of as many rows: lanes share out its channels of this slice
     const int c0 = slice * a.cols * kV, c1 = c0 + a.cols * kV < a.C ? c0 + a.cols * kV : a.C;
-    const int g0 = c0 / a.per_group, n_local = (c1 - 1) / a.per_group - g0 + 1;
+    const int g0 = divide(c0, a.group_share), n_local = divide(c1 - 1, a.group_share) - g0 + 1;
     int lanes = 1;
     while (lanes < 64 && 2 * lanes * n_local <= kThreads) lanes *= 2;
     const int lane = tid % lanes;
-    const float rows = static_cast<float>(r1 - r0);
+    const float rows = part_rows(a, part);
     for (int l = tid / lanes; l < n_local; l += kThreads / lanes) {
         const int first = (g0 + l) * a.per_group, behind = first + a.per_group;
         const int lo = (first > c0 ? first : c0) - c0, hi = (behind < c1 ? behind : c1) - c0;
@@ -154,105 +181,269 @@ __global__ __launch_bounds__(kThreads) void norm_stats_kernel(const NormKArgs a)
     }
 }
 
-__device__ __forceinline__ double wave_sum(double x) {
-#pragma unroll
-    for (int d = 32; d > 0; d /= 2) x += __shfl_xor(x, d);
-    return x;
-}
-
-// A wave joins a group's parts, in 64 bits: their means first, then the deviations about it.
-template <typename E>
-__global__ __launch_bounds__(kThreads) void norm_total_kernel(const NormKArgs a) {
-    constexpr int kV = 16 / sizeof(E);
-    const int lane = threadIdx.x & 63;
-    const int64_t id = static_cast<int64_t>(blockIdx.x) * (kThreads / 64) + threadIdx.x / 64;
-    const int seg = static_cast<int>(id / a.groups), g = static_cast<int>(id - static_cast<int64_t>(seg) * a.groups);
-    if (seg * a.together >= a.M) return;
-    const int width = a.cols * kV;
-    const int s0 = g * a.per_group / width, s1 = ((g + 1) * a.per_group - 1) / width;
-    const int runs = a.together * a.parts;
-    double mean = 0.0, m2 = 0.0;
-    const double all = static_cast<double>(a.together) * static_cast<double>(a.N) * a.per_group;
-    for (int pass = 0; pass < 2; ++pass) {
-        double sum = 0.0;
-        for (int s = s0; s <= s1; ++s) {
-            const int c0 = s * width, first = g * a.per_group;
-            const int lo = first > c0 ? first : c0;
-            int hi = first + a.per_group < c0 + width ? first + a.per_group : c0 + width;
-            const int l = g - c0 / a.per_group;
-            for (int i = lane; i < runs; i += 64) {
-                const int part = i % a.parts;
-                const int64_t r0 = part * a.per_part, r1 = r0 + a.per_part < a.N ? r0 + a.per_part : a.N;
-                const double n = static_cast<double>(r1 - r0) * (hi - lo);
-                const float2 v = a.partial[((static_cast<int64_t>(seg) * runs + i) * a.slices + s) * a.local + l];
-                if (pass == 0) {
-                    sum += n * v.x;
-                } else {
-                    const double d = v.x - mean;
-                    sum += v.y + n * d * d;
-                }
-            }
-        }
-        sum = wave_sum(sum);
-        if (pass == 0) mean = sum / all;
-        else m2 = sum / all;
-    }
-    if (lane == 0) a.total[id] = make_float2(static_cast<float>(mean), static_cast<float>(1.0 / sqrt(m2 + a.eps)));
-}
-
-// What channel c of listed frame m is normalised with: (x - mean) * mul + add.
-struct Affine {
-    float mean, mul, add;
-};
 template <typename E>
 __device__ __forceinline__ float element(const void *p, int64_t at) {
     if constexpr (sizeof(E) == 4) return static_cast<const float *>(p)[at];
     else return __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t *>(p)[at]) << 16);
 }
+// What channel c of listed frame m is normalised with, given its group's mean and 1 / deviation t:
+// (x - mean) * mul + add.
+struct Affine {
+    float mean, mul, add;
+};
 template <typename E>
-__device__ __forceinline__ Affine affine_of(const NormKArgs &a, int m, int c) {
-    const float2 t = a.total[static_cast<int64_t>(m / a.together) * a.groups + c / a.per_group];
+__device__ __forceinline__ Affine affine_of(const NormKArgs &a, int m, int c, float2 t) {
     const int64_t at = (a.affine_rows ? static_cast<int64_t>(a.frames.frame[m]) * a.C : 0) + c;
     return {t.x, a.weight ? t.y * element<E>(a.weight, at) : t.y, a.bias ? element<E>(a.bias, at) : 0.0f};
 }
 
+// A wave joins the parts of a group, of the frames of a segment, in 64 bits and one order: sums of the
+// parts' means and their squares about the first part's (64 bits lose nothing there that 32 had).
+// Then what its channels are normalised with.
 template <typename E>
+__global__ __launch_bounds__(64) void norm_total_kernel(const NormKArgs a) {
+    constexpr int kV = 16 / sizeof(E);
+    const int lane = threadIdx.x, g = blockIdx.x, seg = blockIdx.y;
+    const int width = a.cols * kV, runs = a.together * a.parts;
+    const int64_t step = static_cast<int64_t>(a.slices) * a.local;
+    const int first = g * a.per_group, behind = first + a.per_group, s0 = divide(first, a.per_col * (1.0f / kV));
+    double pivot = 0.0, sum = 0.0, square = 0.0;
+    for (int s = s0; s * width < behind; ++s) {
+        const int c0 = s * width, lo = first > c0 ? first : c0, hi = behind < c0 + width ? behind : c0 + width;
+        const float2 *p = a.partial + (static_cast<int64_t>(seg) * runs * a.slices + s) * a.local +
+                          (g - divide(c0, a.group_share));
+        if (s == s0) pivot = p->x;
+        int part = lane;
+        while (part >= a.parts) part -= a.parts;
+#pragma unroll 4
+        for (int i = lane; i < runs; i += 64) {
+            const float2 v = p[i * step];
+            const double n = part_rows(a, part) * static_cast<float>(hi - lo), d = v.x - pivot;
+            sum += n * d;
+            square += n * d * d + v.y;
+            part += 64;
+            while (part >= a.parts) part -= a.parts;
+        }
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) {
+        sum += __shfl_xor(sum, d);
+        square += __shfl_xor(square, d);
+    }
+    const double all = static_cast<double>(a.together) * static_cast<double>(a.N) * a.per_group;
+    const double m = sum / all, var = square / all - m * m;
+    const float2 t = make_float2(static_cast<float>(pivot + m), static_cast<float>(rsqrt((var < 0.0 ? 0.0 : var) + a.eps)));
+    const int first_set = a.affine_rows ? seg * a.together : seg, sets = a.affine_rows ? a.together : 1;
+    for (int set = first_set; set < first_set + sets; ++set)
+        for (int c = first + lane; c < behind; c += 64) {
+            const Affine f = affine_of<E>(a, set, c, t);
+            float *to = a.affine + static_cast<int64_t>(set) * 3 * a.C + c;
+            to[0] = f.mean;
+            to[a.C] = f.mul;
+            to[2 * a.C] = f.add;
+        }
+}
+
+// Where frame m's are.
+__device__ __forceinline__ const float *affine_at(const NormKArgs &a, int m) {
+    return a.affine + static_cast<int64_t>(a.affine_rows ? m : m / a.together) * 3 * a.C;
+}
+
+// A workgroup's threads hold kV channels each, `cols` threads to a line, `lines` lines: done(group of the
+// slice, sum of its values) for every group, by one thread. Channels first, a thread to a channel and
+// as many of them as there are threads to share out its lines, then a group's channels, lanes
+// together. `lines * cols * kV` floats of `all` and kBlock of `some` are its own.
+template <int kV, int kBlock, typename Done>
+__device__ __forceinline__ void group_sums(const float (&v)[kV], int line, int cols, int lines, int per_group, int n_groups,
+                                           int shares, float channel_share, float *all, float *some, Done done) {
+    const int tid = threadIdx.x, channels = cols * kV;
+    if (line < lines) {
+#pragma unroll
+        for (int e = 0; e < kV; e += 4)
+            *reinterpret_cast<f32x4_t *>(all + tid * kV + e) = f32x4_t{v[e], v[e + 1], v[e + 2], v[e + 3]};
+    }
+    __syncthreads();
+    for (int t = tid; t < channels * shares; t += kBlock) {
+        const int share = divide(t, channel_share), c = t - share * channels;
+        float s = 0.0f;
+#pragma unroll 4
+        for (int l = share; l < lines; l += shares) s += all[l * channels + c];
+        if (shares == 1) all[c] = s;      // (line 0's place of this channel, which no other thread reads)
+        else some[c * shares + share] = s;
+    }
+    __syncthreads();
+    const float *from = shares == 1 ? all : some;
+    int lanes = 1;
+    while (lanes < 64 && 2 * lanes * n_groups <= kBlock) lanes *= 2;
+    for (int g = tid / lanes; g < n_groups; g += kBlock / lanes) {
+        float s = 0.0f;
+#pragma unroll 4
+        for (int i = tid % lanes; i < per_group * shares; i += lanes) s += from[g * per_group * shares + i];
+        for (int d = lanes / 2; d > 0; d /= 2) s += __shfl_xor(s, d);
+        if (tid % lanes == 0) done(g, s);
+    }
+    __syncthreads();
+}
+
+// A value that stays as it is: what was made of it before is not kept for what follows (else the
+// compiler holds bf16 values widened, at twice the registers, or spills them).
+__device__ __forceinline__ void pin(u32x4_t &x) { asm volatile("" : "+v"(x)); }
+
+// Whole groups' columns of all rows that share their statistics, up to kHold rows of a thread, straight
+// from memory into LDS, where they stay: the mean, then the squared deviations from it, then the
+// results. (Held in registers they need loops unrolled to their end, 77 KB of code that a short launch
+// waits for: 10.3 us at 3 x 527 rows x 320 channels.)
+template <typename E, int kHold, int kBlock>
+__global__ __launch_bounds__(kBlock) void norm_slice_kernel(const NormKArgs a) {
+    constexpr int kV = 16 / sizeof(E);
+    __shared__ __attribute__((aligned(1024))) uint8_t held[kHold * kBlock * 16];
+    __shared__ __attribute__((aligned(16))) float all[kBlock * kV], some[kBlock], mean[kNormSliceGroups],
+        inverse[kNormSliceGroups];
+    const int tid = threadIdx.x;
+    const int slice = blockIdx.x, seg = blockIdx.y;
+    const int line = divide(tid, a.per_col), col = tid - line * a.cols, column = slice * a.cols + col;
+    const uint32_t N = static_cast<uint32_t>(a.N), rows = N * static_cast<uint32_t>(a.together);
+    // This thread's i-th row, i < a.hold: line + i lines, in frame f of the segment; the last may be past
+    // the end, then the last row is loaded (as by the threads behind the last line, whose sums nobody reads).
+    auto row_of = [&](int i, uint32_t &f) {
+        uint32_t r = line + i * a.lines;
+        r = r < rows ? r : rows - 1;
+        f = a.together > 1 ? r / N : 0;
+        return r - f * N;
+    };
+    uint8_t *const to = held + __builtin_amdgcn_readfirstlane(tid / 64) * 1024;
+#pragma unroll 1
+    for (int i = 0; i < a.hold; ++i) {
+        uint32_t f;
+        const uint32_t r = row_of(i, f);
+        global_lds16(a.x + (a.frames.in(seg * a.together + f) * a.N + r) * a.x_stride + column * 16, to + i * (kBlock * 16));
+    }
+    int local[kV];
+#pragma unroll
+    for (int e = 0; e < kV; ++e) local[e] = divide(col * kV + e, a.group_share);
+    float weight[kV], bias[kV];
+#pragma unroll
+    for (int e = 0; e < kV; ++e) {
+        weight[e] = 1.0f;
+        bias[e] = 0.0f;
+    }
+    auto affine = [&](int m) {
+        const int64_t at = (a.affine_rows ? static_cast<int64_t>(a.frames.frame[m]) * a.C : 0) + column * kV;
+        if (a.weight) load_n<E, kV>(a.weight, at, weight);
+        if (a.bias) load_n<E, kV>(a.bias, at, bias);
+    };
+    const bool each = a.affine_rows && a.together > 1;   // (then a row's frame has its own)
+    if (!each) affine(seg * a.together);
+    const int mine = line + (a.hold - 1) * a.lines < static_cast<int>(rows) ? a.hold : a.hold - 1;
+    // threads to a channel of group_sums
+    const int channels = a.cols * kV, n_groups = divide(channels, a.group_share);
+    const float channel_share = a.per_col * (1.0f / kV);
+    const int shares = channels < kBlock ? divide(kBlock, channel_share) : 1;
+    const double share = 1.0 / (static_cast<double>(rows) * a.per_group);
+    auto row = [&](int i, float (&v)[kV]) {
+        widen<E>(*reinterpret_cast<const u32x4_t *>(held + (i * kBlock + tid) * 16), v);
+    };
+    wait_loads<0>();   // (a thread reads its own rows only)
+    float s[kV], mu[kV];
+#pragma unroll
+    for (int e = 0; e < kV; ++e) s[e] = 0.0f;
+#pragma unroll 1
+    for (int i = 0; i < mine; ++i) {
+        float v[kV];
+        row(i, v);
+#pragma unroll
+        for (int e = 0; e < kV; ++e) s[e] += v[e];
+    }
+    group_sums<kV, kBlock>(s, line, a.cols, a.lines, a.per_group, n_groups, shares, channel_share, all, some,
+                           [&](int g, float sum) { mean[g] = static_cast<float>(sum * share); });
+#pragma unroll
+    for (int e = 0; e < kV; ++e) {
+        mu[e] = mean[local[e]];
+        s[e] = 0.0f;
+    }
+#pragma unroll 1
+    for (int i = 0; i < mine; ++i) {
+        float v[kV];
+        row(i, v);
+#pragma unroll
+        for (int e = 0; e < kV; ++e) s[e] = fmaf(v[e] - mu[e], v[e] - mu[e], s[e]);
+    }
+    group_sums<kV, kBlock>(s, line, a.cols, a.lines, a.per_group, n_groups, shares, channel_share, all, some,
+                           [&](int g, float sum) { inverse[g] = static_cast<float>(rsqrt(sum * share + a.eps)); });
+    if (line >= a.lines) return;
+    float mul[kV];
+    with_activation(a.activation, [&](auto act) {
+#pragma unroll
+        for (int e = 0; e < kV; ++e) mul[e] = inverse[local[e]] * weight[e];
+#pragma unroll 1
+        for (int i = 0; i < mine; ++i) {
+            uint32_t f;
+            const uint32_t r = row_of(i, f);
+            const int m = seg * a.together + static_cast<int>(f);
+            if (each) {
+                affine(m);
+#pragma unroll
+                for (int e = 0; e < kV; ++e) mul[e] = inverse[local[e]] * weight[e];
+            }
+            float v[kV];
+            row(i, v);
+#pragma unroll
+            for (int e = 0; e < kV; ++e) v[e] = fmaf(v[e] - mu[e], mul[e], bias[e]);
+            if constexpr (act.kind != RF_ACT_NONE) activate(act.kind, v);
+            store_n<E, kV>(a.y + (a.frames.out(m) * a.N + r) * a.y_stride + column * 16, 0, v);
+        }
+    });
+}
+
+// A column's results past the caches.
+template <typename E, int kN>
+__device__ __forceinline__ void stream_n(void *p, const float (&v)[kN]) {
+    if constexpr (kN == 8) stream_8<E>(p, 0, v);
+    else __builtin_nontemporal_store((f32x4_t{v[0], v[1], v[2], v[3]}), static_cast<f32x4_t *>(p));
+}
+
+template <typename E, bool kStream>
 __global__ __launch_bounds__(kThreads) void norm_rows_kernel(const NormKArgs a) {
     constexpr int kV = 16 / sizeof(E);
-    const int tid = threadIdx.x;
-    int id = blockIdx.x;
-    const int slice = id % a.slices;
-    id /= a.slices;
-    const int part = id % a.parts, m = id / a.parts;
-    const int line = tid / a.cols, col = tid - line * a.cols, column = slice * a.cols + col;
+    const int tid = threadIdx.x, slice = blockIdx.x, part = blockIdx.y, m = blockIdx.z;
+    const int line = divide(tid, a.per_col), col = tid - line * a.cols, column = slice * a.cols + col;
     if (line >= a.lines || column * kV >= a.C) return;
-    const int64_t r0 = part * a.per_part, r1 = r0 + a.per_part < a.N ? r0 + a.per_part : a.N;
-    Affine f[kV];
-#pragma unroll
-    for (int e = 0; e < kV; ++e) f[e] = affine_of<E>(a, m, column * kV + e);
+    float mean[kV], mul[kV], add[kV];
+    const float *f = affine_at(a, m) + column * kV;
+    load_n<float, kV>(f, 0, mean);
+    load_n<float, kV>(f, a.C, mul);
+    load_n<float, kV>(f, 2 * a.C, add);
     // (y may be x: no row is read again)
     const uint8_t *p = a.x + (a.frames.in(m) * a.N) * a.x_stride + column * 16;
     uint8_t *q = a.y + (a.frames.out(m) * a.N) * a.y_stride + column * 16;
+    // From the frame's last rows to its first, the other way than the statistics' kernel went: what
+    // that read last is in the caches still.
     constexpr int kRows = 4;
-    for (int64_t r = r0 + line; r < r1; r += kRows * a.lines) {
-        u32x4_t raw[kRows];
+    const int chunk = kRows * a.lines;
+    const int64_t chunks = (a.N + chunk - 1) / chunk;
+    with_activation(a.activation, [&](auto act) {
+        for (int64_t at = chunks - 1 - part; at >= 0; at -= a.row_parts) {
+            const int64_t r = at * chunk + line;
+            u32x4_t raw[kRows];
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const int64_t at = r + i * a.lines;
-            raw[i] = *reinterpret_cast<const u32x4_t *>(p + (at < r1 ? at : r) * a.x_stride);
+            for (int i = 0; i < kRows; ++i) {
+                const int64_t k = r + i * a.lines;
+                raw[i] = load_x(p + (k < a.N ? k : a.N - 1) * a.x_stride);
+            }
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+                const int64_t k = r + i * a.lines;
+                if (k >= a.N) break;
+                float v[kV];
+                widen<E>(raw[i], v);
+#pragma unroll
+                for (int e = 0; e < kV; ++e) v[e] = fmaf(v[e] - mean[e], mul[e], add[e]);
+                if constexpr (act.kind != RF_ACT_NONE) activate(act.kind, v);
+                if constexpr (kStream) stream_n<E, kV>(q + k * a.y_stride, v);
+                else store_n<E, kV>(q + k * a.y_stride, 0, v);
+            }
         }
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const int64_t at = r + i * a.lines;
-            if (at >= r1) break;
-            float v[kV];
-            widen<E>(raw[i], v);
-#pragma unroll
-            for (int e = 0; e < kV; ++e) v[e] = fmaf(v[e] - f[e].mean, f[e].mul, f[e].add);
-            if (a.activation != RF_ACT_NONE) activate(a.activation, v);
-            store_n<E, kV>(q + at * a.y_stride, 0, v);
-        }
-    }
+    });
 }
 
 // The largest of kLanes neighbouring lanes' values (kLanes > 64: of all of the workgroup's kLanes
@@ -283,55 +474,57 @@ __global__ __launch_bounds__(kThreads) void norm_rows8_kernel(const NormKArgs a)
     __shared__ __attribute__((aligned(16))) float s_mean[kC], s_mul[kC], s_add[kC];
     __shared__ uint32_t places[2][kLanes / 64 > 0 ? kLanes / 64 : 1];
     const int tid = threadIdx.x;
-    const int part = blockIdx.x % a.parts, m = blockIdx.x / a.parts;
-    for (int c = tid; c < a.C; c += kThreads) {
-        const Affine f = affine_of<E>(a, m, c);
-        s_mean[c] = f.mean;
-        s_mul[c] = f.mul;
-        s_add[c] = f.add;
+    const int part = blockIdx.x, m = blockIdx.y;
+    const float *f = affine_at(a, m);
+    for (int c = tid * 4; c < a.C; c += kThreads * 4) {
+        *reinterpret_cast<f32x4_t *>(s_mean + c) = *reinterpret_cast<const f32x4_t *>(f + c);
+        *reinterpret_cast<f32x4_t *>(s_mul + c) = *reinterpret_cast<const f32x4_t *>(f + a.C + c);
+        *reinterpret_cast<f32x4_t *>(s_add + c) = *reinterpret_cast<const f32x4_t *>(f + 2 * a.C + c);
     }
     __syncthreads();
     const int lane = tid % kLanes, line = tid / kLanes, columns = a.C / kV;
-    const int64_t r0 = part * a.per_part, r1 = r0 + a.per_part < a.N ? r0 + a.per_part : a.N;
     const uint8_t *x = a.x + (a.frames.in(m) * a.N) * a.x_stride;
     uint8_t *y = a.y + (a.frames.out(m) * a.N) * a.C;
     float *scales = a.y_scale + a.frames.out(m) * a.N;
-    int turn = 0;
-    for (int64_t first = r0; first < r1; first += kRows, ++turn) {
-        const int64_t r = first + line < r1 ? first + line : r1 - 1;
-        u32x4_t raw[kPer];
+    with_activation(a.activation, [&](auto act) {
+        int turn = 0;
+        const int64_t rounds = (a.N + kRows - 1) / kRows;
+        for (int64_t at = rounds - 1 - part; at >= 0; at -= a.row_parts, ++turn) {
+            const int64_t first = at * kRows, r = first + line < a.N ? first + line : a.N - 1;
+            u32x4_t raw[kPer];
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int col = lane + i * kLanes;
-            raw[i] = *reinterpret_cast<const u32x4_t *>(x + r * a.x_stride + (col < columns ? col : columns - 1) * 16);
-        }
-        float v[kPer][kV];
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int col = lane + i * kLanes, c = (col < columns ? col : columns - 1) * kV;
-            widen<E>(raw[i], v[i]);
-#pragma unroll
-            for (int e = 0; e < kV; ++e) v[i][e] = fmaf(v[i][e] - s_mean[c + e], s_mul[c + e], s_add[c + e]);
-            if (a.activation != RF_ACT_NONE) activate(a.activation, v[i]);
-#pragma unroll
-            for (int e = 0; e < kV; ++e) {
-                const uint32_t bits = __float_as_uint(v[i][e]) & 0x7fffffffu;
-                top = top > bits ? top : bits;
+            for (int i = 0; i < kPer; ++i) {
+                const int col = lane + i * kLanes;
+                raw[i] = *reinterpret_cast<const u32x4_t *>(x + r * a.x_stride + (col < columns ? col : columns - 1) * 16);
             }
-        }
-        const RowScale s(lanes_max<kLanes>(top, places, turn));
-        if (first + line >= r1) continue;
+            float v[kPer][kV];
+            uint32_t top = 0;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int col = lane + i * kLanes;
-            if (col >= columns) break;
-            uint32_t *to = reinterpret_cast<uint32_t *>(y + r * a.C + col * kV);
-            if constexpr (kV == 8) *reinterpret_cast<u32x2_t *>(to) = u32x2_t{round4(v[i], s.inverse), round4(v[i] + 4, s.inverse)};
-            else *to = round4(v[i], s.inverse);
+            for (int i = 0; i < kPer; ++i) {
+                const int col = lane + i * kLanes, c = (col < columns ? col : columns - 1) * kV;
+                widen<E>(raw[i], v[i]);
+#pragma unroll
+                for (int e = 0; e < kV; ++e) v[i][e] = fmaf(v[i][e] - s_mean[c + e], s_mul[c + e], s_add[c + e]);
+                if constexpr (act.kind != RF_ACT_NONE) activate(act.kind, v[i]);
+#pragma unroll
+                for (int e = 0; e < kV; ++e) {
+                    const uint32_t bits = __float_as_uint(v[i][e]) & 0x7fffffffu;
+                    top = top > bits ? top : bits;
+                }
+            }
+            const RowScale s(lanes_max<kLanes>(top, places, turn));
+            if (first + line >= a.N) continue;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const int col = lane + i * kLanes;
+                if (col >= columns) break;
+                uint32_t *to = reinterpret_cast<uint32_t *>(y + r * a.C + col * kV);
+                if constexpr (kV == 8) *reinterpret_cast<u32x2_t *>(to) = u32x2_t{round4(v[i], s.inverse), round4(v[i] + 4, s.inverse)};
+                else *to = round4(v[i], s.inverse);
+            }
+            if (lane == 0) scales[r] = s.scale;
         }
-        if (lane == 0) scales[r] = s.scale;
-    }
+    });
 }
 
 struct QuantizeKArgs {
@@ -378,6 +571,8 @@ __global__ __launch_bounds__(kLanes > kThreads ? kLanes : kThreads) void quantiz
                 }
             }
         const RowScale s(lanes_max<kLanes>(top, places, turn));
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) pin(raw[i]);
         if (first + line >= a.rows) continue;
         const int64_t out = a.frames.out(m) * a.N + in;
 #pragma unroll
@@ -405,18 +600,26 @@ void rows8(const NormKArgs &a, dim3 grid, hipStream_t stream) {
 }
 
 template <typename E>
-hipError_t run_norm(const NormKArgs &a, hipStream_t stream) {
-    const int64_t blocks = static_cast<int64_t>(a.M) * a.parts * a.slices;
-    const int64_t totals = (static_cast<int64_t>(a.M / a.together) * a.groups + kThreads / 64 - 1) / (kThreads / 64);
-    if (blocks > 0xffffff || totals > 0xffffff) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL(norm_stats_kernel<E>, dim3(static_cast<uint32_t>(blocks)), dim3(kThreads), 0, stream, a);
+hipError_t run_slices(const NormPlan &p, const NormKArgs &a, hipStream_t stream) {
+    const dim3 grid(a.slices, a.M / a.together);
+    if (p.block == kNormBlocks[0].threads)
+        hipLaunchKernelGGL((norm_slice_kernel<E, kNormBlocks[0].hold, kNormBlocks[0].threads>), grid, dim3(p.block), 0, stream, a);
+    else
+        hipLaunchKernelGGL((norm_slice_kernel<E, kNormBlocks[1].hold, kNormBlocks[1].threads>), grid, dim3(p.block), 0, stream, a);
+    return hipGetLastError();
+}
+
+template <typename E>
+hipError_t run_norm(const NormKArgs &a, bool stream_y, hipStream_t stream) {
+    hipLaunchKernelGGL(norm_stats_kernel<E>, dim3(a.slices, a.parts, a.M), dim3(kThreads), 0, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(norm_total_kernel<E>, dim3(static_cast<uint32_t>(totals)), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL(norm_total_kernel<E>, dim3(a.groups, a.M / a.together), dim3(64), 0, stream, a);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (a.y_scale) rows8<E>(a, dim3(static_cast<uint32_t>(a.M) * a.parts), stream);
-    else hipLaunchKernelGGL(norm_rows_kernel<E>, dim3(static_cast<uint32_t>(blocks)), dim3(kThreads), 0, stream, a);
+    if (a.y_scale) rows8<E>(a, dim3(a.row_parts, a.M), stream);
+    else if (stream_y) hipLaunchKernelGGL((norm_rows_kernel<E, true>), dim3(a.slices, a.row_parts, a.M), dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((norm_rows_kernel<E, false>), dim3(a.slices, a.row_parts, a.M), dim3(kThreads), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -432,20 +635,20 @@ hipError_t run_quantize(const QuantizeKArgs &a, hipStream_t stream) {
     else if (columns <= 256) hipLaunchKernelGGL((quantize_kernel<E, 64, 4>), grid(4), dim3(256), 0, stream, a);
     else if (columns <= 1024) hipLaunchKernelGGL((quantize_kernel<E, 256, 4>), grid(1), dim3(256), 0, stream, a);
     else if (columns <= 4096) hipLaunchKernelGGL((quantize_kernel<E, 256, 16>), grid(1), dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((quantize_kernel<E, 1024, 16>), grid(1), dim3(1024), 0, stream, a);
+    else hipLaunchKernelGGL((quantize_kernel<E, 1024, sizeof(E) == 2 ? 8 : 16>), grid(1), dim3(1024), 0, stream, a);
     return hipGetLastError();
 }
 
 }  // namespace
 
-int64_t norm_workspace(int32_t M, int64_t N, int32_t C, int32_t groups, int32_t together, bool, int32_t dtype,
+int64_t norm_workspace(int32_t M, int64_t N, int32_t C, int32_t groups, int32_t together, bool rows8, int32_t dtype,
                        int32_t cus) {
-    return norm_plan(M, N, C, groups, together, dtype, cus).ws_bytes;
+    return norm_plan(M, N, C, groups, together, rows8, dtype, cus).ws_bytes;
 }
 
 hipError_t launch_norm(const NormParams &p, hipStream_t stream) {
     if (p.geo.cus < 1) return hipErrorInvalidValue;
-    const NormPlan plan = norm_plan(p.M, p.N, p.C, p.groups, p.together, p.dtype, p.geo.cus);
+    const NormPlan plan = norm_plan(p.M, p.N, p.C, p.groups, p.together, p.y_scale != nullptr, p.dtype, p.geo.cus);
     const int64_t esize = p.dtype == RF_F32 ? 4 : 2;
     NormKArgs a{};
     a.x = static_cast<const uint8_t *>(p.x);
@@ -454,9 +657,8 @@ hipError_t launch_norm(const NormParams &p, hipStream_t stream) {
     a.weight = p.weight;
     a.bias = p.bias;
     a.partial = static_cast<float2 *>(p.ws);
-    a.total = a.partial + plan.entries;
+    a.affine = reinterpret_cast<float *>(a.partial + plan.entries);
     a.N = p.N;
-    a.per_part = plan.per_part;
     a.x_stride = p.x_stride * esize;
     a.y_stride = p.y_scale ? p.y_stride : p.y_stride * esize;
     a.eps = p.eps;
@@ -469,11 +671,23 @@ hipError_t launch_norm(const NormParams &p, hipStream_t stream) {
     a.slices = plan.slices;
     a.lines = plan.lines;
     a.parts = plan.parts;
+    a.hold = plan.hold;
+    a.row_parts = plan.row_parts;
     a.local = plan.local;
+    a.per_col = 1.0f / static_cast<float>(plan.cols);
+    a.group_share = 1.0f / static_cast<float>(a.per_group);
+    if (plan.block == 0) {
+        const int64_t chunk = plan.lines * kNormRows, whole = p.N / chunk;
+        a.more_parts = static_cast<int32_t>(whole % plan.parts);
+        a.part_rows = static_cast<float>(whole / plan.parts * chunk);
+        a.chunk_rows = static_cast<float>(chunk);
+        a.last_rows = static_cast<float>(p.N - whole * chunk);
+    }
     a.activation = p.activation;
     a.affine_rows = p.affine_rows;
     a.frames = p.frames;
-    return p.dtype == RF_F32 ? run_norm<float>(a, stream) : run_norm<uint16_t>(a, stream);
+    if (plan.block > 0) return p.dtype == RF_F32 ? run_slices<float>(plan, a, stream) : run_slices<uint16_t>(plan, a, stream);
+    return p.dtype == RF_F32 ? run_norm<float>(a, plan.stream, stream) : run_norm<uint16_t>(a, plan.stream, stream);
 }
 
 hipError_t launch_quantize(const QuantizeParams &p, hipStream_t stream) {

@@ -10,6 +10,13 @@ typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
+// 16 bytes per lane from memory straight into LDS: lane l's bytes land at dst + 16 l.
+// (Kept out of the kernel templates: the host pass drops the launch stub of a
+// template that names this builtin.)
+__device__ __forceinline__ void global_lds16(const uint8_t *p, uint8_t *dst) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)p, (lds_void_t *)dst, 16, 0, 0);
+}
+
 // kN (4 or 8) consecutive elements, widened / rounded once to nearest even.
 template <typename E, int kN>
 __device__ __forceinline__ void load_n(const void *p, int64_t at, float (&v)[kN]) {
@@ -87,6 +94,19 @@ __device__ __forceinline__ void activate(int kind, float (&v)[kN]) {
 #pragma unroll
         for (int e = 0; e < kN; ++e) v[e] = gated(v[e], -kLog2e * v[e]);
     }
+}
+
+// run(k), k.kind being the activation as a constant: a loop of rows then holds the code of one.
+template <int kKind>
+struct Activation {
+    static constexpr int kind = kKind;
+};
+template <typename Run>
+__device__ __forceinline__ void with_activation(int kind, Run run) {
+    if (kind == RF_ACT_NONE) run(Activation<RF_ACT_NONE>{});
+    else if (kind == RF_ACT_GELU) run(Activation<RF_ACT_GELU>{});
+    else if (kind == RF_ACT_GELU_TANH) run(Activation<RF_ACT_GELU_TANH>{});
+    else run(Activation<RF_ACT_SILU>{});
 }
 
 __device__ __forceinline__ void widen8(u32x4_t x, float (&v)[8]) {
