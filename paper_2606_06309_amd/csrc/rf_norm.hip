@@ -389,7 +389,7 @@ __global__ __launch_bounds__(kBlock) void norm_slice_kernel(const NormKArgs a) {
             row(i, v);
 #pragma unroll
             for (int e = 0; e < kV; ++e) v[e] = fmaf(v[e] - mu[e], mul[e], bias[e]);
-            if constexpr (act.kind != RF_ACT_NONE) activate(act.kind, v);
+            if constexpr (act.kind != RF_ACT_NONE) activate_fitted(act.kind, v);
             store_n<E, kV>(a.y + (a.frames.out(m) * a.N + r) * a.y_stride + column * 16, 0, v);
         }
     });
@@ -438,7 +438,7 @@ __global__ __launch_bounds__(kThreads) void norm_rows_kernel(const NormKArgs a) 
                 widen<E>(raw[i], v);
 #pragma unroll
                 for (int e = 0; e < kV; ++e) v[e] = fmaf(v[e] - mean[e], mul[e], add[e]);
-                if constexpr (act.kind != RF_ACT_NONE) activate(act.kind, v);
+                if constexpr (act.kind != RF_ACT_NONE) activate_fitted(act.kind, v);
                 if constexpr (kStream) stream_n<E, kV>(q + k * a.y_stride, v);
                 else store_n<E, kV>(q + k * a.y_stride, 0, v);
             }
@@ -446,14 +446,31 @@ __global__ __launch_bounds__(kThreads) void norm_rows_kernel(const NormKArgs a) 
     });
 }
 
+// The larger of each lane's value and that of the lane kDpp names (0 where there is none).
+template <int kDpp, int kRows>
+__device__ __forceinline__ uint32_t dpp_max(uint32_t v) {
+    const uint32_t o = __builtin_amdgcn_update_dpp(0, v, kDpp, kRows, 0xf, false);
+    return v > o ? v : o;
+}
 // The largest of kLanes neighbouring lanes' values (kLanes > 64: of all of the workgroup's kLanes
 // threads, through LDS; `turn` takes two places in turn, so that one barrier does).
 template <int kLanes>
 __device__ __forceinline__ uint32_t lanes_max(uint32_t v, uint32_t (*places)[kLanes / 64 > 0 ? kLanes / 64 : 1], int turn) {
+    if constexpr (kLanes < 64) {
 #pragma unroll
-    for (int d = 1; d < (kLanes < 64 ? kLanes : 64); d *= 2) {
-        const uint32_t o = __shfl_xor(v, d);
-        v = v > o ? v : o;
+        for (int d = 1; d < kLanes; d *= 2) {
+            const uint32_t o = __shfl_xor(v, d);
+            v = v > o ? v : o;
+        }
+    } else {
+        // rows of 16 lanes to their last lane, that to the next rows', lane 63 has all
+        v = dpp_max<0x111, 0xf>(v);      // row_shr 1, 2, 4, 8
+        v = dpp_max<0x112, 0xf>(v);
+        v = dpp_max<0x114, 0xf>(v);
+        v = dpp_max<0x118, 0xf>(v);
+        v = dpp_max<0x142, 0xa>(v);      // row_bcast 15 into rows 1 and 3
+        v = dpp_max<0x143, 0xc>(v);      // row_bcast 31 into rows 2 and 3
+        v = __builtin_amdgcn_readlane(v, 63);
     }
     if constexpr (kLanes > 64) {
         if ((threadIdx.x & 63) == 0) places[turn & 1][threadIdx.x / 64] = v;
@@ -467,45 +484,57 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v, uint32_t (*places)[kLa
     return v;
 }
 
-// kLanes threads to a row, kPer columns to a thread, lane after lane; kC: most channels.
-template <typename E, int kLanes, int kPer, int kC>
+// kLanes threads to a row, kPer columns to a thread, lane after lane. What they are normalised with stays
+// in registers; so does the row until its scale is known.
+template <typename E, int kLanes, int kPer>
 __global__ __launch_bounds__(kThreads) void norm_rows8_kernel(const NormKArgs a) {
     constexpr int kV = 16 / sizeof(E), kRows = kThreads / kLanes;
-    __shared__ __attribute__((aligned(16))) float s_mean[kC], s_mul[kC], s_add[kC];
     __shared__ uint32_t places[2][kLanes / 64 > 0 ? kLanes / 64 : 1];
     const int tid = threadIdx.x;
     const int part = blockIdx.x, m = blockIdx.y;
-    const float *f = affine_at(a, m);
-    for (int c = tid * 4; c < a.C; c += kThreads * 4) {
-        *reinterpret_cast<f32x4_t *>(s_mean + c) = *reinterpret_cast<const f32x4_t *>(f + c);
-        *reinterpret_cast<f32x4_t *>(s_mul + c) = *reinterpret_cast<const f32x4_t *>(f + a.C + c);
-        *reinterpret_cast<f32x4_t *>(s_add + c) = *reinterpret_cast<const f32x4_t *>(f + 2 * a.C + c);
-    }
-    __syncthreads();
     const int lane = tid % kLanes, line = tid / kLanes, columns = a.C / kV;
     const uint8_t *x = a.x + (a.frames.in(m) * a.N) * a.x_stride;
     uint8_t *y = a.y + (a.frames.out(m) * a.N) * a.C;
     float *scales = a.y_scale + a.frames.out(m) * a.N;
+    // (columns past the last are the last once more)
+    float mean[kPer][kV], mul[kPer][kV], add[kPer][kV];
+    const float *f = affine_at(a, m);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int col = lane + i * kLanes, c = (col < columns ? col : columns - 1) * kV;
+        load_n<float, kV>(f, c, mean[i]);
+        load_n<float, kV>(f, a.C + c, mul[i]);
+        load_n<float, kV>(f, 2 * a.C + c, add[i]);
+    }
     with_activation(a.activation, [&](auto act) {
         int turn = 0;
         const int64_t rounds = (a.N + kRows - 1) / kRows;
+        // (a row ahead: the next one's columns are on their way while this one's are rounded)
+        u32x4_t next[kPer];
+        auto ahead = [&](int64_t at) {
+            const int64_t r = at * kRows + line;
+            const uint8_t *p = x + (at < 0 ? 0 : r < a.N ? r : a.N - 1) * a.x_stride;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const int col = lane + i * kLanes;
+                next[i] = load_x(p + (col < columns ? col : columns - 1) * 16);
+            }
+        };
+        ahead(rounds - 1 - part);
         for (int64_t at = rounds - 1 - part; at >= 0; at -= a.row_parts, ++turn) {
             const int64_t first = at * kRows, r = first + line < a.N ? first + line : a.N - 1;
             u32x4_t raw[kPer];
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                const int col = lane + i * kLanes;
-                raw[i] = *reinterpret_cast<const u32x4_t *>(x + r * a.x_stride + (col < columns ? col : columns - 1) * 16);
-            }
+            for (int i = 0; i < kPer; ++i) raw[i] = next[i];
+            ahead(at - a.row_parts);
             float v[kPer][kV];
             uint32_t top = 0;
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
-                const int col = lane + i * kLanes, c = (col < columns ? col : columns - 1) * kV;
                 widen<E>(raw[i], v[i]);
 #pragma unroll
-                for (int e = 0; e < kV; ++e) v[i][e] = fmaf(v[i][e] - s_mean[c + e], s_mul[c + e], s_add[c + e]);
-                if constexpr (act.kind != RF_ACT_NONE) activate(act.kind, v[i]);
+                for (int e = 0; e < kV; ++e) v[i][e] = fmaf(v[i][e] - mean[i][e], mul[i][e], add[i][e]);
+                if constexpr (act.kind != RF_ACT_NONE) activate_fitted(act.kind, v[i]);
 #pragma unroll
                 for (int e = 0; e < kV; ++e) {
                     const uint32_t bits = __float_as_uint(v[i][e]) & 0x7fffffffu;
@@ -591,12 +620,17 @@ __global__ __launch_bounds__(kLanes > kThreads ? kLanes : kThreads) void quantiz
 
 template <typename E>
 void rows8(const NormKArgs &a, dim3 grid, hipStream_t stream) {
-    const int columns = a.C / (16 / static_cast<int>(sizeof(E)));
-    constexpr int kLong = sizeof(E) == 2 ? 4 : 8;      // 32 channels of a thread
-    if (columns <= 16) hipLaunchKernelGGL((norm_rows8_kernel<E, 16, 1, 128>), grid, dim3(kThreads), 0, stream, a);
-    else if (columns <= 64) hipLaunchKernelGGL((norm_rows8_kernel<E, 64, 1, 512>), grid, dim3(kThreads), 0, stream, a);
-    else if (columns <= 64 * kLong) hipLaunchKernelGGL((norm_rows8_kernel<E, 64, kLong, 2048>), grid, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((norm_rows8_kernel<E, 256, kLong, RF_NORM_CHANNELS>), grid, dim3(kThreads), 0, stream, a);
+    // eights of channels to a thread
+    constexpr int kEight = sizeof(E) / 2;
+    auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, a); };
+    if (a.C <= 128) run(norm_rows8_kernel<E, 16, kEight>);
+    else if (a.C <= 512) run(norm_rows8_kernel<E, 64, kEight>);
+    else if (a.C <= 1024) run(norm_rows8_kernel<E, 64, 2 * kEight>);
+    else if (a.C <= 1536) run(norm_rows8_kernel<E, 64, 3 * kEight>);
+    else if (a.C <= 2048) run(norm_rows8_kernel<E, 64, 4 * kEight>);
+    else if (a.C <= 4096) run(norm_rows8_kernel<E, 256, 2 * kEight>);
+    else if (a.C <= 6144) run(norm_rows8_kernel<E, 256, 3 * kEight>);
+    else run(norm_rows8_kernel<E, 256, 4 * kEight>);
 }
 
 template <typename E>

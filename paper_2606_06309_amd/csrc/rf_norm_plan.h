@@ -90,7 +90,14 @@ inline NormPlan norm_plan(int32_t M, int64_t N, int32_t C, int32_t groups, int32
     // four workgroups to a compute unit, of eight rows a thread at least
     const int64_t want = up(4LL * cus, static_cast<int64_t>(M) * p.slices), most = up(N, kNormRows * p.lines);
     p.parts = static_cast<int32_t>(want < most ? want : most);
-    const int64_t row_want = up(kRowRounds * cus, static_cast<int64_t>(M) * p.slices), row_most = up(N, 4 * p.lines);
+    int64_t row_want = up(kRowRounds * cus, static_cast<int64_t>(M) * p.slices), row_most = up(N, 4 * p.lines);
+    if (rows8) {
+        // whole rows of 16, 64 or 256 threads, which have to fetch what they are normalised with first:
+        // as many workgroups as a compute unit holds
+        const int32_t eights = (C + (C <= 2048 ? 511 : 2047)) / (C <= 2048 ? 512 : 2048);   // of channels, a thread
+        row_want = up((eights == 1 ? 6 : eights == 2 ? 4 : eights == 3 ? 3 : 2) * static_cast<int64_t>(cus), M);
+        row_most = up(N, C <= 128 ? 16 : C <= 2048 ? 4 : 1);
+    }
     p.row_parts = static_cast<int32_t>(row_want < row_most ? row_want : row_most);
     const int64_t local = (static_cast<int64_t>(p.cols) * p.vec - 2) / (C / groups) + 2;
     p.local = static_cast<int32_t>(local < groups ? local : groups);

@@ -179,3 +179,16 @@ def test_a_view_at_an_odd_scale():
     wide = torch.cat([torch.zeros(1, device="cuda"), xs])
     y = rf.rf_frame_linear_i8(xq, wide[1:], wq, ws, dtype=F32)
     block.assert_within(y, *ref.linear_i8(xq, xs, wq, ws))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("rows", [2, 300])
+def test_activations_of_all_arguments(rows, act, dtype):
+    """Arguments from -60 to 60, near 0 and large: of the bias, under sums of zero."""
+    n, K = 2048, 16
+    b = torch.cat([torch.linspace(-60, 60, 1024), torch.linspace(-6, 6, 960), torch.logspace(-30, 30, 64)]).to(dtype).cuda()
+    xq, wq = torch.zeros((rows, K), dtype=torch.int8, device="cuda"), torch.zeros((n, K), dtype=torch.int8, device="cuda")
+    xs, ws = torch.ones(rows, device="cuda"), torch.ones(n, device="cuda")
+    y = rf.rf_frame_linear_i8(xq, xs, wq, ws, b, act)
+    block.assert_within(y, *ref.linear_i8(xq, xs, wq, ws, b, act, dtype=dtype))
