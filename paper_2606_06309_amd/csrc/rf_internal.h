@@ -163,7 +163,7 @@ hipError_t launch_similarity(const SimParams &p, hipStream_t stream);
 // in(m) * N + n of what is read and out(m) * N + n of what is written. In bytes:
 // kernel arguments are written to device memory at every launch.
 struct RowFrames {
-    uint8_t frame[kMaxFrames];
+    alignas(4) uint8_t frame[kMaxFrames];
     uint8_t in_full, out_full;
     __host__ __device__ int32_t in(int32_t m) const { return in_full ? frame[m] : m; }
     __host__ __device__ int32_t out(int32_t m) const { return out_full ? frame[m] : m; }

@@ -227,6 +227,39 @@ __device__ __forceinline__ void finish(const LinearKArgs &a, uint32_t r, int c, 
     f.store(a, c, v);
 }
 
+// Where a wave's product rows are among those written: rows of one frame, or of two with one border, are
+// their own number and a frame's distance (uniform, of scalar loads), others take a division and a
+// load each.
+struct NearRows {
+    bool near;
+    uint32_t border;           // first row of the second frame (of none: behind all)
+    int64_t shift, shift2;
+    int frame, frame2;         // of the list
+    __device__ __forceinline__ NearRows(const LinearKArgs &a, uint32_t first, uint32_t count) {
+        near = true;
+        border = 0xffffffffu;
+        shift = shift2 = 0;
+        frame = frame2 = 0;
+        if (!a.frames.out_full && !a.gate_rows) return;   // (compact rows are at their number)
+        if (first >= a.rows) first = a.rows - 1;
+        const uint32_t last = first + count - 1 < a.rows ? first + count - 1 : a.rows - 1;
+        frame = static_cast<int>(first / a.N);
+        border = (static_cast<uint32_t>(frame) + 1) * a.N;
+        frame2 = last < border ? frame : frame + 1;
+        near = last < border || last - border < a.N;
+        if (last < border) border = 0xffffffffu;
+        if (a.frames.out_full) {
+            shift = static_cast<int64_t>(frame_at(a.frames, frame) - frame) * a.N;
+            shift2 = static_cast<int64_t>(frame_at(a.frames, frame2) - frame2) * a.N;
+        }
+    }
+    __device__ __forceinline__ int64_t operator()(const LinearKArgs &a, uint32_t r) const {
+        if (near) return static_cast<int64_t>(r) + (r < border ? shift : shift2);
+        const uint32_t m = r / a.N;
+        return static_cast<int64_t>(a.frames.out(m)) * a.N + (r - m * a.N);
+    }
+};
+
 // kN neighbouring sums of a part of the reduction, to the workspace.
 template <int kN, typename V>
 __device__ __forceinline__ void store_part(const LinearKArgs &a, int part, uint32_t r, int c, const V (&v)[kN]) {
@@ -259,6 +292,147 @@ __device__ __forceinline__ bool tile_of(const LinearKArgs &a, int bid, int &rt, 
     ct = in / height;
     rt = first + in - ct * height;
     return true;
+}
+
+// A tile's epilogue: 32 rows x 64 features at a time through 8 KB of the wave's own, 256
+// bytes a row, 16-byte units permuted by row % 16; a lane then has 8 neighbouring
+// features of a row, and eight lanes whole lines of y. 256-row tiles, taken where y is
+// large, send it past the caches if it is no wider than x: 50 -> 45 us at 9,360 x 1,536 x
+// 1,536 without residual, 1,977 -> 1,896 at 21,600 x 5,120 x 5,120 and a product that reads
+// it next; wider ones so, a feed-forward's, 1,536 to 6,144 and back: 323 -> 340; 128-row tiles
+// so, the two at 3,600 x 1,536 x 1,536: 54 -> 56.
+// acc, x_scale: a wave's sums and its rows' scales; c: this lane's first feature; mine: 8 KB of the wave's own
+// in LDS; block(b): where residual(b) has brought the residual's rows of block b, if `stage`.
+template <typename In, typename E, int kRB, int kBM, int kScales, typename Block, typename Residual>
+__device__ __forceinline__ void tile_epilogue(const LinearKArgs &a, const typename Sums<In>::of32 (&acc)[2][kRB],
+                                              const float (&x_scale)[kScales], uint32_t row0, int wr, int c, int part,
+                                              bool stage, uint8_t *mine, Block block, Residual residual) {
+    typedef typename Sums<In>::of16 sums4_t;
+    constexpr bool kI8 = sizeof(In) == 1, kStage = sizeof(E) == 2;
+    const int lane = threadIdx.x & 63, col = lane & 31, grp = lane >> 5, sub = lane / 8;
+    // bias and gate of this lane's features, the gate of the frame of the wave's first rows
+    Epilogue<In, 8> ep;
+    const NearRows out(a, row0 + wr * kRB * 32, kRB * 32);
+    int gate_of = -1;
+#pragma unroll
+    for (int b = 0; b < kRB; ++b) {
+        // (a block's rows mostly are of one frame, and of that of the block before)
+        const uint32_t first = row0 + (wr * kRB + b) * 32;
+        const int frame = first < out.border ? out.frame : out.frame2;
+        const bool one_gate = !a.gate_rows || (out.near && (first >= out.border || first + 31 < out.border));
+        if (a.parts == 1 && c + 8 <= a.n_out) {
+            if (b == 0) ep.template load<E>(a, c, one_gate ? (a.gate_rows ? frame_at(a.frames, frame) : 0) : -1);
+            else if (a.gate_rows && one_gate && gate_of != frame) ep.template gate_of<E>(a, c, frame_at(a.frames, frame));
+        }
+        gate_of = one_gate ? frame : -1;
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+            for (int g4 = 0; g4 < 4; ++g4) {
+                const int unit = (f * 8 + g4 * 2 + grp) ^ (col & 15);
+                *reinterpret_cast<sums4_t *>(mine + col * 256 + unit * 16) =
+                    sums4_t{acc[f][b][g4 * 4], acc[f][b][g4 * 4 + 1], acc[f][b][g4 * 4 + 2], acc[f][b][g4 * 4 + 3]};
+            }
+        wait_lds_reads();   // (a wave's LDS accesses run in order; this orders the compiler's)
+        if (stage) {
+            // (block b's loads are older than the stores of the block before, four of them
+            // if any row of this block is stored, and the next block's loads)
+            if (b == 0) wait_loads<0>();
+            else if (b + 1 < kRB) wait_loads<8>();
+            else wait_loads<4>();
+        }
+        typedef typename Value<In>::type value_t;
+        auto row_of = [&](int i) { return first + i * 8 + sub; };
+        auto sums_of = [&](int i, value_t (&sums)[8]) {
+            const int lr = i * 8 + sub;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const sums4_t x =
+                    *reinterpret_cast<const sums4_t *>(mine + lr * 256 + ((((lane % 8) * 2 + h) ^ (lr & 15)) * 16));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sums[h * 4 + e] = x[e];
+            }
+        };
+        // (fp32 may end in the middle of eight features)
+        const bool whole = c + 8 <= a.n_out, broken = sizeof(E) == 4 && c < a.n_out && !whole;
+        if (a.parts > 1) {
+#pragma unroll 1
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t r = row_of(i);
+                if (r >= a.rows) break;
+                value_t sums[8];
+                sums_of(i, sums);
+                if (whole) store_part<8>(a, part, r, c, sums);
+                else if (broken) store_part<4>(a, part, r, c, {sums[0], sums[1], sums[2], sums[3]});
+            }
+        } else {
+            // (fp32 results of 8-bit integers: the residual's next row comes in while this one is finished,
+            // where a load for each row waits for memory four times a block, 22.4 us at 1,581 x 1,360 x 1,004)
+            constexpr bool kAhead = kI8 && sizeof(E) == 4;
+            [[maybe_unused]] float ahead[8] = {};
+            [[maybe_unused]] auto row_ahead = [&](int i) {
+                const uint32_t r = row_of(i);
+                if (a.residual && whole) load_n<E, 8>(a.residual, out(a, r < a.rows ? r : a.rows - 1) * a.n_out + c, ahead);
+            };
+            if constexpr (kAhead) row_ahead(0);
+#pragma unroll 1
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t r = row_of(i);
+                [[maybe_unused]] float here[8];
+                if constexpr (kAhead) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) here[e] = ahead[e];
+                    row_ahead(i < 3 ? i + 1 : 3);
+                }
+                float v[8];
+                if constexpr (kI8) {
+                    // (the row's scale is in lane 32 (b % 2) + its number in the block)
+                    const float row_scale = __shfl(x_scale[b / 2], b % 2 * 32 + i * 8 + sub);
+                    value_t sums[8];
+                    sums_of(i, sums);
+                    ep.scaled(row_scale, sums, v);
+                } else {
+                    sums_of(i, v);
+                }
+                if (r >= a.rows || !whole) continue;
+                const int64_t dst = out(a, r);
+                if (!one_gate) ep.template gate_of<E>(a, c, a.frames.frame[r / a.N]);
+                ep.apply(a, v);
+                if (a.residual) {
+                    float t[8];
+                    if constexpr (kStage) {
+                        widen8(*reinterpret_cast<const u32x4_t *>(block(b) + i * 1024 + lane * 16), t);
+                    } else if constexpr (kAhead) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) t[e] = here[e];
+                    } else {
+                        load_n<E, 8>(a.residual, dst * a.n_out + c, t);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] += t[e];
+                }
+                if (kRB == 4 && a.stream) {
+                    asm volatile("" ::: "memory");   // (without these two the compiler makes one store of both)
+                    stream_8<E>(a.y, dst * a.n_out + c, v);
+                    asm volatile("" ::: "memory");
+                } else {
+                    store_n<E, 8>(a.y, dst * a.n_out + c, v);
+                }
+            }
+            if (broken) {
+#pragma unroll 1
+                for (int i = 0; i < 4; ++i) {
+                    if (row_of(i) >= a.rows) break;
+                    value_t sums[8];
+                    sums_of(i, sums);
+                    value_t lo[4] = {sums[0], sums[1], sums[2], sums[3]};
+                    finish<In, E, 4>(a, row_of(i), c, lo);
+                }
+            }
+        }
+        wait_lds_reads();
+        if (stage && b + 2 < kRB) residual(b + 2);
+    }
 }
 
 // kRB blocks of 32 rows to a wave, kWR x kWC waves of (32 kRB rows x 64 features).
@@ -315,7 +489,7 @@ void linear_tile_kernel(const LinearKArgs a) {
     issue_w(s0, 0);   // W does not wait for where x's rows are
     // the scales of the wave's rows, a lane each
     constexpr int kScales = (kRB + 1) / 2;
-    [[maybe_unused]] float x_scale[kScales];
+    float x_scale[kScales] = {};
     if constexpr (kI8) {
 #pragma unroll
         for (int i = 0; i < kScales; ++i) {
@@ -359,7 +533,6 @@ void linear_tile_kernel(const LinearKArgs a) {
     };
 
     typedef typename Sums<In>::of32 sums_t;
-    typedef typename Sums<In>::of16 sums4_t;
     sums_t acc[2][kRB];
 #pragma unroll
     for (int f = 0; f < 2; ++f)
@@ -474,123 +647,10 @@ void linear_tile_kernel(const LinearKArgs a) {
     wait_lds_reads();
     __syncthreads();
 
-    // ---- epilogue: 32 rows x 64 features at a time through 8 KB of the wave's own, 256
-    // bytes a row, 16-byte units permuted by row % 16; a lane then has 8 neighbouring
-    // features of a row, and eight lanes whole lines of y. 256-row tiles, taken where y is
-    // large, send it past the caches if it is no wider than x: 50 -> 45 us at 9,360 x 1,536 x
-    // 1,536 without residual, 1,977 -> 1,896 at 21,600 x 5,120 x 5,120 and a product that reads
-    // it next; wider ones so, a feed-forward's, 1,536 to 6,144 and back: 323 -> 340; 128-row tiles
-    // so, the two at 3,600 x 1,536 x 1,536: 54 -> 56. ----
-    // bias and gate of this lane's features, where all the tile's rows have one gate
-    const uint32_t last = row0 + kBM - 1 < a.rows ? row0 + kBM - 1 : a.rows - 1;
-    const bool one_gate = !a.gate_rows || row0 / a.N == last / a.N;
-    Epilogue<In, 8> ep;
-    if (a.parts == 1 && c + 8 <= a.n_out) ep.template load<E>(a, c, one_gate ? a.frames.frame[row0 / a.N] : -1);
     // (8 KB of a wave, in the buffers of the last step, and in 64-row tiles all of x's)
     uint8_t *mine = lds + (wave < kWC ? (free_odd ^ 1) * kWBuf + wave * 8192
                                       : 2 * kWBuf + (kRB == 1 ? 0 : (free_odd ^ 1) * kXBuf) + (wave - kWC) * 8192);
-#pragma unroll
-    for (int b = 0; b < kRB; ++b) {
-#pragma unroll
-        for (int f = 0; f < 2; ++f)
-#pragma unroll
-            for (int g4 = 0; g4 < 4; ++g4) {
-                const int unit = (f * 8 + g4 * 2 + grp) ^ (col & 15);
-                *reinterpret_cast<sums4_t *>(mine + col * 256 + unit * 16) =
-                    sums4_t{acc[f][b][g4 * 4], acc[f][b][g4 * 4 + 1], acc[f][b][g4 * 4 + 2], acc[f][b][g4 * 4 + 3]};
-            }
-        wait_lds_reads();   // (a wave's LDS accesses run in order; this orders the compiler's)
-        if (stage) {
-            // (block b's loads are older than the stores of the block before, four of them
-            // if any row of this block is stored, and the next block's loads)
-            if (b == 0) wait_loads<0>();
-            else if (b + 1 < kRB) wait_loads<8>();
-            else wait_loads<4>();
-        }
-        // (fp32 results of 8-bit integers: the residual's next row comes in while this one is finished, where
-        // a load for each row waits for memory four times a block, 22.4 us at 1,581 x 1,360 x 1,004)
-        constexpr bool kAhead = kI8 && sizeof(E) == 4;
-        [[maybe_unused]] float ahead[8] = {};
-        [[maybe_unused]] auto row_ahead = [&](int i) {
-            uint32_t r = row0 + (wr * kRB + b) * 32 + i * 8 + sub;
-            if (r >= a.rows) r = a.rows - 1;
-            const uint32_t m = r / a.N;
-            if (c + 8 <= a.n_out)   // (four features behind the last eight have loads of their own)
-                load_n<E, 8>(a.residual, (static_cast<int64_t>(a.frames.out(m)) * a.N + (r - m * a.N)) * a.n_out + c, ahead);
-        };
-        if constexpr (kAhead) {
-            if (a.residual && a.parts == 1) row_ahead(0);
-        }
-#pragma unroll 1
-        for (int i = 0; i < 4; ++i) {
-            const int lr = i * 8 + sub;
-            const uint32_t r = row0 + (wr * kRB + b) * 32 + lr;
-            [[maybe_unused]] float here[8];
-            if constexpr (kAhead) {
-                if (a.residual && a.parts == 1) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) here[e] = ahead[e];
-                    row_ahead(i < 3 ? i + 1 : 3);
-                }
-            }
-            typename Value<In>::type sums[8];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const sums4_t x =
-                    *reinterpret_cast<const sums4_t *>(mine + lr * 256 + ((((lane % 8) * 2 + h) ^ (lr & 15)) * 16));
-#pragma unroll
-                for (int e = 0; e < 4; ++e) sums[h * 4 + e] = x[e];
-            }
-            // (the row's scale is in lane 32 (b % 2) + lr)
-            [[maybe_unused]] float row_scale = 0.0f;
-            if constexpr (kI8) row_scale = __shfl(x_scale[b / 2], b % 2 * 32 + lr);
-            if (r >= a.rows || c >= a.n_out) continue;
-            // (fp32 may end in the middle of eight features)
-            if (sizeof(E) == 4 && c + 8 > a.n_out) {
-                typename Value<In>::type lo[4] = {sums[0], sums[1], sums[2], sums[3]};
-                if (a.parts > 1) store_part<4>(a, part, r, c, lo);
-                else finish<In, E, 4>(a, r, c, lo);
-                continue;
-            }
-            if (a.parts > 1) {
-                store_part<8>(a, part, r, c, sums);
-                continue;
-            }
-            float v[8];
-            if constexpr (kI8) {
-                ep.scaled(row_scale, sums, v);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = sums[e];
-            }
-            const uint32_t m = r / a.N;
-            const int64_t dst = static_cast<int64_t>(a.frames.out(m)) * a.N + (r - m * a.N);
-            if (!one_gate) ep.template gate_of<E>(a, c, a.frames.frame[m]);
-            ep.apply(a, v);
-            if (a.residual) {
-                float t[8];
-                if constexpr (kStage) {
-                    widen8(*reinterpret_cast<const u32x4_t *>(block(b) + i * 1024 + lane * 16), t);
-                } else if constexpr (kAhead) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) t[e] = here[e];
-                } else {
-                    load_n<E, 8>(a.residual, dst * a.n_out + c, t);
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] += t[e];
-            }
-            if (kRB == 4 && a.stream) {
-                asm volatile("" ::: "memory");   // (without these two the compiler makes one store of both)
-                stream_8<E>(a.y, dst * a.n_out + c, v);
-                asm volatile("" ::: "memory");
-            } else {
-                store_n<E, 8>(a.y, dst * a.n_out + c, v);
-            }
-        }
-        wait_lds_reads();
-        if (stage && b + 2 < kRB) residual(b + 2);
-    }
+    tile_epilogue<In, E, kRB, kBM>(a, acc, x_scale, row0, wr, c, part, stage, mine, block, residual);
 }
 
 constexpr int kFewWaves = kLinearFewWaves;

@@ -122,11 +122,14 @@ inline LinearPlan linear_plan(int64_t rows, int32_t K, int32_t n_out, int32_t dt
         double round;
         double step[3];      // with one, two, three workgroups to a compute unit
     };
-    static const Form forms[2][3] = {{{kTile64, 64, 128, 3, 3.0, {0.53, 0.68, 1.0}},
+    static const Form forms[3][3] = {{{kTile64, 64, 128, 3, 3.0, {0.53, 0.68, 1.0}},
                                       {kTile128, 128, 128, 2, 4.0, {0.80, 0.95, 0.95}},
                                       {kTile256, 256, 256, 1, 8.0, {1.55, 1.55, 1.55}}},
                                      {{kTile64, 64, 128, 3, 3.0, {1.1, 1.95, 2.93}},
-                                      {kTile128, 128, 128, 2, 4.0, {2.4, 3.65, 3.65}}}};
+                                      {kTile128, 128, 128, 2, 4.0, {2.4, 3.65, 3.65}}},
+                                     {{kTile64, 64, 128, 3, 3.0, {0.53, 0.68, 1.0}},
+                                      {kTile128, 128, 128, 2, 4.0, {0.80, 0.95, 0.95}},
+                                      {kTile256, 256, 256, 1, 8.0, {1.55, 1.55, 1.55}}}};
     const int n_forms = dtype == RF_F32 ? 2 : 3;
     constexpr int64_t kLeastSteps = 4, kMostParts = 16;
     constexpr double kJoin = 3.0;
@@ -134,7 +137,7 @@ inline LinearPlan linear_plan(int64_t rows, int32_t K, int32_t n_out, int32_t dt
     p.steps = static_cast<int32_t>(up(bytes, kLinearStep));
     double best = 0.0;
     for (int i = 0; i < n_forms; ++i) {
-        const Form &f = forms[dtype == RF_F32][i];
+        const Form &f = forms[dtype == kI8 ? 2 : dtype == RF_F32][i];
         if (far && f.form != kTile128) continue;
         const int64_t row_tiles = up(rows, f.rows), col_tiles = up(n_out, f.cols);
         for (int64_t parts = 1; parts <= kMostParts; ++parts) {

@@ -17,6 +17,12 @@ __device__ __forceinline__ void global_lds16(const uint8_t *p, uint8_t *dst) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)p, (lds_void_t *)dst, 16, 0, 0);
 }
 
+// Frame m of the list, m the same for all lanes: a scalar load of the four bytes that it is among.
+__device__ __forceinline__ int frame_at(const RowFrames &f, int m) {
+    const uint32_t four = reinterpret_cast<const uint32_t *>(f.frame)[static_cast<uint32_t>(m) / 4];
+    return static_cast<int>((four >> (8 * (m % 4))) & 255);
+}
+
 // kN (4 or 8) consecutive elements, widened / rounded once to nearest even.
 template <typename E, int kN>
 __device__ __forceinline__ void load_n(const void *p, int64_t at, float (&v)[kN]) {
