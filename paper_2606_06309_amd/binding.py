@@ -10,6 +10,7 @@ if the library has not been built.
 import ctypes
 import functools
 import os
+import sys
 
 import numpy as np
 import torch
@@ -1020,21 +1021,52 @@ def rf_frame_linear(x, weight, bias=None, activation: str = "none", gate=None, r
 _FRAME0 = np.zeros(1, dtype=np.int32)
 
 
+# These calls are a few microseconds of a GPU's time at their smallest, so their checks go through each tensor
+# once, and the ids travel as the bytes of their array (its address costs more to ask for than a copy).
+
+_ID0 = (0).to_bytes(4, sys.byteorder)
+
+
 def _frame_rows(frame_ids, T, rows_per_frame, in_full, out_full, rows):
-    """(ids, their address, M, T, rows_per_frame, rows read, rows written) of a call on the rows of listed frames, or
-    without a list on all `rows` rows as one frame."""
+    """(ids as bytes, M, T, rows_per_frame, rows written, flags) of a call on the rows of listed frames, or without
+    a list on all `rows` rows as one frame."""
     if frame_ids is None:
         if T is not None or rows_per_frame is not None or in_full or out_full:
             raise ValueError("T, rows_per_frame, in_full and out_full go with frame_ids")
-        frame_ids, T, rows_per_frame = _FRAME0, 1, rows
-    elif T is None or rows_per_frame is None:
+        return _ID0, 1, 1, rows, rows, 0
+    if T is None or rows_per_frame is None:
         raise ValueError("frame_ids needs T and rows_per_frame")
-    ids, ids_p = _ids(frame_ids)
+    ids = frame_ids if _fits(frame_ids, _I32) else np.asarray(list(frame_ids), dtype=np.int32)
     M = ids.size
-    rows_in, rows_out = rows_per_frame * (T if in_full else M), rows_per_frame * (T if out_full else M)
-    if rows != rows_in:
-        raise ValueError(f"x has {rows} rows, the layout asks for {rows_in}")
-    return ids, ids_p, M, T, rows_per_frame, rows_in, rows_out
+    if rows != rows_per_frame * (T if in_full else M):
+        raise ValueError(f"x has {rows} rows, the layout asks for {rows_per_frame * (T if in_full else M)}")
+    return (ids.tobytes(), M, T, rows_per_frame, rows_per_frame * (T if out_full else M),
+            (RF_ROWS_IN_FULL if in_full else 0) | (RF_ROWS_OUT_FULL if out_full else 0))
+
+
+def _addresses(tensors):
+    """_on_device of (tensor or None, name, dtype, contiguous) with these checked."""
+    index, out = -2, []
+    for t, name, dtype, contiguous in tensors:
+        if t is None:
+            out.append(None)
+            continue
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name} must be a torch.Tensor")
+        if t.dtype is not dtype:
+            raise TypeError(f"{name} has dtype {t.dtype}, not {dtype}")
+        if contiguous and not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+        on = t.get_device()
+        if on != index:
+            if on < 0:
+                raise ValueError(f"{name} must be a device tensor")
+            if index < 0:
+                index = torch.cuda.current_device()
+            if on != index:
+                raise ValueError(f"{name} is on {t.device}, the current device is cuda:{index}")
+        out.append(t.data_ptr())
+    return index, out
 
 
 def _row_stride(t, name, rows, features):
@@ -1052,17 +1084,19 @@ def _row_stride(t, name, rows, features):
 
 
 def _rows_8bit(out, out_scale, rows, features, x, whole, stream):
-    """out and out_scale of rows in 8 bits, checked or allocated (`whole`: every row of the layout is written)."""
-    if not whole and (out is None or out_scale is None):
-        raise ValueError("out and out_scale must be given with out_full: rows of other frames are left as they are")
-    if out is None:
-        out = _empty((rows, features), torch.int8, x.device, stream)
-    if out_scale is None:
-        out_scale = _empty((rows,), torch.float32, x.device, stream)
-    if out.dtype != torch.int8 or out.shape != (rows, features) or not out.is_contiguous():
-        raise ValueError(f"out must be contiguous int8 [{rows}][{features}]")
-    if out_scale.dtype != torch.float32 or out_scale.shape != (rows,) or not out_scale.is_contiguous():
-        raise ValueError(f"out_scale must be contiguous float32 [{rows}]")
+    """out and out_scale of rows in 8 bits, their shapes checked, or allocated (`whole`: every row of the layout is
+    written)."""
+    if out is None or out_scale is None:
+        if not whole:
+            raise ValueError("out and out_scale must be given with out_full: rows of other frames are left as they are")
+        if out is None:
+            out = _empty((rows, features), torch.int8, x.device, stream)
+        if out_scale is None:
+            out_scale = _empty((rows,), torch.float32, x.device, stream)
+    if out.shape != (rows, features) or out.dtype is not torch.int8:
+        raise ValueError(f"out must be int8 [{rows}][{features}]")
+    if out_scale.shape != (rows,) or out_scale.dtype is not torch.float32:
+        raise ValueError(f"out_scale must be float32 [{rows}]")
     return out, out_scale
 
 
@@ -1075,14 +1109,14 @@ def rf_frame_quantize(x, frame_ids=None, T=None, rows_per_frame=None, in_full: b
     (required then unless M = T). A weight [out_features][in_features] is rounded so too."""
     if x.dim() != 2:
         raise ValueError("x must be [rows][features]")
-    K = x.shape[1]
-    ids, ids_p, M, T, N, rows_in, rows_out = _frame_rows(frame_ids, T, rows_per_frame, in_full, out_full, x.shape[0])
-    stride = _row_stride(x, "x", rows_in, K)
+    rows, K = x.shape
+    ids, M, T, N, rows_out, flags = _frame_rows(frame_ids, T, rows_per_frame, in_full, out_full, rows)
+    stride = _row_stride(x, "x", rows, K)
     out, out_scale = _rows_8bit(out, out_scale, rows_out, K, x, not out_full or M == T, stream)
     code = _dtype_code(x.dtype)
-    index, ptrs = _on_device(((x, "x"), (out, "out"), (out_scale, "out_scale")))
-    flags = (RF_ROWS_IN_FULL if in_full else 0) | (RF_ROWS_OUT_FULL if out_full else 0)
-    _check(lib.rf_frame_quantize(*ptrs, ids_p, M, T, N, K, stride, flags, code, _stream_on(stream, index)))
+    index, (x_p, out_p, scale_p) = _addresses(((x, "x", x.dtype, False), (out, "out", torch.int8, True),
+                                               (out_scale, "out_scale", torch.float32, True)))
+    _check(lib.rf_frame_quantize(x_p, out_p, scale_p, ids, M, T, N, K, stride, flags, code, _stream_on(stream, index)))
     return out, out_scale
 
 
@@ -1106,50 +1140,47 @@ def rf_frame_linear_i8(x, x_scale, weight, weight_scale, bias=None, activation: 
     [out][in] and weight_scale float32 [out], as rf_frame_quantize makes them; bias, gate,
     residual and out as rf_frame_linear, all of the result's type: dtype, or out's or
     theirs if given, else bfloat16. The workspace is allocated here if not given."""
-    if x.dim() != 2 or weight.dim() != 2 or weight.shape[1] != x.shape[1]:
+    if x.dim() != 2 or weight.dim() != 2:
         raise ValueError("x must be [rows][in_features], weight [out_features][in_features]")
-    if activation not in ACTIVATIONS:
+    (rows, K), (n_out, K_w) = x.shape, weight.shape
+    if K != K_w:
+        raise ValueError("x must be [rows][in_features], weight [out_features][in_features]")
+    act = ACTIVATIONS.get(activation)
+    if act is None:
         raise ValueError(f"unknown activation {activation!r}: one of {sorted(ACTIVATIONS)}")
-    n_out, K = weight.shape
-    ids, ids_p, M, T, N, rows_in, rows_out = _frame_rows(frame_ids, T, rows_per_frame, in_full, out_full, x.shape[0])
+    ids, M, T, N, rows_out, flags = _frame_rows(frame_ids, T, rows_per_frame, in_full, out_full, rows)
     if dtype is None:
-        dtype = next((t.dtype for t in (out, residual, bias, gate) if t is not None), torch.bfloat16)
+        dtype = torch.bfloat16
+        for t in (out, residual, bias, gate):
+            if t is not None:
+                dtype = t.dtype
+                break
     if out is None:
         if out_full and M != T:
             raise ValueError("out must be given with out_full: rows of other frames are left as they are")
         out = _empty((rows_out, n_out), dtype, x.device, stream)
-    for t, name in ((out, "out"), (residual, "residual")):
-        if t is not None and t.shape != (rows_out, n_out):
-            raise ValueError(f"{name} must be [{rows_out}][{n_out}]")
+    elif out.shape != (rows_out, n_out):
+        raise ValueError(f"out must be [{rows_out}][{n_out}]")
+    if residual is not None and residual.shape != (rows_out, n_out):
+        raise ValueError(f"residual must be [{rows_out}][{n_out}]")
     if bias is not None and bias.shape != (n_out,):
         raise ValueError(f"bias must be [{n_out}]")
-    if x_scale.shape != (rows_in,) or weight_scale.shape != (n_out,):
-        raise ValueError(f"x_scale must be [{rows_in}], weight_scale [{n_out}]")
-    for t, name, want in ((x, "x", torch.int8), (weight, "weight", torch.int8), (x_scale, "x_scale", torch.float32),
-                          (weight_scale, "weight_scale", torch.float32)):
-        if t.dtype != want:
-            raise TypeError(f"{name} has dtype {t.dtype}, not {want}")
-    flags = (RF_ROWS_IN_FULL if in_full else 0) | (RF_ROWS_OUT_FULL if out_full else 0)
+    if x_scale.shape != (rows,) or weight_scale.shape != (n_out,):
+        raise ValueError(f"x_scale must be [{rows}], weight_scale [{n_out}]")
     if gate is not None and gate.shape != (n_out,):
         if gate.shape != (T, n_out):
             raise ValueError(f"gate must be [{n_out}] or [{T}][{n_out}]")
         flags |= RF_GATE_PER_FRAME
-    tensors = ((x, "x"), (x_scale, "x_scale"), (weight, "weight"), (weight_scale, "weight_scale"), (bias, "bias"),
-               (gate, "gate"), (residual, "residual"), (out, "out"))
     code = _dtype_code(dtype)
-    for t, name in tensors[4:]:
-        if t is not None and t.dtype != dtype:
-            raise TypeError(f"{name} has dtype {t.dtype}, the result's is {dtype}")
-    for t, name in tensors:
-        if t is not None and not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous")
-    index, ptrs = _on_device(tensors)
-    if workspace is None and M > 0 and N > 0 and weight.numel() > 0:
+    index, ptrs = _addresses(((x, "x", torch.int8, True), (x_scale, "x_scale", torch.float32, True),
+                              (weight, "weight", torch.int8, True), (weight_scale, "weight_scale", torch.float32, True),
+                              (bias, "bias", dtype, True), (gate, "gate", dtype, True), (residual, "residual", dtype, True),
+                              (out, "out", dtype, True)))
+    if workspace is None and M > 0 and N > 0 and n_out > 0 and K > 0:
         need = _linear_i8_need(index, M, N, K, n_out, code)
         workspace = _empty(need, torch.uint8, x.device, stream) if need > 0 else None
     ws_p, wbytes = _workspace_arg(workspace)
-    _check(lib.rf_frame_linear_i8(*ptrs, ids_p, M, T, N, K, n_out, ACTIVATIONS[activation], flags, code, ws_p, wbytes,
-                                  _stream_on(stream, index)))
+    _check(lib.rf_frame_linear_i8(*ptrs, ids, M, T, N, K, n_out, act, flags, code, ws_p, wbytes, _stream_on(stream, index)))
     return out
 
 
@@ -1179,39 +1210,44 @@ def rf_frame_group_norm(x, groups: int, weight=None, bias=None, eps: float = 1e-
     but for rows in 8 bits. The workspace is allocated here if not given."""
     if x.dim() != 2:
         raise ValueError("x must be [rows][channels]")
-    if activation not in ACTIVATIONS:
+    act = ACTIVATIONS.get(activation)
+    if act is None:
         raise ValueError(f"unknown activation {activation!r}: one of {sorted(ACTIVATIONS)}")
-    C = x.shape[1]
-    ids, ids_p, M, T, N, rows_in, rows_out = _frame_rows(frame_ids, T, rows_per_frame, in_full, out_full, x.shape[0])
-    xs, ys = _row_stride(x, "x", rows_in, C), 0
-    int8 = int8 or out_scale is not None or (out is not None and out.dtype == torch.int8)
-    if int8:
+    rows, C = x.shape
+    ids, M, T, N, rows_out, flags = _frame_rows(frame_ids, T, rows_per_frame, in_full, out_full, rows)
+    xs, ys = _row_stride(x, "x", rows, C), 0
+    dtype = x.dtype
+    if int8 or out_scale is not None or (out is not None and out.dtype is torch.int8):
+        int8 = True
         out, out_scale = _rows_8bit(out, out_scale, rows_out, C, x, not out_full or M == T, stream)
     else:
         if out is None:
             if out_full and M != T:
                 raise ValueError("out must be given with out_full: rows of other frames are left as they are")
-            out = _empty((rows_out, C), x.dtype, x.device, stream)
+            out = _empty((rows_out, C), dtype, x.device, stream)
         ys = _row_stride(out, "out", rows_out, C)
-    flags = (RF_ROWS_IN_FULL if in_full else 0) | (RF_ROWS_OUT_FULL if out_full else 0)
-    per_frame = {t.shape == (T, C) for t in (weight, bias) if t is not None}
+    shapes = set()
     for t, name in ((weight, "weight"), (bias, "bias")):
-        if t is not None and ((t.shape != (C,) and t.shape != (T, C)) or not t.is_contiguous()):
-            raise ValueError(f"{name} must be contiguous [{C}] or [{T}][{C}]")
-    if len(per_frame) > 1:
+        if t is not None:
+            shape = t.shape
+            if shape != (C,) and shape != (T, C):
+                raise ValueError(f"{name} must be [{C}] or [{T}][{C}]")
+            shapes.add(len(shape))
+    if len(shapes) > 1:
         raise ValueError("weight and bias must both be of each frame, or neither")
-    if True in per_frame:
+    if 2 in shapes:
         flags |= RF_AFFINE_PER_FRAME
-    code = _same_dtype(((x, "x"), (weight, "weight"), (bias, "bias"), (None if int8 else out, "out")))
-    index, ptrs = _on_device(((x, "x"), (weight, "weight"), (bias, "bias"), (out, "out"), (out_scale, "out_scale")))
+    code = _dtype_code(dtype)
+    index, ptrs = _addresses(((x, "x", dtype, False), (weight, "weight", dtype, True), (bias, "bias", dtype, True),
+                              (out, "out", torch.int8 if int8 else dtype, int8),
+                              (out_scale, "out_scale", torch.float32, True)))
     if workspace is None and M > 0 and N > 0 and C > 0 and groups > 0 and frames_together > 0:
         need = _norm_need(index, M, N, C, groups, frames_together, int8, code)
         workspace = _empty(need, torch.uint8, x.device, stream) if need > 0 else None
     ws_p, wbytes = _workspace_arg(workspace)
-    _check(lib.rf_frame_group_norm(*ptrs, ids_p, M, T, N, C, groups, frames_together, eps, ACTIVATIONS[activation], xs, ys,
-                                   flags, code, ws_p, wbytes, _stream_on(stream, index)))
+    _check(lib.rf_frame_group_norm(*ptrs, ids, M, T, N, C, groups, frames_together, eps, act, xs, ys, flags, code, ws_p,
+                                   wbytes, _stream_on(stream, index)))
     return (out, out_scale) if int8 else out
-
 
 
 # --- device probes (measurement support) ------------------------------------------

@@ -807,9 +807,12 @@ void run(const LinearPlan &p, const LinearKArgs &a, bool far, dim3 grid, hipStre
         case kFew16: hipLaunchKernelGGL((linear_few_kernel<In, E, 1, 1>), grid, dim3(512), 0, stream, a); break;
         case kFew32: hipLaunchKernelGGL((linear_few_kernel<In, E, 2, 2>), grid, dim3(512), 0, stream, a); break;
         case kFew64: hipLaunchKernelGGL((linear_few_kernel<In, E, 4, 1>), grid, dim3(512), 0, stream, a); break;
-        case kStream32: hipLaunchKernelGGL((linear_tile_kernel<In, E, 1, 1, 4, false>), grid, dim3(256), 0, stream, a); break;
+        case kStream32:   // (no 8-bit product is planned so, nor in the next)
+            if constexpr (sizeof(In) > 1)
+                hipLaunchKernelGGL((linear_tile_kernel<In, E, 1, 1, 4, false>), grid, dim3(256), 0, stream, a);
+            break;
         case kStream64:
-            if constexpr (kLarge)
+            if constexpr (sizeof(In) == 2)
                 hipLaunchKernelGGL((linear_tile_kernel<In, E, 2, 1, 4, false>), grid, dim3(256), 0, stream, a);
             break;
         case kTile64: hipLaunchKernelGGL((linear_tile_kernel<In, E, 1, 2, 2, false>), grid, dim3(256), 0, stream, a); break;

@@ -73,8 +73,11 @@ inline LinearPlan linear_plan(int64_t rows, int32_t K, int32_t n_out, int32_t dt
         // 4,096 x 4,096 18.5 / 16.2, 10,240 x 5,120 36 / 29, 20,480 x 5,120 61 / 73; 24 rows: 1,536 x
         // 6,144 12.5 / 12.0, in fp32 17 / 21.
         const double w_mb = static_cast<double>(n_out) * static_cast<double>(bytes) * 1e-6;
-        const bool few = w_mb < (dtype == RF_F32 ? 2 : 1) * (rows <= 16 ? 40 : rows <= 32 ? 8 : 4);
-        const bool stream = !few && (rows <= 32 || (dtype != RF_F32 && w_mb >= 150));
+        // 8-bit integers, registers / LDS / tiles of 64 x 128: 16 x 5,120 x 5,120 12.4 / 14.7 / 14.3, 16 x 20,480 x
+        // 5,120 50 / 31 / 29, 24 x 1,536 x 9,216 11.4 / 14.0 / 11.7, 24 x 5,120 x 5,120 14.5 / 15.0 / 14.4, 48 x 1,536
+        // x 9,216 14.3 / 14.8 / 12.2, 48 x 20,480 x 5,120 93 / 36 / 31: the tiles are as fast as LDS for any weight.
+        const bool few = w_mb < (dtype == RF_F32 ? 2 : 1) * (rows <= 16 ? 40 : rows <= 32 ? (dtype == kI8 ? 16 : 8) : 4);
+        const bool stream = dtype != kI8 && !few && (rows <= 32 || (dtype == RF_BF16 && w_mb >= 150));
         if (stream) {
             p.form = rows <= 32 ? kStream32 : kStream64;
             p.row_tiles = 1;
