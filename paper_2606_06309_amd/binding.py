@@ -1045,8 +1045,8 @@ def _frame_rows(frame_ids, T, rows_per_frame, in_full, out_full, rows):
 
 
 def _addresses(tensors):
-    """_on_device of (tensor or None, name, dtype, contiguous) with these checked."""
-    index, out = -2, []
+    """_on_device of (tensor or None, name, dtype, contiguous), after these have been checked for all."""
+    index, out, away = -2, [], None
     for t, name, dtype, contiguous in tensors:
         if t is None:
             out.append(None)
@@ -1059,13 +1059,16 @@ def _addresses(tensors):
             raise ValueError(f"{name} must be contiguous")
         on = t.get_device()
         if on != index:
-            if on < 0:
-                raise ValueError(f"{name} must be a device tensor")
-            if index < 0:
+            if index == -2 and on >= 0:
                 index = torch.cuda.current_device()
             if on != index:
-                raise ValueError(f"{name} is on {t.device}, the current device is cuda:{index}")
+                away = away or (name, t.device)
         out.append(t.data_ptr())
+    if away is not None:
+        name, device = away
+        if device.type != "cuda":
+            raise ValueError(f"{name} must be a device tensor")
+        raise ValueError(f"{name} is on {device}, the current device is cuda:{index}")
     return index, out
 
 

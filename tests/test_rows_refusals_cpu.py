@@ -183,7 +183,7 @@ def test_binding_linear():
     with pytest.raises(TypeError):
         rf.rf_frame_linear_i8(x, s, w, t, dtype=torch.float16)
     for args in ((z(64, 12, dtype=torch.int8).t(), s, w, t), (x, z(24, dtype=torch.float32)[::2], w, t)):
-        with pytest.raises(ValueError):
+        with pytest.raises(ValueError, match="contiguous"):
             rf.rf_frame_linear_i8(*args)
 
 
@@ -209,6 +209,31 @@ def test_binding_norm():
         rf.rf_frame_group_norm(x, 8, out=z(12, 64, dtype=torch.float32), **kw)
     with pytest.raises(ValueError):
         rf.rf_frame_group_norm(x[0], 8)
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    class Fake(torch.Tensor):
+        is_cuda = True
+        index = 0
+
+        def get_device(self):
+            return self.index
+
+        @property
+        def device(self):
+            return torch.device("cuda", self.index)
+    a, b = z(4, 8).as_subclass(Fake), z(4, 8).as_subclass(Fake)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    both = ((a, "a", torch.bfloat16, True), (None, "none", torch.int8, True), (b, "b", torch.bfloat16, True))
+    assert rf._addresses(both) == (0, [a.data_ptr(), None, b.data_ptr()])
+    b.index = 1
+    with pytest.raises(ValueError, match="b is on cuda:1, the current device is cuda:0"):
+        rf._addresses(both)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    with pytest.raises(ValueError, match="a is on cuda:0, the current device is cuda:1"):
+        rf._addresses(both)
+    with pytest.raises(ValueError, match="c must be a device tensor"):
+        rf._addresses(((b, "b", torch.bfloat16, True), (z(3), "c", torch.bfloat16, True)))
 
 
 def test_constants_match_the_header():
