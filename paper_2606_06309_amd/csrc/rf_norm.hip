@@ -10,7 +10,8 @@
 //    squared deviations from it, joined to those so far (a sum of squares about another
 //    point than the mean would lose what small deviations around a large mean are). The
 //    threads' rows, then the channels of each group, meet in LDS.
-//  * norm_total_kernel: a wave joins the parts of a group.
+//  * norm_total_kernel: a wave joins the parts of a group; where these are few, each workgroup of the
+//    next kernel does so itself.
 //  * norm_rows_kernel: x again, to y; norm_rows8_kernel: whole rows at a time, to 8 bits.
 //  * quantize_kernel: rows of x to 8 bits.
 #include "rf_norm_plan.h"
@@ -33,21 +34,10 @@ struct NormKArgs {
     int32_t M, C, groups, together, per_group;
     int32_t cols, slices, lines, hold, parts, row_parts, local;
     float per_col, group_share;    // 1 / cols, 1 / per_group
-    int32_t more_parts;            // parts with one whole chunk more than the others; the next has the last rows
-    float part_rows, chunk_rows, last_rows;
+    NormParts runs;
     int32_t activation, affine_rows;
     RowFrames frames;
 };
-
-// i / n for 0 <= i < 8192 and n <= 8192, given `share` = 1 / n: (i + 1/2) / n is 1 / (2 n) from a whole number at
-// least, which is more than the product's rounding, (i + 1/2) / n * 2^-23.
-__device__ __forceinline__ int divide(int i, float share) { return static_cast<int>((static_cast<float>(i) + 0.5f) * share); }
-
-// Rows of a part: every parts-th chunk of a frame, the last of which may be short. (Whole numbers
-// below 2^24: frames have four parts to a compute unit, and no memory holds 2^34 rows.)
-__device__ __forceinline__ float part_rows(const NormKArgs &a, int part) {
-    return a.part_rows + (part < a.more_parts ? a.chunk_rows : part == a.more_parts ? a.last_rows : 0.0f);
-}
 
 // n values of mean `mean` and squared deviations `m2`, joined by n_b more: the means' distance adds
 // n n_b / (n + n_b) of its square.
@@ -163,7 +153,7 @@ __global__ __launch_bounds__(kThreads) void norm_stats_kernel(const NormKArgs a)
     int lanes = 1;
     while (lanes < 64 && 2 * lanes * n_local <= kThreads) lanes *= 2;
     const int lane = tid % lanes;
-    const float rows = part_rows(a, part);
+    const float rows = a.runs.rows(part);
     for (int l = tid / lanes; l < n_local; l += kThreads / lanes) {
         const int first = (g0 + l) * a.per_group, behind = first + a.per_group;
         const int lo = (first > c0 ? first : c0) - c0, hi = (behind < c1 ? behind : c1) - c0;
@@ -197,56 +187,91 @@ __device__ __forceinline__ Affine affine_of(const NormKArgs &a, int m, int c, fl
     return {t.x, a.weight ? t.y * element<E>(a.weight, at) : t.y, a.bias ? element<E>(a.bias, at) : 0.0f};
 }
 
-// A wave joins the parts of a group, of the frames of a segment, in 64 bits and one order: sums of the
-// parts' means and their squares about the first part's (64 bits lose nothing there that 32 had).
-// Then what its channels are normalised with.
-template <typename E>
-__global__ __launch_bounds__(64) void norm_total_kernel(const NormKArgs a) {
-    constexpr int kV = 16 / sizeof(E);
-    const int lane = threadIdx.x, g = blockIdx.x, seg = blockIdx.y;
-    const int width = a.cols * kV, runs = a.together * a.parts;
+// Mean and 1 / deviation of n_groups groups from g0 on, of the frames of a segment, by kBlock threads:
+// lanes together join a group's parts, in 64 bits and one order: sums of the parts' means and their squares
+// about the first part's (64 bits lose nothing there that 32 had).
+template <int kV, int kBlock, typename Done>
+__device__ __forceinline__ void totals(const NormKArgs &a, int seg, int g0, int n_groups, Done done) {
+    int lanes = 1;
+    while (lanes < 64 && 2 * lanes * n_groups <= kBlock) lanes *= 2;
+    const int lane = threadIdx.x % lanes, width = a.cols * kV, runs = a.together * a.parts;
     const int64_t step = static_cast<int64_t>(a.slices) * a.local;
-    const int first = g * a.per_group, behind = first + a.per_group, s0 = divide(first, a.per_col * (1.0f / kV));
-    double pivot = 0.0, sum = 0.0, square = 0.0;
-    for (int s = s0; s * width < behind; ++s) {
-        const int c0 = s * width, lo = first > c0 ? first : c0, hi = behind < c0 + width ? behind : c0 + width;
-        const float2 *p = a.partial + (static_cast<int64_t>(seg) * runs * a.slices + s) * a.local +
-                          (g - divide(c0, a.group_share));
-        if (s == s0) pivot = p->x;
-        int part = lane;
-        while (part >= a.parts) part -= a.parts;
-#pragma unroll 4
-        for (int i = lane; i < runs; i += 64) {
-            const float2 v = p[i * step];
-            const double n = part_rows(a, part) * static_cast<float>(hi - lo), d = v.x - pivot;
-            sum += n * d;
-            square += n * d * d + v.y;
-            part += 64;
-            while (part >= a.parts) part -= a.parts;
-        }
-    }
-#pragma unroll
-    for (int d = 32; d > 0; d /= 2) {
-        sum += __shfl_xor(sum, d);
-        square += __shfl_xor(square, d);
-    }
     const double all = static_cast<double>(a.together) * static_cast<double>(a.N) * a.per_group;
-    const double m = sum / all, var = square / all - m * m;
-    const float2 t = make_float2(static_cast<float>(pivot + m), static_cast<float>(rsqrt((var < 0.0 ? 0.0 : var) + a.eps)));
-    const int first_set = a.affine_rows ? seg * a.together : seg, sets = a.affine_rows ? a.together : 1;
-    for (int set = first_set; set < first_set + sets; ++set)
-        for (int c = first + lane; c < behind; c += 64) {
-            const Affine f = affine_of<E>(a, set, c, t);
-            float *to = a.affine + static_cast<int64_t>(set) * 3 * a.C + c;
-            to[0] = f.mean;
-            to[a.C] = f.mul;
-            to[2 * a.C] = f.add;
+    for (int l = threadIdx.x / lanes; l < n_groups; l += kBlock / lanes) {
+        const int first = (g0 + l) * a.per_group, behind = first + a.per_group, s0 = divide(first, a.per_col * (1.0f / kV));
+        double pivot = 0.0, sum = 0.0, square = 0.0;
+        for (int s = s0; s * width < behind; ++s) {
+            const int c0 = s * width, lo = first > c0 ? first : c0, hi = behind < c0 + width ? behind : c0 + width;
+            const float2 *p = a.partial + (static_cast<int64_t>(seg) * runs * a.slices + s) * a.local +
+                              (g0 + l - divide(c0, a.group_share));
+            if (s == s0) pivot = p->x;
+            int part = lane;
+            while (part >= a.parts) part -= a.parts;
+#pragma unroll 8
+            for (int i = lane; i < runs; i += lanes) {
+                const float2 v = p[i * step];
+                const double n = a.runs.rows(part) * static_cast<float>(hi - lo), d = v.x - pivot;
+                sum += n * d;
+                square += n * d * d + v.y;
+                part += lanes;
+                while (part >= a.parts) part -= a.parts;
+            }
         }
+        for (int d = lanes / 2; d > 0; d /= 2) {
+            sum += __shfl_xor(sum, d);
+            square += __shfl_xor(square, d);
+        }
+        const double m = sum / all, var = square / all - m * m;
+        done(l, lane, lanes,
+             make_float2(static_cast<float>(pivot + m), static_cast<float>(rsqrt((var < 0.0 ? 0.0 : var) + a.eps))));
+    }
 }
 
-// Where frame m's are.
-__device__ __forceinline__ const float *affine_at(const NormKArgs &a, int m) {
-    return a.affine + static_cast<int64_t>(a.affine_rows ? m : m / a.together) * 3 * a.C;
+// A wave to a group; then what its channels are normalised with.
+template <typename E>
+__global__ __launch_bounds__(64) void norm_total_kernel(const NormKArgs a) {
+    const int g = blockIdx.x, seg = blockIdx.y;
+    totals<16 / sizeof(E), 64>(a, seg, g, 1, [&](int, int lane, int lanes, float2 t) {
+        const int set0 = a.affine_rows ? seg * a.together : seg, sets = a.affine_rows ? a.together : 1;
+        for (int set = set0; set < set0 + sets; ++set)
+            for (int c = g * a.per_group + lane; c < (g + 1) * a.per_group; c += lanes) {
+                const Affine f = affine_of<E>(a, set, c, t);
+                float *to = a.affine + static_cast<int64_t>(set) * 3 * a.C + c;
+                to[0] = f.mean;
+                to[a.C] = f.mul;
+                to[2 * a.C] = f.add;
+            }
+    });
+}
+
+// What kV channels from c on are normalised with, as that kernel left it, or (kOwn) of its workgroup's own
+// totals of the groups from g0 on.
+template <typename E, bool kOwn>
+__device__ __forceinline__ void affine_at(const NormKArgs &a, int m, int c, const float2 *own, int g0,
+                                          float (&mean)[16 / sizeof(E)], float (&mul)[16 / sizeof(E)],
+                                          float (&add)[16 / sizeof(E)]) {
+    constexpr int kV = 16 / sizeof(E);
+    if constexpr (kOwn) {
+        const int64_t at = (a.affine_rows ? static_cast<int64_t>(frame_at(a.frames, m)) * a.C : 0) + c;
+#pragma unroll
+        for (int e = 0; e < kV; ++e) {
+            mul[e] = 1.0f;
+            add[e] = 0.0f;
+        }
+        if (a.weight) load_n<E, kV>(a.weight, at, mul);
+        if (a.bias) load_n<E, kV>(a.bias, at, add);
+#pragma unroll
+        for (int e = 0; e < kV; ++e) {
+            const float2 t = own[divide(c + e, a.group_share) - g0];
+            mean[e] = t.x;
+            mul[e] *= t.y;
+        }
+    } else {
+        const float *f = a.affine + static_cast<int64_t>(a.affine_rows ? m : m / a.together) * 3 * a.C + c;
+        load_n<float, kV>(f, 0, mean);
+        load_n<float, kV>(f, a.C, mul);
+        load_n<float, kV>(f, 2 * a.C, add);
+    }
 }
 
 // A workgroup's threads hold kV channels each, `cols` threads to a line, `lines` lines: done(group of the
@@ -402,17 +427,25 @@ __device__ __forceinline__ void stream_n(void *p, const float (&v)[kN]) {
     else __builtin_nontemporal_store((f32x4_t{v[0], v[1], v[2], v[3]}), static_cast<f32x4_t *>(p));
 }
 
-template <typename E, bool kStream>
+template <typename E, bool kStream, bool kOwn>
 __global__ __launch_bounds__(kThreads) void norm_rows_kernel(const NormKArgs a) {
     constexpr int kV = 16 / sizeof(E);
     const int tid = threadIdx.x, slice = blockIdx.x, part = blockIdx.y, m = blockIdx.z;
     const int line = divide(tid, a.per_col), col = tid - line * a.cols, column = slice * a.cols + col;
+    __shared__ float2 own[kOwn ? kNormFewGroups : 1];
+    int g0 = 0;
+    if constexpr (kOwn) {
+        const int c0 = slice * a.cols * kV, c1 = c0 + a.cols * kV < a.C ? c0 + a.cols * kV : a.C;
+        g0 = divide(c0, a.group_share);
+        totals<kV, kThreads>(a, m / a.together, g0, divide(c1 - 1, a.group_share) - g0 + 1,
+                             [&](int l, int lane, int, float2 t) {
+                                 if (lane == 0) own[l] = t;
+                             });
+        __syncthreads();
+    }
     if (line >= a.lines || column * kV >= a.C) return;
     float mean[kV], mul[kV], add[kV];
-    const float *f = affine_at(a, m) + column * kV;
-    load_n<float, kV>(f, 0, mean);
-    load_n<float, kV>(f, a.C, mul);
-    load_n<float, kV>(f, 2 * a.C, add);
+    affine_at<E, kOwn>(a, m, column * kV, own, g0, mean, mul, add);
     // (y may be x: no row is read again)
     const uint8_t *p = a.x + (a.frames.in(m) * a.N) * a.x_stride + column * 16;
     uint8_t *q = a.y + (a.frames.out(m) * a.N) * a.y_stride + column * 16;
@@ -486,7 +519,7 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v, uint32_t (*places)[kLa
 
 // kLanes threads to a row, kPer columns to a thread, lane after lane. What they are normalised with stays
 // in registers; so does the row until its scale is known.
-template <typename E, int kLanes, int kPer>
+template <typename E, int kLanes, int kPer, bool kOwn>
 __global__ __launch_bounds__(kThreads) void norm_rows8_kernel(const NormKArgs a) {
     constexpr int kV = 16 / sizeof(E), kRows = kThreads / kLanes;
     __shared__ uint32_t places[2][kLanes / 64 > 0 ? kLanes / 64 : 1];
@@ -498,13 +531,17 @@ __global__ __launch_bounds__(kThreads) void norm_rows8_kernel(const NormKArgs a)
     float *scales = a.y_scale + a.frames.out(m) * a.N;
     // (columns past the last are the last once more)
     float mean[kPer][kV], mul[kPer][kV], add[kPer][kV];
-    const float *f = affine_at(a, m);
+    __shared__ float2 own[kOwn ? kNormFewGroups : 1];
+    if constexpr (kOwn) {
+        totals<kV, kThreads>(a, m / a.together, 0, a.groups, [&](int l, int lane_of, int, float2 t) {
+            if (lane_of == 0) own[l] = t;
+        });
+        __syncthreads();
+    }
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-        const int col = lane + i * kLanes, c = (col < columns ? col : columns - 1) * kV;
-        load_n<float, kV>(f, c, mean[i]);
-        load_n<float, kV>(f, a.C + c, mul[i]);
-        load_n<float, kV>(f, 2 * a.C + c, add[i]);
+        const int col = lane + i * kLanes;
+        affine_at<E, kOwn>(a, m, (col < columns ? col : columns - 1) * kV, own, 0, mean[i], mul[i], add[i]);
     }
     with_activation(a.activation, [&](auto act) {
         int turn = 0;
@@ -618,19 +655,19 @@ __global__ __launch_bounds__(kLanes > kThreads ? kLanes : kThreads) void quantiz
     }
 }
 
-template <typename E>
+template <typename E, bool kOwn>
 void rows8(const NormKArgs &a, dim3 grid, hipStream_t stream) {
     // eights of channels to a thread
     constexpr int kEight = sizeof(E) / 2;
     auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, a); };
-    if (a.C <= 128) run(norm_rows8_kernel<E, 16, kEight>);
-    else if (a.C <= 512) run(norm_rows8_kernel<E, 64, kEight>);
-    else if (a.C <= 1024) run(norm_rows8_kernel<E, 64, 2 * kEight>);
-    else if (a.C <= 1536) run(norm_rows8_kernel<E, 64, 3 * kEight>);
-    else if (a.C <= 2048) run(norm_rows8_kernel<E, 64, 4 * kEight>);
-    else if (a.C <= 4096) run(norm_rows8_kernel<E, 256, 2 * kEight>);
-    else if (a.C <= 6144) run(norm_rows8_kernel<E, 256, 3 * kEight>);
-    else run(norm_rows8_kernel<E, 256, 4 * kEight>);
+    if (a.C <= 128) run(norm_rows8_kernel<E, 16, kEight, kOwn>);
+    else if (a.C <= 512) run(norm_rows8_kernel<E, 64, kEight, kOwn>);
+    else if (a.C <= 1024) run(norm_rows8_kernel<E, 64, 2 * kEight, kOwn>);
+    else if (a.C <= 1536) run(norm_rows8_kernel<E, 64, 3 * kEight, kOwn>);
+    else if (a.C <= 2048) run(norm_rows8_kernel<E, 64, 4 * kEight, kOwn>);
+    else if (a.C <= 4096) run(norm_rows8_kernel<E, 256, 2 * kEight, kOwn>);
+    else if (a.C <= 6144) run(norm_rows8_kernel<E, 256, 3 * kEight, kOwn>);
+    else run(norm_rows8_kernel<E, 256, 4 * kEight, kOwn>);
 }
 
 template <typename E>
@@ -644,16 +681,21 @@ hipError_t run_slices(const NormPlan &p, const NormKArgs &a, hipStream_t stream)
 }
 
 template <typename E>
-hipError_t run_norm(const NormKArgs &a, bool stream_y, hipStream_t stream) {
+hipError_t run_norm(const NormPlan &p, const NormKArgs &a, hipStream_t stream) {
     hipLaunchKernelGGL(norm_stats_kernel<E>, dim3(a.slices, a.parts, a.M), dim3(kThreads), 0, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(norm_total_kernel<E>, dim3(a.groups, a.M / a.together), dim3(64), 0, stream, a);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    if (a.y_scale) rows8<E>(a, dim3(a.row_parts, a.M), stream);
-    else if (stream_y) hipLaunchKernelGGL((norm_rows_kernel<E, true>), dim3(a.slices, a.row_parts, a.M), dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((norm_rows_kernel<E, false>), dim3(a.slices, a.row_parts, a.M), dim3(kThreads), 0, stream, a);
+    if (!p.few_parts) {
+        hipLaunchKernelGGL(norm_total_kernel<E>, dim3(a.groups, a.M / a.together), dim3(64), 0, stream, a);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    const dim3 grid8(a.row_parts, a.M), grid(a.slices, a.row_parts, a.M);
+    if (a.y_scale && p.few_parts) rows8<E, true>(a, grid8, stream);
+    else if (a.y_scale) rows8<E, false>(a, grid8, stream);
+    else if (p.few_parts) hipLaunchKernelGGL((norm_rows_kernel<E, false, true>), grid, dim3(kThreads), 0, stream, a);
+    else if (p.stream) hipLaunchKernelGGL((norm_rows_kernel<E, true, false>), grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((norm_rows_kernel<E, false, false>), grid, dim3(kThreads), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -710,18 +752,12 @@ hipError_t launch_norm(const NormParams &p, hipStream_t stream) {
     a.local = plan.local;
     a.per_col = 1.0f / static_cast<float>(plan.cols);
     a.group_share = 1.0f / static_cast<float>(a.per_group);
-    if (plan.block == 0) {
-        const int64_t chunk = plan.lines * kNormRows, whole = p.N / chunk;
-        a.more_parts = static_cast<int32_t>(whole % plan.parts);
-        a.part_rows = static_cast<float>(whole / plan.parts * chunk);
-        a.chunk_rows = static_cast<float>(chunk);
-        a.last_rows = static_cast<float>(p.N - whole * chunk);
-    }
+    a.runs = plan.runs;
     a.activation = p.activation;
     a.affine_rows = p.affine_rows;
     a.frames = p.frames;
     if (plan.block > 0) return p.dtype == RF_F32 ? run_slices<float>(plan, a, stream) : run_slices<uint16_t>(plan, a, stream);
-    return p.dtype == RF_F32 ? run_norm<float>(a, plan.stream, stream) : run_norm<uint16_t>(a, plan.stream, stream);
+    return p.dtype == RF_F32 ? run_norm<float>(plan, a, stream) : run_norm<uint16_t>(plan, a, stream);
 }
 
 hipError_t launch_quantize(const QuantizeParams &p, hipStream_t stream) {

@@ -7,6 +7,23 @@ namespace rf {
 
 constexpr int kNormThreads = 256;
 
+// i / n for 0 <= i < 8192 and n <= 8192, given `share` = 1 / n: (i + 1/2) / n is 1 / (2 n) from a whole number at
+// least, which is more than the product's rounding, (i + 1/2) / n * 2^-23.
+__host__ __device__ inline int32_t divide(int32_t i, float share) {
+    return static_cast<int32_t>((static_cast<float>(i) + 0.5f) * share);
+}
+
+// Rows of a thread in a chunk.
+constexpr int kNormRows = 8;
+
+// Rows of a part: every parts-th chunk of a frame, the last of which may be short. (Whole numbers below 2^24:
+// frames have four parts to a compute unit, and no memory holds 2^34 rows.)
+struct NormParts {
+    int32_t more;           // parts with one whole chunk more than the others; the next has the last rows
+    float each, chunk, last;
+    __host__ __device__ float rows(int32_t part) const { return each + (part < more ? chunk : part == more ? last : 0.0f); }
+};
+
 // Two forms.
 //  * slices: a workgroup has whole groups' columns of all rows that share their statistics, few
 //    enough to stay in its LDS: one launch, x read once.
@@ -19,15 +36,20 @@ struct NormPlan {
     int32_t block, hold;    // slices: threads of a workgroup, rows of a thread; parts: 0
     int32_t cols, slices, lines;
     int32_t parts;          // of a frame's rows
+    NormParts runs;
     int32_t row_parts;      // those of the second launch
     int32_t local;          // groups that a slice meets at most
     int32_t stream;         // y is written past the caches
+    int32_t few_parts;      // a group's parts are joined by the workgroups that use them
     int64_t entries;        // partial sums: [M][parts][slices][local], an even number
     int64_t ws_bytes;       // they, then what each frame's channels are normalised with, three numbers each
 };
 
-// Rows of a thread in a chunk.
-constexpr int kNormRows = 8;
+// Where the workgroups of the second launch join the parts of the groups that they use, instead of a launch
+// between: parts of a group and groups of a workgroup up to these (24.0 -> 21.4 us for a norm of 11 parts
+// into 8 bits and its product; with 65 parts the second launch takes 14 us, where it and the one between
+// take 12).
+constexpr int kNormFewParts = 16, kNormFewGroups = 64;
 // Workgroups of the second launch to a compute unit. They are short, as many as have four rows to a
 // thread: 130 us at 409 MB, 141 with 16 to a compute unit, 142 with 4.
 constexpr int64_t kRowRounds = 64;
@@ -71,17 +93,20 @@ inline NormPlan norm_plan(int32_t M, int64_t N, int32_t C, int32_t groups, int32
     const int64_t columns = C / p.vec;
     if (!rows8) {
         // whole groups in whole columns: the least, and from there on rows of 64 bytes and no more
-        // workgroups than four rounds
+        // workgroups than a round. All of one round (two workgroups of 512 to a compute unit, one of
+        // 1,024): 16 us at 6 x 700 rows x 1,280 channels, 192 of the latter, where parts take 19, but 46 and
+        // 33 at 21 x 700 x 1,280, 24.5 and 22.5 at 33 x 400 x 640.
         int64_t unit = C / groups;
         while (unit % p.vec != 0) unit += C / groups;
         unit /= p.vec;
         const int64_t segments = M / together, rows = together * N;
         bool fits = norm_slice(&p, columns, unit, rows, C / groups);
         for (int64_t cols = unit + unit; fits && cols <= columns; cols += unit) {
-            if (p.cols * 16 >= 64 && segments * p.slices <= 4LL * cus) break;
+            if (p.cols * 16 >= 64 && segments * p.slices <= 2LL * cus) break;
             if (columns % cols == 0 && !norm_slice(&p, columns, cols, rows, C / groups)) break;
         }
-        if (fits) return p;
+        if (fits && segments * p.slices <= static_cast<int64_t>(cus) * (p.block == kNormBlocks[0].threads ? 2 : 1)) return p;
+        p.block = 0;
     }
     p.slices = static_cast<int32_t>(up(columns, kNormThreads));
     p.cols = static_cast<int32_t>(up(columns, p.slices));
@@ -89,7 +114,13 @@ inline NormPlan norm_plan(int32_t M, int64_t N, int32_t C, int32_t groups, int32
     p.lines = kNormThreads / p.cols;
     // four workgroups to a compute unit, of eight rows a thread at least
     const int64_t want = up(4LL * cus, static_cast<int64_t>(M) * p.slices), most = up(N, kNormRows * p.lines);
-    p.parts = static_cast<int32_t>(want < most ? want : most);
+    const int64_t parts = want < most ? want : most;
+    p.parts = static_cast<int32_t>(parts < 65535 ? parts : 65535);
+    const int64_t chunk = kNormRows * p.lines, whole = N / chunk;
+    p.runs.more = static_cast<int32_t>(whole % p.parts);
+    p.runs.each = static_cast<float>(whole / p.parts * chunk);
+    p.runs.chunk = static_cast<float>(chunk);
+    p.runs.last = static_cast<float>(N - whole * chunk);
     int64_t row_want = up(kRowRounds * cus, static_cast<int64_t>(M) * p.slices), row_most = up(N, 4 * p.lines);
     if (rows8) {
         // whole rows of 16, 64 or 256 threads, which have to fetch what they are normalised with first:
@@ -98,10 +129,12 @@ inline NormPlan norm_plan(int32_t M, int64_t N, int32_t C, int32_t groups, int32
         row_want = up((eights == 1 ? 6 : eights == 2 ? 4 : eights == 3 ? 3 : 2) * static_cast<int64_t>(cus), M);
         row_most = up(N, C <= 128 ? 16 : C <= 2048 ? 4 : 1);
     }
-    p.row_parts = static_cast<int32_t>(row_want < row_most ? row_want : row_most);
+    const int64_t row_parts = row_want < row_most ? row_want : row_most;
+    p.row_parts = static_cast<int32_t>(row_parts < 65535 ? row_parts : 65535);   // (an axis of a grid)
     const int64_t local = (static_cast<int64_t>(p.cols) * p.vec - 2) / (C / groups) + 2;
     p.local = static_cast<int32_t>(local < groups ? local : groups);
     p.stream = static_cast<double>(M) * static_cast<double>(N) * C * (16 / p.vec) > kNormCached;
+    p.few_parts = p.parts * together <= kNormFewParts && (rows8 ? groups : p.local) <= kNormFewGroups;
     p.entries = (static_cast<int64_t>(M) * p.parts * p.slices * p.local + 1) / 2 * 2;
     p.ws_bytes = p.entries * 8 + static_cast<int64_t>(M) * C * 12;
     return p;

@@ -40,7 +40,8 @@ def check8(got, y, err, what=""):
 # more channels than a workgroup has columns
 SIZES = [(1, 8, 1), (1, 16, 16), (2, 48, 3), (64, 128, 32), (527, 320, 32), (33, 336, 7), (100, 72, 9), (1000, 64, 64),
          (257, 1536, 32), (70, 2048, 1), (40, 2064, 43), (9, 4112, 257), (5, 8192, 32), (3, 8176, 8176), (1560, 640, 32),
-         (6000, 512, 32), (20000, 128, 32), (30011, 24, 2), (4099, 8, 8), (700, 5120, 40)]
+         (6000, 512, 32), (20000, 128, 32), (30011, 24, 2), (4099, 8, 8), (700, 5120, 40),
+         (37, 1024, 64), (21, 4096, 16), (3000, 16, 4), (11, 6160, 55), (800, 1280, 32), (1500, 32, 8)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
