@@ -300,7 +300,10 @@ __device__ __forceinline__ bool tile_of(const LinearKArgs &a, int bid, int &rt, 
 // large, send it past the caches if it is no wider than x: 50 -> 45 us at 9,360 x 1,536 x
 // 1,536 without residual, 1,977 -> 1,896 at 21,600 x 5,120 x 5,120 and a product that reads
 // it next; wider ones so, a feed-forward's, 1,536 to 6,144 and back: 323 -> 340; 128-row tiles
-// so, the two at 3,600 x 1,536 x 1,536: 54 -> 56.
+// so, the two at 3,600 x 1,536 x 1,536: 54 -> 56. Results of 8-bit integers are read next by a rounding to 8
+// bits, to which the caches are worth less: wider ones go past them too, 139 -> 132 us at 9,360 x 1,536 x
+// 6,144, 232 either way with the roundings and the product back, 4,105 -> 3,799 us for these at 21,600 x 5,120 x
+// 20,480.
 // acc, x_scale: a wave's sums and its rows' scales; c: this lane's first feature; mine: 8 KB of the wave's own
 // in LDS; block(b): where residual(b) has brought the residual's rows of block b, if `stage`.
 template <typename In, typename E, int kRB, int kBM, int kScales, typename Block, typename Residual>
@@ -870,7 +873,7 @@ hipError_t launch_product(const LinearParams &p, int32_t in, const float *x_scal
     a.parts = plan.parts;
     a.activation = p.activation;
     a.gate_rows = p.gate_rows;
-    a.stream = p.n_out <= p.K;
+    a.stream = in == kI8 || p.n_out <= p.K;
     a.frames = p.frames;
     const int64_t tiles = plan.row_tiles * plan.col_tiles;
     if (tiles > 0x7fffffffLL / 64) return hipErrorInvalidConfiguration;
