@@ -48,8 +48,10 @@ struct NormPlan {
 // Where the workgroups of the second launch join the parts of the groups that they use, instead of a launch
 // between: parts of a group and groups of a workgroup up to these (24.0 -> 21.4 us for a norm of 11 parts
 // into 8 bits and its product; with 65 parts the second launch takes 14 us, where it and the one between
-// take 12).
-constexpr int kNormFewParts = 16, kNormFewGroups = 64;
+// take 12), and of workgroups no more than run at once, eight to a compute unit (5 to 6 of them: 22.3 us at
+// 64 x 300 rows x 512 channels, 26.7 at 128 x 300 x 320, where the launch between makes it 23.4 and 28.1; 14 and
+// 31: 45.6 at 64 x 900 x 512, 67.2 at 200 x 160 x 1,280, and 43.0 and 59.9 with it). Rows in 8 bits never have more.
+constexpr int kNormFewParts = 16, kNormFewGroups = 64, kNormFewWorkgroups = 8;
 // Workgroups of the second launch to a compute unit. They are short, as many as have four rows to a
 // thread: 130 us at 409 MB, 141 with 16 to a compute unit, 142 with 4.
 constexpr int64_t kRowRounds = 64;
@@ -134,7 +136,8 @@ inline NormPlan norm_plan(int32_t M, int64_t N, int32_t C, int32_t groups, int32
     const int64_t local = (static_cast<int64_t>(p.cols) * p.vec - 2) / (C / groups) + 2;
     p.local = static_cast<int32_t>(local < groups ? local : groups);
     p.stream = static_cast<double>(M) * static_cast<double>(N) * C * (16 / p.vec) > kNormCached;
-    p.few_parts = p.parts * together <= kNormFewParts && (rows8 ? groups : p.local) <= kNormFewGroups;
+    p.few_parts = p.parts * together <= kNormFewParts && (rows8 ? groups : p.local) <= kNormFewGroups &&
+                  (rows8 || static_cast<int64_t>(p.row_parts) * M * p.slices <= static_cast<int64_t>(kNormFewWorkgroups) * cus);
     p.entries = (static_cast<int64_t>(M) * p.parts * p.slices * p.local + 1) / 2 * 2;
     p.ws_bytes = p.entries * 8 + static_cast<int64_t>(M) * C * 12;
     return p;

@@ -61,6 +61,7 @@ static int check(int32_t M, int64_t N, int32_t C, int32_t G, int32_t together, b
     if (p.few_parts) {
         ++*few;
         CHECK(p.parts * together <= rf::kNormFewParts && (rows8 ? G : p.local) <= rf::kNormFewGroups);
+        CHECK(rows8 || (p.row_parts * static_cast<int64_t>(M) * p.slices <= 8LL * cus && !p.stream));
     }
     // launches of fewer than 2^32 threads
     const double threads = 256.0 * M * p.slices;

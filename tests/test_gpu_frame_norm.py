@@ -194,3 +194,19 @@ def test_results_repeat():
     runs = [rf.rf_frame_group_norm(x, 24, activation="silu", frame_ids=[0, 1, 2], T=3, rows_per_frame=7000, frames_together=3)
             for _ in range(4)]
     assert all(torch.equal(runs[0], r) for r in runs[1:])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("M,N,C,G", [(60, 130, 320, 32), (256, 1200, 64, 8), (90, 700, 640, 32)])
+def test_many_frames_of_few_parts(M, N, C, G, dtype):
+    """A frame's rows in two to sixteen parts, joined by the workgroups that use them or, where these are many, before."""
+    x = draw((M * N, C), dtype, 25) + torch.arange(M, device="cuda").repeat_interleave(N)[:, None].to(dtype)
+    check(x, G, draw((C,), dtype, 26), draw((C,), dtype, 27), act="silu", M=M, T=M, what=f"{M}x{N}x{C}")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N,C,G", [(50, 64, 4), (9000, 320, 32)])
+def test_large_magnitudes(N, C, G, dtype):
+    """Up to 2^40, where squares are sums of 2^80: results as of the same values near 1."""
+    x = draw((N, C), dtype, 28).clamp(-4, 4) * 2.0 ** 38
+    check(x, G, draw((C,), dtype, 29))
