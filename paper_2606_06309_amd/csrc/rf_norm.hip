@@ -5,8 +5,8 @@
 //
 //  * norm_slice_kernel: where all rows that share statistics fit, a few groups' channels of them, a
 //    workgroup's LDS: x is read once, in one launch.
-//  * norm_stats_kernel: else a workgroup has a run of a frame's rows and up to 256 16-byte columns;
-//    a thread keeps its column's channels and walks rows, eight at a time: their mean and
+//  * norm_stats_kernel: else a workgroup has every parts-th chunk of a frame's rows and up to 256 16-byte
+//    columns; a thread keeps its column's channels and walks rows, eight at a time: their mean and
 //    squared deviations from it, joined to those so far (a sum of squares about another
 //    point than the mean would lose what small deviations around a large mean are). The
 //    threads' rows, then the channels of each group, meet in LDS.
@@ -14,6 +14,16 @@
 //    next kernel does so itself.
 //  * norm_rows_kernel: x again, to y; norm_rows8_kernel: whole rows at a time, to 8 bits.
 //  * quantize_kernel: rows of x to 8 bits.
+//
+// What bounds them, and what they measure (bf16 but for the first):
+//  * Slices: what one launch takes, its loads, two sums through LDS and its stores one after the other:
+//    6.3 us at 3 x 64 rows x 128 channels of fp32, 9.1 at 3 x 527 x 320.
+//  * Short launches (6 x 1,560 rows x 640 channels, 12 MB: 7.2, 3 and 7.5 us, 18.5 together): their starts and ends
+//    and the parts' way from one to the next; 12 MB in and out take 4 us at the rate of a large copy.
+//  * Large ones: memory, x read twice as it does not fit the chip: 62,400 rows x 1,024 channels, 128 MB in and
+//    out, 66 us (the second time it is in the caches behind the L2s in part), 409 MB 200, 6.1 TB/s.
+//  * Rows to 8 bits: memory, with about ten vector instructions an element beside three bytes: 21,600 x 20,480,
+//    227 us, 5.9 TB/s, vector instructions busy 63 % of the cycles.
 #include "rf_norm_plan.h"
 #include "rf_rows.h"
 
@@ -27,7 +37,7 @@ struct NormKArgs {
     float *y_scale;
     const void *weight, *bias;
     float2 *partial;               // [M][parts][slices][local]: mean, sum of squared deviations
-    float *affine;                 // [M / together, or M with affine_rows][3][C]: (x - mean) * mul + add
+    float2 *total;                 // [M / together][groups]: mean, 1 / deviation
     int64_t N;
     int64_t x_stride, y_stride;    // bytes
     double eps;
@@ -57,11 +67,11 @@ __device__ __forceinline__ void widen(u32x4_t x, float (&v)[16 / sizeof(E)]) {
     }
 }
 
-// A column of x, past the caches: every launch reads it once, and beyond what they hold a walk that
-// leaves nothing behind does not drive out what is still to be written (409 MB: 65 us, where it
-// takes 95 to 105 otherwise).
+// A column of x; kPast: past the caches.
+template <bool kPast>
 __device__ __forceinline__ u32x4_t load_x(const uint8_t *p) {
-    return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p));
+    if constexpr (kPast) return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p));
+    else return *reinterpret_cast<const u32x4_t *>(p);
 }
 
 template <typename E>
@@ -83,7 +93,7 @@ __global__ __launch_bounds__(kThreads) void norm_stats_kernel(const NormKArgs a)
             if (first + chunk <= a.N) {
                 u32x4_t raw[kNormRows];
 #pragma unroll
-                for (int i = 0; i < kNormRows; ++i) raw[i] = load_x(p + i * step);
+                for (int i = 0; i < kNormRows; ++i) raw[i] = load_x<false>(p + i * step);
                 float v[kNormRows][kV];
 #pragma unroll
                 for (int i = 0; i < kNormRows; ++i) widen<E>(raw[i], v[i]);
@@ -104,7 +114,7 @@ __global__ __launch_bounds__(kThreads) void norm_stats_kernel(const NormKArgs a)
 #pragma unroll
                 for (int i = 0; i < kNormRows; ++i) {
                     const int64_t r = first + line + i * a.lines;
-                    raw[i] = load_x(x + (r < a.N ? r : a.N - 1) * a.x_stride);
+                    raw[i] = load_x<false>(x + (r < a.N ? r : a.N - 1) * a.x_stride);
                 }
 #pragma unroll
                 for (int i = 0; i < kNormRows; ++i) {
@@ -171,27 +181,11 @@ __global__ __launch_bounds__(kThreads) void norm_stats_kernel(const NormKArgs a)
     }
 }
 
-template <typename E>
-__device__ __forceinline__ float element(const void *p, int64_t at) {
-    if constexpr (sizeof(E) == 4) return static_cast<const float *>(p)[at];
-    else return __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t *>(p)[at]) << 16);
-}
-// What channel c of listed frame m is normalised with, given its group's mean and 1 / deviation t:
-// (x - mean) * mul + add.
-struct Affine {
-    float mean, mul, add;
-};
-template <typename E>
-__device__ __forceinline__ Affine affine_of(const NormKArgs &a, int m, int c, float2 t) {
-    const int64_t at = (a.affine_rows ? static_cast<int64_t>(a.frames.frame[m]) * a.C : 0) + c;
-    return {t.x, a.weight ? t.y * element<E>(a.weight, at) : t.y, a.bias ? element<E>(a.bias, at) : 0.0f};
-}
-
 // Mean and 1 / deviation of n_groups groups from g0 on, of the frames of a segment, by kBlock threads:
 // lanes together join a group's parts, in 64 bits and one order: sums of the parts' means and their squares
 // about the first part's (64 bits lose nothing there that 32 had).
-template <int kV, int kBlock, typename Done>
-__device__ __forceinline__ void totals(const NormKArgs &a, int seg, int g0, int n_groups, Done done) {
+template <int kV, int kBlock>
+__device__ __forceinline__ void totals(const NormKArgs &a, int seg, int g0, int n_groups, float2 *to) {
     int lanes = 1;
     while (lanes < 64 && 2 * lanes * n_groups <= kBlock) lanes *= 2;
     const int lane = threadIdx.x % lanes, width = a.cols * kV, runs = a.together * a.parts;
@@ -222,55 +216,51 @@ __device__ __forceinline__ void totals(const NormKArgs &a, int seg, int g0, int 
             square += __shfl_xor(square, d);
         }
         const double m = sum / all, var = square / all - m * m;
-        done(l, lane, lanes,
-             make_float2(static_cast<float>(pivot + m), static_cast<float>(rsqrt((var < 0.0 ? 0.0 : var) + a.eps))));
+        if (lane == 0)
+            to[l] = make_float2(static_cast<float>(pivot + m), static_cast<float>(rsqrt((var < 0.0 ? 0.0 : var) + a.eps)));
     }
 }
 
-// A wave to a group; then what its channels are normalised with.
+// A wave to a group.
 template <typename E>
 __global__ __launch_bounds__(64) void norm_total_kernel(const NormKArgs a) {
     const int g = blockIdx.x, seg = blockIdx.y;
-    totals<16 / sizeof(E), 64>(a, seg, g, 1, [&](int, int lane, int lanes, float2 t) {
-        const int set0 = a.affine_rows ? seg * a.together : seg, sets = a.affine_rows ? a.together : 1;
-        for (int set = set0; set < set0 + sets; ++set)
-            for (int c = g * a.per_group + lane; c < (g + 1) * a.per_group; c += lanes) {
-                const Affine f = affine_of<E>(a, set, c, t);
-                float *to = a.affine + static_cast<int64_t>(set) * 3 * a.C + c;
-                to[0] = f.mean;
-                to[a.C] = f.mul;
-                to[2 * a.C] = f.add;
-            }
-    });
+    totals<16 / sizeof(E), 64>(a, seg, g, 1, a.total + static_cast<int64_t>(seg) * a.groups + g);
 }
 
-// What kV channels from c on are normalised with, as that kernel left it, or (kOwn) of its workgroup's own
-// totals of the groups from g0 on.
-template <typename E, bool kOwn>
-__device__ __forceinline__ void affine_at(const NormKArgs &a, int m, int c, const float2 *own, int g0,
+// What kV channels from c on of listed frame m are normalised with, (x - mean) * mul + add; total: of the groups from
+// g0 on.
+template <typename E>
+__device__ __forceinline__ void affine_at(const NormKArgs &a, int m, int c, const float2 *total, int g0,
                                           float (&mean)[16 / sizeof(E)], float (&mul)[16 / sizeof(E)],
                                           float (&add)[16 / sizeof(E)]) {
     constexpr int kV = 16 / sizeof(E);
-    if constexpr (kOwn) {
-        const int64_t at = (a.affine_rows ? static_cast<int64_t>(frame_at(a.frames, m)) * a.C : 0) + c;
+    const int64_t at = (a.affine_rows ? static_cast<int64_t>(frame_at(a.frames, m)) * a.C : 0) + c;
+#pragma unroll
+    for (int e = 0; e < kV; ++e) {
+        mul[e] = 1.0f;
+        add[e] = 0.0f;
+    }
+    if (a.weight) load_n<E, kV>(a.weight, at, mul);
+    if (a.bias) load_n<E, kV>(a.bias, at, add);
+    if (a.per_group >= kV) {      // (one group, or two with one border)
+        const int first = divide(c, a.group_share), last = divide(c + kV - 1, a.group_share);
+        const float2 t = total[first - g0], t2 = total[last - g0];
+        const int border = (first + 1) * a.per_group - c;
 #pragma unroll
         for (int e = 0; e < kV; ++e) {
-            mul[e] = 1.0f;
-            add[e] = 0.0f;
-        }
-        if (a.weight) load_n<E, kV>(a.weight, at, mul);
-        if (a.bias) load_n<E, kV>(a.bias, at, add);
-#pragma unroll
-        for (int e = 0; e < kV; ++e) {
-            const float2 t = own[divide(c + e, a.group_share) - g0];
-            mean[e] = t.x;
-            mul[e] *= t.y;
+            mean[e] = e < border ? t.x : t2.x;
+            mul[e] *= e < border ? t.y : t2.y;
         }
     } else {
-        const float *f = a.affine + static_cast<int64_t>(a.affine_rows ? m : m / a.together) * 3 * a.C + c;
-        load_n<float, kV>(f, 0, mean);
-        load_n<float, kV>(f, a.C, mul);
-        load_n<float, kV>(f, 2 * a.C, add);
+        float2 t[kV];
+#pragma unroll
+        for (int e = 0; e < kV; ++e) t[e] = total[divide(c + e, a.group_share) - g0];
+#pragma unroll
+        for (int e = 0; e < kV; ++e) {
+            mean[e] = t[e].x;
+            mul[e] *= t[e].y;
+        }
     }
 }
 
@@ -427,25 +417,24 @@ __device__ __forceinline__ void stream_n(void *p, const float (&v)[kN]) {
     else __builtin_nontemporal_store((f32x4_t{v[0], v[1], v[2], v[3]}), static_cast<f32x4_t *>(p));
 }
 
-template <typename E, bool kStream, bool kOwn>
+template <typename E, bool kStream, bool kPast, bool kOwn>
 __global__ __launch_bounds__(kThreads) void norm_rows_kernel(const NormKArgs a) {
     constexpr int kV = 16 / sizeof(E);
     const int tid = threadIdx.x, slice = blockIdx.x, part = blockIdx.y, m = blockIdx.z;
     const int line = divide(tid, a.per_col), col = tid - line * a.cols, column = slice * a.cols + col;
     __shared__ float2 own[kOwn ? kNormFewGroups : 1];
+    const float2 *total = a.total + static_cast<int64_t>(m / a.together) * a.groups;
     int g0 = 0;
     if constexpr (kOwn) {
         const int c0 = slice * a.cols * kV, c1 = c0 + a.cols * kV < a.C ? c0 + a.cols * kV : a.C;
         g0 = divide(c0, a.group_share);
-        totals<kV, kThreads>(a, m / a.together, g0, divide(c1 - 1, a.group_share) - g0 + 1,
-                             [&](int l, int lane, int, float2 t) {
-                                 if (lane == 0) own[l] = t;
-                             });
+        totals<kV, kThreads>(a, m / a.together, g0, divide(c1 - 1, a.group_share) - g0 + 1, own);
+        total = own;
         __syncthreads();
     }
     if (line >= a.lines || column * kV >= a.C) return;
     float mean[kV], mul[kV], add[kV];
-    affine_at<E, kOwn>(a, m, column * kV, own, g0, mean, mul, add);
+    affine_at<E>(a, m, column * kV, total, g0, mean, mul, add);
     // (y may be x: no row is read again)
     const uint8_t *p = a.x + (a.frames.in(m) * a.N) * a.x_stride + column * 16;
     uint8_t *q = a.y + (a.frames.out(m) * a.N) * a.y_stride + column * 16;
@@ -461,7 +450,7 @@ __global__ __launch_bounds__(kThreads) void norm_rows_kernel(const NormKArgs a) 
 #pragma unroll
             for (int i = 0; i < kRows; ++i) {
                 const int64_t k = r + i * a.lines;
-                raw[i] = load_x(p + (k < a.N ? k : a.N - 1) * a.x_stride);
+                raw[i] = load_x<kPast>(p + (k < a.N ? k : a.N - 1) * a.x_stride);
             }
 #pragma unroll
             for (int i = 0; i < kRows; ++i) {
@@ -519,7 +508,7 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v, uint32_t (*places)[kLa
 
 // kLanes threads to a row, kPer columns to a thread, lane after lane. What they are normalised with stays
 // in registers; so does the row until its scale is known.
-template <typename E, int kLanes, int kPer, bool kOwn>
+template <typename E, int kLanes, int kPer, bool kPast, bool kOwn>
 __global__ __launch_bounds__(kThreads) void norm_rows8_kernel(const NormKArgs a) {
     constexpr int kV = 16 / sizeof(E), kRows = kThreads / kLanes;
     __shared__ uint32_t places[2][kLanes / 64 > 0 ? kLanes / 64 : 1];
@@ -532,16 +521,16 @@ __global__ __launch_bounds__(kThreads) void norm_rows8_kernel(const NormKArgs a)
     // (columns past the last are the last once more)
     float mean[kPer][kV], mul[kPer][kV], add[kPer][kV];
     __shared__ float2 own[kOwn ? kNormFewGroups : 1];
+    const float2 *total = a.total + static_cast<int64_t>(m / a.together) * a.groups;
     if constexpr (kOwn) {
-        totals<kV, kThreads>(a, m / a.together, 0, a.groups, [&](int l, int lane_of, int, float2 t) {
-            if (lane_of == 0) own[l] = t;
-        });
+        totals<kV, kThreads>(a, m / a.together, 0, a.groups, own);
+        total = own;
         __syncthreads();
     }
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int col = lane + i * kLanes;
-        affine_at<E, kOwn>(a, m, (col < columns ? col : columns - 1) * kV, own, 0, mean[i], mul[i], add[i]);
+        affine_at<E>(a, m, (col < columns ? col : columns - 1) * kV, total, 0, mean[i], mul[i], add[i]);
     }
     with_activation(a.activation, [&](auto act) {
         int turn = 0;
@@ -554,7 +543,7 @@ __global__ __launch_bounds__(kThreads) void norm_rows8_kernel(const NormKArgs a)
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
                 const int col = lane + i * kLanes;
-                next[i] = load_x(p + (col < columns ? col : columns - 1) * 16);
+                next[i] = load_x<kPast>(p + (col < columns ? col : columns - 1) * 16);
             }
         };
         ahead(rounds - 1 - part);
@@ -655,19 +644,19 @@ __global__ __launch_bounds__(kLanes > kThreads ? kLanes : kThreads) void quantiz
     }
 }
 
-template <typename E, bool kOwn>
+template <typename E, bool kPast, bool kOwn>
 void rows8(const NormKArgs &a, dim3 grid, hipStream_t stream) {
     // eights of channels to a thread
     constexpr int kEight = sizeof(E) / 2;
     auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, a); };
-    if (a.C <= 128) run(norm_rows8_kernel<E, 16, kEight, kOwn>);
-    else if (a.C <= 512) run(norm_rows8_kernel<E, 64, kEight, kOwn>);
-    else if (a.C <= 1024) run(norm_rows8_kernel<E, 64, 2 * kEight, kOwn>);
-    else if (a.C <= 1536) run(norm_rows8_kernel<E, 64, 3 * kEight, kOwn>);
-    else if (a.C <= 2048) run(norm_rows8_kernel<E, 64, 4 * kEight, kOwn>);
-    else if (a.C <= 4096) run(norm_rows8_kernel<E, 256, 2 * kEight, kOwn>);
-    else if (a.C <= 6144) run(norm_rows8_kernel<E, 256, 3 * kEight, kOwn>);
-    else run(norm_rows8_kernel<E, 256, 4 * kEight, kOwn>);
+    if (a.C <= 128) run(norm_rows8_kernel<E, 16, kEight, kPast, kOwn>);
+    else if (a.C <= 512) run(norm_rows8_kernel<E, 64, kEight, kPast, kOwn>);
+    else if (a.C <= 1024) run(norm_rows8_kernel<E, 64, 2 * kEight, kPast, kOwn>);
+    else if (a.C <= 1536) run(norm_rows8_kernel<E, 64, 3 * kEight, kPast, kOwn>);
+    else if (a.C <= 2048) run(norm_rows8_kernel<E, 64, 4 * kEight, kPast, kOwn>);
+    else if (a.C <= 4096) run(norm_rows8_kernel<E, 256, 2 * kEight, kPast, kOwn>);
+    else if (a.C <= 6144) run(norm_rows8_kernel<E, 256, 3 * kEight, kPast, kOwn>);
+    else run(norm_rows8_kernel<E, 256, 4 * kEight, kPast, kOwn>);
 }
 
 template <typename E>
@@ -691,11 +680,13 @@ hipError_t run_norm(const NormPlan &p, const NormKArgs &a, hipStream_t stream) {
         if (e != hipSuccess) return e;
     }
     const dim3 grid8(a.row_parts, a.M), grid(a.slices, a.row_parts, a.M);
-    if (a.y_scale && p.few_parts) rows8<E, true>(a, grid8, stream);
-    else if (a.y_scale) rows8<E, false>(a, grid8, stream);
-    else if (p.few_parts) hipLaunchKernelGGL((norm_rows_kernel<E, false, true>), grid, dim3(kThreads), 0, stream, a);
-    else if (p.stream) hipLaunchKernelGGL((norm_rows_kernel<E, true, false>), grid, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((norm_rows_kernel<E, false, false>), grid, dim3(kThreads), 0, stream, a);
+    auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, a); };
+    if (a.y_scale && p.x_past) p.few_parts ? rows8<E, true, true>(a, grid8, stream) : rows8<E, true, false>(a, grid8, stream);
+    else if (a.y_scale) p.few_parts ? rows8<E, false, true>(a, grid8, stream) : rows8<E, false, false>(a, grid8, stream);
+    else if (p.few_parts) run(norm_rows_kernel<E, false, false, true>);
+    else if (p.x_past) run(norm_rows_kernel<E, true, true, false>);
+    else if (p.y_past) run(norm_rows_kernel<E, true, false, false>);
+    else run(norm_rows_kernel<E, false, false, false>);
     return hipGetLastError();
 }
 
@@ -733,7 +724,7 @@ hipError_t launch_norm(const NormParams &p, hipStream_t stream) {
     a.weight = p.weight;
     a.bias = p.bias;
     a.partial = static_cast<float2 *>(p.ws);
-    a.affine = reinterpret_cast<float *>(a.partial + plan.entries);
+    a.total = a.partial + plan.entries;
     a.N = p.N;
     a.x_stride = p.x_stride * esize;
     a.y_stride = p.y_scale ? p.y_stride : p.y_stride * esize;

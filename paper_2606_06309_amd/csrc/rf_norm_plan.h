@@ -39,29 +39,29 @@ struct NormPlan {
     NormParts runs;
     int32_t row_parts;      // those of the second launch
     int32_t local;          // groups that a slice meets at most
-    int32_t stream;         // y is written past the caches
+    int32_t x_past, y_past; // the second launch reads x, writes y past the caches
     int32_t few_parts;      // a group's parts are joined by the workgroups that use them
     int64_t entries;        // partial sums: [M][parts][slices][local], an even number
-    int64_t ws_bytes;       // they, then what each frame's channels are normalised with, three numbers each
+    int64_t ws_bytes;       // they, then the groups' mean and 1 / deviation
 };
 
 // Where the workgroups of the second launch join the parts of the groups that they use, instead of a launch
-// between: parts of a group and groups of a workgroup up to these (24.0 -> 21.4 us for a norm of 11 parts
-// into 8 bits and its product; with 65 parts the second launch takes 14 us, where it and the one between
-// take 12), and of workgroups no more than run at once, eight to a compute unit (5 to 6 of them: 22.3 us at
-// 64 x 300 rows x 512 channels, 26.7 at 128 x 300 x 320, where the launch between makes it 23.4 and 28.1; 14 and
-// 31: 45.6 at 64 x 900 x 512, 67.2 at 200 x 160 x 1,280, and 43.0 and 59.9 with it). Rows in 8 bits never have more.
-constexpr int kNormFewParts = 16, kNormFewGroups = 64, kNormFewWorkgroups = 8;
+// between: parts of a group and groups of a workgroup up to these (22.0 us for a norm of 11 parts into 8 bits and
+// its product, 24.7 with the launch between; 19.4 with 65 parts, and 18.5), and workgroups to a compute unit: 20.4 us
+// at 64 x 300 rows x 512 channels, five of them, 46.0 at 64 x 900 x 512, 14, where the launch between makes it 21.9
+// and 47.2; 63.0 at 200 x 160 x 1,280, 31, and 61.3 with it. (Rows in 8 bits never have more than seven.)
+constexpr int kNormFewParts = 16, kNormFewGroups = 64, kNormFewWorkgroups = 16;
 // Workgroups of the second launch to a compute unit. They are short, as many as have four rows to a
-// thread: 130 us at 409 MB, 141 with 16 to a compute unit, 142 with 4.
+// thread: 200 us for a norm of 409 MB, 203 with 16 to a compute unit, 211 with 8.
 constexpr int64_t kRowRounds = 64;
-// Bytes of y from which it goes past the caches: 219 us at 409 MB, 246 through them; smaller ones
-// stay there for the product that reads them.
+// Bytes of y from which it goes past the caches: 66 us at 128 MB, 83 through them (157 and 152 with the product
+// that reads it next), 200 and 240 at 409; smaller ones stay there for that product (75 and 72 us at 42 MB).
 constexpr double kNormCached = 96e6;
-__host__ __device__ inline int64_t part_rows(int64_t N, int64_t chunk, int64_t parts, int64_t part) {
-    const int64_t whole = N / chunk, turn = whole / parts, over = whole - turn * parts;
-    return (turn + (part < over)) * chunk + (part == over ? N - whole * chunk : 0);
-}
+// Bytes of x from which the second launch reads it past the caches; smaller ones it finds there in part, going the
+// other way than the first (which always leaves behind what it read): with a product of as many channels between,
+// 10 x 3,120 x 640 takes 71.5 us a layer, 75 if both read past them, 21 x 1,560 x 1,536 into 8 bits and on, with
+// residual, 163 and 181. 410 MB: 641 us a layer with the first only leaving x behind, 653 with both, 653 with neither.
+constexpr double kNormHeld = 256e6;
 
 // Workgroups of slices: threads, and rows of a thread that it holds at most (16 bytes each, in LDS with 32
 // or 16 more bytes of a thread, of 160 KB); groups of a slice.
@@ -135,11 +135,13 @@ inline NormPlan norm_plan(int32_t M, int64_t N, int32_t C, int32_t groups, int32
     p.row_parts = static_cast<int32_t>(row_parts < 65535 ? row_parts : 65535);   // (an axis of a grid)
     const int64_t local = (static_cast<int64_t>(p.cols) * p.vec - 2) / (C / groups) + 2;
     p.local = static_cast<int32_t>(local < groups ? local : groups);
-    p.stream = static_cast<double>(M) * static_cast<double>(N) * C * (16 / p.vec) > kNormCached;
+    const double bytes = static_cast<double>(M) * static_cast<double>(N) * C * (16 / p.vec);
+    p.y_past = bytes > kNormCached;
+    p.x_past = bytes > kNormHeld;
     p.few_parts = p.parts * together <= kNormFewParts && (rows8 ? groups : p.local) <= kNormFewGroups &&
                   (rows8 || static_cast<int64_t>(p.row_parts) * M * p.slices <= static_cast<int64_t>(kNormFewWorkgroups) * cus);
     p.entries = (static_cast<int64_t>(M) * p.parts * p.slices * p.local + 1) / 2 * 2;
-    p.ws_bytes = p.entries * 8 + static_cast<int64_t>(M) * C * 12;
+    p.ws_bytes = (p.entries + static_cast<int64_t>(M / together) * groups) * 8;
     return p;
 }
 

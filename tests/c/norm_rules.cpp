@@ -57,11 +57,11 @@ static int check(int32_t M, int64_t N, int32_t C, int32_t G, int32_t together, b
         CHECK((c1 - 1) / per - c0 / per + 1 <= p.local);
     }
     CHECK(p.entries % 2 == 0 && p.entries >= static_cast<int64_t>(M) * p.parts * p.slices * p.local);
-    CHECK(p.ws_bytes == p.entries * 8 + static_cast<int64_t>(M) * C * 12);
+    CHECK(p.ws_bytes == p.entries * 8 + static_cast<int64_t>(M / together) * G * 8);
     if (p.few_parts) {
         ++*few;
         CHECK(p.parts * together <= rf::kNormFewParts && (rows8 ? G : p.local) <= rf::kNormFewGroups);
-        CHECK(rows8 || (p.row_parts * static_cast<int64_t>(M) * p.slices <= 8LL * cus && !p.stream));
+        CHECK(rows8 || (p.row_parts * static_cast<int64_t>(M) * p.slices <= rf::kNormFewWorkgroups * static_cast<int64_t>(cus) && !p.y_past));
     }
     // launches of fewer than 2^32 threads
     const double threads = 256.0 * M * p.slices;
