@@ -77,7 +77,8 @@ __device__ __forceinline__ u32x4_t load_x(const uint8_t *p) {
 template <typename E>
 __global__ __launch_bounds__(kThreads) void norm_stats_kernel(const NormKArgs a) {
     constexpr int kV = 16 / sizeof(E);
-    __shared__ float s_mean[kV][kThreads], s_m2[kV][kThreads], s_n[kThreads];
+    // (a channel's columns a bank on from the one's before: neighbouring channels are read together)
+    __shared__ float s_mean[kV][kThreads + 1], s_m2[kV][kThreads + 1], s_n[kThreads];
     const int tid = threadIdx.x, slice = blockIdx.x, part = blockIdx.y, m = blockIdx.z;
     const int line = divide(tid, a.per_col), col = tid - line * a.cols, column = slice * a.cols + col;
     const bool active = line < a.lines && column * kV < a.C;
