@@ -1,11 +1,12 @@
 // Matrix product with bias, activation, gate and residual in its epilogue for
-// gfx950: y = residual + gate * act(x W^T + bias), on the rows of listed frames.
+// gfx950: y = residual + gate * act(x W^T + bias), on the rows of listed frames. Of
+// 8-bit integers the sums are exact and times a scale of their row and one of their feature.
 //
 // x and W both hold their reduction index contiguously, so a 16-byte piece of a
-// row of either is a lane's operand of a matrix instruction as it stands. Both
-// types work in the same bytes: a step is 128 bytes of every row, 64 bf16 or 32
-// fp32, and a pair of 16-byte pieces feeds one 32x32x16 bf16 instruction or four
-// 32x32x2 fp32 ones (whose two half-waves then hold reduction indices that are four
+// row of either is a lane's operand of a matrix instruction as it stands. All
+// types work in the same bytes: a step is 128 bytes of every row, 128 8-bit integers,
+// 64 bf16 or 32 fp32, and a pair of 16-byte pieces feeds one 32x32x32 or 32x32x16
+// instruction or four 32x32x2 fp32 ones (whose two half-waves then hold reduction indices that are four
 // apart; both operands agree on it, and a sum's order is free).
 //
 // W's rows are the A operand, x's rows the B operand: a lane then holds one row
@@ -30,9 +31,13 @@
 //    same loop without the loads runs at 1,570. Four waves of 128 x 128 (1,225 TFLOP/s
 //    where this had 1,323), a ring of four half steps (1,218) and loads between the
 //    matrix instructions (1,248) were slower.
-//  * One round of tiles (9,360 x 1,536 x 1,536: 45 us, 47 with rows read at full positions, 52
-//    to 54 with gate and residual): 24
+//  * One round of tiles (9,360 x 1,536 x 1,536: 45 us, 47 with rows read at full positions, 51
+//    to 52 with gate and residual): 24
 //    steps of 1.55 us, the first loads and the epilogue's memory time.
+//  * Large products of 8-bit integers (21,600 x 20,480 x 5,120: 1.96 to 2.00 ms, 2.27 to 2.31 POP/s): matrix
+//    instructions are busy 60 % of the cycles, at 1.67 GHz under that load; the same bytes come through LDS as for
+//    bf16 in a step of the same length. Half as many steps leave what a tile does before and after them, 13 us a round, in the
+//    open: 35 to 36 us at 9,360 x 1,536 x 1,536 with gate and residual, 124 to 130 at x 6,144.
 //  * fp32 (7,800 x 1,536 x 1,536: 280 us, 131 TFLOP/s): the matrix instructions, busy 82 %.
 //  * Few rows (6 x 1,536 x 9,216: 10.0 us, 2.9 TB/s): 576 workgroups in two rounds and a
 //    quarter, each with loads that wait for one another and the waves' sums. A library's

@@ -117,7 +117,11 @@ inline LinearPlan linear_plan(int64_t rows, int32_t K, int32_t n_out, int32_t dt
     // at hand: 512 x 1,536 x 1,536 11.6 / 17.5 / 41; 500 x 8,960 x 1,536 29.5* / 29.8* / 36*; 3,600 x 1,536 x 1,536 27 / 26 /
     // 41; 9,360 x 1,536 x 1,536 64 / 53 / 47; fp32: 512 x 1,536 x 1,536 31* / 41* / 74*; 7,800 x
     // 1,536 x 1,536 279 / 353 / 363; 9,360 x 1,536 x 6,144 - / 1,247 / 1,438 (the largest form is never
-    // the best in fp32: two rounds of 128 x 128 take less than one of its rounds).
+    // the best in fp32: two rounds of 128 x 128 take less than one of its rounds). 8-bit integers: 1,000 x 1,536 x
+    // 4,608 15.8 / 17.6 / 26; 1,581 x 5,120 x 5,120 68 / 77 / 58; 3,600 x 1,536 x 1,536 17.1 / 18.5 / 26; 3,600 x 1,536 x
+    // 6,144 56 / 55 / 53; 9,360 x 640 x 640 11.1 / 13.3 / 18.3; 9,360 x 1,536 x 1,536 41 / 36 / 28; 21,600 x 256 x 512
+    // 14.9 / 17.3 / 15.2: steps of as many bytes and a longer epilogue, for which bf16's counts choose forms that
+    // take 69, 18.9 and 13.4 us where these take 62, 17.6 and 11.4: the second, third and fifth.
     struct Form {
         LinearForm form;
         int64_t rows, cols;
@@ -131,8 +135,8 @@ inline LinearPlan linear_plan(int64_t rows, int32_t K, int32_t n_out, int32_t dt
                                      {{kTile64, 64, 128, 3, 3.0, {1.1, 1.95, 2.93}},
                                       {kTile128, 128, 128, 2, 4.0, {2.4, 3.65, 3.65}}},
                                      {{kTile64, 64, 128, 3, 3.0, {0.53, 0.68, 1.0}},
-                                      {kTile128, 128, 128, 2, 4.0, {0.80, 0.95, 0.95}},
-                                      {kTile256, 256, 256, 1, 8.0, {1.55, 1.55, 1.55}}}};
+                                      {kTile128, 128, 128, 2, 5.0, {0.80, 0.95, 0.95}},
+                                      {kTile256, 256, 256, 1, 12.0, {1.25, 1.25, 1.25}}}};
     const int n_forms = dtype == RF_F32 ? 2 : 3;
     constexpr int64_t kLeastSteps = 4, kMostParts = 16;
     constexpr double kJoin = 3.0;
