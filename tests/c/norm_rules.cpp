@@ -1,9 +1,10 @@
-/* Host rules of the group norm's launches against plain walks over rows and channels. Prints "ok <checks>"; exits 1 at
-   the first mismatch. */
+/* Host rules of the group norm's launches against plain walks over rows and channels, and of products of 8-bit integers.
+   Prints "ok <checks>"; exits 1 at the first mismatch. */
 #include <cmath>
 #include <cstdio>
 #include <random>
 
+#include "rf_linear_plan.h"
 #include "rf_norm_plan.h"
 
 static long checks;
@@ -69,7 +70,34 @@ static int check(int32_t M, int64_t N, int32_t C, int32_t G, int32_t together, b
     return 0;
 }
 
+// A plan covers its product, by a form that 8-bit integers have, each of which is some product's best.
+static int products() {
+    std::mt19937_64 rng(11);
+    auto upto = [&](double most) { return static_cast<int64_t>(std::exp(std::uniform_real_distribution<>(0, std::log(most))(rng))); };
+    int64_t seen[rf::kLinearForms] = {}, split = 0;
+    for (int i = 0; i < 100000; ++i) {
+        const int64_t rows = i % 3 ? upto(100000) : upto(64), K = 16 * upto(4096), n = 4 * upto(8000);
+        const bool far = i % 5 == 0, ws = i % 4 != 0;
+        const rf::LinearPlan p = rf::linear_plan(rows, static_cast<int32_t>(K), static_cast<int32_t>(n), rf::kI8, 256, far, ws);
+        CHECK(p.form >= 0 && p.form < rf::kLinearForms && p.form != rf::kStream32 && p.form != rf::kStream64);
+        CHECK(!far || p.form == rf::kTile128);
+        const int64_t tile_rows[] = {16, 32, 64, 32, 64, 64, 128, 256}, tile_cols[] = {16, 32, 16, 256, 256, 128, 128, 256};
+        CHECK(p.row_tiles == (rows + tile_rows[p.form] - 1) / tile_rows[p.form]);
+        CHECK(p.col_tiles == (n + tile_cols[p.form] - 1) / tile_cols[p.form]);
+        const int64_t step = p.form <= rf::kFew64 ? 64 : rf::kLinearStep;
+        CHECK(p.steps == (K + step - 1) / step && p.parts >= 1 && (ws || p.parts == 1));
+        CHECK(static_cast<int64_t>(p.parts) * p.per_part >= p.steps && static_cast<int64_t>(p.parts - 1) * p.per_part < p.steps);
+        ++seen[p.form];
+        split += p.parts > 1;
+    }
+    for (int form = 0; form < rf::kLinearForms; ++form)
+        CHECK(form == rf::kStream32 || form == rf::kStream64 || seen[form] > 0);
+    CHECK(split > 0);
+    return 0;
+}
+
 int main() {
+    if (products()) return 1;
     for (int32_t n = 1; n <= 8192; ++n) {
         const float share = 1.0f / static_cast<float>(n);
         for (int32_t i = 0; i < 8192; ++i)

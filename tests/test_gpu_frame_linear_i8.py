@@ -192,3 +192,48 @@ def test_activations_of_all_arguments(rows, act, dtype):
     xs, ws = torch.ones(rows, device="cuda"), torch.ones(n, device="cuda")
     y = rf.rf_frame_linear_i8(xq, xs, wq, ws, b, act)
     block.assert_within(y, *ref.linear_i8(xq, xs, wq, ws, b, act, dtype=dtype))
+
+
+# tiles of 128 x 128 and of 256 x 256, whole and ragged, with one, two and many frames in a tile
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("K,n", [(2064, 1032), (1040, 2312)])
+@pytest.mark.parametrize("M,N", [(1, 5201), (7, 743), (20, 260), (130, 40), (250, 21)])
+@pytest.mark.parametrize("full", [False, True])
+def test_frames_in_large_tiles(M, N, K, n, full, dtype):
+    T = min(M + 3, 256)
+    ids = sorted(set(range(T)) - set([0, T // 2, T - 1][:T - M]))
+    x, s, w, ws = operands(M * N, K, n, 40)
+    b, gate, res = draw((n,), dtype, 41), draw((T, n), dtype, 42), draw((M * N, n), dtype, 43)
+    g = gate[torch.tensor(ids, device="cuda")].repeat_interleave(N, 0)
+    want, bound = ref.linear_i8(x, s, w, ws, b, "silu", g, res, dtype)
+    kw = dict(frame_ids=ids, T=T, rows_per_frame=N)
+    if not full:
+        block.assert_within(rf.rf_frame_linear_i8(x, s, w, ws, b, "silu", gate, res, **kw), want, bound)
+        return
+    pos = block.positions(ids, N, "cuda")
+    xf, sf = torch.zeros((T * N, K), dtype=torch.int8, device="cuda"), torch.full((T * N,), float("nan"), device="cuda")
+    xf[pos], sf[pos] = x, s
+    y = draw((T * N, n), dtype, 44)
+    y[pos] = res
+    old = y.clone()
+    rf.rf_frame_linear_i8(xf, sf, w, ws, b, "silu", gate, y, in_full=True, out_full=True, out=y, **kw)
+    block.assert_within(y[pos], want, bound)
+    listed = torch.zeros(T * N, dtype=torch.bool, device="cuda")
+    listed[pos] = True
+    assert torch.equal(y[~listed], old[~listed])
+
+
+@pytest.mark.parametrize("rows,K,n", [(5201, 1040, 2316), (5201, 2064, 1036), (1101, 20480, 1540)])
+def test_features_of_four_in_large_tiles(rows, K, n):
+    """fp32, with a residual and without; in parts, too."""
+    xq, xs, wq, ws = operands(rows, K, n, 45)
+    b, g, r = draw((n,), F32, 46), draw((n,), F32, 47), draw((rows, n), F32, 48)
+    block.assert_within(rf.rf_frame_linear_i8(xq, xs, wq, ws, b, "gelu", g, r), *ref.linear_i8(xq, xs, wq, ws, b, "gelu", g, r))
+    block.assert_within(rf.rf_frame_linear_i8(xq, xs, wq, ws, dtype=F32), *ref.linear_i8(xq, xs, wq, ws))
+
+
+@pytest.mark.parametrize("rows,K,n", [(1000, 8208, 2056), (1101, 20480, 1544), (5201, 1040, 2312), (700, 16400, 5128)])
+def test_large_tiles_do_not_depend_on_the_workspace(rows, K, n):
+    xq, xs, wq, ws = operands(rows, K, n, 49)
+    b = draw((n,), BF16, 50)
+    assert torch.equal(rf.rf_frame_linear_i8(xq, xs, wq, ws, b, "silu"), _no_workspace(xq, xs, wq, ws, b))

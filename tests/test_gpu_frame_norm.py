@@ -210,3 +210,13 @@ def test_large_magnitudes(N, C, G, dtype):
     """Up to 2^40, where squares are sums of 2^80: results as of the same values near 1."""
     x = draw((N, C), dtype, 28).clamp(-4, 4) * 2.0 ** 38
     check(x, G, draw((C,), dtype, 29))
+
+
+@pytest.mark.parametrize("M,N,C,G,dtype", [(2, 110001, 640, 32, BF16), (1, 70003, 1000, 8, F32), (64, 3600, 640, 20, BF16),
+                                           (3, 21000, 512, 512, F32), (1, 50000, 1016, 127, BF16)])
+def test_beyond_the_caches(M, N, C, G, dtype):
+    """Rows of 96 and of 256 MB and more, which go past the caches."""
+    x = draw((M * N, C), dtype, 30, 2.0, 1.0)
+    check(x, G, draw((C,), dtype, 31, 0.3, 1.0), draw((C,), dtype, 32, 0.4), act="silu", M=M, T=M, what=f"{M}x{N}x{C}")
+    want = rf.rf_frame_group_norm(x, G, frame_ids=range(M), T=M, rows_per_frame=N)
+    assert torch.equal(rf.rf_frame_group_norm(x, G, frame_ids=range(M), T=M, rows_per_frame=N, out=x), want)

@@ -1,4 +1,5 @@
-"""Host rules of the group norm's launches (csrc/rf_norm_plan.h), run by a small C++ program without a GPU."""
+"""Host rules of the group norm's launches (csrc/rf_norm_plan.h) and of 8-bit products (csrc/rf_linear_plan.h), run by a
+small C++ program without a GPU."""
 import os
 import shutil
 import subprocess
