@@ -18,10 +18,10 @@
 // What bounds them, and what they measure (bf16 but for the first):
 //  * Slices: what one launch takes, its loads, two sums through LDS and its stores one after the other:
 //    6.3 us at 3 x 64 rows x 128 channels of fp32, 9.1 at 3 x 527 x 320.
-//  * Short launches (6 x 1,560 rows x 640 channels, 12 MB: 7.2, 3 and 7.5 us, 18.5 together): their starts and ends
+//  * Short launches (6 x 1,560 rows x 640 channels, 12 MB: 7, 3 and 8 us, 18.2 together): their starts and ends
 //    and the parts' way from one to the next; 12 MB in and out take 4 us at the rate of a large copy.
-//  * Large ones: memory, x read twice as it does not fit the chip: 62,400 rows x 1,024 channels, 128 MB in and
-//    out, 66 us (the second time it is in the caches behind the L2s in part), 409 MB 200, 6.1 TB/s.
+//  * Large ones: memory, x read twice as it does not fit the chip: 5 x 24,960 rows x 512 channels, 128 MB in and
+//    out, 66 to 73 us (the second time it is in the caches behind the L2s in part), 409 MB 200, 6.1 TB/s.
 //  * Rows to 8 bits: memory, with about ten vector instructions an element beside three bytes: 21,600 x 20,480,
 //    227 us, 5.9 TB/s, vector instructions busy 63 % of the cycles.
 #include "rf_norm_plan.h"
