@@ -808,7 +808,8 @@ int rf_frame_linear_i8_workspace(int32_t M, int64_t rows_per_frame, int32_t in_f
  * the list and the channels / groups channels of a group: 1 is a norm of each frame
  * by itself, M one over the whole clip. An infinity or a NaN makes its group's results
  * of those frames NaN. Deviations are squared and summed in fp32: magnitudes up to
- * 2^40.
+ * 2^40. A mean of fp32 rows is held in more than fp32, so that results are as exact as
+ * the rows' deviations, and a group of equal values gives the bias.
  *
  * x: device rows of `channels` elements, x_stride elements from row to row (0: the
  *   rows are contiguous), compact, or full with RF_ROWS_IN_FULL.

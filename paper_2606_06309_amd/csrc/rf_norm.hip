@@ -10,6 +10,9 @@
 //    squared deviations from it, joined to those so far (a sum of squares about another
 //    point than the mean would lose what small deviations around a large mean are). The
 //    threads' rows, then the channels of each group, meet in LDS.
+//    A mean of fp32 rows is two numbers everywhere, itself and the rest that its rounding left, so that deviations
+//    are as exact as the rows are, and values that do not deviate come out as 0 (summed and held in one number, 192 rows x 16
+//    channels of 10,000.3 normalise to 0.29 with eps 1e-5). Sums of bf16 rows have the bits to spare.
 //  * norm_total_kernel: a wave joins the parts of a group; where these are few, each workgroup of the
 //    next kernel does so itself.
 //  * norm_rows_kernel: x again, to y; norm_rows8_kernel: whole rows at a time, to 8 bits.
@@ -38,6 +41,7 @@ struct NormKArgs {
     const void *weight, *bias;
     float2 *partial;               // [M][parts][slices][local]: mean, sum of squared deviations
     float2 *total;                 // [M / together][groups]: mean, 1 / deviation
+    float *partial_rest, *total_rest;   // of fp32 rows: what the means' rounding left
     int64_t N;
     int64_t x_stride, y_stride;    // bytes
     double eps;
@@ -74,18 +78,30 @@ __device__ __forceinline__ u32x4_t load_x(const uint8_t *p) {
     else return *reinterpret_cast<const u32x4_t *>(p);
 }
 
+// The same of means in two numbers, mean + rest.
+__device__ __forceinline__ void join(float n, float &mean, float &rest, float &m2, float n_b, float mean_b, float rest_b,
+                                     float m2_b, float share_b) {
+    const float far = mean_b - mean, near = rest_b - rest, d = far + near, step = far * share_b, sum = mean + step;
+    rest = fmaf(near, share_b, rest) + (step - (sum - mean));
+    mean = sum;
+    m2 += fmaf(d * d, n * share_b, m2_b);
+}
+
 template <typename E>
 __global__ __launch_bounds__(kThreads) void norm_stats_kernel(const NormKArgs a) {
     constexpr int kV = 16 / sizeof(E);
+    constexpr bool kRest = sizeof(E) == 4;
     // (a channel's columns a bank on from the one's before: neighbouring channels are read together)
     __shared__ float s_mean[kV][kThreads + 1], s_m2[kV][kThreads + 1], s_n[kThreads];
+    __shared__ float s_rest[kRest ? kV : 1][kRest ? kThreads + 1 : 1];
     const int tid = threadIdx.x, slice = blockIdx.x, part = blockIdx.y, m = blockIdx.z;
     const int line = divide(tid, a.per_col), col = tid - line * a.cols, column = slice * a.cols + col;
     const bool active = line < a.lines && column * kV < a.C;
     const int chunk = a.lines * kNormRows;
     float n = 0.0f, mean[kV], m2[kV];
+    [[maybe_unused]] float rest[kV];
 #pragma unroll
-    for (int e = 0; e < kV; ++e) mean[e] = m2[e] = 0.0f;
+    for (int e = 0; e < kV; ++e) mean[e] = m2[e] = rest[e] = 0.0f;
     if (active) {
         const uint8_t *const x = a.x + a.frames.in(m) * a.N * a.x_stride + column * 16;
         const int64_t step = a.lines * a.x_stride;
@@ -105,9 +121,21 @@ __global__ __launch_bounds__(kThreads) void norm_stats_kernel(const NormKArgs a)
 #pragma unroll
                     for (int i = 0; i < kNormRows; ++i) s += v[i][e];
                     s *= 1.0f / kNormRows;
+                    if constexpr (kRest) {
+                        // (deviations about a mean that is off by their mean, which their squares are then too many by)
+                        float off = 0.0f;
 #pragma unroll
-                    for (int i = 0; i < kNormRows; ++i) q = fmaf(v[i][e] - s, v[i][e] - s, q);
-                    join(n, mean[e], m2[e], kNormRows, s, q, share);
+                        for (int i = 0; i < kNormRows; ++i) {
+                            off += v[i][e] - s;
+                            q = fmaf(v[i][e] - s, v[i][e] - s, q);
+                        }
+                        q = fmaf(off * (-1.0f / kNormRows), off, q);
+                        join(n, mean[e], rest[e], m2[e], kNormRows, s, off * (1.0f / kNormRows), q, share);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < kNormRows; ++i) q = fmaf(v[i][e] - s, v[i][e] - s, q);
+                        join(n, mean[e], m2[e], kNormRows, s, q, share);
+                    }
                 }
                 n += kNormRows;
             } else {      // the frame's last rows, one by one (but in flight together)
@@ -124,7 +152,10 @@ __global__ __launch_bounds__(kThreads) void norm_stats_kernel(const NormKArgs a)
                     widen<E>(raw[i], v);
                     const float share = 1.0f / (n + 1.0f);
 #pragma unroll
-                    for (int e = 0; e < kV; ++e) join(n, mean[e], m2[e], 1.0f, v[e], 0.0f, share);
+                    for (int e = 0; e < kV; ++e) {
+                        if constexpr (kRest) join(n, mean[e], rest[e], m2[e], 1.0f, v[e], 0.0f, 0.0f, share);
+                        else join(n, mean[e], m2[e], 1.0f, v[e], 0.0f, share);
+                    }
                     n += 1.0f;
                 }
             }
@@ -135,6 +166,7 @@ __global__ __launch_bounds__(kThreads) void norm_stats_kernel(const NormKArgs a)
     for (int e = 0; e < kV; ++e) {
         s_mean[e][tid] = mean[e];
         s_m2[e][tid] = m2[e];
+        if constexpr (kRest) s_rest[e][tid] = rest[e];
     }
     // lines of a column, in halves
     for (int width = a.lines; width > 1;) {
@@ -147,7 +179,12 @@ __global__ __launch_bounds__(kThreads) void norm_stats_kernel(const NormKArgs a)
                 const float share = n_b / (n + n_b);
 #pragma unroll
                 for (int e = 0; e < kV; ++e) {
-                    join(n, mean[e], m2[e], n_b, s_mean[e][other], s_m2[e][other], share);
+                    if constexpr (kRest) {
+                        join(n, mean[e], rest[e], m2[e], n_b, s_mean[e][other], s_rest[e][other], s_m2[e][other], share);
+                        s_rest[e][tid] = rest[e];
+                    } else {
+                        join(n, mean[e], m2[e], n_b, s_mean[e][other], s_m2[e][other], share);
+                    }
                     s_mean[e][tid] = mean[e];
                     s_m2[e][tid] = m2[e];
                 }
@@ -169,24 +206,41 @@ __global__ __launch_bounds__(kThreads) void norm_stats_kernel(const NormKArgs a)
         const int first = (g0 + l) * a.per_group, behind = first + a.per_group;
         const int lo = (first > c0 ? first : c0) - c0, hi = (behind < c1 ? behind : c1) - c0;
         float s = 0.0f, q = 0.0f;
-        for (int c = lo + lane; c < hi; c += lanes) s += s_mean[c % kV][c / kV];
-        for (int d = lanes / 2; d > 0; d /= 2) s += __shfl_xor(s, d);
-        s /= static_cast<float>(hi - lo);
+        [[maybe_unused]] float left = 0.0f;
+        if constexpr (kRest) {
+            double sum = 0.0;
+            for (int c = lo + lane; c < hi; c += lanes)
+                sum += static_cast<double>(s_mean[c % kV][c / kV]) + static_cast<double>(s_rest[c % kV][c / kV]);
+            for (int d = lanes / 2; d > 0; d /= 2) sum += __shfl_xor(sum, d);
+            sum /= static_cast<double>(hi - lo);
+            s = static_cast<float>(sum);
+            left = static_cast<float>(sum - static_cast<double>(s));
+        } else {
+            for (int c = lo + lane; c < hi; c += lanes) s += s_mean[c % kV][c / kV];
+            for (int d = lanes / 2; d > 0; d /= 2) s += __shfl_xor(s, d);
+            s /= static_cast<float>(hi - lo);
+        }
         for (int c = lo + lane; c < hi; c += lanes) {
-            const float d = s_mean[c % kV][c / kV] - s;
+            float d = s_mean[c % kV][c / kV] - s;
+            if constexpr (kRest) d += s_rest[c % kV][c / kV] - left;
             q += fmaf(rows * d, d, s_m2[c % kV][c / kV]);
         }
         for (int d = lanes / 2; d > 0; d /= 2) q += __shfl_xor(q, d);
-        if (lane == 0)
-            a.partial[((static_cast<int64_t>(m) * a.parts + part) * a.slices + slice) * a.local + l] = make_float2(s, q);
+        if (lane == 0) {
+            const int64_t at = ((static_cast<int64_t>(m) * a.parts + part) * a.slices + slice) * a.local + l;
+            a.partial[at] = make_float2(s, q);
+            if constexpr (kRest) a.partial_rest[at] = left;
+        }
     }
 }
 
-// Mean and 1 / deviation of n_groups groups from g0 on, of the frames of a segment, by kBlock threads:
-// lanes together join a group's parts, in 64 bits and one order: sums of the parts' means and their squares
-// about the first part's (64 bits lose nothing there that 32 had).
-template <int kV, int kBlock>
-__device__ __forceinline__ void totals(const NormKArgs &a, int seg, int g0, int n_groups, float2 *to) {
+// Mean and 1 / deviation of n_groups groups from g0 on, of the frames of a segment, by kBlock threads (of fp32 rows
+// what the mean's rounding left besides): lanes together join a group's parts, in 64 bits and one order: sums of the
+// parts' means and their squares about the first part's (64 bits lose nothing there that 32 had).
+template <typename E, int kBlock>
+__device__ __forceinline__ void totals(const NormKArgs &a, int seg, int g0, int n_groups, float2 *to, float *rest_to) {
+    constexpr int kV = 16 / sizeof(E);
+    constexpr bool kRest = sizeof(E) == 4;
     int lanes = 1;
     while (lanes < 64 && 2 * lanes * n_groups <= kBlock) lanes *= 2;
     const int lane = threadIdx.x % lanes, width = a.cols * kV, runs = a.together * a.parts;
@@ -197,15 +251,17 @@ __device__ __forceinline__ void totals(const NormKArgs &a, int seg, int g0, int 
         double pivot = 0.0, sum = 0.0, square = 0.0;
         for (int s = s0; s * width < behind; ++s) {
             const int c0 = s * width, lo = first > c0 ? first : c0, hi = behind < c0 + width ? behind : c0 + width;
-            const float2 *p = a.partial + (static_cast<int64_t>(seg) * runs * a.slices + s) * a.local +
-                              (g0 + l - divide(c0, a.group_share));
+            const int64_t from = (static_cast<int64_t>(seg) * runs * a.slices + s) * a.local + (g0 + l - divide(c0, a.group_share));
+            const float2 *p = a.partial + from;
             if (s == s0) pivot = p->x;
             int part = lane;
             while (part >= a.parts) part -= a.parts;
 #pragma unroll 8
             for (int i = lane; i < runs; i += lanes) {
                 const float2 v = p[i * step];
-                const double n = a.runs.rows(part) * static_cast<float>(hi - lo), d = v.x - pivot;
+                const double n = a.runs.rows(part) * static_cast<float>(hi - lo);
+                double d = v.x - pivot;
+                if constexpr (kRest) d += static_cast<double>(a.partial_rest[from + i * step]);
                 sum += n * d;
                 square += n * d * d + v.y;
                 part += lanes;
@@ -217,8 +273,11 @@ __device__ __forceinline__ void totals(const NormKArgs &a, int seg, int g0, int 
             square += __shfl_xor(square, d);
         }
         const double m = sum / all, var = square / all - m * m;
-        if (lane == 0)
-            to[l] = make_float2(static_cast<float>(pivot + m), static_cast<float>(rsqrt((var < 0.0 ? 0.0 : var) + a.eps)));
+        if (lane == 0) {
+            const float mean = static_cast<float>(pivot + m);
+            to[l] = make_float2(mean, static_cast<float>(rsqrt((var < 0.0 ? 0.0 : var) + a.eps)));
+            if constexpr (kRest) rest_to[l] = static_cast<float>(pivot - static_cast<double>(mean) + m);
+        }
     }
 }
 
@@ -226,16 +285,19 @@ __device__ __forceinline__ void totals(const NormKArgs &a, int seg, int g0, int 
 template <typename E>
 __global__ __launch_bounds__(64) void norm_total_kernel(const NormKArgs a) {
     const int g = blockIdx.x, seg = blockIdx.y;
-    totals<16 / sizeof(E), 64>(a, seg, g, 1, a.total + static_cast<int64_t>(seg) * a.groups + g);
+    const int64_t at = static_cast<int64_t>(seg) * a.groups + g;
+    totals<E, 64>(a, seg, g, 1, a.total + at, a.total_rest + at);
 }
 
-// What kV channels from c on of listed frame m are normalised with, (x - mean) * mul + add; total: of the groups from
-// g0 on.
+// What kV channels from c on of listed frame m are normalised with, (x - mean) * mul + add; total and rests: of the
+// groups from g0 on.
 template <typename E>
-__device__ __forceinline__ void affine_at(const NormKArgs &a, int m, int c, const float2 *total, int g0,
+__device__ __forceinline__ void affine_at(const NormKArgs &a, int m, int c, const float2 *total, const float *rests, int g0,
                                           float (&mean)[16 / sizeof(E)], float (&mul)[16 / sizeof(E)],
                                           float (&add)[16 / sizeof(E)]) {
     constexpr int kV = 16 / sizeof(E);
+    constexpr bool kRest = sizeof(E) == 4;
+    [[maybe_unused]] float rest[kV];
     const int64_t at = (a.affine_rows ? static_cast<int64_t>(frame_at(a.frames, m)) * a.C : 0) + c;
 #pragma unroll
     for (int e = 0; e < kV; ++e) {
@@ -253,15 +315,27 @@ __device__ __forceinline__ void affine_at(const NormKArgs &a, int m, int c, cons
             mean[e] = e < border ? t.x : e < border2 ? t2.x : t3.x;
             mul[e] *= e < border ? t.y : e < border2 ? t2.y : t3.y;
         }
+        if constexpr (kRest) {
+            const float r = rests[first - g0], r2 = rests[(first < last ? first + 1 : last) - g0], r3 = rests[last - g0];
+#pragma unroll
+            for (int e = 0; e < kV; ++e) rest[e] = e < border ? r : e < border2 ? r2 : r3;
+        }
     } else {
         float2 t[kV];
 #pragma unroll
-        for (int e = 0; e < kV; ++e) t[e] = total[divide(c + e, a.group_share) - g0];
+        for (int e = 0; e < kV; ++e) {
+            t[e] = total[divide(c + e, a.group_share) - g0];
+            if constexpr (kRest) rest[e] = rests[divide(c + e, a.group_share) - g0];
+        }
 #pragma unroll
         for (int e = 0; e < kV; ++e) {
             mean[e] = t[e].x;
             mul[e] *= t[e].y;
         }
+    }
+    if constexpr (kRest) {
+#pragma unroll
+        for (int e = 0; e < kV; ++e) add[e] = fmaf(-rest[e], mul[e], add[e]);
     }
 }
 
@@ -313,8 +387,9 @@ template <typename E, int kHold, int kBlock>
 __global__ __launch_bounds__(kBlock) void norm_slice_kernel(const NormKArgs a) {
     constexpr int kV = 16 / sizeof(E);
     __shared__ __attribute__((aligned(1024))) uint8_t held[kHold * kBlock * 16];
+    constexpr bool kRest = sizeof(E) == 4;
     __shared__ __attribute__((aligned(16))) float all[kBlock * kV], some[kBlock], mean[kNormSliceGroups],
-        inverse[kNormSliceGroups];
+        inverse[kNormSliceGroups], rest[kRest ? kNormSliceGroups : 1];
     const int tid = threadIdx.x;
     const int slice = blockIdx.x, seg = blockIdx.y;
     const int line = divide(tid, a.per_col), col = tid - line * a.cols, column = slice * a.cols + col;
@@ -361,6 +436,17 @@ __global__ __launch_bounds__(kBlock) void norm_slice_kernel(const NormKArgs a) {
     };
     wait_loads<0>();   // (a thread reads its own rows only)
     float s[kV], mu[kV];
+    // fp32 values are summed as what they are above their group's first one in the segment's first row
+    [[maybe_unused]] float above[kV];
+    auto first_of = [&](int g) {
+        const int c = g * a.per_group;
+        return *reinterpret_cast<const float *>(held + c / kV * 16 + c % kV * 4);
+    };
+    if constexpr (kRest) {
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < kV; ++e) above[e] = first_of(local[e]);
+    }
 #pragma unroll
     for (int e = 0; e < kV; ++e) s[e] = 0.0f;
 #pragma unroll 1
@@ -368,10 +454,18 @@ __global__ __launch_bounds__(kBlock) void norm_slice_kernel(const NormKArgs a) {
         float v[kV];
         row(i, v);
 #pragma unroll
-        for (int e = 0; e < kV; ++e) s[e] += v[e];
+        for (int e = 0; e < kV; ++e) s[e] += kRest ? v[e] - above[e] : v[e];
     }
     group_sums<kV, kBlock>(s, line, a.cols, a.lines, a.per_group, n_groups, shares, channel_share, all, some,
-                           [&](int g, float sum) { mean[g] = static_cast<float>(sum * share); });
+                           [&](int g, float sum) {
+                               if constexpr (kRest) {
+                                   const double m = static_cast<double>(first_of(g)) + sum * share;
+                                   mean[g] = static_cast<float>(m);
+                                   rest[g] = static_cast<float>(m - static_cast<double>(mean[g]));
+                               } else {
+                                   mean[g] = static_cast<float>(sum * share);
+                               }
+                           });
 #pragma unroll
     for (int e = 0; e < kV; ++e) {
         mu[e] = mean[local[e]];
@@ -385,12 +479,25 @@ __global__ __launch_bounds__(kBlock) void norm_slice_kernel(const NormKArgs a) {
         for (int e = 0; e < kV; ++e) s[e] = fmaf(v[e] - mu[e], v[e] - mu[e], s[e]);
     }
     group_sums<kV, kBlock>(s, line, a.cols, a.lines, a.per_group, n_groups, shares, channel_share, all, some,
-                           [&](int g, float sum) { inverse[g] = static_cast<float>(rsqrt(sum * share + a.eps)); });
+                           [&](int g, float sum) {
+                               double var = sum * share;
+                               if constexpr (kRest) {      // (of deviations from the mean without its rest)
+                                   var -= static_cast<double>(rest[g]) * static_cast<double>(rest[g]);
+                                   var = var < 0.0 ? 0.0 : var;
+                               }
+                               inverse[g] = static_cast<float>(rsqrt(var + a.eps));
+                           });
     if (line >= a.lines) return;
-    float mul[kV];
-    with_activation(a.activation, [&](auto act) {
+    float mul[kV], add[kV];
+    auto factors = [&]() {
 #pragma unroll
-        for (int e = 0; e < kV; ++e) mul[e] = inverse[local[e]] * weight[e];
+        for (int e = 0; e < kV; ++e) {
+            mul[e] = inverse[local[e]] * weight[e];
+            add[e] = kRest ? fmaf(-rest[kRest ? local[e] : 0], mul[e], bias[e]) : bias[e];
+        }
+    };
+    with_activation(a.activation, [&](auto act) {
+        factors();
 #pragma unroll 1
         for (int i = 0; i < mine; ++i) {
             uint32_t f;
@@ -398,13 +505,12 @@ __global__ __launch_bounds__(kBlock) void norm_slice_kernel(const NormKArgs a) {
             const int m = seg * a.together + static_cast<int>(f);
             if (each) {
                 affine(m);
-#pragma unroll
-                for (int e = 0; e < kV; ++e) mul[e] = inverse[local[e]] * weight[e];
+                factors();
             }
             float v[kV];
             row(i, v);
 #pragma unroll
-            for (int e = 0; e < kV; ++e) v[e] = fmaf(v[e] - mu[e], mul[e], bias[e]);
+            for (int e = 0; e < kV; ++e) v[e] = fmaf(v[e] - mu[e], mul[e], add[e]);
             if constexpr (act.kind != RF_ACT_NONE) activate_fitted(act.kind, v);
             store_n<E, kV>(a.y + (a.frames.out(m) * a.N + r) * a.y_stride + column * 16, 0, v);
         }
@@ -424,18 +530,22 @@ __global__ __launch_bounds__(kThreads) void norm_rows_kernel(const NormKArgs a) 
     const int tid = threadIdx.x, slice = blockIdx.x, part = blockIdx.y, m = blockIdx.z;
     const int line = divide(tid, a.per_col), col = tid - line * a.cols, column = slice * a.cols + col;
     __shared__ float2 own[kOwn ? kNormFewGroups : 1];
-    const float2 *total = a.total + static_cast<int64_t>(m / a.together) * a.groups;
+    __shared__ float own_rest[kOwn && sizeof(E) == 4 ? kNormFewGroups : 1];
+    const int64_t segment = static_cast<int64_t>(m / a.together) * a.groups;
+    const float2 *total = a.total + segment;
+    const float *rests = a.total_rest + segment;
     int g0 = 0;
     if constexpr (kOwn) {
         const int c0 = slice * a.cols * kV, c1 = c0 + a.cols * kV < a.C ? c0 + a.cols * kV : a.C;
         g0 = divide(c0, a.group_share);
-        totals<kV, kThreads>(a, m / a.together, g0, divide(c1 - 1, a.group_share) - g0 + 1, own);
+        totals<E, kThreads>(a, m / a.together, g0, divide(c1 - 1, a.group_share) - g0 + 1, own, own_rest);
         total = own;
+        rests = own_rest;
         __syncthreads();
     }
     if (line >= a.lines || column * kV >= a.C) return;
     float mean[kV], mul[kV], add[kV];
-    affine_at<E>(a, m, column * kV, total, g0, mean, mul, add);
+    affine_at<E>(a, m, column * kV, total, rests, g0, mean, mul, add);
     // (y may be x: no row is read again)
     const uint8_t *p = a.x + (a.frames.in(m) * a.N) * a.x_stride + column * 16;
     uint8_t *q = a.y + (a.frames.out(m) * a.N) * a.y_stride + column * 16;
@@ -522,16 +632,20 @@ __global__ __launch_bounds__(kThreads) void norm_rows8_kernel(const NormKArgs a)
     // (columns past the last are the last once more)
     float mean[kPer][kV], mul[kPer][kV], add[kPer][kV];
     __shared__ float2 own[kOwn ? kNormFewGroups : 1];
-    const float2 *total = a.total + static_cast<int64_t>(m / a.together) * a.groups;
+    __shared__ float own_rest[kOwn && sizeof(E) == 4 ? kNormFewGroups : 1];
+    const int64_t segment = static_cast<int64_t>(m / a.together) * a.groups;
+    const float2 *total = a.total + segment;
+    const float *rests = a.total_rest + segment;
     if constexpr (kOwn) {
-        totals<kV, kThreads>(a, m / a.together, 0, a.groups, own);
+        totals<E, kThreads>(a, m / a.together, 0, a.groups, own, own_rest);
         total = own;
+        rests = own_rest;
         __syncthreads();
     }
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int col = lane + i * kLanes;
-        affine_at<E>(a, m, (col < columns ? col : columns - 1) * kV, total, 0, mean[i], mul[i], add[i]);
+        affine_at<E>(a, m, (col < columns ? col : columns - 1) * kV, total, rests, 0, mean[i], mul[i], add[i]);
     }
     with_activation(a.activation, [&](auto act) {
         int turn = 0;
@@ -726,6 +840,8 @@ hipError_t launch_norm(const NormParams &p, hipStream_t stream) {
     a.bias = p.bias;
     a.partial = static_cast<float2 *>(p.ws);
     a.total = a.partial + plan.entries;
+    a.partial_rest = reinterpret_cast<float *>(a.partial + plan.sums);
+    a.total_rest = a.partial_rest + plan.sums;
     a.N = p.N;
     a.x_stride = p.x_stride * esize;
     a.y_stride = p.y_scale ? p.y_stride : p.y_stride * esize;

@@ -41,8 +41,9 @@ struct NormPlan {
     int32_t local;          // groups that a slice meets at most
     int32_t x_past, y_past; // the second launch reads x, writes y past the caches
     int32_t few_parts;      // a group's parts are joined by the workgroups that use them
-    int64_t entries;        // partial sums: [M][parts][slices][local], an even number
-    int64_t ws_bytes;       // they, then the groups' mean and 1 / deviation
+    int64_t sums;           // partial sums: [M][parts][slices][local]
+    int64_t entries;        // of 8 bytes: they and, of fp32, their and the groups' means' rests (4 bytes each); an even number
+    int64_t ws_bytes;       // these, then the groups' mean and 1 / deviation
 };
 
 // Where the workgroups of the second launch join the parts of the groups that they use, instead of a launch
@@ -140,8 +141,10 @@ inline NormPlan norm_plan(int32_t M, int64_t N, int32_t C, int32_t groups, int32
     p.x_past = bytes > kNormHeld;
     p.few_parts = p.parts * together <= kNormFewParts && (rows8 ? groups : p.local) <= kNormFewGroups &&
                   (rows8 || static_cast<int64_t>(p.row_parts) * M * p.slices <= static_cast<int64_t>(kNormFewWorkgroups) * cus);
-    p.entries = (static_cast<int64_t>(M) * p.parts * p.slices * p.local + 1) / 2 * 2;
-    p.ws_bytes = (p.entries + static_cast<int64_t>(M / together) * groups) * 8;
+    const int64_t totals = static_cast<int64_t>(M / together) * groups;
+    p.sums = static_cast<int64_t>(M) * p.parts * p.slices * p.local;
+    p.entries = up(p.sums + (dtype == RF_F32 ? up(p.sums + totals, 2) : 0), 2) * 2;
+    p.ws_bytes = (p.entries + totals) * 8;
     return p;
 }
 
