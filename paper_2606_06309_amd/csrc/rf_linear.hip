@@ -13,15 +13,15 @@
 // of y and runs of four features.
 //
 //  * linear_tile_kernel: a workgroup owns kBM rows x kBN features, 8 or 4 waves of
-//    32 kRB x 64: (bf16) 256 x 256, 128 x 128 and 64 x 128, and 32 x 256 and (bf16) 64 x
-//    256 where rows are few and W large. Steps go from memory straight into LDS,
+//    32 kRB x 64: (bf16 and 8 bits) 256 x 256, 128 x 128 and 64 x 128, and (bf16 and fp32) 32 x 256
+//    and (bf16) 64 x 256 where rows are few and W large. Steps go from memory straight into LDS,
 //    double-buffered, one barrier a step. Rows of 128 bytes are stored without
 //    padding, their eight 16-byte slots permuted by (row / 2) % 8, so the 16 lanes of
 //    a read pass meet 16 different slots of the 256-byte bank window.
 //  * linear_few_kernel: up to 64 rows of a small W, where reading W is all that
 //    costs: a workgroup owns 16 or 32 features, its 8 waves share out the reduction
 //    index, operands go straight to registers, and the waves' sums meet in LDS.
-//  * A reduction index may also be split over workgroups, whose fp32 parts go to the
+//  * A reduction index may also be split over workgroups, whose parts (fp32, or 32-bit integers) go to the
 //    workspace; linear_join_kernel adds them in order and runs the epilogue.
 //
 // What bounds them, and what they measure:
@@ -60,7 +60,7 @@ struct LinearKArgs {
     const uint8_t *x, *w;
     const void *bias, *gate, *residual;
     void *y;
-    float *ws;                 // parts > 1: [part][rows][n_out]
+    void *ws;                  // parts > 1: [part][rows][n_out] sums, fp32 or of 8-bit integers int32
     int64_t row_bytes;         // of x and W
     uint32_t rows, N;          // N: rows per frame
     int32_t n_out;
@@ -269,7 +269,7 @@ struct NearRows {
 template <int kN, typename V>
 __device__ __forceinline__ void store_part(const LinearKArgs &a, int part, uint32_t r, int c, const V (&v)[kN]) {
     typedef V v4_t __attribute__((ext_vector_type(4)));
-    V *to = reinterpret_cast<V *>(a.ws) + (static_cast<int64_t>(part) * a.rows + r) * a.n_out + c;
+    V *to = static_cast<V *>(a.ws) + (static_cast<int64_t>(part) * a.rows + r) * a.n_out + c;
 #pragma unroll
     for (int i = 0; i < kN; i += 4) *reinterpret_cast<v4_t *>(to + i) = v4_t{v[i], v[i + 1], v[i + 2], v[i + 3]};
 }
@@ -796,7 +796,7 @@ __global__ __launch_bounds__(256) void linear_join_kernel(const LinearKArgs a) {
     fin.frames(a, r);
     fin.load(a, r, c);
     sums4_t x = {};
-    const value_t *p = reinterpret_cast<const value_t *>(a.ws) + static_cast<int64_t>(r) * a.n_out + c;
+    const value_t *p = static_cast<const value_t *>(a.ws) + static_cast<int64_t>(r) * a.n_out + c;
     const int64_t step = static_cast<int64_t>(a.rows) * a.n_out;
 #pragma unroll 8
     for (int i = 0; i < a.parts; ++i) {
@@ -810,17 +810,17 @@ __global__ __launch_bounds__(256) void linear_join_kernel(const LinearKArgs a) {
 
 template <typename In, typename E>
 void run(const LinearPlan &p, const LinearKArgs &a, bool far, dim3 grid, hipStream_t stream) {
-    constexpr bool kLarge = sizeof(In) < 4;   // (fp32 has neither of the largest forms)
+    constexpr int32_t kIn = sizeof(In) == 1 ? kI8 : sizeof(In) == 2 ? RF_BF16 : RF_F32;
     switch (p.form) {
         case kFew16: hipLaunchKernelGGL((linear_few_kernel<In, E, 1, 1>), grid, dim3(512), 0, stream, a); break;
         case kFew32: hipLaunchKernelGGL((linear_few_kernel<In, E, 2, 2>), grid, dim3(512), 0, stream, a); break;
         case kFew64: hipLaunchKernelGGL((linear_few_kernel<In, E, 4, 1>), grid, dim3(512), 0, stream, a); break;
-        case kStream32:   // (no 8-bit product is planned so, nor in the next)
-            if constexpr (sizeof(In) > 1)
+        case kStream32:
+            if constexpr (linear_has(kStream32, kIn))
                 hipLaunchKernelGGL((linear_tile_kernel<In, E, 1, 1, 4, false>), grid, dim3(256), 0, stream, a);
             break;
         case kStream64:
-            if constexpr (sizeof(In) == 2)
+            if constexpr (linear_has(kStream64, kIn))
                 hipLaunchKernelGGL((linear_tile_kernel<In, E, 2, 1, 4, false>), grid, dim3(256), 0, stream, a);
             break;
         case kTile64: hipLaunchKernelGGL((linear_tile_kernel<In, E, 1, 2, 2, false>), grid, dim3(256), 0, stream, a); break;
@@ -829,7 +829,7 @@ void run(const LinearPlan &p, const LinearKArgs &a, bool far, dim3 grid, hipStre
             else hipLaunchKernelGGL((linear_tile_kernel<In, E, 2, 2, 2, false>), grid, dim3(256), 0, stream, a);
             break;
         case kTile256:
-            if constexpr (kLarge)
+            if constexpr (linear_has(kTile256, kIn))
                 hipLaunchKernelGGL((linear_tile_kernel<In, E, 4, 2, 4, false>), grid, dim3(512), 0, stream, a);
             break;
         case kLinearForms: break;
@@ -859,6 +859,7 @@ hipError_t launch_product(const LinearParams &p, int32_t in, const float *x_scal
     const int64_t row_bytes = static_cast<int64_t>(p.K) * linear_size(in);
     const bool far = linear_far(p.frames, p.M, p.N, row_bytes);
     const LinearPlan plan = linear_plan(rows, p.K, p.n_out, in, p.geo.cus, far, p.ws != nullptr);
+    if (!linear_has(plan.form, in)) return hipErrorInvalidConfiguration;
     LinearKArgs a{};
     a.x = static_cast<const uint8_t *>(p.x);
     a.w = static_cast<const uint8_t *>(p.weight);
@@ -868,7 +869,7 @@ hipError_t launch_product(const LinearParams &p, int32_t in, const float *x_scal
     a.gate = p.gate;
     a.residual = p.residual;
     a.y = p.y;
-    a.ws = static_cast<float *>(p.ws);
+    a.ws = p.ws;
     a.row_bytes = row_bytes;
     a.rows = static_cast<uint32_t>(rows);
     a.N = static_cast<uint32_t>(p.N);

@@ -38,9 +38,17 @@ inline bool linear_far(const RowFrames &f, int32_t M, int64_t N, int64_t row_byt
     return static_cast<double>(linear_gap(f, M, N) + kLinearTileRows + 1) * static_cast<double>(row_bytes) >= 2147483647.0;
 }
 
-// The kernels' forms: up to 16, 32 or 64 rows straight to registers; up to 32 or 64 (bf16) rows of a
-// large W, and tiles of 64 x 128, 128 x 128 or (bf16) 256 x 256 (rows x features), through LDS.
+// The kernels' forms: up to 16, 32 or 64 rows straight to registers; up to 32 or 64 rows of a
+// large W, and tiles of 64 x 128, 128 x 128 or 256 x 256 (rows x features), through LDS.
 enum LinearForm { kFew16, kFew32, kFew64, kStream32, kStream64, kTile64, kTile128, kTile256, kLinearForms };
+// Those that operands of type `in` have, all that linear_plan takes for them and no others: of the streams of a
+// large W 8-bit integers neither, fp32 only that of 32 rows, nor fp32 the largest tiles.
+constexpr bool linear_has(int32_t form, int32_t in) {
+    if (form == kStream32) return in != kI8;
+    if (form == kStream64) return in == RF_BF16;
+    if (form == kTile256) return in != RF_F32;
+    return form >= 0 && form < kLinearForms;
+}
 struct LinearPlan {
     LinearForm form;
     int64_t row_tiles, col_tiles;
@@ -104,7 +112,7 @@ inline LinearPlan linear_plan(int64_t rows, int32_t K, int32_t n_out, int32_t dt
             return p;
         }
     }
-    // Tiles of 64 x 128, 128 x 128 or in bf16 256 x 256 (rows x features) and parts of the reduction,
+    // Tiles of 64 x 128, 128 x 128 or but for fp32 256 x 256 (rows x features) and parts of the reduction,
     // by the time in us that they come to, counted in rounds of the device: a round has a
     // fixed part and its steps, which take the longer the more workgroups share a compute
     // unit; a split adds the second kernel and its parts, written and read again. The
