@@ -573,9 +573,10 @@ int rf_async_schedule(int32_t T, int32_t T_w, int32_t T_mid, int32_t n_small, in
 /* ---- A block's operators around the attention ----
  * What a DiT block does with the rows of the listed frames directly before and
  * after keyframe-query attention: rotary positions of queries and keys,
- * attention to an encoder's states (the prompt), the matrix products with their
- * bias, activation, gate and residual, also of 8-bit integers, and the group norm
- * before them.
+ * attention to an encoder's states (the prompt), and the matrix products with their
+ * bias, activation, gate and residual, also of 8-bit integers. Beside them the group
+ * norm that blocks of spatial and temporal transformers begin with and decoders of
+ * latents have throughout (a DiT block's norm of each token over its channels is another).
  *
  * Rows of frames come and go in one of two layouts, per call and side:
  *   compact: M*N rows, row m*N + n is row n of the m-th listed frame (what a
@@ -587,7 +588,7 @@ int rf_async_schedule(int32_t T, int32_t T_w, int32_t T_mid, int32_t n_small, in
  */
 #define RF_ROWS_IN_FULL 1u      /* input rows are read at full positions (default: compact) */
 #define RF_ROWS_OUT_FULL 2u     /* output rows (and the residual's) are at full positions (default: compact) */
-#define RF_GATE_PER_FRAME 4u    /* rf_frame_linear: gate is [T][out_features], frames have their own */
+#define RF_GATE_PER_FRAME 4u    /* rf_frame_linear, rf_frame_linear_i8: gate is [T][out_features], frames have their own */
 #define RF_AFFINE_PER_FRAME 8u  /* rf_frame_group_norm: weight and bias are [T][channels], frames have their own */
 #define RF_ROTARY_HALVES 16u    /* rf_rotary: pair p is dimensions p and p + R/2 (default: 2p and 2p + 1) */
 #define RF_ROTARY_INVERSE 32u   /* rf_rotary: rotate by the negative angles */

@@ -39,9 +39,9 @@
 //    bf16 in a step of the same length. Half as many steps leave what a tile does before and after them, 13 us a round, in the
 //    open: 35 to 36 us at 9,360 x 1,536 x 1,536 with gate and residual, 124 to 130 at x 6,144.
 //  * fp32 (7,800 x 1,536 x 1,536: 280 us, 131 TFLOP/s): the matrix instructions, busy 82 %.
-//  * Few rows (6 x 1,536 x 9,216: 10.0 us, 2.9 TB/s): 576 workgroups in two rounds and a
-//    quarter, each with loads that wait for one another and the waves' sums. A library's
-//    product without epilogue takes 6.5: this is not the least that it can take.
+//  * Few rows (6 x 1,536 x 9,216: 10.0 us, 2.9 TB/s; 7.3 in 8 bits): 576 workgroups, two or three to a compute unit
+//    and all there at once (four fit: 64 registers a lane at most, 8 KB of LDS), each with loads that wait for one another and
+//    the waves' sums. A library's product without epilogue takes 6.5 in bf16: this is not the least that it can take.
 #include "rf_device.h"
 #include "rf_linear_plan.h"
 #include "rf_rows.h"

@@ -16,11 +16,13 @@
 //  * norm_total_kernel: a wave joins the parts of a group; where these are few, each workgroup of the
 //    next kernel does so itself.
 //  * norm_rows_kernel: x again, to y; norm_rows8_kernel: whole rows at a time, to 8 bits.
-//  * quantize_kernel: rows of x to 8 bits.
+//  * quantize_kernel: rows of x to 8 bits. (fp32 rows of more than 16,384 features, 16 columns to each of 1,024
+//    threads, leave 18 of a lane's registers in memory: 148 us at 5,120 x 20,480, 3.6 TB/s, where 5,120 x 16,384
+//    takes 82, 5.1 TB/s.)
 //
 // What bounds them, and what they measure (bf16 but for the first):
 //  * Slices: what one launch takes, its loads, two sums through LDS and its stores one after the other:
-//    6.3 us at 3 x 64 rows x 128 channels of fp32, 9.1 at 3 x 527 x 320.
+//    6.7 us at 3 x 64 rows x 128 channels of fp32, 9.3 at 3 x 527 x 320.
 //  * Short launches (6 x 1,560 rows x 640 channels, 12 MB: 7, 3 and 8 us, 18.2 together): their starts and ends
 //    and the parts' way from one to the next; 12 MB in and out take 4 us at the rate of a large copy.
 //  * Large ones: memory, x read twice as it does not fit the chip: 5 x 24,960 rows x 512 channels, 128 MB in and
@@ -707,7 +709,8 @@ struct QuantizeKArgs {
     RowFrames frames;
 };
 
-// kLanes threads to a row, up to kPer columns to a thread, which stay in registers as they came.
+// kLanes threads to a row, up to kPer columns to a thread, which stay in registers as they came (but for 18 of the
+// widest fp32 form's).
 template <typename E, int kLanes, int kPer>
 __global__ __launch_bounds__(kLanes > kThreads ? kLanes : kThreads) void quantize_kernel(const QuantizeKArgs a) {
     constexpr int kV = 16 / sizeof(E), kBlock = kLanes > kThreads ? kLanes : kThreads, kRows = kBlock / kLanes;

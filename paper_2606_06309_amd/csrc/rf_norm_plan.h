@@ -48,7 +48,8 @@ struct NormPlan {
 
 // Where the workgroups of the second launch join the parts of the groups that they use, instead of a launch
 // between: parts of a group and groups of a workgroup up to these (22.0 us for a norm of 11 parts into 8 bits and
-// its product, 24.7 with the launch between; 19.4 with 65 parts, and 18.5), and workgroups to a compute unit: 20.4 us
+// its product, 24.7 with the launch between; 19.4 with 65 parts, and 18.5; from 11 to 65 it was not measured where it
+// turns), and workgroups to a compute unit: 20.4 us
 // at 64 x 300 rows x 512 channels, five of them, 46.0 at 64 x 900 x 512, 14, where the launch between makes it 21.9
 // and 47.2; 63.0 at 200 x 160 x 1,280, 31, and 61.3 with it. (Rows in 8 bits never have more than seven.)
 constexpr int kNormFewParts = 16, kNormFewGroups = 64, kNormFewWorkgroups = 16;
@@ -56,7 +57,8 @@ constexpr int kNormFewParts = 16, kNormFewGroups = 64, kNormFewWorkgroups = 16;
 // thread: 200 us for a norm of 409 MB, 203 with 16 to a compute unit, 211 with 8.
 constexpr int64_t kRowRounds = 64;
 // Bytes of y from which it goes past the caches: 66 us at 128 MB, 83 through them (157 and 152 with the product
-// that reads it next), 200 and 240 at 409; smaller ones stay there for that product (75 and 72 us at 42 MB).
+// that reads it next), 200 and 240 at 409; smaller ones stay there for that product (75 and 72 us at 42 MB). The times at
+// 128 MB are of two inputs in turn; where more take turns, 73 us for the 66.
 constexpr double kNormCached = 96e6;
 // Bytes of x from which the second launch reads it past the caches; smaller ones it finds there in part, going the
 // other way than the first (which always leaves behind what it read): with a product of as many channels between,

@@ -108,7 +108,7 @@ __device__ __forceinline__ void activate(int kind, float (&v)[kN]) {
 // by exchange of extrema: off by 9e-8 of erfc at most in 64 bits. With x = |z| / sqrt 2, z times half of it is gelu
 // below 0, and z less that above; the base is 2 and the half is in the constant. In fp32, where the exponent's
 // roundings grow with z^2, results are off by 6e-7 of themselves for |z| < 1, 1e-6 down to -3, 2e-6 to -6, 4e-6 to -9 and 8e-6
-// beyond, above 1 by 1.3e-7 (measured; z (1 + erf) / 2 in fp32 by 3e-7, 1.2e-5, and below -5 it is 0).
+// beyond, above 1 by 1.3e-7 (measured; z (1 + erf) / 2 in fp32 by 3e-7, 1.2e-5, and below -5.5 it is 0).
 template <int kN>
 __device__ __forceinline__ void gelu_fitted(float (&v)[kN]) {
     constexpr float p[9] = {-3.1477283157f, 1.4446996621f, 0.5797163299f, 0.4226135587f, -0.6163823429f, 1.4100290353f, -2.1181933443f, 1.3223464084f, -0.2971011160f};
