@@ -88,3 +88,44 @@ def test_deviations_around_a_large_mean(M, N, C, G, together, mean):
     w, b = torch.randn(C, generator=g, device="cuda"), torch.randn(C, generator=g, device="cuda")
     y, err = around_the_mean(x.view(M, N, C), G, w, b, 1e-5, together)
     block.assert_within(norm(x, G, M, N, together, weight=w, bias=b), y, err)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("M,N,C,G,together", SIZES)
+@pytest.mark.parametrize("int8", [False, True])
+def test_a_workspace_of_exactly_its_bytes(M, N, C, G, together, int8, dtype):
+    """Whatever it held before; nothing behind it is written."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(4)
+    x = (torch.randn((M * N, C), generator=g, device="cuda") + 100.0).to(dtype)
+    need = rf.rf_frame_group_norm_workspace(M, N, C, G, dtype, int8=int8, frames_together=together)
+    runs = []
+    for fill in (0, 255):       # (the second: NaN in every place)
+        space = torch.full((need + 256,), fill, dtype=torch.uint8, device="cuda")
+        got = norm(x, G, M, N, together, int8=int8, workspace=space[:need] if need else None)
+        runs.append(got if int8 else (got,))
+        assert bool((space[need:] == fill).all())
+    assert all(torch.equal(a, b) for a, b in zip(*runs))
+
+
+def test_a_captured_norm_of_fp32_rows():
+    """Replayed on other rows, with eager norms between."""
+    M, N, C, G = 3, 2000, 320, 32
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    draws = [torch.randn((M * N, C), generator=g, device="cuda") + 1000.0 * i for i in range(4)]
+    want = [norm(x, G, M, N, 1, activation="silu") for x in draws]
+    x, out = draws[0].clone(), torch.empty_like(draws[0])
+    space = torch.empty(rf.rf_frame_group_norm_workspace(M, N, C, G, F32), dtype=torch.uint8, device="cuda")
+    norm(x, G, M, N, 1, activation="silu", out=out, workspace=space)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        norm(x, G, M, N, 1, activation="silu", out=out, workspace=space)
+    for turn in range(3):
+        for i in (1, 3, 0, 2):
+            x.copy_(draws[i])
+            graph.replay()
+            again = norm(draws[i], G, M, N, 1, activation="silu")
+            torch.cuda.synchronize()
+            assert torch.equal(out, want[i]) and torch.equal(again, want[i]), (turn, i)
